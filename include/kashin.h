@@ -64,7 +64,9 @@ typedef enum {
   KD_ERR_TIMEOUT = 6        /* a bounded wait inside a kernel expired (device-detected) */
 } kd_status;
 
-typedef enum { KD_F32 = 0, KD_F16 = 1, KD_BF16 = 2 } kd_dtype;
+/* KD_E4M3 (8-bit floats, 4 exponent and 3 mantissa bits, largest value 448) is taken by
+ * kd_matmul_4bit's activations only. */
+typedef enum { KD_F32 = 0, KD_F16 = 1, KD_BF16 = 2, KD_E4M3 = 3 } kd_dtype;
 
 typedef enum { KD_VEC_ROWS = 0, KD_VEC_COLUMNS = 1 } kd_layout;
 
@@ -490,6 +492,118 @@ kd_status kd_matmul_2bit_bf16_batch(const kd_fold_mat_f16* mats, int count, int6
 int64_t kd_rht_block(int64_t n); /* block length b for vectors of length n, 0 if unsupported */
 kd_status kd_rht(const void* x, kd_dtype dtype, int64_t n, int64_t m, int64_t ldx, uint64_t seed, int inverse,
                  float* y, int64_t ldy, uint32_t* status, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Serving operators around the coded layers: the norm that makes a product's
+ * activations, the product with 4-bit weights for layers that 2 bits do not carry (an
+ * output head, sensitive projections), and the log probabilities that a model is scored
+ * with.  They have no counterpart in the paper.  As everywhere, arguments are checked
+ * first and nothing is enqueued on an error; no call allocates or needs a workspace.
+ * Outputs must not overlap inputs or each other except where a call says so.
+ * --------------------------------------------------------------------------- */
+
+/* Root-mean-square norm of rows, with the residual's addition and 8-bit output:
+ *   h = x + residual                        (32 bits; h = x without a residual)
+ *   new_residual = h                        (optional, rounded to dtype)
+ *   yv = h / sqrt(mean_i h_i^2 + eps) * weight
+ *   y = yv                                  (optional, rounded to y_dtype)
+ *   scale = max_i |yv_i| / 448, q = e4m3(yv / scale)   (optional, both or neither)
+ * per row; one rounding to nearest (ties to even) per output; scale = 1 where
+ * max |yv_i| < 2^-100 (a row of zeros).  All arithmetic is fp32.
+ *   x, residual, new_residual   device, dtype, `rows` rows of n, row r at base + r*ld.
+ *                  new_residual may be the residual itself (in place) with the same ld.
+ *   weight         device, n values, weight_dtype = dtype or KD_F32.
+ *   q, scale       device, rows of n e4m3 bytes (row stride ldq bytes) and rows fp32.
+ *   y              device, y_dtype any of KD_F32, KD_F16, KD_BF16.  y may be x itself
+ *                  with the same dtype and ld.
+ * At least one of q and y is wanted (rows > 0).  A row whose sum of squares is not
+ * finite (an infinity or NaN in it, or fp32/bf16 values past 1e19) gives NaN in y, q and
+ * scale.  Rows of 16-byte aligned base and stride and n a multiple of 8 take 128-bit
+ * accesses, others element accesses.
+ * Errors: KD_ERR_UNSUPPORTED_N unless 1 <= n <= 16384; KD_ERR_INVALID_ARG for rows < 0
+ * or above 2^31 - 1, a bad dtype or ld, a negative or NaN eps, q without scale or the
+ * reverse, new_residual without residual, missing or unaligned (to their element)
+ * pointers; KD_ERR_CUDA (launch).  rows == 0 enqueues nothing. */
+kd_status kd_rmsnorm(const void* x, kd_dtype dtype, int64_t n, int64_t rows, int64_t ldx, const void* weight,
+                     kd_dtype weight_dtype, float eps, const void* residual, int64_t ld_residual, void* new_residual,
+                     int64_t ld_new_residual, uint8_t* q, int64_t ldq, float* scale, void* y, kd_dtype y_dtype,
+                     int64_t ldy, void* stream);
+
+/* A matrix of 4-bit weights with a scale (and optionally a zero point) for each group of
+ * `group` consecutive inputs of an output channel:
+ *   w[j][i] = scale[j][i / group] * (code[j][i] - zero[j][i / group]).
+ *   codes   device, 16-byte aligned, m rows of 4 ceil(n/32) uint32: code i of a row at
+ *           bits 4(i % 8) of word i/8; the padding codes past n are read but do not count.
+ *   scales  device, m rows of ceil(n/group) values of scale_dtype (KD_F16 or KD_BF16).
+ *   zeros   device, m rows of ceil(n/group) bytes in 0..15, or NULL: 8 everywhere.
+ *   group   32, 64 or 128. */
+typedef struct kd_weight4 {
+  const uint32_t* codes;
+  const void* scales;
+  const uint8_t* zeros;
+  int64_t n;
+  int64_t m;
+  int32_t group;
+  int32_t scale_dtype;
+} kd_weight4;
+
+/* Quantises w (m rows of n, dtype, row j at w + j*ld) into `out`, whose codes, scales and
+ * (optional) zeros this call writes.  Per group, with lo and hi its extremes:
+ *   without zeros: s = max(hi / 7, -lo / 8), z = 8;
+ *   with zeros:    lo' = min(lo, 0), hi' = max(hi, 0), s = (hi' - lo') / 15,
+ *                  z = min(15, max(0, rint(-lo' / s)));
+ * s is rounded to scale_dtype first, and the codes are rint(w / s) + z held to 0..15
+ * (nearest, ties to even; all divisions fp32).  A group whose rounded scale is 0 gets
+ * z = 0 (8 without zeros) and codes z.  A group with an infinity or NaN, or whose scale
+ * does not fit the type, gets a NaN or infinite scale and codes z.
+ * Errors: KD_ERR_INVALID_ARG (sizes, group, types, ld, pointers missing with m > 0 or
+ * unaligned), KD_ERR_CUDA.  m == 0 enqueues nothing. */
+kd_status kd_quantise_4bit(const void* w, kd_dtype dtype, int64_t ld, const kd_weight4* out, void* stream);
+
+/* The dense matrix of 4-bit weights: out[j*ld + i] = w[j][i], i < n, rounded to
+ * out_dtype (for large batches, with a dense product).  Errors as kd_quantise_4bit. */
+kd_status kd_dequantise_4bit(const kd_weight4* w, kd_dtype out_dtype, void* out, int64_t ld, void* stream);
+
+/* Products of activation rows with 4-bit weights, without expanding them in memory:
+ *   y[r*ldy + j] = xs[r] * sum_i w[j][i] x[r*ldx + i],   r < rows, j < m.
+ *   x       device, x_dtype KD_F16, KD_BF16 or KD_E4M3; x_scale: rows fp32 (the e4m3
+ *           rows' scales, as kd_rmsnorm leaves them), or NULL: 1.
+ *   y       device, y_dtype KD_F32, KD_F16 or KD_BF16.
+ * Meant for few rows (decoding): 32 rows share one pass over the weights, more rows take
+ * more passes.  Within a group the sum over integers code - zero is formed on the tensor
+ * cores (exact products, fp32 sums); groups are added in fp32 with their scale, and the
+ * whole is rounded once.  The order of the sums is fixed (deterministic results), and a
+ * row's result does not depend on the other rows' values.
+ * Rows of 16-byte aligned base and stride (8-byte for e4m3) take wide loads.
+ * Errors: KD_ERR_INVALID_ARG (sizes, group, types, ld < n or ldy < m, pointers missing
+ * with m > 0 and rows > 0, or unaligned), KD_ERR_CUDA.  m == 0 or rows == 0 enqueues
+ * nothing. */
+kd_status kd_matmul_4bit(const kd_weight4* w, const void* x, kd_dtype x_dtype, const float* x_scale, int64_t rows,
+                         int64_t ldx, void* y, kd_dtype y_dtype, int64_t ldy, void* stream);
+
+/* Log probabilities under softmax(logits), row by row:
+ *   lse      = ln sum_v exp(logits[r][v])
+ *   logprob  = logits[r][id] - lse for each of `tokens` given ids of the row
+ *   entropy  = -sum_v p_v ln p_v (nats; entries of p = 0 count 0)
+ *   top      the `top` largest logits: ids and log probabilities, largest first, equal
+ *            values by lowest id.
+ *   logits   device, dtype, `rows` rows of `vocab`, row r at logits + r*ld.
+ *   ids      device int64, rows x tokens contiguous; a negative id is padding (its output
+ *            is 0), an id >= vocab gives NaN.  NULL with tokens = 0.
+ *   logprobs fp32 rows x tokens (NULL with tokens = 0); lse, entropy fp32 rows, each
+ *            optional (NULL); top_ids int64 and top_logprobs fp32, rows x top (NULL with
+ *            top = 0), 0 <= top <= min(vocab, KD_MAX_TOP).
+ * Masked entries may hold -infinity (probability 0) or the type's lowest value.  A row of
+ * -infinity only: lse and every log probability -infinity, entropy 0, the lowest ids.  A
+ * row that holds +infinity: lse +infinity, log probabilities and entropy NaN.  A row that
+ * holds NaN: NaN throughout, top ids -1.
+ * fp32 arithmetic in a fixed order (deterministic).  Errors: KD_ERR_INVALID_ARG (rows < 0
+ * or above 2^31 - 1, vocab < 1 or above 2^30, tokens < 0, top out of range, dtype, ld,
+ * missing or unaligned pointers), KD_ERR_CUDA.  rows == 0 enqueues nothing. */
+#define KD_MAX_TOP 32
+kd_status kd_token_logprobs(const void* logits, kd_dtype dtype, int64_t rows, int64_t vocab, int64_t ld,
+                            const int64_t* ids, int64_t tokens, int top, float* logprobs, float* lse, float* entropy,
+                            int64_t* top_ids, float* top_logprobs, void* stream);
 
 #ifdef __cplusplus
 }

@@ -15,7 +15,9 @@ Two layers:
   ``prepare_p`` + ``apply_p_prepared``), ``reconstruct`` (``reconstruct_batch``),
   ``dequantise`` (``dequantise_batch``), ``rht``, and the products from the 2-bit
   planes ``matmul_2bit`` (fp32) and ``matmul_2bit_f16`` (fp16 or bf16 activations,
-  tensor cores), each with a ``_batch`` form.
+  tensor cores), each with a ``_batch`` form; and the serving operators around them,
+  ``rmsnorm`` (residual addition, 8-bit output), ``quantise_4bit`` / ``dequantise_4bit`` /
+  ``matmul_4bit`` (4-bit weights with group scales) and ``token_logprobs``.
 """
 
 from __future__ import annotations
@@ -31,7 +33,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libkashin.so")
 
 KD_OK, KD_ERR_INVALID_ARG, KD_ERR_UNSUPPORTED_N, KD_ERR_CUDA, KD_ERR_NONFINITE, KD_ERR_WORKSPACE, KD_ERR_TIMEOUT = range(7)
-KD_F32, KD_F16, KD_BF16 = 0, 1, 2
+KD_F32, KD_F16, KD_BF16, KD_E4M3 = 0, 1, 2, 3
 KD_VEC_ROWS, KD_VEC_COLUMNS = 0, 1
 
 EXPORTS = ("kd_status_string", "kd_version", "kd_supported", "kd_tuned", "kd_workspace_size", "kd_signs",
@@ -41,8 +43,10 @@ EXPORTS = ("kd_status_string", "kd_version", "kd_supported", "kd_tuned", "kd_wor
            "kd_matmul_2bit_bf16", "kd_matmul_2bit_bf16_batch",
            "kd_apply_p_batch", "kd_prepare_p", "kd_apply_p_prepared",
            "kd_rht_block", "kd_rht", "kd_dequantise", "kd_dequantise_batch", "kd_measure_fp32_peak",
-           "kd_workspace_size_batch", "kd_decompose_batch", "kd_reconstruct_batch")
+           "kd_workspace_size_batch", "kd_decompose_batch", "kd_reconstruct_batch",
+           "kd_rmsnorm", "kd_quantise_4bit", "kd_dequantise_4bit", "kd_matmul_4bit", "kd_token_logprobs")
 KD_MAX_BATCH = 32
+KD_MAX_TOP = 32
 
 
 class KdPlane(ctypes.Structure):
@@ -88,6 +92,13 @@ class KdMatrix(ctypes.Structure):
     _fields_ = [("w", ctypes.c_void_p), ("m", ctypes.c_int64), ("ld", ctypes.c_int64),
                 ("sign_seed", ctypes.c_uint64), ("codes_u", ctypes.c_void_p), ("codes_v", ctypes.c_void_p),
                 ("centres_u", ctypes.c_void_p), ("centres_v", ctypes.c_void_p), ("coeffs", ctypes.c_void_p)]
+
+
+class KdWeight4(ctypes.Structure):
+    """Mirror of kd_weight4 (include/kashin.h)."""
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("zeros", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("m", ctypes.c_int64), ("group", ctypes.c_int32),
+                ("scale_dtype", ctypes.c_int32)]
 
 
 def _load() -> ctypes.CDLL:
@@ -163,6 +174,18 @@ def _load() -> ctypes.CDLL:
     lib.kd_rht_block.restype = c_i64
     lib.kd_rht.argtypes = [c_vp, c_int, c_i64, c_i64, c_i64, c_u64, c_int, c_vp, c_i64, c_vp, c_vp]
     lib.kd_rht.restype = c_int
+    lib.kd_rmsnorm.argtypes = [c_vp, c_int, c_i64, c_i64, c_i64, c_vp, c_int, ctypes.c_float, c_vp, c_i64, c_vp, c_i64,
+                               c_vp, c_i64, c_vp, c_vp, c_int, c_i64, c_vp]
+    lib.kd_rmsnorm.restype = c_int
+    lib.kd_quantise_4bit.argtypes = [c_vp, c_int, c_i64, c_vp, c_vp]
+    lib.kd_quantise_4bit.restype = c_int
+    lib.kd_dequantise_4bit.argtypes = [c_vp, c_int, c_vp, c_i64, c_vp]
+    lib.kd_dequantise_4bit.restype = c_int
+    lib.kd_matmul_4bit.argtypes = [c_vp, c_vp, c_int, c_vp, c_i64, c_i64, c_vp, c_int, c_i64, c_vp]
+    lib.kd_matmul_4bit.restype = c_int
+    lib.kd_token_logprobs.argtypes = [c_vp, c_int, c_i64, c_i64, c_i64, c_vp, c_i64, c_int, c_vp, c_vp, c_vp, c_vp,
+                                      c_vp, c_vp]
+    lib.kd_token_logprobs.restype = c_int
     return lib
 
 
@@ -294,6 +317,30 @@ def kd_rht_block(n) -> int:
 def kd_rht(x, dtype, n, m, ldx, seed, inverse, y, ldy, status, stream) -> int:
     return lib.kd_rht(x, dtype, n, m, ldx, ctypes.c_uint64(int(seed) & ((1 << 64) - 1)), inverse, y, ldy, status,
                       stream)
+
+
+def kd_rmsnorm(x, dtype, n, rows, ldx, weight, weight_dtype, eps, residual, ld_residual, new_residual,
+               ld_new_residual, q, ldq, scale, y, y_dtype, ldy, stream) -> int:
+    return lib.kd_rmsnorm(x, dtype, n, rows, ldx, weight, weight_dtype, eps, residual, ld_residual, new_residual,
+                          ld_new_residual, q, ldq, scale, y, y_dtype, ldy, stream)
+
+
+def kd_quantise_4bit(w, dtype, ld, out, stream) -> int:
+    return lib.kd_quantise_4bit(w, dtype, ld, out, stream)
+
+
+def kd_dequantise_4bit(w, out_dtype, out, ld, stream) -> int:
+    return lib.kd_dequantise_4bit(w, out_dtype, out, ld, stream)
+
+
+def kd_matmul_4bit(w, x, x_dtype, x_scale, rows, ldx, y, y_dtype, ldy, stream) -> int:
+    return lib.kd_matmul_4bit(w, x, x_dtype, x_scale, rows, ldx, y, y_dtype, ldy, stream)
+
+
+def kd_token_logprobs(logits, dtype, rows, vocab, ld, ids, tokens, top, logprobs, lse, entropy, top_ids, top_logprobs,
+                      stream) -> int:
+    return lib.kd_token_logprobs(logits, dtype, rows, vocab, ld, ids, tokens, top, logprobs, lse, entropy, top_ids,
+                                 top_logprobs, stream)
 
 
 # ---------------------------------------------------------------------------
@@ -815,3 +862,240 @@ def unpack_codes(words, n: int):
     m = w.shape[0]
     idx = np.arange(n)
     return ((w[:, idx // 16] >> (2 * (idx % 16)).astype(np.uint64)) & np.uint64(3)).astype(np.int64).reshape(m, n)
+
+
+# ---------------------------------------------------------------------------
+# serving operators around the coded layers
+# ---------------------------------------------------------------------------
+
+def _rows(t, name, dtypes, device, shape=None):
+    """Checks one operand of a serving operator (a CUDA tensor of one of ``dtypes`` on
+    ``device``, rows of unit inner stride) and returns its row stride."""
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} has dtype {t.dtype}: one of {', '.join(map(str, dtypes))} is wanted")
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"{name} must be a CUDA tensor on {device}")
+    size = t.shape
+    if shape is not None and tuple(size) != shape:
+        raise ValueError(f"{name} has shape {tuple(size)}: {shape} is wanted")
+    if len(size) == 1:
+        if size[0] > 1 and t.stride(0) != 1:
+            raise ValueError(f"{name} must be contiguous")
+        return size[0]
+    if len(size) != 2:
+        raise ValueError(f"{name} must be 2-D")
+    rows, cols = size
+    a, b = t.stride()
+    if cols > 1 and b != 1:
+        raise ValueError(f"{name} needs unit inner stride")
+    if rows <= 1:
+        return cols
+    if a < cols:
+        raise ValueError(f"{name}'s rows must not overlap")
+    return a
+
+
+def _new(stream, shape, dtype, device):
+    """An output allocated here: the allocator learns of the stream that it is used on."""
+    t = _torch().empty(shape, dtype=dtype, device=device)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
+def _call(what, fn, device, stream, *args):
+    """fn(*args, stream) on ``device``; KashinError for any status but KD_OK."""
+    torch = _torch()
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    if device.index is None or device.index == torch.cuda.current_device():
+        st = fn(*args, stream.cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, stream.cuda_stream)
+    if st != KD_OK:
+        raise KashinError(st, what)
+
+
+def _float_types():
+    torch = _torch()
+    return torch.float16, torch.bfloat16, torch.float32
+
+
+@dataclasses.dataclass
+class Normed:
+    """rmsnorm's outputs; a field that is None is not computed."""
+    q: "object" = None         # float8_e4m3fn (rows, n)
+    scale: "object" = None     # float32 (rows,): q * scale is the normed row
+    y: "object" = None         # fp16, bf16 or fp32 (rows, n)
+    residual: "object" = None  # x + residual, x's dtype (rows, n)
+
+
+def rmsnorm(x, weight, eps: float = 1e-5, residual=None, out: Optional[Normed] = None, stream=None) -> Normed:
+    """Root-mean-square norm of the rows of ``x`` (plus ``residual``), in 8 bits with one
+    scale a row and/or in a float type (kd_rmsnorm).
+
+    ``x``, ``residual``: (rows, n) CUDA tensors of one dtype (fp16, bf16, fp32), n <= 16384;
+    ``weight``: (n,) of that dtype or fp32.  ``out``: the tensors to write (``Normed``; set
+    ``y`` for the 16- or 32-bit rows that the 2-bit products and apply_p read, and
+    ``residual`` -- it may be the ``residual`` argument itself -- for the sum); without it
+    ``q``, ``scale`` and, given a residual, ``residual`` are allocated."""
+    torch = _torch()
+    if x.dim() != 2:
+        raise ValueError("x must be 2-D")
+    dev, (rows, n) = x.device, x.shape
+    types = (x.dtype,)
+    ldx = _rows(x, "x", _float_types(), dev)
+    _rows(weight, "weight", (x.dtype, torch.float32), dev, (n,))
+    shape = (rows, n)
+    if out is None:
+        out = Normed(q=_new(stream, shape, torch.float8_e4m3fn, dev), scale=_new(stream, (rows,), torch.float32, dev),
+                     residual=None if residual is None else _new(stream, shape, x.dtype, dev))
+    ldr = ldn = ldq = ldy = 0
+    if residual is not None:
+        ldr = _rows(residual, "residual", types, dev, shape)
+    if out.residual is not None:
+        if residual is None:
+            raise ValueError("out.residual is written only where a residual is given")
+        ldn = _rows(out.residual, "out.residual", types, dev, shape)
+    if (out.q is None) != (out.scale is None):
+        raise ValueError("out.q and out.scale come together")
+    if out.q is not None:
+        ldq = _rows(out.q, "out.q", (torch.float8_e4m3fn,), dev, shape)
+        _rows(out.scale, "out.scale", (torch.float32,), dev, (rows,))
+    ydt = KD_F32
+    if out.y is not None:
+        ldy = _rows(out.y, "out.y", _float_types(), dev, shape)
+        ydt = _dtype_code(out.y.dtype)
+    if out.q is None and out.y is None:
+        raise ValueError("out wants q and scale, or y, or all three")
+    _call("kd_rmsnorm", kd_rmsnorm, dev, stream, x.data_ptr(), _dtype_code(x.dtype), n, rows, ldx, weight.data_ptr(),
+          _dtype_code(weight.dtype), eps, _ptr(residual), ldr, _ptr(out.residual), ldn, _ptr(out.q), ldq,
+          _ptr(out.scale), _ptr(out.y), ydt, ldy)
+    return out
+
+
+class Weight4:
+    """A matrix of 4-bit weights (kd_weight4): ``codes`` int32 (m, 4 ceil(n/32)), code i of a
+    row at bits 4 (i % 8) of word i // 8; ``scales`` fp16 or bf16 (m, ceil(n/group));
+    ``zeros`` uint8 of that shape with values 0..15, or None for 8 everywhere.  The weight is
+    ``scale * (code - zero)``; all tensors contiguous on one GPU."""
+
+    __slots__ = ("codes", "scales", "zeros", "n", "m", "group", "device", "desc", "ref")
+
+    def __init__(self, codes, scales, zeros=None, *, n: int, group: int = 128):
+        torch = _torch()
+        if group not in (32, 64, 128):
+            raise ValueError("group must be 32, 64 or 128")
+        if n < 1 or codes.dim() != 2 or codes.shape[1] != (n + 31) // 32 * 4 or codes.dtype != torch.int32:
+            raise ValueError("codes must be int32 (m, 4 ceil(n/32))")
+        m = codes.shape[0]
+        shape = (m, (n + group - 1) // group)
+        if tuple(scales.shape) != shape or scales.dtype not in (torch.float16, torch.bfloat16):
+            raise ValueError(f"scales must be fp16 or bf16 {shape}")
+        if zeros is not None and (tuple(zeros.shape) != shape or zeros.dtype != torch.uint8):
+            raise ValueError(f"zeros must be uint8 {shape}")
+        for t in (codes, scales, zeros):
+            if t is not None and (not t.is_cuda or t.device != codes.device or not t.is_contiguous()):
+                raise ValueError("codes, scales and zeros must be contiguous CUDA tensors on one device")
+        self.codes, self.scales, self.zeros = codes, scales, zeros
+        self.n, self.m, self.group, self.device = int(n), m, int(group), codes.device
+        self.desc = KdWeight4(codes.data_ptr(), scales.data_ptr(), _ptr(zeros), n, m, group,
+                              _dtype_code(scales.dtype))
+        self.ref = ctypes.addressof(self.desc)
+
+
+def quantise_4bit(w, group: int = 128, zeros: bool = False, scale_dtype=None, stream=None) -> Weight4:
+    """4-bit weights with a scale for each ``group`` inputs from the (m, n) matrix ``w``
+    (nn.Linear layout, fp16, bf16 or fp32; kd_quantise_4bit).  ``zeros``: a zero point per
+    group too; ``scale_dtype``: fp16 (the default for fp16 weights) or bf16."""
+    torch = _torch()
+    if w.dim() != 2:
+        raise ValueError("w must be 2-D")
+    dev, (m, n) = w.device, w.shape
+    ld = _rows(w, "w", _float_types(), dev)
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128")
+    if n < 1:
+        raise ValueError("w has no inputs")
+    sdt = scale_dtype or (torch.float16 if w.dtype == torch.float16 else torch.bfloat16)
+    groups = (n + group - 1) // group
+    out = Weight4(_new(stream, (m, (n + 31) // 32 * 4), torch.int32, dev), _new(stream, (m, groups), sdt, dev),
+                  _new(stream, (m, groups), torch.uint8, dev) if zeros else None, n=n, group=group)
+    _call("kd_quantise_4bit", kd_quantise_4bit, dev, stream, w.data_ptr(), _dtype_code(w.dtype), ld, out.ref)
+    return out
+
+
+def dequantise_4bit(w: Weight4, dtype=None, out=None, stream=None):
+    """The dense (m, n) matrix of 4-bit weights (kd_dequantise_4bit)."""
+    torch = _torch()
+    y = out if out is not None else _new(stream, (w.m, w.n), dtype or torch.float32, w.device)
+    ld = _rows(y, "out", _float_types(), w.device, (w.m, w.n))
+    _call("kd_dequantise_4bit", kd_dequantise_4bit, w.device, stream, w.ref, _dtype_code(y.dtype), y.data_ptr(), ld)
+    return y
+
+
+def matmul_4bit(w: Weight4, x, scale=None, out=None, out_dtype=None, stream=None):
+    """``Y = X W^T`` for few rows ``x`` (rows, n) in fp16, bf16 or float8_e4m3fn (then with
+    ``scale``, fp32 (rows,), as rmsnorm leaves them) and 4-bit weights (kd_matmul_4bit);
+    returns (rows, m), fp32 unless ``out`` or ``out_dtype`` says otherwise."""
+    torch = _torch()
+    if x.dim() != 2 or x.shape[1] != w.n:
+        raise ValueError(f"x must be (rows, {w.n})")
+    dev, rows = w.device, x.shape[0]
+    ldx = _rows(x, "x", (torch.float16, torch.bfloat16, torch.float8_e4m3fn), dev)
+    if scale is not None:
+        _rows(scale, "scale", (torch.float32,), dev, (rows,))
+    y = out if out is not None else _new(stream, (rows, w.m), out_dtype or torch.float32, dev)
+    ldy = _rows(y, "out", _float_types(), dev, (rows, w.m))
+    xdt = KD_E4M3 if x.dtype == torch.float8_e4m3fn else _dtype_code(x.dtype)
+    _call("kd_matmul_4bit", kd_matmul_4bit, dev, stream, w.ref, x.data_ptr(), xdt, _ptr(scale), rows, ldx,
+          y.data_ptr(), _dtype_code(y.dtype), ldy)
+    return y
+
+
+@dataclasses.dataclass
+class TokenLogprobs:
+    logprobs: "object"      # float32 (rows, tokens)
+    lse: "object"           # float32 (rows,) or None
+    entropy: "object"       # float32 (rows,) or None
+    top_ids: "object"       # int64 (rows, top)
+    top_logprobs: "object"  # float32 (rows, top)
+
+
+def token_logprobs(logits, ids, top: int = 0, out: Optional[TokenLogprobs] = None, stream=None) -> TokenLogprobs:
+    """Log probabilities of the tokens ``ids`` (int64 (rows,) or (rows, tokens); negative:
+    padding, 0) under softmax of the rows of ``logits`` (rows, vocab), the entropy and the
+    ``top`` (0..32) likeliest alternatives (kd_token_logprobs)."""
+    torch = _torch()
+    if logits.dim() != 2:
+        raise ValueError("logits must be 2-D")
+    dev, (rows, vocab) = logits.device, logits.shape
+    ld = _rows(logits, "logits", _float_types(), dev)
+    if ids.dim() == 1:
+        ids = ids[:, None]
+    if ids.dim() != 2 or ids.shape[0] != rows or ids.dtype != torch.int64 or ids.device != dev \
+            or not ids.is_contiguous():
+        raise ValueError("ids must be a contiguous int64 (rows,) or (rows, tokens) tensor on the logits' device")
+    tokens = ids.shape[1]
+    top = int(top)
+    if not 0 <= top <= min(vocab, KD_MAX_TOP):
+        raise ValueError(f"top must be 0..{min(vocab, KD_MAX_TOP)}")
+    f32 = torch.float32
+    if out is None:
+        out = TokenLogprobs(_new(stream, (rows, tokens), f32, dev), _new(stream, (rows,), f32, dev),
+                            _new(stream, (rows,), f32, dev), _new(stream, (rows, top), torch.int64, dev),
+                            _new(stream, (rows, top), f32, dev))
+    else:
+        for t, name, dt, shape in ((out.logprobs, "logprobs", f32, (rows, tokens)), (out.lse, "lse", f32, (rows,)),
+                                   (out.entropy, "entropy", f32, (rows,)),
+                                   (out.top_ids, "top_ids", torch.int64, (rows, top)),
+                                   (out.top_logprobs, "top_logprobs", f32, (rows, top))):
+            if t is None and name in ("lse", "entropy"):
+                continue
+            if t is None or t.dtype != dt or t.shape != shape or t.device != dev or not t.is_contiguous():
+                raise ValueError(f"out.{name} must be a contiguous {dt} {shape} tensor on the logits' device")
+    _call("kd_token_logprobs", kd_token_logprobs, dev, stream, logits.data_ptr(), _dtype_code(logits.dtype), rows,
+          vocab, ld, ids.data_ptr(), tokens, top, out.logprobs.data_ptr(), _ptr(out.lse), _ptr(out.entropy),
+          out.top_ids.data_ptr(), out.top_logprobs.data_ptr())
+    return out
