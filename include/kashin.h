@@ -531,11 +531,13 @@ kd_status kd_rmsnorm(const void* x, kd_dtype dtype, int64_t n, int64_t rows, int
 
 /* A matrix of 4-bit weights with a scale (and optionally a zero point) for each group of
  * `group` consecutive inputs of an output channel:
- *   w[j][i] = scale[j][i / group] * (code[j][i] - zero[j][i / group]).
+ *   w[j][i] = scale[i / group][j] * (code[j][i] - zero[i / group][j]).
  *   codes   device, 16-byte aligned, m rows of 4 ceil(n/32) uint32: code i of a row at
  *           bits 4(i % 8) of word i/8; the padding codes past n are read but do not count.
- *   scales  device, m rows of ceil(n/group) values of scale_dtype (KD_F16 or KD_BF16).
- *   zeros   device, m rows of ceil(n/group) bytes in 0..15, or NULL: 8 everywhere.
+ *   scales  device, ceil(n/group) rows of m values of scale_dtype (KD_F16 or KD_BF16):
+ *           the scales of one group of inputs for all channels are consecutive, as a tile
+ *           of channels reads them.
+ *   zeros   device, ceil(n/group) rows of m bytes in 0..15, or NULL: 8 everywhere.
  *   group   32, 64 or 128. */
 typedef struct kd_weight4 {
   const uint32_t* codes;
@@ -569,15 +571,16 @@ kd_status kd_dequantise_4bit(const kd_weight4* w, kd_dtype out_dtype, void* out,
  *   x       device, x_dtype KD_F16, KD_BF16 or KD_E4M3; x_scale: rows fp32 (the e4m3
  *           rows' scales, as kd_rmsnorm leaves them), or NULL: 1.
  *   y       device, y_dtype KD_F32, KD_F16 or KD_BF16.
- * Meant for few rows (decoding): 32 rows share one pass over the weights, more rows take
- * more passes.  Within a group the sum over integers code - zero is formed on the tensor
+ * Meant for few rows (decoding): up to 32 rows share one pass over the weights, more rows
+ * take more passes.  Within a group the sum over integers code - zero is formed on the tensor
  * cores (exact products, fp32 sums); groups are added in fp32 with their scale, and the
- * whole is rounded once.  The order of the sums is fixed (deterministic results), and a
- * row's result does not depend on the other rows' values.
+ * whole is rounded once.  The order of the sums is fixed (deterministic results), and is
+ * the same for all calls of at most eight rows: a row's bits do not depend on what shares
+ * its batch.  An infinity or NaN in a row leaves nothing finite in that row alone.
  * Rows of 16-byte aligned base and stride (8-byte for e4m3) take wide loads.
  * Errors: KD_ERR_INVALID_ARG (sizes, group, types, ld < n or ldy < m, pointers missing
- * with m > 0 and rows > 0, or unaligned), KD_ERR_CUDA.  m == 0 or rows == 0 enqueues
- * nothing. */
+ * with m > 0 and rows > 0, or unaligned), KD_ERR_UNSUPPORTED_N (n > 65536), KD_ERR_CUDA.
+ * m == 0 or rows == 0 enqueues nothing. */
 kd_status kd_matmul_4bit(const kd_weight4* w, const void* x, kd_dtype x_dtype, const float* x_scale, int64_t rows,
                          int64_t ldx, void* y, kd_dtype y_dtype, int64_t ldy, void* stream);
 

@@ -5,15 +5,43 @@ namespace kd {
 namespace mat4 {
 namespace {
 
-constexpr int kPassRows = 32;
+constexpr int64_t kMaxN = 65536;
+constexpr size_t kSmem = 227 * 1024;
 
-// CTAs that share a tile's inputs: enough CTAs for two on each of 152 SMs, as long as
-// every warp keeps at least one chunk.
-int split_of(int m, int chunks) {
-  const int tiles = (m + kTile - 1) / kTile;
-  int s = 1;
-  while (s < 8 && tiles * s < 304 && chunks >= 2 * s * kWarps) s *= 2;
-  return s;
+// CTAs of one launch that run at a time, one an SM: clusters of `split` on 152 SMs, less what
+// the GPU's partitions leave over.
+int room(int split) { return split == 1 ? 152 : split == 2 ? 76 : split == 4 ? 36 : 15; }
+
+// How the work is split: CTAs of a cluster (split) and warps (kw) that share a tile's
+// inputs, for `rows` rows in nt tiles of eight.  The cost counts chunks of one warp, one
+// after the other: a tile's chunks, and what joining its sums takes (half a chunk, one and a
+// half across a cluster: fitted to layers of 4096, 11008 and 32000 channels at all splits).
+// False if the rows fit no CTA's shared memory.
+bool plan(Params& p, int nt, int rows) {
+  bool found = false;
+  double least = 0;
+  for (int split = 1; split <= 8; split *= 2) {
+    const int per = (p.chunks + split - 1) / split;
+    if (split > 1 && per < 2) break;
+    for (int kw = warps_of(nt); kw >= 1; kw /= 2) {
+      if (smem_bytes(nt, rows, per, split, kw) > kSmem) continue;
+      const int channels = kTile * warps_of(nt) / kw;
+      const int tiles = (p.m + channels - 1) / channels;
+      const int at_once = room(split);
+      const double rounds = (tiles + at_once - 1) / at_once;
+      const double cost = rounds * ((per + kw - 1) / kw + (split > 1 ? 1.5 : 0.5));
+      if (!found || cost < least) {
+        found = true;
+        least = cost;
+        p.split = split;
+        p.kw = kw;
+        p.kw_log = kw == 16 ? 4 : kw == 8 ? 3 : kw == 4 ? 2 : kw - 1;
+        p.per = per;
+        p.tiles = tiles;
+      }
+    }
+  }
+  return found;
 }
 
 }  // namespace
@@ -28,13 +56,14 @@ extern "C" kd_status kd_matmul_4bit(const kd_weight4* w, const void* x, kd_dtype
   if (!weight4_sizes_ok(w) || rows < 0 || (x_dtype != KD_F16 && x_dtype != KD_BF16 && x_dtype != KD_E4M3) ||
       !float_type(y_dtype) || ldx < w->n || ldy < w->m)
     return KD_ERR_INVALID_ARG;
+  if (w->n > kMaxN) return KD_ERR_UNSUPPORTED_N;
   if (w->m == 0 || rows == 0) return KD_OK;
   const int64_t xb = type_bytes(x_dtype), yb = type_bytes(y_dtype);
   if (!x || !y || !weight4_pointers_ok(w) || !aligned(x, (size_t)xb) || !aligned(y, (size_t)yb) ||
       !aligned(x_scale, 4))
     return KD_ERR_INVALID_ARG;
   Params p{};
-  p.codes = w->codes;
+  p.codes = reinterpret_cast<const uint8_t*>(w->codes);
   p.scales = static_cast<const uint16_t*>(w->scales);
   p.zeros = w->zeros;
   p.ldx = ldx;
@@ -44,22 +73,38 @@ extern "C" kd_status kd_matmul_4bit(const kd_weight4* w, const void* x, kd_dtype
   p.groups = (int)((w->n + w->group - 1) / w->group);
   p.pieces = (int)((w->n + 31) / 32);
   p.chunks = (int)((w->n + kChunk - 1) / kChunk);
-  p.split = split_of(p.m, p.chunks);
-  p.per = (p.chunks + p.split - 1) / p.split;
+  p.scale_vec = w->m % 4 == 0 && aligned(w->scales, 8) && aligned(w->zeros, 4);
   p.scale_bf16 = w->scale_dtype == KD_BF16;
   p.ydtype = (int)y_dtype;
-  const size_t wide = x_dtype == KD_E4M3 ? 8 : 16;
+  p.e4m3 = x_dtype == KD_E4M3;
+  const bool bf = x_dtype == KD_BF16;
+  const int gs = w->group / 32;
+  const size_t wide = p.e4m3 ? 8 : 16;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  for (int64_t r0 = 0; r0 < rows; r0 += kPassRows) {
-    p.rows = (int)(rows - r0 < kPassRows ? rows - r0 : kPassRows);
+  // passes of equal numbers of rows, at most 8 most
+  bool planned = false;
+  int nt = 0;
+  int64_t pass = 0;
+  for (int most = 4; most && !planned; most /= 2) {
+    const int64_t passes = (rows + 8 * most - 1) / (8 * most);
+    pass = (rows + passes - 1) / passes;
+    nt = pass > 16 ? 4 : pass > 8 ? 2 : 1;
+    // up to eight rows split the work alike, so that a row's sums have one order whatever
+    // else is in the batch
+    planned = plan(p, nt, nt == 1 ? 8 : (int)pass);
+  }
+  if (!planned) return KD_ERR_UNSUPPORTED_N;
+  p.turns_of_row_inv = 1.f / (float)((p.per * 16 + 31) / 32);
+  const int clusters = p.tiles < room(p.split) ? p.tiles : room(p.split);
+  for (int64_t r0 = 0; r0 < rows; r0 += pass) {
+    p.rows = (int)(rows - r0 < pass ? rows - r0 : pass);
     p.x = static_cast<const uint8_t*>(x) + r0 * ldx * xb;
     p.xs = x_scale ? x_scale + r0 : nullptr;
     p.y = static_cast<uint8_t*>(y) + r0 * ldy * yb;
-    p.xvec = aligned(p.x, wide) && (p.rows == 1 || ldx * xb % (int64_t)wide == 0);
-    const int gs = w->group / 32;
-    const cudaError_t e = x_dtype == KD_F16   ? launch_half(p, gs, s)
-                          : x_dtype == KD_BF16 ? launch_bf16(p, gs, s)
-                                               : launch_e4m3(p, gs, s);
+    p.x_vec = aligned(p.x, wide) && (p.rows == 1 || ldx * xb % (int64_t)wide == 0);
+    const cudaError_t e = gs == 1   ? launch_group32(p, bf, nt, clusters, s)
+                          : gs == 2 ? launch_group64(p, bf, nt, clusters, s)
+                                    : launch_group128(p, bf, nt, clusters, s);
     if (e != cudaSuccess || cudaGetLastError() != cudaSuccess) return KD_ERR_CUDA;
   }
   return KD_OK;

@@ -1,29 +1,39 @@
 // Products of few activation rows with 4-bit weights and group scales (kd_matmul_4bit):
 //
-//     y[r][j] = xs[r] sum_g s[j][g] sum_{i in g} (c[j][i] - z[j][g]) x[r][i]
+//     y[r][j] = xs[r] sum_g s[g][j] sum_{i in g} (c[j][i] - z[g][j]) x[r][i]
 //
-// on the tensor cores with the weights as the mma's A operand (16 channels) and the
-// activation rows as B (8 rows), so that 8 rows fill a tile.
+// on the tensor cores in 16 bits (mma.sync m16n8k16), with the weights as the A operand (16
+// channels) and the activation rows as B, so that 8 rows fill a tile.  e4m3 rows are taken
+// as the fp16 values they are.
 //
-// Mapping.  A CTA owns 32 channels; its eight warps, and the CTAs of a cluster, split the
-// inputs into chunks of 128 and add their partial sums in a fixed order.  Per chunk a warp
-// copies its 32 x 64 bytes of codes and its rows' inputs to its own ring of stages in
-// shared memory (cp.async), so that several chunks are in flight and no barrier of the
-// CTA stands in the loop.
+// Codes.  Masked into the mantissa of a power of two a code makes 1024 + c (fp16, in a
+// half's low bits) or 64 + c (four bits higher) or 128 + c (bf16), and a packed subtraction
+// leaves the integer c - z.  Products are exact, sums fp32.  A word of eight takes one shift
+// (bf16, whose mantissa holds one place only: three) and four mask-ors, on the integer pipe
+// of half the issue rate that this costs most.  (Products in e4m3, in which a code is a byte
+// without any arithmetic, were measured at half the speed: mma.sync runs them as fp16 with
+// conversions of both operands.)
+//
+// Mapping.  One CTA per SM stays and walks tiles of channels.  A warp owns 32 channels of
+// the tile; kw warps split the inputs among them (chunks of 128), and where that is not
+// enough CTAs of a cluster do too.  The partial sums are added in a fixed order.  The rows
+// of the CTA's inputs are laid out once in shared memory as the B operands that the lanes
+// will want.  The codes stream through a ring of stages that each lane fills and reads for
+// itself (cp.async; smaller groups: the lanes of a warp for each other): no barrier of the CTA stands in the loop, and the copies of the next tile are in
+// flight while this one's sums are joined.
 //
 // K order.  The product is a sum over inputs, so A and B may enumerate them in any common
-// order.  Step q of a chunk covers inputs 32q .. 32q + 31; the lanes with t = lane % 4
-// take code word 4q + t of their channel (inputs 32q + 8t .. + 7) and the same eight
-// inputs of their row.
+// order.  A group of GS x 32 inputs is 4 GS code words of a channel; the lanes with
+// t = lane % 4 take the words GS t .. GS t + GS - 1, one a step, and the same inputs of
+// their row.
 //
-// Codes to operands.  16-bit inputs: a mask and a shift bring codes i and i + 4 of a word
-// to the low bits of two halves, an OR makes them 1024 + c (fp16) or 128 + c (bf16), and
-// one packed subtraction makes c - z: every step is exact.  e4m3 inputs: the byte c in
-// 0..15 read as e4m3 is exactly c 2^-9 (subnormals and the first binade are evenly
-// spaced), so a mask suffices; the byte 0x80 | z is -z 2^-9, and a second mma with it as A
-// subtracts the zero point.
+// Channel order.  Rows g, g + 8 of the two mma tiles (g = lane / 4) are channels 4g .. 4g + 3
+// of the warp's 32, so that a lane's four scales are one load of 8 bytes.
 #pragma once
 #include <cooperative_groups.h>
+#include <cuda_fp8.h>
+
+#include <atomic>
 
 #include "kd_weight4.cuh"
 
@@ -32,15 +42,14 @@ namespace mat4 {
 
 using namespace serve;
 
-constexpr int kWarps = 8;
-constexpr int kThreads = 32 * kWarps;
-constexpr int kTile = 32;    // output channels of a CTA: two m16 tiles
+constexpr int kTile = 32;    // output channels of a warp: two m16 tiles
 constexpr int kChunk = 128;  // inputs of a chunk
-
-enum { kHalf = 0, kBf16 = 1, kE4M3 = 2 };
+constexpr int kStages = 3;
+constexpr int kStageUnits = 128;  // 16-byte units of a stage: 32 channels x 64 bytes
+constexpr int kSumStride = 36;    // floats of one row's 32 partial sums, padded
 
 struct Params {
-  const uint32_t* codes;
+  const uint8_t* codes;
   const uint16_t* scales;
   const uint8_t* zeros;
   const uint8_t* x;
@@ -48,352 +57,448 @@ struct Params {
   void* y;
   int64_t ldx, ldy;
   int n, m, rows;
-  int groups, pieces, chunks;  // per row: scales, 16-byte pieces of codes; chunks of 128 inputs
+  int e4m3;                    // x holds bytes
+  int groups, pieces, chunks;  // per channel: scales, 16-byte pieces of codes; chunks of 128 inputs
   int per;                     // chunks of one CTA of a cluster
+  float turns_of_row_inv;      // 1 / (32-item turns of a row's inputs in one CTA)
   int split;                   // CTAs of a cluster
-  int xvec, scale_bf16, ydtype;
+  int kw, kw_log;              // warps that split the inputs of a tile (a power of two)
+  int tiles;                   // of 32 * warps / kw channels
+  int x_vec, scale_vec, scale_bf16, ydtype;
 };
 
-template <int XK>
-constexpr int x_bytes = XK == kE4M3 ? 1 : 2;
-// 16-byte units of one stage of one warp: codes, then inputs
-template <int XK, int NT>
-constexpr int stage_units = 128 + NT * 64 * x_bytes<XK>;
-template <int XK, int NT>
-constexpr int stages = NT == 1 ? (XK == kE4M3 ? 4 : 3) : NT == 2 ? (XK == kE4M3 ? 3 : 2) : 2;
-template <int XK, int NT>
-constexpr size_t smem_bytes = (size_t)kWarps * stages<XK, NT> * stage_units<XK, NT> * 16;
+// warps of a CTA for nt tiles of rows: several tiles' sums want twice the registers
+template <int NT>
+constexpr int kWarps = NT == 1 ? 16 : 8;
+inline int warps_of(int nt) { return nt == 1 ? 16 : 8; }
+// Shared memory, in bytes: the ring; the warps' partial sums; the rows; for clusters two
+// sets of the CTA's sums.
+constexpr size_t kRingBytes = (size_t)kStages * kStageUnits * 16;  // of a warp
+constexpr size_t kRedBytes = (size_t)8 * kSumStride * 4;           // of a warp, for each 8 rows
+inline size_t smem_bytes(int nt, int rows, int per, int split, int kw) {
+  const size_t outputs = (size_t)kTile * (warps_of(nt) / kw) * rows;
+  return warps_of(nt) * (kRingBytes + nt * kRedBytes) + (size_t)per * nt * 2048 +
+         (split > 1 ? 2 * outputs * 4 : 0);
+}
 
-__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-// `bytes` of N from src, the rest of the N zero
-template <int N>
-__device__ __forceinline__ void copy_async(void* dst, const void* src, int bytes) {
-  if constexpr (N == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(dst)), "l"(src), "r"(bytes) : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(smem_addr(dst)), "l"(src), "r"(bytes) : "memory");
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// this CTA's rank in its cluster, the cluster's index, the launch's clusters (CTAs without one
+// are clusters of their own)
+enum { kRank, kCluster, kClusters };
+template <int WHAT>
+__device__ __forceinline__ int special() {
+  int r;
+  if constexpr (WHAT == kRank) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  else if constexpr (WHAT == kCluster) asm("mov.u32 %0, %%clusterid.x;" : "=r"(r));
+  else asm("mov.u32 %0, %%nclusterid.x;" : "=r"(r));
+  return r;
+}
 template <int N>
 __device__ __forceinline__ void wait_group() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-template <int XK>
+// D = A B (+ D unless FIRST)
+template <bool BF, bool FIRST>
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                     uint32_t b1) {
-  if constexpr (XK == kHalf)
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-        "{%0, %1, %2, %3};\n"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  else if constexpr (XK == kBf16)
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-        "{%0, %1, %2, %3};\n"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  else
-    asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-        "{%0, %1, %2, %3};\n"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+#define KD_MMA(TYPE)                                                                                             \
+  if constexpr (FIRST)                                                                                           \
+    asm("mma.sync.aligned.m16n8k16.row.col.f32." TYPE "." TYPE ".f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, " \
+        "{%10, %10, %10, %10};\n"                                                                                \
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])                                                         \
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));                                       \
+  else                                                                                                           \
+    asm("mma.sync.aligned.m16n8k16.row.col.f32." TYPE "." TYPE ".f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, " \
+        "{%0, %1, %2, %3};\n"                                                                                    \
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])                                                         \
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1))
+  if constexpr (BF) {
+    KD_MMA("bf16");
+  } else {
+    KD_MMA("f16");
+  }
+#undef KD_MMA
 }
 
-// the zero point as the decode wants it: packed 1024 + z or 128 + z, or four bytes -z 2^-9
-template <int XK>
-__device__ __forceinline__ uint32_t zero_word(uint32_t z) {
-  if constexpr (XK == kHalf) return (0x6400u + z) * 0x10001u;
-  else if constexpr (XK == kBf16) return (0x4300u + z) * 0x10001u;
-  else return (0x80u | z) * 0x01010101u;
+// (a & MASK) | b in one operation: b comes in a register, the mask is its one immediate
+template <uint32_t MASK>
+__device__ __forceinline__ uint32_t mask_or(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(a), "n"(MASK), "r"(b));
+  return r;
 }
-// codes i and i + 4 of a word, less the zero point, as two 16-bit values
-template <int XK>
-__device__ __forceinline__ uint32_t code_pair(uint32_t w, int i, uint32_t zw) {
-  if constexpr (XK == kHalf) {
-    const uint32_t v = ((w >> (4 * i)) & 0x000F000Fu) | 0x64006400u;
-    const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&zw));
+// What the codes are or-ed into, in registers whose values the compiler does not know (a
+// constant would be a second immediate, and a second operation).
+template <bool BF>
+struct Magic {
+  uint32_t low, high;
+  __device__ __forceinline__ Magic() {
+    if constexpr (BF) {
+      asm volatile("mov.u32 %0, 0x43004300;" : "=r"(low));
+      high = 0;
+    } else {
+      asm volatile("mov.u32 %0, 0x64006400;" : "=r"(low));
+      asm volatile("mov.u32 %0, 0x54005400;" : "=r"(high));
+    }
+  }
+};
+// a zero point as it comes off: 1024 + z and 64 + z (fp16), or 128 + z (bf16), twice a word
+template <bool BF>
+__device__ __forceinline__ uint2 zero_words(uint32_t z) {
+  if constexpr (BF) return make_uint2((0x4300u + z) * 0x10001u, 0u);
+  else return make_uint2((0x6400u + z) * 0x10001u, (0x5400u + 16u * z) * 0x10001u);
+}
+template <bool BF>
+__device__ __forceinline__ uint32_t minus2(uint32_t a, uint32_t b) {
+  if constexpr (BF) {
+    const __nv_bfloat162 d =
+        __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
     return *reinterpret_cast<const uint32_t*>(&d);
   } else {
-    const uint32_t v = ((w >> (4 * i)) & 0x000F000Fu) | 0x43004300u;
-    const __nv_bfloat162 d =
-        __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), *reinterpret_cast<const __nv_bfloat162*>(&zw));
+    const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
     return *reinterpret_cast<const uint32_t*>(&d);
   }
 }
+// codes 2h, 2h + 4 and 2h + 1, 2h + 5 of a word, less the zero point
+template <bool BF>
+__device__ __forceinline__ uint2 code_pairs(uint32_t w, int h, const Magic<BF>& k, uint2 zero) {
+  w >>= 8 * h;
+  if constexpr (BF)
+    return make_uint2(minus2<BF>(mask_or<0x000F000Fu>(w, k.low), zero.x),
+                      minus2<BF>(mask_or<0x000F000Fu>(w >> 4, k.low), zero.x));
+  else
+    return make_uint2(minus2<BF>(mask_or<0x000F000Fu>(w, k.low), zero.x),
+                      minus2<BF>(mask_or<0x00F000F0u>(w, k.high), zero.y));
+}
 
-// GS: 32-input steps of a group (1, 2, 4); NT: 8-row tiles of one pass
-template <int XK, int GS, int NT>
-__global__ void __launch_bounds__(kThreads) mat4_kernel(const __grid_constant__ Params p) {
-  constexpr int kStages = stages<XK, NT>, kUnits = stage_units<XK, NT>, kGroups = 4 / GS;
-  constexpr int XB = x_bytes<XK>;
+// eight consecutive inputs of a row from k on as four words of 16-bit values (e4m3: two words
+// of bytes): all of them and aligned, or one by one and zero past n
+__device__ __forceinline__ uint4 load_inputs(const Params& p, int64_t at) {
+  if (p.e4m3) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p.x + at);
+    return make_uint4(u.x, u.y, 0, 0);
+  }
+  return *reinterpret_cast<const uint4*>(p.x + 2 * at);
+}
+static __device__ __noinline__ uint4 load_inputs_one_by_one(const uint8_t* x, int e4m3, int64_t at, int have) {
+  uint32_t v[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < have) {
+      if (e4m3) v[e / 4] |= (uint32_t)x[at + e] << (8 * (e % 4));
+      else v[e / 2] |= (uint32_t) reinterpret_cast<const uint16_t*>(x)[at + e] << (16 * (e % 2));
+    }
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ uint4 bytes_to_half(uint4 v) {
+  auto two = [](uint32_t w) {
+    const __half2 h(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, __NV_E4M3));
+    return *reinterpret_cast<const uint32_t*>(&h);
+  };
+  return make_uint4(two(v.x & 0xFFFFu), two(v.x >> 16), two(v.y & 0xFFFFu), two(v.y >> 16));
+}
+
+// BF: bf16 rows; GS: 32-input steps of a group (1, 2, 4); NT: 8-row tiles of one pass; ZEROS:
+// zero points by group
+template <bool BF, int GS, int NT, bool ZEROS>
+__global__ void __launch_bounds__(32 * kWarps<NT>, 1) mat4_kernel(const __grid_constant__ Params p) {
+  constexpr int W = kWarps<NT>, kThreads = 32 * W;
+  constexpr int kGroups = 4 / GS;  // groups of a chunk
+  constexpr int kCols = 8 * NT;
+  constexpr int kBatch = 4;        // loads of rows in flight
+  namespace cg = cooperative_groups;
   extern __shared__ uint4 smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const int rank = p.split > 1 ? (int)(blockIdx.x % p.split) : 0;
-  const int j0 = (int)(blockIdx.x / p.split) * kTile;
-  const int c_end = min(p.chunks, (rank + 1) * p.per);
-  uint4* ring = smem + warp * kStages * kUnits;
+  const int mw = W >> p.kw_log, mi = warp >> p.kw_log, ki = warp & (p.kw - 1);
+  const int tile_log = (W == 16 ? 9 : 8) - p.kw_log;  // of the CTA's channels, 32 mw
+  const int rank = special<kRank>(), first = special<kCluster>(), step = special<kClusters>();
+  const int c0 = rank * p.per, mine = min(p.per, p.chunks - c0);  // this CTA's chunks
+  const int outputs = p.rows << tile_log;
 
-  // inputs of rows past the batch stay zero in every stage
-  for (int st = 0; st < kStages; ++st)
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-      if (8 * j + g >= p.rows)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          if constexpr (XB == 2) ring[st * kUnits + 128 + (j * 4 + q) * 32 + lane] = make_uint4(0, 0, 0, 0);
-          else reinterpret_cast<uint2*>(ring + st * kUnits + 128)[(j * 4 + q) * 32 + lane] = make_uint2(0, 0);
-        }
+  float* red = reinterpret_cast<float*>(smem + W * kRingBytes / 16);
+  uint4* xb = reinterpret_cast<uint4*>(red + W * NT * kRedBytes / 4);
+  float* csum = reinterpret_cast<float*>(xb + p.per * NT * 128);
 
-  auto issue = [&](int c, int st) {
-    uint4* to = ring + st * kUnits;
-    const int piece = 4 * c + t;  // of the row's codes
+  // The rows.  An item is 8 inputs of one row, the operands of step q for the lane (row,
+  // ot): 16 items a chunk.  A warp takes 32 consecutive items of a row at a time.  The first
+  // loads go out before anything else: the CTA's first barrier waits for them.
+  const int turns_of_row = (p.per * 16 + 31) / 32, turns = p.rows * turns_of_row;
+  auto take = [&](int turn, int& row, int& item) {
+    row = (int)((turn + 0.5f) * p.turns_of_row_inv);  // exact: turns are few
+    item = (turn - row * turns_of_row) * 32 + lane;
+    const int k = c0 * kChunk + 8 * item;
+    const int64_t at = (int64_t)row * p.ldx + k;
+    if (turn >= turns || k >= p.n) return make_uint4(0, 0, 0, 0);
+    return p.x_vec && k + 8 <= p.n ? load_inputs(p, at) : load_inputs_one_by_one(p.x, p.e4m3, at, p.n - k);
+  };
+  uint4 v0[kBatch];
+  int row0[kBatch], item0[kBatch];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = g + 8 * i, row = j0 + r;
-      const bool in = row < p.m && piece < p.pieces;
-      copy_async<16>(to + r * 4 + (t ^ ((r >> 1) & 3)),
-                     p.codes + (in ? ((int64_t)row * p.pieces + piece) * 4 : 0), in ? 16 : 0);
-    }
+  for (int b = 0; b < kBatch; ++b) v0[b] = take(warp + b * W, row0[b], item0[b]);
+
+  // The warp's ring of codes.  This lane copies piece t of channels 4g + i to row 8i + g of
+  // a stage, at a place that lets a row's words be read 4, 8 or 16 bytes a lane without
+  // bank conflicts.
+  uint4* ring = smem + warp * (kRingBytes / 16);
+  const int swizzle = (g >> 1 & 1) * 2 + (g >> 2);
+  const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring + g * 4 + (t ^ swizzle));
+  int i_tile = first, i_l = ki, i_slot = 0;  // the next chunk to copy
+  const uint8_t* base = nullptr;  // of the tile's codes, and this lane's channels from there
+  uint32_t src[4];
+  auto point = [&](int tile) {
+    const int ch0 = tile * mw * kTile;
+    base = p.codes + (int64_t)ch0 * p.pieces * 16;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const int r = 8 * j + g;
-      if (r < p.rows) {
-        const uint8_t* xr = p.x + (int64_t)r * p.ldx * XB;
+    for (int i = 0; i < 4; ++i) src[i] = (uint32_t)(min(ch0 + mi * kTile + 4 * g + i, p.m - 1) - ch0) * p.pieces * 16u;
+  };
+  point(first);
+  auto issue = [&]() {
+    if (i_tile < p.tiles && ki < mine) {
+      // pieces past the row's end meet inputs that are zero: any piece will do
+      const uint32_t off = (uint32_t)min(4 * (c0 + i_l) + t, p.pieces - 1) * 16u;
+      const uint32_t to = ring_at + i_slot * (kStageUnits * 16);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int k = c * kChunk + 32 * q + 8 * t;
-          const int have = min(8, max(0, p.n - k));
-          if constexpr (XB == 2) {
-            uint4* slot = to + 128 + (j * 4 + q) * 32 + lane;
-            if (p.xvec) {
-              copy_async<16>(slot, xr + (have ? (int64_t)k * 2 : 0), 2 * have);
-            } else {
-              uint16_t v[8];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] = e < have ? reinterpret_cast<const uint16_t*>(xr)[k + e] : (uint16_t)0;
-              *slot = make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16,
-                                 v[4] | (uint32_t)v[5] << 16, v[6] | (uint32_t)v[7] << 16);
-            }
-          } else {
-            uint2* slot = reinterpret_cast<uint2*>(to + 128) + (j * 4 + q) * 32 + lane;
-            if (p.xvec) {
-              copy_async<8>(slot, xr + (have ? k : 0), have);
-            } else {
-              uint32_t v[2] = {0, 0};
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (e < have) v[e / 4] |= (uint32_t)xr[k + e] << (8 * (e % 4));
-              *slot = make_uint2(v[0], v[1]);
-            }
-          }
-        }
+      for (int i = 0; i < 4; ++i) copy16(to + i * 512, base + (src[i] + off));
+      i_slot = i_slot + 1 == kStages ? 0 : i_slot + 1;
+      i_l += p.kw;
+      if (i_l >= mine) {
+        i_l = ki;
+        i_tile += step;
+        if (i_tile < p.tiles) point(i_tile);
       }
     }
+    commit();
   };
-
-  // this lane's four channels: scales and zero points of a chunk's groups
-  int at[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) at[i] = min(j0 + g + 8 * i, p.m - 1);
-  uint32_t sraw[4][kGroups], zraw[4][kGroups];
-  auto fetch_scales = [&](int c) {
+  for (int s = 0; s < kStages - 1; ++s) issue();
+
+  // scales and zero points of this lane's four channels in a chunk's groups
+  uint32_t sraw[kGroups][2], zraw[kGroups];
+  auto fetch_scales = [&](int tile, int l) {
+    const int ch = (tile * mw + mi) * kTile + 4 * g;
 #pragma unroll
     for (int k = 0; k < kGroups; ++k) {
-      const int gi = min(c * kGroups + k, p.groups - 1);
+      const int gi = (c0 + l) * kGroups + k;  // past the last group: inputs that are zero
+      const int64_t row = (int64_t)(GS == 4 ? gi : min(gi, p.groups - 1)) * p.m;
+      if (p.scale_vec) {
+        const int64_t at = row + min(ch, p.m - 4);
+        const uint2 v = *reinterpret_cast<const uint2*>(p.scales + at);
+        sraw[k][0] = v.x; sraw[k][1] = v.y;
+        if constexpr (ZEROS) zraw[k] = *reinterpret_cast<const uint32_t*>(p.zeros + at);
+      } else {
+        uint32_t s[4], z[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t o = (int64_t)at[i] * p.groups + gi;
-        sraw[i][k] = p.scales[o];
-        zraw[i][k] = p.zeros ? p.zeros[o] : 8u;
+        for (int i = 0; i < 4; ++i) {
+          const int64_t at = row + min(ch + i, p.m - 1);
+          s[i] = p.scales[at];
+          if constexpr (ZEROS) z[i] = p.zeros[at];
+        }
+        sraw[k][0] = s[0] | s[1] << 16; sraw[k][1] = s[2] | s[3] << 16;
+        if constexpr (ZEROS) zraw[k] = z[0] | z[1] << 8 | z[2] << 16 | z[3] << 24;
       }
     }
   };
+  if (ki < mine) fetch_scales(first, ki);
 
-  float acc[2][NT][4];
+  // Operands without a row are left as they are: a column of B meets one column of the sums.
+  auto put = [&](int row, int i, uint4 v) {
+    const int l = i >> 4, w = i & 15;  // w: the item's word of the chunk
+    if (l >= p.per) return;
+    const int ot = w / GS & 3, q = w / (4 * GS) * GS + w % GS;
+    const uint4 h = p.e4m3 ? bytes_to_half(v) : v;
+    // (x0, x4) (x1, x5) (x2, x6) (x3, x7), as the codes of a word come out
+    xb[((l * NT + row / 8) * 4 + q) * 32 + (row % 8) * 4 + ot] =
+        make_uint4(__byte_perm(h.x, h.z, 0x5410), __byte_perm(h.x, h.z, 0x7632), __byte_perm(h.y, h.w, 0x5410),
+                   __byte_perm(h.y, h.w, 0x7632));
+  };
 #pragma unroll
-  for (int mt = 0; mt < 2; ++mt)
+  for (int b = 0; b < kBatch; ++b)
+    if (warp + b * W < turns) put(row0[b], item0[b], v0[b]);
+#pragma unroll 1
+  for (int turn0 = warp + kBatch * W; turn0 < turns; turn0 += kBatch * W) {
+    uint4 v[kBatch];
+    int row[kBatch], item[kBatch];
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int b = 0; b < kBatch; ++b) v[b] = take(turn0 + b * W, row[b], item[b]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[mt][j][e] = 0.f;
-
-  int c = rank * p.per + warp;  // this warp's chunks: c, c + kWarps, ...
-#pragma unroll
-  for (int st = 0; st < kStages - 1; ++st) {
-    if (c + st * kWarps < c_end) issue(c + st * kWarps, st);
-    commit();
+    for (int b = 0; b < kBatch; ++b)
+      if (turn0 + b * W < turns) put(row[b], item[b], v[b]);
   }
-  if (c < c_end) fetch_scales(c);
+  __syncthreads();
 
-  for (int it = 0; c < c_end; ++it, c += kWarps) {
-    const int ahead = c + (kStages - 1) * kWarps;
-    if (ahead < c_end) issue(ahead, (it + kStages - 1) % kStages);
-    commit();
-    float sc[4][kGroups];
-    uint32_t zw[4][kGroups];
+  const Magic<BF> magic;
+  int slot = 0, parity = 0;
+  for (int tile = first; tile < p.tiles; tile += step) {
+    float acc[2][NT][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[mt][j][e] = 0.f;
+
+    for (int l = ki; l < mine; l += p.kw) {
+      if constexpr (GS != 4) __syncwarp();  // the stage filled next has been read by every lane
+      issue();
+      uint32_t sr[kGroups][2], zs[kGroups];
 #pragma unroll
       for (int k = 0; k < kGroups; ++k) {
-        sc[i][k] = p.scale_bf16 ? __uint_as_float(sraw[i][k] << 16) : __half2float(__ushort_as_half((unsigned short)sraw[i][k]));
-        zw[i][k] = zero_word<XK>(zraw[i][k]);
+        sr[k][0] = sraw[k][0]; sr[k][1] = sraw[k][1];
+        if constexpr (ZEROS) zs[k] = zraw[k];
       }
-    if (c + kWarps < c_end) fetch_scales(c + kWarps);
-    wait_group<kStages - 1>();
-    __syncwarp();
-    const uint4* from = ring + (it % kStages) * kUnits;
-    const uint32_t* words = reinterpret_cast<const uint32_t*>(from);
-    float part[2][NT][4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int k = q / GS;
-      if (q % GS == 0) {
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) part[mt][j][e] = 0.f;
-      }
-      uint32_t w[4];
+      if (l + p.kw < mine) fetch_scales(tile, l + p.kw);
+      else if (tile + step < p.tiles) fetch_scales(tile + step, ki);
+      wait_group<kStages - 1>();  // this lane's own copies (a group of 128: nobody else reads them)
+      if constexpr (GS != 4) __syncwarp();  // pieces of other lanes are wanted
+      const uint4* from = ring + slot * kStageUnits;
+      uint32_t raw[4][4];  // by channel: word of step q
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int r = g + 8 * i;
-        w[i] = words[(r * 4 + (q ^ ((r >> 1) & 3))) * 4 + t];
-      }
-      if constexpr (XB == 2) {
-        uint32_t b[NT][4];
+        const uint4* row = from + (8 * i + g) * 4;
+        if constexpr (GS == 4) {
+          const uint4 v = row[t ^ swizzle];
+          raw[i][0] = v.x; raw[i][1] = v.y; raw[i][2] = v.z; raw[i][3] = v.w;
+        } else if constexpr (GS == 2) {
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const uint4 v = from[128 + (j * 4 + q) * 32 + lane];
-          b[j][0] = __byte_perm(v.x, v.z, 0x5410);
-          b[j][1] = __byte_perm(v.x, v.z, 0x7632);
-          b[j][2] = __byte_perm(v.y, v.w, 0x5410);
-          b[j][3] = __byte_perm(v.y, v.w, 0x7632);
-        }
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t a0 = code_pair<XK>(w[2 * mt], 2 * h, zw[2 * mt][k]);
-            const uint32_t a1 = code_pair<XK>(w[2 * mt + 1], 2 * h, zw[2 * mt + 1][k]);
-            const uint32_t a2 = code_pair<XK>(w[2 * mt], 2 * h + 1, zw[2 * mt][k]);
-            const uint32_t a3 = code_pair<XK>(w[2 * mt + 1], 2 * h + 1, zw[2 * mt + 1][k]);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) mma<XK>(part[mt][j], a0, a1, a2, a3, b[j][2 * h], b[j][2 * h + 1]);
+          for (int k = 0; k < 2; ++k) {
+            const uint2 v = reinterpret_cast<const uint2*>(row + ((2 * k + t / 2) ^ swizzle))[t % 2];
+            raw[i][2 * k] = v.x; raw[i][2 * k + 1] = v.y;
           }
-      } else {
-        uint32_t b[NT][2];
+        } else {
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const uint2 v = reinterpret_cast<const uint2*>(from + 128)[(j * 4 + q) * 32 + lane];
-          b[j][0] = __byte_perm(v.x, v.y, 0x6420);
-          b[j][1] = __byte_perm(v.x, v.y, 0x7531);
-        }
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
-          const uint32_t a0 = w[2 * mt] & 0x0F0F0F0Fu, a1 = w[2 * mt + 1] & 0x0F0F0F0Fu;
-          const uint32_t a2 = (w[2 * mt] >> 4) & 0x0F0F0F0Fu, a3 = (w[2 * mt + 1] >> 4) & 0x0F0F0F0Fu;
-          const uint32_t z0 = zw[2 * mt][k], z1 = zw[2 * mt + 1][k];
-#pragma unroll
-          for (int j = 0; j < NT; ++j) {
-            mma<XK>(part[mt][j], z0, z1, z0, z1, b[j][0], b[j][1]);
-            mma<XK>(part[mt][j], a0, a1, a2, a3, b[j][0], b[j][1]);
-          }
+          for (int k = 0; k < 4; ++k) raw[i][k] = reinterpret_cast<const uint32_t*>(row + (k ^ swizzle))[t];
         }
       }
-      if (q % GS == GS - 1) {
+      slot = slot + 1 == kStages ? 0 : slot + 1;
+      const uint4* xl = xb + l * NT * 128 + lane;
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
+      for (int k = 0; k < kGroups; ++k) {
+        uint2 zero[4];
 #pragma unroll
-          for (int j = 0; j < NT; ++j)
+        for (int i = 0; i < 4; ++i) zero[i] = zero_words<BF>(ZEROS ? zs[k] >> (8 * i) & 255u : 8u);
+        float part[2][NT][4];
+#pragma unroll
+        for (int i = 0; i < GS; ++i) {
+          const int q = k * GS + i;
+          uint4 b[NT];
+#pragma unroll
+          for (int j = 0; j < NT; ++j) b[j] = xl[(j * 4 + q) * 32];
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint2 u = code_pairs<BF>(raw[2 * mt][q], h, magic, zero[2 * mt]);
+              const uint2 v = code_pairs<BF>(raw[2 * mt + 1][q], h, magic, zero[2 * mt + 1]);
+#pragma unroll
+              for (int j = 0; j < NT; ++j) {
+                if (i == 0 && h == 0) mma<BF, true>(part[mt][j], u.x, v.x, u.y, v.y, b[j].x, b[j].y);
+                else mma<BF, false>(part[mt][j], u.x, v.x, u.y, v.y, h ? b[j].z : b[j].x, h ? b[j].w : b[j].y);
+              }
+            }
+        }
+        float2 sc[2];
+        if (p.scale_bf16) {
+          sc[0] = unpack2<KD_BF16>(sr[k][0]); sc[1] = unpack2<KD_BF16>(sr[k][1]);
+        } else {
+          sc[0] = unpack2<KD_F16>(sr[k][0]); sc[1] = unpack2<KD_F16>(sr[k][1]);
+        }
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              acc[mt][j][e] = __fmaf_rn(sc[2 * mt + e / 2][k], part[mt][j][e], acc[mt][j][e]);
+              acc[mt][j][e] = __fmaf_rn(e / 2 ? sc[mt].y : sc[mt].x, part[mt][j][e], acc[mt][j][e]);
       }
     }
-    __syncwarp();  // every lane has read the stage before it is filled again
-  }
 
-  // the warps' sums, added in warp order; then the CTAs' of the cluster, in rank order
-  wait_group<0>();
-  __syncthreads();
-  float* red = reinterpret_cast<float*>(smem);
-  constexpr int kCols = 8 * NT, kStride = kTile + 1, kOut = kTile * kCols;
-#pragma unroll
-  for (int mt = 0; mt < 2; ++mt)
+    // the warps' sums of a channel, added in the order of their inputs
+    __syncthreads();  // the last tile's sums have been read
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        red[(warp * kCols + 8 * j + 2 * t + (e & 1)) * kStride + 16 * mt + g + 8 * (e >> 1)] = acc[mt][j][e];
-  __syncthreads();
-  float* sum = red;  // warp 0's part receives the CTA's sums
-  for (int o = threadIdx.x; o < kOut; o += kThreads) {
-    const int at0 = (o / kTile) * kStride + o % kTile;
-    float s = red[at0];
-#pragma unroll
-    for (int w = 1; w < kWarps; ++w) s += red[w * kCols * kStride + at0];
-    sum[at0] = s;
-  }
-  auto finish = [&](int o, float s) {
-    const int r = o / kTile, j = j0 + o % kTile;
-    if (r >= p.rows || j >= p.m) return;
-    if constexpr (XK == kE4M3) s *= 512.f;
-    if (p.xs) s *= p.xs[r];
-    store1_any(p.y, p.ydtype, (int64_t)r * p.ldy + j, s);
-  };
-  if (p.split == 1) {
-    for (int o = threadIdx.x; o < kOut; o += kThreads) finish(o, sum[(o / kTile) * kStride + o % kTile]);
-  } else {
-    namespace cg = cooperative_groups;
-    cg::cluster_group cl = cg::this_cluster();
-    cl.sync();
-    for (int o = rank * kThreads + threadIdx.x; o < kOut; o += p.split * kThreads) {
-      const int at0 = (o / kTile) * kStride + o % kTile;
-      float s = 0.f;
-      for (int k = 0; k < p.split; ++k) s += cl.map_shared_rank(sum, k)[at0];
-      finish(o, s);
+      for (int e = 0; e < 2; ++e)
+        *reinterpret_cast<float4*>(red + (warp * kCols + 8 * j + 2 * t + e) * kSumStride + 4 * g) =
+            make_float4(acc[0][j][e], acc[0][j][e + 2], acc[1][j][e], acc[1][j][e + 2]);
+    __syncthreads();
+    const int j0 = tile << tile_log;
+    auto finish = [&](int r, int ch, float s) {
+      if (j0 + ch >= p.m) return;
+      if (p.xs) s *= p.xs[r];
+      store1_any(p.y, p.ydtype, (int64_t)r * p.ldy + j0 + ch, s);
+    };
+    // output o: row o / (32 mw), channel o % (32 mw) of the tile
+    for (int o = threadIdx.x; o < outputs; o += kThreads) {
+      const int r = o >> tile_log, ch = o & ((1 << tile_log) - 1);
+      const float* at = red + (((ch / kTile) << p.kw_log) * kCols + r) * kSumStride + ch % kTile;
+      float s = at[0];
+#pragma unroll 5
+      for (int w = 1; w < p.kw; ++w) s += at[w * kCols * kSumStride];
+      if (p.split == 1) finish(r, ch, s);
+      else csum[parity * outputs + o] = s;
     }
-    cl.sync();  // no CTA leaves while its sums are read
+    if (p.split > 1) {
+      cg::cluster_group cl = cg::this_cluster();
+      cl.sync();
+      // two sets of sums: the barrier of the next tile comes before this one is written again
+      for (int o = rank * kThreads + threadIdx.x; o < outputs; o += p.split * kThreads) {
+        float s = 0.f;
+        for (int k = 0; k < p.split; ++k) s += cl.map_shared_rank(csum, k)[parity * outputs + o];
+        finish(o >> tile_log, o & ((1 << tile_log) - 1), s);
+      }
+      parity ^= 1;
+    }
   }
+  wait_group<0>();
+  if (p.split > 1) cg::this_cluster().sync();  // no CTA leaves while its sums are read
 }
 
-// the launch of one pass (at most 32 rows)
-template <int XK, int GS, int NT>
-cudaError_t launch_one(const Params& p, cudaStream_t s) {
-  auto kernel = mat4_kernel<XK, GS, NT>;
-  constexpr size_t bytes = smem_bytes<XK, NT>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+// the launch of one pass
+template <bool BF, int GS, int NT, bool ZEROS>
+cudaError_t launch_one(const Params& p, int clusters, cudaStream_t s) {
+  auto kernel = mat4_kernel<BF, GS, NT, ZEROS>;
+  static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use its shared memory
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
+  if (dev >= 64 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+    if (e != cudaSuccess) return e;
+    if (dev < 64) ready.fetch_or((uint64_t)1 << dev, std::memory_order_relaxed);
+  }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((p.m + kTile - 1) / kTile * p.split));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = bytes;
+  cfg.gridDim = dim3((unsigned)(clusters * p.split));
+  cfg.blockDim = dim3(32 * kWarps<NT>);
+  cfg.dynamicSmemBytes = smem_bytes(NT, p.rows, p.per, p.split, p.kw);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)p.split;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = p.split > 1 ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-template <int XK>
-cudaError_t launch(const Params& p, int gs, cudaStream_t s) {
-  const int nt = p.rows <= 8 ? 1 : p.rows <= 16 ? 2 : 4;
-#define KD_MAT4(G, N) \
-  if (gs == G && nt == N) return launch_one<XK, G, N>(p, s);
-  KD_MAT4(1, 1) KD_MAT4(1, 2) KD_MAT4(1, 4) KD_MAT4(2, 1) KD_MAT4(2, 2) KD_MAT4(2, 4) KD_MAT4(4, 1) KD_MAT4(4, 2)
-  KD_MAT4(4, 4)
-#undef KD_MAT4
-  return cudaErrorInvalidValue;
+template <bool BF, int GS>
+cudaError_t launch(const Params& p, int nt, int clusters, cudaStream_t s) {
+  if (p.zeros)
+    return nt == 1   ? launch_one<BF, GS, 1, true>(p, clusters, s)
+           : nt == 2 ? launch_one<BF, GS, 2, true>(p, clusters, s)
+                     : launch_one<BF, GS, 4, true>(p, clusters, s);
+  return nt == 1   ? launch_one<BF, GS, 1, false>(p, clusters, s)
+         : nt == 2 ? launch_one<BF, GS, 2, false>(p, clusters, s)
+                   : launch_one<BF, GS, 4, false>(p, clusters, s);
 }
 
-cudaError_t launch_half(const Params& p, int gs, cudaStream_t s);
-cudaError_t launch_bf16(const Params& p, int gs, cudaStream_t s);
-cudaError_t launch_e4m3(const Params& p, int gs, cudaStream_t s);
+// bf: bf16 rows
+cudaError_t launch_group32(const Params& p, bool bf, int nt, int clusters, cudaStream_t s);
+cudaError_t launch_group64(const Params& p, bool bf, int nt, int clusters, cudaStream_t s);
+cudaError_t launch_group128(const Params& p, bool bf, int nt, int clusters, cudaStream_t s);
 
 }  // namespace mat4
 }  // namespace kd

@@ -18,7 +18,7 @@ struct QuantParams {
   uint32_t* codes;
   void* scales;
   uint8_t* zeros;
-  int64_t n, m, ld, words, groups, chunks;
+  int64_t n, m, ld, words, chunks;
   int dtype, scale_dtype, group;
 };
 
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(256) quantise4_kernel(const __grid_constant__ 
     const int64_t word = i0 / 8;
     if (!(lane & 1) && word < p.words) p.codes[j * p.words + word] = c | (up << 16);
     if (lane % lanes == 0 && i0 < p.n) {
-      const int64_t at = j * p.groups + i0 / p.group;
+      const int64_t at = i0 / p.group * p.m + j;
       store1_any(p.scales, p.scale_dtype, at, s);
       if (p.zeros) p.zeros[at] = (uint8_t)z;
     }
@@ -83,7 +83,7 @@ struct DequantParams {
   const void* scales;
   const uint8_t* zeros;
   void* out;
-  int64_t n, m, ld, words, groups;
+  int64_t n, m, ld, words;
   int dtype, scale_dtype, group, vec;
 };
 
@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(256) dequantise4_kernel(const __grid_constant_
     const int64_t i0 = (u - j * p.words) * 8;
     if (i0 >= p.n) continue;
     const uint32_t c = p.codes[u];
-    const int64_t at = j * p.groups + i0 / p.group;
+    const int64_t at = i0 / p.group * p.m + j;
     const float s = load1_any(p.scales, p.scale_dtype, at);
     const float z = p.zeros ? (float)p.zeros[at] : 8.f;
     float v[8];
@@ -127,7 +127,7 @@ extern "C" kd_status kd_quantise_4bit(const void* w, kd_dtype dtype, int64_t ld,
   if (!w || !aligned(w, (size_t)type_bytes(dtype)) || !weight4_pointers_ok(out)) return KD_ERR_INVALID_ARG;
   QuantParams p{w, const_cast<uint32_t*>(out->codes), const_cast<void*>(out->scales),
                 const_cast<uint8_t*>(out->zeros), out->n, out->m, ld, weight4_words(out->n),
-                (out->n + out->group - 1) / out->group, (out->n + 127) / 128, (int)dtype, out->scale_dtype,
+                (out->n + 127) / 128, (int)dtype, out->scale_dtype,
                 out->group};
   quantise4_kernel<<<grid_for((p.m * p.chunks + 7) / 8), 256, 0, static_cast<cudaStream_t>(stream)>>>(p);
   return cudaGetLastError() == cudaSuccess ? KD_OK : KD_ERR_CUDA;
@@ -140,7 +140,7 @@ extern "C" kd_status kd_dequantise_4bit(const kd_weight4* w, kd_dtype out_dtype,
   if (w->m == 0) return KD_OK;
   if (!out || !aligned(out, (size_t)type_bytes(out_dtype)) || !weight4_pointers_ok(w)) return KD_ERR_INVALID_ARG;
   DequantParams p{w->codes, w->scales, w->zeros, out, w->n, w->m, ld, weight4_words(w->n),
-                  (w->n + w->group - 1) / w->group, (int)out_dtype, w->scale_dtype, w->group,
+                  (int)out_dtype, w->scale_dtype, w->group,
                   rows_aligned16(out, ld, w->m, out_dtype)};
   dequantise4_kernel<<<grid_for((p.m * p.words + 255) / 256), 256, 0, static_cast<cudaStream_t>(stream)>>>(p);
   return cudaGetLastError() == cudaSuccess ? KD_OK : KD_ERR_CUDA;

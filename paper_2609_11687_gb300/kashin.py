@@ -24,6 +24,7 @@ from __future__ import annotations
 
 import ctypes
 import dataclasses
+import functools
 import os
 from typing import Optional
 
@@ -868,31 +869,58 @@ def unpack_codes(words, n: int):
 # serving operators around the coded layers
 # ---------------------------------------------------------------------------
 
-def _rows(t, name, dtypes, device, shape=None):
-    """Checks one operand of a serving operator (a CUDA tensor of one of ``dtypes`` on
-    ``device``, rows of unit inner stride) and returns its row stride."""
-    if t.dtype not in dtypes:
-        raise ValueError(f"{name} has dtype {t.dtype}: one of {', '.join(map(str, dtypes))} is wanted")
-    if not t.is_cuda or t.device != device:
-        raise ValueError(f"{name} must be a CUDA tensor on {device}")
-    size = t.shape
-    if shape is not None and tuple(size) != shape:
-        raise ValueError(f"{name} has shape {tuple(size)}: {shape} is wanted")
-    if len(size) == 1:
-        if size[0] > 1 and t.stride(0) != 1:
-            raise ValueError(f"{name} must be contiguous")
-        return size[0]
-    if len(size) != 2:
+@functools.lru_cache(maxsize=None)
+def _serve():
+    """What every call of a serving operator asks torch for, looked up once: the C codes of
+    the element types, and the function that gives a device's current stream handle."""
+    torch = _torch()
+    floats = {torch.float32: KD_F32, torch.float16: KD_F16, torch.bfloat16: KD_BF16}
+    rows4 = {torch.float16: KD_F16, torch.bfloat16: KD_BF16, torch.float8_e4m3fn: KD_E4M3}
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is None:
+        def raw(index):
+            return torch.cuda.current_stream(index).cuda_stream
+    return floats, rows4, torch.float32, torch.float8_e4m3fn, raw, torch.cuda.current_device
+
+
+def _refuse(t, name, types, index, shape):
+    """Says what is wrong with one operand of a serving operator."""
+    if len(t.shape) != 2 and (shape is None or len(shape) == 2):
         raise ValueError(f"{name} must be 2-D")
-    rows, cols = size
-    a, b = t.stride()
-    if cols > 1 and b != 1:
+    if t.dtype not in types:
+        raise ValueError(f"{name} has dtype {t.dtype}: one of {', '.join(map(str, types))} is wanted")
+    if not t.is_cuda or t.get_device() != index:
+        raise ValueError(f"{name} must be a CUDA tensor on " + ("one device with the others" if index < 0 else f"cuda:{index}"))
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}: {tuple(shape)} is wanted")
+    if t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name} needs unit inner stride")
+    raise ValueError(f"{name}'s rows must not overlap")
+
+
+def _ld2(t, name, types, index, shape=None):
+    """Row stride of a 2-D operand after its checks: a CUDA tensor of one of ``types`` on
+    device ``index``, of ``shape``, with unit inner stride and rows that do not overlap."""
+    size, stride = t.shape, t.stride()
+    if len(size) != 2 or t.dtype not in types or t.get_device() != index or index < 0 \
+            or (shape is not None and size != shape):
+        _refuse(t, name, types, index, shape)
+    rows, cols = size
+    if cols > 1 and stride[1] != 1:
+        _refuse(t, name, types, index, shape)
     if rows <= 1:
         return cols
-    if a < cols:
-        raise ValueError(f"{name}'s rows must not overlap")
-    return a
+    if stride[0] < cols:
+        _refuse(t, name, types, index, shape)
+    return stride[0]
+
+
+def _vec(t, name, types, index, length):
+    """Checks a contiguous vector operand."""
+    if t.dtype not in types or t.get_device() != index or index < 0 or t.shape != (length,):
+        _refuse(t, name, types, index, (length,))
+    if length > 1 and t.stride(0) != 1:
+        raise ValueError(f"{name} must be contiguous")
 
 
 def _new(stream, shape, dtype, device):
@@ -903,23 +931,16 @@ def _new(stream, shape, dtype, device):
     return t
 
 
-def _call(what, fn, device, stream, *args):
-    """fn(*args, stream) on ``device``; KashinError for any status but KD_OK."""
-    torch = _torch()
-    if stream is None:
-        stream = torch.cuda.current_stream(device)
-    if device.index is None or device.index == torch.cuda.current_device():
-        st = fn(*args, stream.cuda_stream)
+def _call(what, fn, index, stream, *args):
+    """fn(*args, stream handle) on device ``index``; KashinError for any status but KD_OK."""
+    raw, current = _serve()[4:]
+    if current() == index:
+        st = fn(*args, raw(index) if stream is None else stream.cuda_stream)
     else:
-        with torch.cuda.device(device):
-            st = fn(*args, stream.cuda_stream)
-    if st != KD_OK:
+        with _torch().cuda.device(index):
+            st = fn(*args, raw(index) if stream is None else stream.cuda_stream)
+    if st:
         raise KashinError(st, what)
-
-
-def _float_types():
-    torch = _torch()
-    return torch.float16, torch.bfloat16, torch.float32
 
 
 @dataclasses.dataclass
@@ -940,48 +961,53 @@ def rmsnorm(x, weight, eps: float = 1e-5, residual=None, out: Optional[Normed] =
     ``y`` for the 16- or 32-bit rows that the 2-bit products and apply_p read, and
     ``residual`` -- it may be the ``residual`` argument itself -- for the sum); without it
     ``q``, ``scale`` and, given a residual, ``residual`` are allocated."""
-    torch = _torch()
-    if x.dim() != 2:
-        raise ValueError("x must be 2-D")
-    dev, (rows, n) = x.device, x.shape
-    types = (x.dtype,)
-    ldx = _rows(x, "x", _float_types(), dev)
-    _rows(weight, "weight", (x.dtype, torch.float32), dev, (n,))
-    shape = (rows, n)
+    floats, _, f32, e4m3, _, _ = _serve()
+    dt, shape, index = x.dtype, x.shape, x.get_device()
+    ldx = _ld2(x, "x", floats, index)
+    rows, n = shape
+    wdt = weight.dtype
+    _vec(weight, "weight", (dt, f32), index, n)
     if out is None:
-        out = Normed(q=_new(stream, shape, torch.float8_e4m3fn, dev), scale=_new(stream, (rows,), torch.float32, dev),
-                     residual=None if residual is None else _new(stream, shape, x.dtype, dev))
-    ldr = ldn = ldq = ldy = 0
+        dev = x.device
+        out = Normed(q=_new(stream, shape, e4m3, dev), scale=_new(stream, (rows,), f32, dev),
+                     residual=None if residual is None else _new(stream, shape, dt, dev))
+    q, scale, y, new = out.q, out.scale, out.y, out.residual
+    ldr = ldn = ldq = ldy = ydt = 0
+    residual_ptr = new_ptr = q_ptr = scale_ptr = y_ptr = None
     if residual is not None:
-        ldr = _rows(residual, "residual", types, dev, shape)
-    if out.residual is not None:
+        ldr, residual_ptr = _ld2(residual, "residual", (dt,), index, shape), residual.data_ptr()
+    if new is not None:
         if residual is None:
             raise ValueError("out.residual is written only where a residual is given")
-        ldn = _rows(out.residual, "out.residual", types, dev, shape)
-    if (out.q is None) != (out.scale is None):
+        ldn, new_ptr = _ld2(new, "out.residual", (dt,), index, shape), new.data_ptr()
+    if q is not None and scale is not None:
+        ldq, q_ptr = _ld2(q, "out.q", (e4m3,), index, shape), q.data_ptr()
+        _vec(scale, "out.scale", (f32,), index, rows)
+        scale_ptr = scale.data_ptr()
+    elif q is not None or scale is not None:
         raise ValueError("out.q and out.scale come together")
-    if out.q is not None:
-        ldq = _rows(out.q, "out.q", (torch.float8_e4m3fn,), dev, shape)
-        _rows(out.scale, "out.scale", (torch.float32,), dev, (rows,))
-    ydt = KD_F32
-    if out.y is not None:
-        ldy = _rows(out.y, "out.y", _float_types(), dev, shape)
-        ydt = _dtype_code(out.y.dtype)
-    if out.q is None and out.y is None:
+    elif y is None:
         raise ValueError("out wants q and scale, or y, or all three")
-    _call("kd_rmsnorm", kd_rmsnorm, dev, stream, x.data_ptr(), _dtype_code(x.dtype), n, rows, ldx, weight.data_ptr(),
-          _dtype_code(weight.dtype), eps, _ptr(residual), ldr, _ptr(out.residual), ldn, _ptr(out.q), ldq,
-          _ptr(out.scale), _ptr(out.y), ydt, ldy)
+    if y is not None:
+        ldy, y_ptr, ydt = _ld2(y, "out.y", floats, index, shape), y.data_ptr(), floats[y.dtype]
+    _call("kd_rmsnorm", lib.kd_rmsnorm, index, stream, x.data_ptr(), floats[dt], n, rows, ldx, weight.data_ptr(),
+          floats[wdt], eps, residual_ptr, ldr, new_ptr, ldn, q_ptr, ldq, scale_ptr, y_ptr, ydt, ldy)
     return out
+
+
+def _by_group(t):
+    """A (channels, groups) tensor whose memory holds one group's channels together."""
+    return t if t.t().is_contiguous() else t.t().contiguous().t()
 
 
 class Weight4:
     """A matrix of 4-bit weights (kd_weight4): ``codes`` int32 (m, 4 ceil(n/32)), code i of a
     row at bits 4 (i % 8) of word i // 8; ``scales`` fp16 or bf16 (m, ceil(n/group));
     ``zeros`` uint8 of that shape with values 0..15, or None for 8 everywhere.  The weight is
-    ``scale * (code - zero)``; all tensors contiguous on one GPU."""
+    ``scale * (code - zero)``.  ``codes`` is contiguous; scales and zeros are kept group by
+    group (a tensor in another order is laid out anew here, once)."""
 
-    __slots__ = ("codes", "scales", "zeros", "n", "m", "group", "device", "desc", "ref")
+    __slots__ = ("codes", "scales", "zeros", "n", "m", "group", "device", "index", "desc", "ref")
 
     def __init__(self, codes, scales, zeros=None, *, n: int, group: int = 128):
         torch = _torch()
@@ -996,10 +1022,14 @@ class Weight4:
         if zeros is not None and (tuple(zeros.shape) != shape or zeros.dtype != torch.uint8):
             raise ValueError(f"zeros must be uint8 {shape}")
         for t in (codes, scales, zeros):
-            if t is not None and (not t.is_cuda or t.device != codes.device or not t.is_contiguous()):
-                raise ValueError("codes, scales and zeros must be contiguous CUDA tensors on one device")
+            if t is not None and (not t.is_cuda or t.device != codes.device):
+                raise ValueError("codes, scales and zeros must be CUDA tensors on one device")
+        if not codes.is_contiguous():
+            raise ValueError("codes must be contiguous")
+        scales, zeros = _by_group(scales), None if zeros is None else _by_group(zeros)
         self.codes, self.scales, self.zeros = codes, scales, zeros
         self.n, self.m, self.group, self.device = int(n), m, int(group), codes.device
+        self.index = codes.get_device()
         self.desc = KdWeight4(codes.data_ptr(), scales.data_ptr(), _ptr(zeros), n, m, group,
                               _dtype_code(scales.dtype))
         self.ref = ctypes.addressof(self.desc)
@@ -1010,28 +1040,28 @@ def quantise_4bit(w, group: int = 128, zeros: bool = False, scale_dtype=None, st
     (nn.Linear layout, fp16, bf16 or fp32; kd_quantise_4bit).  ``zeros``: a zero point per
     group too; ``scale_dtype``: fp16 (the default for fp16 weights) or bf16."""
     torch = _torch()
-    if w.dim() != 2:
-        raise ValueError("w must be 2-D")
-    dev, (m, n) = w.device, w.shape
-    ld = _rows(w, "w", _float_types(), dev)
+    floats, index, dev = _serve()[0], w.get_device(), w.device
+    ld = _ld2(w, "w", floats, index)
+    m, n = w.shape
     if group not in (32, 64, 128):
         raise ValueError("group must be 32, 64 or 128")
     if n < 1:
         raise ValueError("w has no inputs")
     sdt = scale_dtype or (torch.float16 if w.dtype == torch.float16 else torch.bfloat16)
     groups = (n + group - 1) // group
-    out = Weight4(_new(stream, (m, (n + 31) // 32 * 4), torch.int32, dev), _new(stream, (m, groups), sdt, dev),
-                  _new(stream, (m, groups), torch.uint8, dev) if zeros else None, n=n, group=group)
-    _call("kd_quantise_4bit", kd_quantise_4bit, dev, stream, w.data_ptr(), _dtype_code(w.dtype), ld, out.ref)
+    out = Weight4(_new(stream, (m, (n + 31) // 32 * 4), torch.int32, dev), _new(stream, (groups, m), sdt, dev).t(),
+                  _new(stream, (groups, m), torch.uint8, dev).t() if zeros else None, n=n, group=group)
+    _call("kd_quantise_4bit", lib.kd_quantise_4bit, index, stream, w.data_ptr(), floats[w.dtype], ld, out.ref)
     return out
 
 
 def dequantise_4bit(w: Weight4, dtype=None, out=None, stream=None):
-    """The dense (m, n) matrix of 4-bit weights (kd_dequantise_4bit)."""
-    torch = _torch()
-    y = out if out is not None else _new(stream, (w.m, w.n), dtype or torch.float32, w.device)
-    ld = _rows(y, "out", _float_types(), w.device, (w.m, w.n))
-    _call("kd_dequantise_4bit", kd_dequantise_4bit, w.device, stream, w.ref, _dtype_code(y.dtype), y.data_ptr(), ld)
+    """The dense (m, n) matrix of 4-bit weights (kd_dequantise_4bit), fp32 unless ``dtype``
+    or ``out`` says otherwise."""
+    floats, _, f32, _, _, _ = _serve()
+    y = out if out is not None else _new(stream, (w.m, w.n), dtype or f32, w.device)
+    ld = _ld2(y, "out", floats, w.index, (w.m, w.n))
+    _call("kd_dequantise_4bit", lib.kd_dequantise_4bit, w.index, stream, w.ref, floats[y.dtype], y.data_ptr(), ld)
     return y
 
 
@@ -1039,19 +1069,22 @@ def matmul_4bit(w: Weight4, x, scale=None, out=None, out_dtype=None, stream=None
     """``Y = X W^T`` for few rows ``x`` (rows, n) in fp16, bf16 or float8_e4m3fn (then with
     ``scale``, fp32 (rows,), as rmsnorm leaves them) and 4-bit weights (kd_matmul_4bit);
     returns (rows, m), fp32 unless ``out`` or ``out_dtype`` says otherwise."""
-    torch = _torch()
-    if x.dim() != 2 or x.shape[1] != w.n:
+    floats, types, f32, _, _, _ = _serve()
+    index, shape = w.index, x.shape
+    ldx = _ld2(x, "x", types, index)
+    rows = shape[0]
+    if shape[1] != w.n:
         raise ValueError(f"x must be (rows, {w.n})")
-    dev, rows = w.device, x.shape[0]
-    ldx = _rows(x, "x", (torch.float16, torch.bfloat16, torch.float8_e4m3fn), dev)
+    scale_ptr = None
     if scale is not None:
-        _rows(scale, "scale", (torch.float32,), dev, (rows,))
-    y = out if out is not None else _new(stream, (rows, w.m), out_dtype or torch.float32, dev)
-    ldy = _rows(y, "out", _float_types(), dev, (rows, w.m))
-    xdt = KD_E4M3 if x.dtype == torch.float8_e4m3fn else _dtype_code(x.dtype)
-    _call("kd_matmul_4bit", kd_matmul_4bit, dev, stream, w.ref, x.data_ptr(), xdt, _ptr(scale), rows, ldx,
-          y.data_ptr(), _dtype_code(y.dtype), ldy)
-    return y
+        _vec(scale, "scale", (f32,), index, rows)
+        scale_ptr = scale.data_ptr()
+    if out is None:
+        out = _new(stream, (rows, w.m), out_dtype or f32, w.device)
+    ldy = _ld2(out, "out", floats, index, (rows, w.m))
+    _call("kd_matmul_4bit", lib.kd_matmul_4bit, index, stream, w.ref, x.data_ptr(), types[x.dtype], scale_ptr, rows,
+          ldx, out.data_ptr(), floats[out.dtype], ldy)
+    return out
 
 
 @dataclasses.dataclass
@@ -1067,35 +1100,34 @@ def token_logprobs(logits, ids, top: int = 0, out: Optional[TokenLogprobs] = Non
     """Log probabilities of the tokens ``ids`` (int64 (rows,) or (rows, tokens); negative:
     padding, 0) under softmax of the rows of ``logits`` (rows, vocab), the entropy and the
     ``top`` (0..32) likeliest alternatives (kd_token_logprobs)."""
-    torch = _torch()
-    if logits.dim() != 2:
-        raise ValueError("logits must be 2-D")
-    dev, (rows, vocab) = logits.device, logits.shape
-    ld = _rows(logits, "logits", _float_types(), dev)
+    floats, _, f32, _, _, _ = _serve()
+    index = logits.get_device()
+    ld = _ld2(logits, "logits", floats, index)
+    rows, vocab = logits.shape
     if ids.dim() == 1:
         ids = ids[:, None]
-    if ids.dim() != 2 or ids.shape[0] != rows or ids.dtype != torch.int64 or ids.device != dev \
+    i64 = _torch().int64
+    if ids.dim() != 2 or ids.shape[0] != rows or ids.dtype != i64 or ids.get_device() != index \
             or not ids.is_contiguous():
         raise ValueError("ids must be a contiguous int64 (rows,) or (rows, tokens) tensor on the logits' device")
     tokens = ids.shape[1]
-    top = int(top)
     if not 0 <= top <= min(vocab, KD_MAX_TOP):
         raise ValueError(f"top must be 0..{min(vocab, KD_MAX_TOP)}")
-    f32 = torch.float32
     if out is None:
+        dev = logits.device
         out = TokenLogprobs(_new(stream, (rows, tokens), f32, dev), _new(stream, (rows,), f32, dev),
-                            _new(stream, (rows,), f32, dev), _new(stream, (rows, top), torch.int64, dev),
+                            _new(stream, (rows,), f32, dev), _new(stream, (rows, top), i64, dev),
                             _new(stream, (rows, top), f32, dev))
     else:
-        for t, name, dt, shape in ((out.logprobs, "logprobs", f32, (rows, tokens)), (out.lse, "lse", f32, (rows,)),
-                                   (out.entropy, "entropy", f32, (rows,)),
-                                   (out.top_ids, "top_ids", torch.int64, (rows, top)),
-                                   (out.top_logprobs, "top_logprobs", f32, (rows, top))):
-            if t is None and name in ("lse", "entropy"):
+        for name, dt, size in (("logprobs", f32, (rows, tokens)), ("lse", f32, (rows,)), ("entropy", f32, (rows,)),
+                               ("top_ids", i64, (rows, top)), ("top_logprobs", f32, (rows, top))):
+            t = getattr(out, name)
+            if t is None and (name == "lse" or name == "entropy"):
                 continue
-            if t is None or t.dtype != dt or t.shape != shape or t.device != dev or not t.is_contiguous():
-                raise ValueError(f"out.{name} must be a contiguous {dt} {shape} tensor on the logits' device")
-    _call("kd_token_logprobs", kd_token_logprobs, dev, stream, logits.data_ptr(), _dtype_code(logits.dtype), rows,
-          vocab, ld, ids.data_ptr(), tokens, top, out.logprobs.data_ptr(), _ptr(out.lse), _ptr(out.entropy),
-          out.top_ids.data_ptr(), out.top_logprobs.data_ptr())
+            if t is None or t.dtype != dt or t.shape != size or t.get_device() != index or not t.is_contiguous():
+                raise ValueError(f"out.{name} must be a contiguous {dt} {size} tensor on the logits' device")
+    lse, entropy = out.lse, out.entropy
+    _call("kd_token_logprobs", lib.kd_token_logprobs, index, stream, logits.data_ptr(), floats[logits.dtype], rows,
+          vocab, ld, ids.data_ptr(), tokens, top, out.logprobs.data_ptr(), None if lse is None else lse.data_ptr(),
+          None if entropy is None else entropy.data_ptr(), out.top_ids.data_ptr(), out.top_logprobs.data_ptr())
     return out
