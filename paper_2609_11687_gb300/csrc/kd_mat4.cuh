@@ -85,17 +85,6 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-// this CTA's rank in its cluster, the cluster's index, the launch's clusters (CTAs without one
-// are clusters of their own)
-enum { kRank, kCluster, kClusters };
-template <int WHAT>
-__device__ __forceinline__ int special() {
-  int r;
-  if constexpr (WHAT == kRank) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  else if constexpr (WHAT == kCluster) asm("mov.u32 %0, %%clusterid.x;" : "=r"(r));
-  else asm("mov.u32 %0, %%nclusterid.x;" : "=r"(r));
-  return r;
-}
 template <int N>
 __device__ __forceinline__ void wait_group() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
@@ -235,6 +224,7 @@ __global__ void __launch_bounds__(32 * kWarps<NT>, 1) mat4_kernel(const __grid_c
     if (turn >= turns || k >= p.n) return make_uint4(0, 0, 0, 0);
     return p.x_vec && k + 8 <= p.n ? load_inputs(p, at) : load_inputs_one_by_one(p.x, p.e4m3, at, p.n - k);
   };
+  depend_on_last();
   uint4 v0[kBatch];
   int row0[kBatch], item0[kBatch];
 #pragma unroll
@@ -475,12 +465,13 @@ cudaError_t launch_one(const Params& p, int clusters, cudaStream_t s) {
   cfg.blockDim = dim3(32 * kWarps<NT>);
   cfg.dynamicSmemBytes = smem_bytes(NT, p.rows, p.per, p.split, p.kw);
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)p.split;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cudaLaunchAttribute attr[2];
+  launch_early(attr[0]);
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)p.split;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = p.split > 1 ? 1 : 0;
+  cfg.numAttrs = p.split > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 

@@ -52,6 +52,7 @@ __global__ void __launch_bounds__(512) norm_kernel(const __grid_constant__ NormP
   const int n = (int)p.n;
   auto index = [&](int c, int e) { return VEC ? 8 * (c * T + tid) + e : (8 * c + e) * T + tid; };
 
+  depend_on_last();
   float h[C][8], w[C][8];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
@@ -161,16 +162,22 @@ __global__ void __launch_bounds__(512) norm_kernel(const __grid_constant__ NormP
 }
 
 template <int DT, bool VEC>
-void launch(const NormParams& p, cudaStream_t s) {
+cudaError_t launch(const NormParams& p, cudaStream_t s) {
   const int64_t pieces = (p.n + 7) / 8;
   const int C = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : 4;
   const int T = (int)(((pieces + C - 1) / C + 31) / 32 * 32);
   const int R = T <= 128 ? 256 / T : 1;
-  const dim3 block(T, R);
-  const unsigned grid = (unsigned)((p.rows + R - 1) / R);
-  if (C == 1) norm_kernel<DT, 1, VEC><<<grid, block, 0, s>>>(p);
-  else if (C == 2) norm_kernel<DT, 2, VEC><<<grid, block, 0, s>>>(p);
-  else norm_kernel<DT, 4, VEC><<<grid, block, 0, s>>>(p);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((p.rows + R - 1) / R));
+  cfg.blockDim = dim3(T, R);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  launch_early(attr[0]);
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return C == 1   ? cudaLaunchKernelEx(&cfg, norm_kernel<DT, 1, VEC>, p)
+         : C == 2 ? cudaLaunchKernelEx(&cfg, norm_kernel<DT, 2, VEC>, p)
+                  : cudaLaunchKernelEx(&cfg, norm_kernel<DT, 4, VEC>, p);
 }
 
 }  // namespace
@@ -200,8 +207,8 @@ extern "C" kd_status kd_rmsnorm(const void* x, kd_dtype dtype, int64_t n, int64_
                    (!q || (aligned(q, 8) && (rows == 1 || ldq % 8 == 0))) &&
                    (!y || rows_aligned16(y, ldy, rows, y_dtype));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (dtype == KD_F32) vec ? launch<KD_F32, true>(p, s) : launch<KD_F32, false>(p, s);
-  else if (dtype == KD_F16) vec ? launch<KD_F16, true>(p, s) : launch<KD_F16, false>(p, s);
-  else vec ? launch<KD_BF16, true>(p, s) : launch<KD_BF16, false>(p, s);
-  return cudaGetLastError() == cudaSuccess ? KD_OK : KD_ERR_CUDA;
+  const cudaError_t e = dtype == KD_F32   ? (vec ? launch<KD_F32, true>(p, s) : launch<KD_F32, false>(p, s))
+                        : dtype == KD_F16 ? (vec ? launch<KD_F16, true>(p, s) : launch<KD_F16, false>(p, s))
+                                          : (vec ? launch<KD_BF16, true>(p, s) : launch<KD_BF16, false>(p, s));
+  return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? KD_OK : KD_ERR_CUDA;
 }

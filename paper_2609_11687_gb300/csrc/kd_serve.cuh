@@ -20,6 +20,30 @@ inline bool rows_aligned16(const void* p, int64_t ld, int64_t rows, int d) {
   return aligned(p, 16) && (rows <= 1 || ld * type_bytes(d) % 16 == 0);
 }
 
+// Programmatic dependent launch: a kernel launched with launch_early may be set up while the
+// one before it in the stream still runs; depend_on_last, before its first access to
+// global memory, waits for that one's end and results, and lets the next be set up in turn.
+inline void launch_early(cudaLaunchAttribute& a) {
+  a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  a.val.programmaticStreamSerializationAllowed = 1;
+}
+__device__ __forceinline__ void depend_on_last() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+// this CTA's rank in its cluster, the cluster's index, the launch's clusters (CTAs without one
+// are clusters of their own)
+enum { kRank, kCluster, kClusters };
+template <int WHAT>
+__device__ __forceinline__ int special() {
+  int r;
+  if constexpr (WHAT == kRank) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  else if constexpr (WHAT == kCluster) asm("mov.u32 %0, %%clusterid.x;" : "=r"(r));
+  else asm("mov.u32 %0, %%nclusterid.x;" : "=r"(r));
+  return r;
+}
+
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
