@@ -8,6 +8,10 @@
 // One pass over the row: a thread keeps its elements of h and w in registers, and one
 // reduction over the row yields both sum(h^2) and max|h w| (max|y| is that times the
 // row's positive factor), so x and r are read once and nothing is read again.
+//
+// Bound by HBM for many rows, by latency for few.  A CTA walks rows: it keeps w, and loads
+// its next row before it reduces this one, so that loads are in flight all the time (a CTA
+// a row reached half of the bandwidth: most of its life is the reduction).
 #include <cuda_fp8.h>
 
 #include "kd_serve.cuh"
@@ -30,7 +34,7 @@ struct NormParams {
   void* y;
   int64_t n, rows, ldx, ldr, ldro, ldq, ldy;
   float eps;
-  int wdtype, ydtype;
+  int ydtype;
 };
 
 __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
@@ -39,145 +43,186 @@ __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
   return lo | (hi << 16);
 }
 
+// eight elements as they come: 16 bytes of a 16-bit type, 32 of fp32; without VEC one by one
+template <int DT, bool VEC>
+struct Piece {
+  uint4 v[DT == KD_F32 ? 2 : 1];
+  // element e is at index + e (VEC) or index + e * stride; nothing past n
+  __device__ __forceinline__ void load(const void* base, int64_t row, int index, int stride, int n) {
+    if constexpr (VEC) {
+      if (index < n) {
+        const uint4* p = reinterpret_cast<const uint4*>(static_cast<const char*>(base) + (row + index) * (DT == KD_F32 ? 4 : 2));
+        v[0] = p[0];
+        if constexpr (DT == KD_F32) v[1] = p[1];
+        return;
+      }
+    }
+    uint32_t u[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if constexpr (!VEC) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int i = index + e * stride;
+        if (i < n) {
+          if constexpr (DT == KD_F32) u[e] = static_cast<const uint32_t*>(base)[row + i];
+          else u[e / 2] |= (uint32_t) static_cast<const uint16_t*>(base)[row + i] << (16 * (e % 2));
+        }
+      }
+    }
+    v[0] = make_uint4(u[0], u[1], u[2], u[3]);
+    if constexpr (DT == KD_F32) v[1] = make_uint4(u[4], u[5], u[6], u[7]);
+  }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    if constexpr (DT == KD_F32) {
+      f[0] = __uint_as_float(v[0].x); f[1] = __uint_as_float(v[0].y);
+      f[2] = __uint_as_float(v[0].z); f[3] = __uint_as_float(v[0].w);
+      f[4] = __uint_as_float(v[1].x); f[5] = __uint_as_float(v[1].y);
+      f[6] = __uint_as_float(v[1].z); f[7] = __uint_as_float(v[1].w);
+    } else {
+      const float2 a = unpack2<DT>(v[0].x), b = unpack2<DT>(v[0].y), c = unpack2<DT>(v[0].z), d = unpack2<DT>(v[0].w);
+      f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
+      f[4] = c.x; f[5] = c.y; f[6] = d.x; f[7] = d.y;
+    }
+  }
+};
+
+constexpr int kNormThreads = 1024;  // of a CTA at most: two pieces each cover the longest row
+
 // blockDim = (threads of one row, rows of one CTA); C: 8-element pieces a thread holds.
 // VEC: rows start on 16-byte boundaries and n is a multiple of 8, a piece is 8 consecutive
 // elements; else the 8 elements of a piece lie blockDim.x apart (coalesced element loads).
-template <int DT, int C, bool VEC>
-__global__ void __launch_bounds__(512) norm_kernel(const __grid_constant__ NormParams p) {
-  __shared__ float red[2][16];
-  const int tid = threadIdx.x, T = blockDim.x;
-  const int64_t row_at = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-  const bool live = row_at < p.rows;
-  const int64_t row = live ? row_at : p.rows - 1;
-  const int n = (int)p.n;
-  auto index = [&](int c, int e) { return VEC ? 8 * (c * T + tid) + e : (8 * c + e) * T + tid; };
-
+template <int DT, int WT, int C, bool VEC>
+__global__ void __launch_bounds__(kNormThreads) norm_kernel(const __grid_constant__ NormParams p) {
+  __shared__ float2 red[2][kNormThreads / 32];
+  const int tid = threadIdx.x, T = blockDim.x, n = (int)p.n;
+  const int64_t step = (int64_t)gridDim.x * blockDim.y;
+  auto index = [&](int c) { return VEC ? 8 * (c * T + tid) : 8 * c * T + tid; };
   depend_on_last();
-  float h[C][8], w[C][8];
+
+  Piece<WT, VEC> w[C];
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    if constexpr (VEC) {
-      const int i = index(c, 0);
-      if (i < n) {
-        load8<DT>(p.x, row * p.ldx + i, h[c]);
-        if (p.wdtype == DT) load8<DT>(p.w, i, w[c]);
-        else load8<KD_F32>(p.w, i, w[c]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[c][e] = w[c][e] = 0.f;
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int i = index(c, e);
-        h[c][e] = i < n ? load1<DT>(p.x, row * p.ldx + i) : 0.f;
-        w[c][e] = i >= n ? 0.f : p.wdtype == DT ? load1<DT>(p.w, i) : load1<KD_F32>(p.w, i);
-      }
-    }
-  }
-  if (p.r) {
+  for (int c = 0; c < C; ++c) w[c].load(p.w, 0, index(c), T, n);
+  Piece<DT, VEC> x[C], r[C];
+  auto fetch = [&](int64_t row) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      if constexpr (VEC) {
-        const int i = index(c, 0);
-        if (i < n) {
-          float v[8];
-          load8<DT>(p.r, row * p.ldr + i, v);
+      x[c].load(p.x, row * p.ldx, index(c), T, n);
+      if (p.r) r[c].load(p.r, row * p.ldr, index(c), T, n);
+    }
+  };
+  const int64_t first = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  if (first < p.rows) fetch(first);
+  int parity = 0;
+  // the rows of a CTA take turns together: one past the last takes part in the barrier only
+  for (int64_t row = first; row - threadIdx.y < p.rows; row += step, parity ^= 1) {
+    const bool live = row < p.rows;
+    float h[C][8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) h[c][e] += v[e];
+    for (int c = 0; c < C; ++c) {
+      x[c].get(h[c]);
+      if (p.r) {
+        float v[8];
+        r[c].get(v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[c][e] += v[e];
+      }
+    }
+    if (row + step < p.rows) fetch(row + step);
+    float ss = 0.f, big = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      float v[8];
+      w[c].get(v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        ss = __fmaf_rn(h[c][e], h[c][e], ss);
+        big = max_nan(big, fabsf(h[c][e] * v[e]));
+      }
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      ss += __shfl_xor_sync(~0u, ss, o);
+      big = max_nan(big, __shfl_xor_sync(~0u, big, o));
+    }
+    if (T > 32) {
+      // the warps of a row are consecutive: slots of one row stay together
+      const int per = T >> 5, at = threadIdx.y * per;
+      if ((tid & 31) == 0) red[parity][at + (tid >> 5)] = make_float2(ss, big);
+      __syncthreads();
+      ss = big = 0.f;
+      for (int k = 0; k < per; ++k) {
+        const float2 v = red[parity][at + k];
+        ss += v.x;
+        big = max_nan(big, v.y);
+      }
+    }
+    if (!live) continue;
+
+    const float nan = __int_as_float(0x7FC00000);
+    // a row whose sum of squares is no finite number has no norm: NaN, not zeros
+    const float rstd = isfinite(ss) ? 1.f / sqrtf(ss / (float)n + p.eps) : nan;
+    const float amax = big * rstd;
+    const float scale = amax < 0x1p-100f ? 1.f : amax / kE4M3Max;
+    const float inv = 1.f / scale;
+    if (p.scale && tid == 0) p.scale[row] = scale;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      float y[8];
+      w[c].get(y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = h[c][e] * rstd * y[e];
+      if constexpr (VEC) {
+        const int i = index(c);
+        if (i >= n) break;
+        if (p.r_out) store8<DT>(p.r_out, row * p.ldro + i, h[c]);
+        if (p.y) {
+          if (p.ydtype == KD_F32) store8<KD_F32>(p.y, row * p.ldy + i, y);
+          else if (p.ydtype == KD_F16) store8<KD_F16>(p.y, row * p.ldy + i, y);
+          else store8<KD_BF16>(p.y, row * p.ldy + i, y);
         }
+        if (p.q)
+          *reinterpret_cast<uint2*>(p.q + row * p.ldq + i) =
+              make_uint2(e4m3x4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv),
+                         e4m3x4(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int i = index(c, e);
-          if (i < n) h[c][e] += load1<DT>(p.r, row * p.ldr + i);
+          const int i = index(c) + e * T;
+          if (i >= n) break;
+          if (p.r_out) store1<DT>(p.r_out, row * p.ldro + i, h[c][e]);
+          if (p.y) store1_any(p.y, p.ydtype, row * p.ldy + i, y[e]);
+          if (p.q) p.q[row * p.ldq + i] = __nv_cvt_float_to_fp8(y[e] * inv, __NV_SATFINITE, __NV_E4M3);
         }
-      }
-    }
-  }
-
-  float ss = 0.f, big = 0.f;
-#pragma unroll
-  for (int c = 0; c < C; ++c)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      ss = __fmaf_rn(h[c][e], h[c][e], ss);
-      big = max_nan(big, fabsf(h[c][e] * w[c][e]));
-    }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    ss += __shfl_xor_sync(~0u, ss, o);
-    big = max_nan(big, __shfl_xor_sync(~0u, big, o));
-  }
-  if (T > 32) {
-    // the warps of a row are consecutive: slots of one row stay together
-    const int warp = (threadIdx.y * T + tid) >> 5, per = T >> 5;
-    if ((tid & 31) == 0) { red[0][warp] = ss; red[1][warp] = big; }
-    __syncthreads();
-    ss = big = 0.f;
-    for (int k = 0; k < per; ++k) {
-      ss += red[0][threadIdx.y * per + k];
-      big = max_nan(big, red[1][threadIdx.y * per + k]);
-    }
-  }
-  if (!live) return;
-
-  const float nan = __int_as_float(0x7FC00000);
-  // a row whose sum of squares is no finite number has no norm: NaN, not zeros
-  const float rstd = isfinite(ss) ? 1.f / sqrtf(ss / (float)n + p.eps) : nan;
-  const float amax = big * rstd;
-  const float scale = amax < 0x1p-100f ? 1.f : amax / kE4M3Max;
-  const float inv = 1.f / scale;
-  if (p.scale && tid == 0) p.scale[row] = scale;
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    if constexpr (VEC) {
-      const int i = index(c, 0);
-      if (i >= n) break;
-      if (p.r_out) store8<DT>(p.r_out, row * p.ldro + i, h[c]);
-      float y[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = h[c][e] * rstd * w[c][e];
-      if (p.y) {
-        if (p.ydtype == KD_F32) store8<KD_F32>(p.y, row * p.ldy + i, y);
-        else if (p.ydtype == KD_F16) store8<KD_F16>(p.y, row * p.ldy + i, y);
-        else store8<KD_BF16>(p.y, row * p.ldy + i, y);
-      }
-      if (p.q)
-        *reinterpret_cast<uint2*>(p.q + row * p.ldq + i) =
-            make_uint2(e4m3x4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv),
-                       e4m3x4(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int i = index(c, e);
-        if (i >= n) break;
-        if (p.r_out) store1<DT>(p.r_out, row * p.ldro + i, h[c][e]);
-        const float y = h[c][e] * rstd * w[c][e];
-        if (p.y) store1_any(p.y, p.ydtype, row * p.ldy + i, y);
-        if (p.q) p.q[row * p.ldq + i] = __nv_cvt_float_to_fp8(y * inv, __NV_SATFINITE, __NV_E4M3);
       }
     }
   }
 }
 
-template <int DT, bool VEC>
+template <int DT, int WT, bool VEC>
 cudaError_t launch(const NormParams& p, cudaStream_t s) {
   const int64_t pieces = (p.n + 7) / 8;
-  const int C = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : 4;
+  // two pieces a thread once the rows fill the GPU; for few rows more threads are sooner done
+  const bool many = p.rows > 4 * 152;
+  const int C = pieces <= (many ? 32 : 512) ? 1 : 2;
   const int T = (int)(((pieces + C - 1) / C + 31) / 32 * 32);
   const int R = T <= 128 ? 256 / T : 1;
+  const int64_t groups = (p.rows + R - 1) / R;
+  const int64_t at_once = 152 * (int64_t)(1024 / (T * R));  // about 64 registers a thread
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((p.rows + R - 1) / R));
+  cfg.gridDim = dim3((unsigned)(groups < at_once ? groups : at_once));
   cfg.blockDim = dim3(T, R);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   launch_early(attr[0]);
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return C == 1   ? cudaLaunchKernelEx(&cfg, norm_kernel<DT, 1, VEC>, p)
-         : C == 2 ? cudaLaunchKernelEx(&cfg, norm_kernel<DT, 2, VEC>, p)
-                  : cudaLaunchKernelEx(&cfg, norm_kernel<DT, 4, VEC>, p);
+  return C == 1 ? cudaLaunchKernelEx(&cfg, norm_kernel<DT, WT, 1, VEC>, p)
+                : cudaLaunchKernelEx(&cfg, norm_kernel<DT, WT, 2, VEC>, p);
+}
+
+template <int DT>
+cudaError_t launch(const NormParams& p, int wt, bool vec, cudaStream_t s) {
+  if (wt == DT) return vec ? launch<DT, DT, true>(p, s) : launch<DT, DT, false>(p, s);
+  return vec ? launch<DT, KD_F32, true>(p, s) : launch<DT, KD_F32, false>(p, s);
 }
 
 }  // namespace
@@ -200,15 +245,15 @@ extern "C" kd_status kd_rmsnorm(const void* x, kd_dtype dtype, int64_t n, int64_
       !aligned(new_residual, eb) || !aligned(scale, 4) || (y && !aligned(y, (size_t)type_bytes(y_dtype))))
     return KD_ERR_INVALID_ARG;
   NormParams p{x, weight, residual, new_residual, q, scale, y, n, rows, ldx, ld_residual, ld_new_residual, ldq, ldy,
-               eps, (int)weight_dtype, (int)y_dtype};
+               eps, (int)y_dtype};
   const bool vec = n % 8 == 0 && rows_aligned16(x, ldx, rows, dtype) && aligned(weight, 16) &&
                    (!residual || rows_aligned16(residual, ld_residual, rows, dtype)) &&
                    (!new_residual || rows_aligned16(new_residual, ld_new_residual, rows, dtype)) &&
                    (!q || (aligned(q, 8) && (rows == 1 || ldq % 8 == 0))) &&
                    (!y || rows_aligned16(y, ldy, rows, y_dtype));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = dtype == KD_F32   ? (vec ? launch<KD_F32, true>(p, s) : launch<KD_F32, false>(p, s))
-                        : dtype == KD_F16 ? (vec ? launch<KD_F16, true>(p, s) : launch<KD_F16, false>(p, s))
-                                          : (vec ? launch<KD_BF16, true>(p, s) : launch<KD_BF16, false>(p, s));
+  const cudaError_t e = dtype == KD_F32   ? launch<KD_F32>(p, weight_dtype, vec, s)
+                        : dtype == KD_F16 ? launch<KD_F16>(p, weight_dtype, vec, s)
+                                          : launch<KD_BF16>(p, weight_dtype, vec, s);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? KD_OK : KD_ERR_CUDA;
 }
