@@ -44,6 +44,24 @@ bool plan(Params& p, int nt, int rows) {
   return found;
 }
 
+// The same for the kernel for many rows, whose CTAs do not stay: 256 channels each, a cost
+// of a chunk, three for a CTA's start and end and two more for a cluster's.
+void plan_wide(Params& p) {
+  double least = 0;
+  p.tiles = (p.m + 255) / 256;
+  p.kw = 1;
+  for (int split = 1; split <= 8; split *= 2) {
+    const int per = (p.chunks + split - 1) / split;
+    const double rounds = (p.tiles + room(split) - 1) / room(split);
+    const double cost = rounds * (per + (split > 1 ? 5 : 3));
+    if (split == 1 || cost < least) {
+      least = cost;
+      p.split = split;
+      p.per = per;
+    }
+  }
+}
+
 }  // namespace
 }  // namespace mat4
 }  // namespace kd
@@ -81,21 +99,27 @@ extern "C" kd_status kd_matmul_4bit(const kd_weight4* w, const void* x, kd_dtype
   const int gs = w->group / 32;
   const size_t wide = p.e4m3 ? 8 : 16;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  // passes of equal numbers of rows, at most 8 most
-  bool planned = false;
-  int nt = 0;
+  // passes of equal numbers of rows: from 17 rows on of at most 64, by the kernel for many
+  // rows; else one of at most 16 (or, where an input is so long that those fit no CTA's
+  // shared memory, of 8)
+  int nt = 0, clusters = 0;
   int64_t pass = 0;
-  for (int most = 4; most && !planned; most /= 2) {
-    const int64_t passes = (rows + 8 * most - 1) / (8 * most);
+  if (rows > 16) {
+    const int64_t passes = (rows + 63) / 64;
     pass = (rows + passes - 1) / passes;
-    nt = pass > 16 ? 4 : pass > 8 ? 2 : 1;
+    plan_wide(p);
+  } else {
+    nt = rows > 8 ? 2 : 1;
+    pass = rows;
     // up to eight rows split the work alike, so that a row's sums have one order whatever
     // else is in the batch
-    planned = plan(p, nt, nt == 1 ? 8 : (int)pass);
+    if (!plan(p, nt, nt == 1 ? 8 : (int)rows)) {
+      if (nt == 1 || !plan(p, nt = 1, 8)) return KD_ERR_UNSUPPORTED_N;
+      pass = 8;
+    }
+    p.turns_of_row_inv = 1.f / (float)((p.per * 16 + 31) / 32);
+    clusters = p.tiles < room(p.split) ? p.tiles : room(p.split);
   }
-  if (!planned) return KD_ERR_UNSUPPORTED_N;
-  p.turns_of_row_inv = 1.f / (float)((p.per * 16 + 31) / 32);
-  const int clusters = p.tiles < room(p.split) ? p.tiles : room(p.split);
   for (int64_t r0 = 0; r0 < rows; r0 += pass) {
     p.rows = (int)(rows - r0 < pass ? rows - r0 : pass);
     p.x = static_cast<const uint8_t*>(x) + r0 * ldx * xb;

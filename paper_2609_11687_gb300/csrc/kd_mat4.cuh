@@ -447,19 +447,24 @@ __global__ void __launch_bounds__(32 * kWarps<NT>, 1) mat4_kernel(const __grid_c
   if (p.split > 1) cg::this_cluster().sync();  // no CTA leaves while its sums are read
 }
 
+// lets a kernel have all of an SM's shared memory; `ready` holds the devices where it does
+template <class Kernel>
+cudaError_t allow_shared_memory(Kernel kernel, std::atomic<uint64_t>& ready) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev < 64 && ready.load(std::memory_order_relaxed) >> dev & 1)) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+  if (e == cudaSuccess && dev < 64) ready.fetch_or((uint64_t)1 << dev, std::memory_order_relaxed);
+  return e;
+}
+
 // the launch of one pass
 template <bool BF, int GS, int NT, bool ZEROS>
 cudaError_t launch_one(const Params& p, int clusters, cudaStream_t s) {
   auto kernel = mat4_kernel<BF, GS, NT, ZEROS>;
-  static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use its shared memory
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
+  static std::atomic<uint64_t> ready{0};
+  const cudaError_t e = allow_shared_memory(kernel, ready);
   if (e != cudaSuccess) return e;
-  if (dev >= 64 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-    if (e != cudaSuccess) return e;
-    if (dev < 64) ready.fetch_or((uint64_t)1 << dev, std::memory_order_relaxed);
-  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(clusters * p.split));
   cfg.blockDim = dim3(32 * kWarps<NT>);
@@ -477,16 +482,11 @@ cudaError_t launch_one(const Params& p, int clusters, cudaStream_t s) {
 
 template <bool BF, int GS>
 cudaError_t launch(const Params& p, int nt, int clusters, cudaStream_t s) {
-  if (p.zeros)
-    return nt == 1   ? launch_one<BF, GS, 1, true>(p, clusters, s)
-           : nt == 2 ? launch_one<BF, GS, 2, true>(p, clusters, s)
-                     : launch_one<BF, GS, 4, true>(p, clusters, s);
-  return nt == 1   ? launch_one<BF, GS, 1, false>(p, clusters, s)
-         : nt == 2 ? launch_one<BF, GS, 2, false>(p, clusters, s)
-                   : launch_one<BF, GS, 4, false>(p, clusters, s);
+  if (p.zeros) return nt == 1 ? launch_one<BF, GS, 1, true>(p, clusters, s) : launch_one<BF, GS, 2, true>(p, clusters, s);
+  return nt == 1 ? launch_one<BF, GS, 1, false>(p, clusters, s) : launch_one<BF, GS, 2, false>(p, clusters, s);
 }
 
-// bf: bf16 rows
+// bf: bf16 rows; nt: tiles of eight rows, 0: the kernel for many (kd_mat4_wide.cuh)
 cudaError_t launch_group32(const Params& p, bool bf, int nt, int clusters, cudaStream_t s);
 cudaError_t launch_group64(const Params& p, bool bf, int nt, int clusters, cudaStream_t s);
 cudaError_t launch_group128(const Params& p, bool bf, int nt, int clusters, cudaStream_t s);
