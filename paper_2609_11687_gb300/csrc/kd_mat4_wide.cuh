@@ -2,18 +2,22 @@
 // (kd_matmul_4bit), on the fifth-generation tensor cores.
 //
 // From 17 rows on mma.sync is what bounds the product of kd_mat4.cuh; here tcgen05.mma takes
-// the decoded codes c - z (exact in 16 bits, see kd_mat4.cuh) from shared memory as its A
-// operand, 128 channels by 64 inputs at a time, the rows as B, and sums in tensor memory.
+// the decoded codes c - z (exact in 16 bits, see kd_mat4.cuh) as its A operand, 128 channels
+// by 64 inputs at a time, the rows as B, and sums in tensor memory.  A goes through tensor
+// memory too: a channel is a lane of it, so the thread that decodes a channel stores its own
+// lane (through shared memory, which is then written and read once per stage by A's 32 KB,
+// 32000 x 4096 at 64 rows took 51 us instead of 48 when this was changed).
 //
 // Roles in a CTA, which owns 256 channels (two A tiles for each B tile, which halves the
 // traffic of the rows) and its share of the inputs:
 //   warps 0-7   a thread a channel: after each group of inputs its sums are read from tensor
 //               memory, scaled and added in fp32 registers, while the next group's form in
 //               the other of two accumulators; one thread of warp 0 issues the products;
-//   warps 8-15  a thread a channel: 64 codes a stage become 128 bytes of A; the same threads
-//               lay out B.  Loads run four stages ahead in registers.
-// Stages of A and B, and the accumulators, pass between them by mbarriers.  Operands are
-// K-major with 128-byte swizzle: 16-byte piece c of row r lies at c ^ (r % 8).
+//   warps 8-15  a thread a channel: 64 codes a stage become 32 columns of its lane of A, two
+//               inputs each; the same threads lay out B in shared memory.  Codes and rows come
+//               through a ring that each thread fills and reads for itself (cp.async).
+// Stages of A and B, and the accumulators, pass between them by mbarriers.  B is K-major
+// with 128-byte swizzle: 16-byte piece c of row r lies at c ^ (r % 8).
 //
 // K order: a piece of eight inputs holds them as the codes of a word come out, (0 4 1 5 2 6
 // 3 7), in A and B alike.
@@ -29,13 +33,23 @@ namespace mat4 {
 
 constexpr int kWideChannels = 256;
 constexpr int kWideThreads = 512;
-constexpr int kWideStages = 4;
+constexpr int kWideStages = 4;  // of A and B
+constexpr int kWideRing = 7;    // of codes and rows as they come
 constexpr int kStageInputs = 64;
-constexpr int kHalfTile = 128 * 128;  // bytes of 128 channels' A of a stage
 template <int N>
-constexpr int kWideStageBytes = 2 * kHalfTile + N * 128;
+constexpr int kWideStageBytes = N * 128;  // of B
+// B's stages, or in the end the CTA's sums; the barriers; the ring of raw codes and rows;
+// room to align
 template <int N>
-constexpr size_t kWideSmem = (size_t)kWideStages * kWideStageBytes<N> + 1024 + 256;
+constexpr size_t kWideSums = (size_t)N * kWideChannels * 4;
+template <int N>
+constexpr size_t kWideSmem = kWideSums<N> + 256 + (size_t)kWideRing * (2 + N / 32) * 256 * 16 + 1024;
+// Columns of tensor memory, all 512 taken (one CTA an SM): two accumulators of two times 128
+// channels, N columns each; A's stages, 32 columns for each 128 channels.
+constexpr int kTensorColumns = 512;
+template <int N>
+constexpr int kColumnsOfA = 4 * N;
+static_assert(kColumnsOfA<64> + kWideStages * 64 <= kTensorColumns, "tensor memory");
 
 struct WideBarriers {
   uint64_t full[kWideStages], empty[kWideStages];
@@ -63,12 +77,23 @@ __device__ __forceinline__ uint64_t operand_descriptor(uint32_t address) {
   return (uint64_t)(address >> 4 & 0x3FFF) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
          (uint64_t)2 << 61;
 }
-__device__ __forceinline__ void tensor_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
+// One lane of a converged warp.  The products' operands want uniform registers: behind this
+// instruction the compiler knows a single thread to run, behind a comparison of the lane's
+// number it does not, and a product takes 57 cycles to issue (80 with a predicate in place of
+// the branch) instead of the 31 that N = 64 takes to run.
+__device__ __forceinline__ bool elect() {
+  uint32_t one;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+  return one;
+}
+// D (+)= A B with A and D in tensor memory
+__device__ __forceinline__ void tensor_mma(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add) {
   asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-      "l"(a), "l"(b), "r"(what), "r"((uint32_t)add)
+      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
+      "r"(a), "l"(b), "r"(what), "r"((uint32_t)add)
       : "memory");
 }
+// the arrival on a barrier once all products so far are done
 __device__ __forceinline__ void tensor_commit(uint64_t* b) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b))
                : "memory");
@@ -86,23 +111,41 @@ __device__ __forceinline__ void tensor_load(uint32_t address, float (&v)[32]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
+// 32 columns of this warp's 32 lanes, and until they are there
+__device__ __forceinline__ void tensor_store(uint32_t address, const uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(address),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]),
+      "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]),
+      "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+      : "memory");
+}
+__device__ __forceinline__ void tensor_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void copy8(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
+
 // BF: bf16 rows; GS: groups of 32 GS inputs; N: rows of a pass at most (32, 64); ZEROS: zero
 // points by group.  Grid: one cluster of `split` CTAs for each 256 channels.
 template <bool BF, int GS, int N, bool ZEROS>
 __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid_constant__ Params p) {
   namespace cg = cooperative_groups;
   extern __shared__ uint4 smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>(
-      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);  // operands start on 1024 bytes
-  WideBarriers& sh = *reinterpret_cast<WideBarriers*>(smem + kWideStages * kWideStageBytes<N>);
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t pad = -smem_u32(smem_raw) & 1023u;  // operands start on 1024 bytes
+  uint8_t* smem = reinterpret_cast<uint8_t*>(smem_raw) + pad;
+  WideBarriers& sh = *reinterpret_cast<WideBarriers*>(smem + kWideSums<N>);
+  // by shuffle: so the compiler knows a warp's role to be the same for all its lanes
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(~0u, tid >> 5, 0);
   const int rank = special<kRank>(), tile = special<kCluster>();
   const int c0 = rank * p.per, mine = max(0, min(p.per, p.chunks - c0));
   const int stages = 2 * mine, groups = mine * (4 / GS);
 
   if (warp == 0) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)),
-                 "r"(4 * N)
+                 "r"(kTensorColumns)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -121,7 +164,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  const uint32_t tmem = sh.tmem;
+  constexpr uint32_t tmem = 0;  // all of it
   depend_on_last();
 
   const float nan = __int_as_float(0x7FC00000);
@@ -137,39 +180,44 @@ __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid
     const int ch = min(tile * kWideChannels + tid, p.m - 1);
     const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + (warp >> 2) * N;
     auto fetch = [&](int k) { return p.scales[(int64_t)min(c0 * (4 / GS) + k, p.groups - 1) * p.m + ch]; };
-    // one thread: the products of group k
+    // warp 0: the products of group k
     auto issue = [&](int k) {
-      // fp32 sums of fp16 or bf16 products, M = 128, N, both operands K-major
+      // fp32 sums of fp16 or bf16 products, M = 128, N, B K-major
       constexpr uint32_t kWhat = 1u << 4 | (BF ? 1u : 0u) << 7 | (BF ? 1u : 0u) << 10 | (N / 8) << 17 | (128 / 16) << 24;
       if (k >= 2) {
         barrier_wait(&sh.taken[k & 1], (k >> 1) - 1 & 1, &sh.failed);
+        __syncwarp();
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       }
       const uint32_t to = tmem + (k & 1) * 2 * N;
 #pragma unroll
       for (int i = 0; i < 2 * GS; ++i) {  // 16 inputs each: 32 bytes further along the rows
         const int s = (2 * GS * k + i) / 4, slot = s % kWideStages, q = (GS == 1 ? 2 * (k & 1) : 0) + i % 4;
-        const uint32_t at = smem_u32(smem) + slot * kWideStageBytes<N>;
         if (q == 0) {
           barrier_wait(&sh.full[slot], s / kWideStages & 1, &sh.failed);
+          __syncwarp();
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         }
-        const uint64_t a = operand_descriptor(at) + 2 * q, b = operand_descriptor(at + 2 * kHalfTile) + 2 * q;
-        tensor_mma(to, a, b, kWhat, i > 0);
-        tensor_mma(to + N, a + (kHalfTile >> 4), b, kWhat, i > 0);
-        if (q == 3) tensor_commit(&sh.empty[slot]);
+        const uint32_t a = tmem + kColumnsOfA<N> + slot * 64 + 8 * q;
+        const uint64_t b = operand_descriptor(smem_u32(smem) + slot * kWideStageBytes<N>) + 2 * q;
+        if (elect()) {
+          tensor_mma(to, a, b, kWhat, i > 0);
+          tensor_mma(to + N, a + 32, b, kWhat, i > 0);
+          if (q == 3) tensor_commit(&sh.empty[slot]);
+          if (i == 2 * GS - 1) tensor_commit(&sh.sums[k & 1]);
+        }
+        __syncwarp();
       }
-      tensor_commit(&sh.sums[k & 1]);
     };
     float acc[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) acc[j] = 0.f;
     uint16_t next = groups ? fetch(0) : 0;
-    if (tid == 0 && groups) issue(0);
+    if (warp == 0 && groups) issue(0);
     for (int k = 0; k < groups; ++k) {
       const uint16_t raw = next;
       if (k + 1 < groups) next = fetch(k + 1);
-      if (tid == 0 && k + 1 < groups) issue(k + 1);
+      if (warp == 0 && k + 1 < groups) issue(k + 1);
       __syncwarp();
       const float s = p.scale_bf16 ? __uint_as_float((uint32_t)raw << 16) : __half2float(__ushort_as_half(raw));
       barrier_wait(&sh.sums[k & 1], k >> 1 & 1, &sh.failed);
@@ -201,63 +249,82 @@ __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid
     // decode: thread d is channel d of the tile; and lay out the rows
     const int d = tid - 256, ch = min(tile * kWideChannels + d, p.m - 1);
     const uint4* codes = reinterpret_cast<const uint4*>(p.codes + (int64_t)ch * p.pieces * 16);
+    const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21) + kColumnsOfA<N> + (d >> 7) * 32;
     const Magic<BF> magic;
     constexpr int kUnits = N * 8 / 256;  // 16-byte pieces of B a thread lays out
-    uint4 code[kWideStages][2], row[kWideStages][kUnits];
-    uint32_t zero[kWideStages];
-    auto fetch = [&](int s, int slot) {
-      const int piece = 4 * c0 + 2 * s;
-      code[slot][0] = codes[min(piece, p.pieces - 1)];
-      code[slot][1] = codes[min(piece + 1, p.pieces - 1)];
+    // This thread's own places in the ring of raw stages: two pieces of codes, then its
+    // pieces of the rows (8 inputs of row u / 8, u = d + 256 i).  Rows past the batch repeat
+    // its last one: a column of B meets one column of the sums.
+    uint4* ring = reinterpret_cast<uint4*>(smem + kWideSums<N> + 256) + d;
+    const uint8_t* x[kUnits];
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i)
+      x[i] = p.x + ((int64_t)min((d + 256 * i) >> 3, p.rows - 1) * p.ldx + c0 * kChunk + 8 * (d & 7)) * (p.e4m3 ? 1 : 2);
+    auto fetch = [&](int s) {
+      if (s < stages) {
+        uint4* to = ring + s % kWideRing * (2 + kUnits) * 256;
+        const int piece = 4 * c0 + 2 * s;
+        copy16(smem_u32(to), codes + min(piece, p.pieces - 1));
+        copy16(smem_u32(to + 256), codes + min(piece + 1, p.pieces - 1));
+        const int have = p.n - c0 * kChunk - s * kStageInputs - 8 * (d & 7);  // inputs from this piece on
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+          uint4* slot = to + (2 + i) * 256;
+          if (p.x_vec && have >= 8) {
+            if (p.e4m3) copy8(smem_u32(slot), x[i] + s * kStageInputs);
+            else copy16(smem_u32(slot), x[i] + s * (2 * kStageInputs));
+          } else {
+            *slot = have > 0 ? load_inputs_one_by_one(x[i], p.e4m3, s * kStageInputs, have) : make_uint4(0, 0, 0, 0);
+          }
+        }
+      }
+      commit();
+    };
+    uint32_t zero = 0;
+    for (int s = 0; s < kWideRing - 1; ++s) fetch(s);
+    for (int s = 0; s < stages; ++s) {
+      const int slot = s % kWideStages;
       if constexpr (ZEROS) {
         // the group of the stage's first and second 32 inputs
         const int g0 = (4 * c0 + 2 * s) / GS;
-        zero[slot] = p.zeros[(int64_t)min(g0, p.groups - 1) * p.m + ch];
-        if constexpr (GS == 1) zero[slot] |= (uint32_t)p.zeros[(int64_t)min(g0 + 1, p.groups - 1) * p.m + ch] << 8;
-        else zero[slot] *= 0x101u;
+        zero = p.zeros[(int64_t)min(g0, p.groups - 1) * p.m + ch];
+        if constexpr (GS == 1) zero |= (uint32_t)p.zeros[(int64_t)min(g0 + 1, p.groups - 1) * p.m + ch] << 8;
+        else zero *= 0x101u;
       }
+      fetch(s + kWideRing - 1);
+      wait_group<kWideRing - 1>();  // this thread's own copies: nobody else reads them
+      const uint4* raw = ring + s % kWideRing * (2 + kUnits) * 256;
+      uint32_t a[32];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const uint4 v = raw[c / 4 * 256];
+        const uint32_t w = c % 4 == 0 ? v.x : c % 4 == 1 ? v.y : c % 4 == 2 ? v.z : v.w;
+        const uint2 z = zero_words<BF>(ZEROS ? zero >> (8 * (c / 4)) & 255u : 8u);
+        const uint2 lo = code_pairs<BF>(w, 0, magic, z), hi = code_pairs<BF>(w, 1, magic, z);
+        a[4 * c] = lo.x; a[4 * c + 1] = lo.y; a[4 * c + 2] = hi.x; a[4 * c + 3] = hi.y;
+      }
+      if (s >= kWideStages) {
+        barrier_wait(&sh.empty[slot], s / kWideStages - 1 & 1, &sh.failed);
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      }
+      __syncwarp();
+      tensor_store(lanes + slot * 64, a);
+      uint8_t* b = smem + slot * kWideStageBytes<N>;
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
-        const int u = d + 256 * i, r = u >> 3, k = c0 * kChunk + s * kStageInputs + 8 * (u & 7);
-        const int64_t at = (int64_t)r * p.ldx + k;
-        row[slot][i] = make_uint4(0, 0, 0, 0);
-        if (r < p.rows && k < p.n)
-          row[slot][i] = p.x_vec && k + 8 <= p.n ? load_inputs(p, at) : load_inputs_one_by_one(p.x, p.e4m3, at, p.n - k);
+        const int u = d + 256 * i, r = u >> 3, c = u & 7;
+        const uint4 v = raw[(2 + i) * 256], h = p.e4m3 ? bytes_to_half(v) : v;
+        *reinterpret_cast<uint4*>(b + r * 128 + ((c ^ (r & 7)) << 4)) =
+            make_uint4(__byte_perm(h.x, h.z, 0x5410), __byte_perm(h.x, h.z, 0x7632), __byte_perm(h.y, h.w, 0x5410),
+                       __byte_perm(h.y, h.w, 0x7632));
       }
-    };
-#pragma unroll
-    for (int j = 0; j < kWideStages; ++j)
-      if (j < stages) fetch(j, j);
-    for (int s0 = 0, turn = 0; s0 < stages; s0 += kWideStages, ++turn) {
-#pragma unroll
-      for (int j = 0; j < kWideStages; ++j) {
-        const int s = s0 + j;
-        if (s >= stages) break;
-        if (turn) barrier_wait(&sh.empty[j], (turn - 1) & 1, &sh.failed);
-        uint8_t* a = smem + j * kWideStageBytes<N> + (d >> 7) * kHalfTile + (d & 127) * 128;
-        uint8_t* b = smem + j * kWideStageBytes<N> + 2 * kHalfTile;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          const uint4 v = code[j][c / 4];
-          const uint32_t w = c % 4 == 0 ? v.x : c % 4 == 1 ? v.y : c % 4 == 2 ? v.z : v.w;
-          const uint2 z = zero_words<BF>(ZEROS ? zero[j] >> (8 * (c / 4)) & 255u : 8u);
-          const uint2 lo = code_pairs<BF>(w, 0, magic, z), hi = code_pairs<BF>(w, 1, magic, z);
-          *reinterpret_cast<uint4*>(a + ((c ^ (d & 7)) << 4)) = make_uint4(lo.x, lo.y, hi.x, hi.y);
-        }
-#pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-          const int u = d + 256 * i, r = u >> 3, c = u & 7;
-          const uint4 h = p.e4m3 ? bytes_to_half(row[j][i]) : row[j][i];
-          *reinterpret_cast<uint4*>(b + r * 128 + ((c ^ (r & 7)) << 4)) =
-              make_uint4(__byte_perm(h.x, h.z, 0x5410), __byte_perm(h.x, h.z, 0x7632), __byte_perm(h.y, h.w, 0x5410),
-                         __byte_perm(h.y, h.w, 0x7632));
-        }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) barrier_arrive(&sh.full[j]);
-        if (s + kWideStages < stages) fetch(s + kWideStages, j);
-      }
+      fence_proxy_async_smem();
+      tensor_store_wait();
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) barrier_arrive(&sh.full[slot]);
     }
+    wait_group<0>();
   }
   __syncwarp();
   if (p.split > 1) {
@@ -274,7 +341,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   if (warp == 0)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(4 * N));
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sh.tmem), "r"(kTensorColumns));
 }
 
 template <bool BF, int GS, int N, bool ZEROS>
