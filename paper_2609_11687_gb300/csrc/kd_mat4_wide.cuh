@@ -8,16 +8,20 @@
 // lane (through shared memory, which is then written and read once per stage by A's 32 KB,
 // 32000 x 4096 at 64 rows took 51 us instead of 48 when this was changed).
 //
-// Roles in a CTA, which owns 256 channels (two A tiles for each B tile, which halves the
-// traffic of the rows) and its share of the inputs:
-//   warps 0-7   a thread a channel: after each group of inputs its sums are read from tensor
-//               memory, scaled and added in fp32 registers, while the next group's form in
-//               the other of two accumulators; one thread of warp 0 issues the products;
-//   warps 8-15  a thread a channel: 64 codes a stage become 32 columns of its lane of A, two
-//               inputs each; the same threads lay out B in shared memory.  Codes and rows come
-//               through a ring that each thread fills and reads for itself (cp.async).
-// Stages of A and B, and the accumulators, pass between them by mbarriers.  B is K-major
-// with 128-byte swizzle: 16-byte piece c of row r lies at c ^ (r % 8).
+// A CTA owns 256 channels (two A tiles for each B, which halves the traffic of the rows) and
+// its share of the inputs, in chunks of 128.  Its 16 warps all do the same: a thread has one
+// channel (the warp's place among the lanes of tensor memory gives it) and one half of what
+// belongs to that channel.  Per chunk it turns 64 codes into 32 columns of its lane of A and
+// lays out its share of B; per group of inputs it reads its half of the group's sums from
+// tensor memory, scales and adds them in fp32 registers, while the next group's form in the
+// other of two accumulators.  One thread issues the products.  Codes and rows come through a
+// ring (cp.async); the two warps of 32 channels copy those together, four lanes a channel:
+// a lane for each channel's 64 bytes is 32 lines a load, and the lines a load touches are
+// what it costs.
+//
+// Stages of A and B, and the accumulators, pass between threads and tensor cores by
+// mbarriers.  B is K-major with 128-byte swizzle: 16-byte piece c of row r lies at
+// c ^ (r % 8), chunks in two halves of 64 inputs.
 //
 // K order: a piece of eight inputs holds them as the codes of a word come out, (0 4 1 5 2 6
 // 3 7), in A and B alike.
@@ -33,26 +37,30 @@ namespace mat4 {
 
 constexpr int kWideChannels = 256;
 constexpr int kWideThreads = 512;
-constexpr int kWideStages = 4;  // of A and B
-constexpr int kWideRing = 7;    // of codes and rows as they come
-constexpr int kStageInputs = 64;
+constexpr int kWideWarps = kWideThreads / 32;
+constexpr int kWideStages = 2;  // of A and B
+constexpr int kWideRing = 5;    // of codes and rows as they come
 template <int N>
-constexpr int kWideStageBytes = N * 128;  // of B
-// B's stages, or in the end the CTA's sums; the barriers; the ring of raw codes and rows;
-// room to align
+constexpr int kWideUnits = N * 16 / kWideThreads;  // 16-byte pieces of B a thread lays out
 template <int N>
-constexpr size_t kWideSums = (size_t)N * kWideChannels * 4;
+constexpr int kWideStageBytes = N * 256;  // of B
 template <int N>
-constexpr size_t kWideSmem = kWideSums<N> + 256 + (size_t)kWideRing * (2 + N / 32) * 256 * 16 + 1024;
+constexpr int kWideRingBytes = (2 + kWideUnits<N>) * kWideThreads * 16;  // of a chunk
+// The barriers (and what aligns B), B's stages, the ring; in the end the CTA's sums in their place.
+template <int N>
+constexpr size_t kWideSmem = 1024 + 1024 + kWideStages * kWideStageBytes<N> + kWideRing * kWideRingBytes<N>;
+static_assert(kWideSmem<64> <= 227 * 1024 && kWideSmem<32> >= 2048 + 32 * kWideChannels * 4 &&
+                  kWideSmem<64> >= 2048 + 64 * kWideChannels * 4,
+              "shared memory");
 // Columns of tensor memory, all 512 taken (one CTA an SM): two accumulators of two times 128
-// channels, N columns each; A's stages, 32 columns for each 128 channels.
+// channels, N columns each; A's stages, 64 columns for each 128 channels.
 constexpr int kTensorColumns = 512;
 template <int N>
 constexpr int kColumnsOfA = 4 * N;
-static_assert(kColumnsOfA<64> + kWideStages * 64 <= kTensorColumns, "tensor memory");
+static_assert(kColumnsOfA<64> + kWideStages * 128 <= kTensorColumns, "tensor memory");
 
 struct WideBarriers {
-  uint64_t full[kWideStages], empty[kWideStages];
+  uint64_t full[kWideStages], empty[kWideStages];  // a stage of A and B is laid out; its products are done
   uint64_t sums[2], taken[2];  // an accumulator holds a group's sums; they have been read
   uint32_t tmem;
   int failed;
@@ -98,7 +106,16 @@ __device__ __forceinline__ void tensor_commit(uint64_t* b) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b))
                : "memory");
 }
-// 32 columns of this warp's 32 lanes
+// 16 or 32 columns of this warp's 32 lanes
+__device__ __forceinline__ void tensor_load(uint32_t address, float (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, "
+      "[%16];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+        "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+      : "r"(address));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
 __device__ __forceinline__ void tensor_load(uint32_t address, float (&v)[32]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
@@ -136,12 +153,14 @@ __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid
   extern __shared__ uint4 smem_raw[];
   const uint32_t pad = -smem_u32(smem_raw) & 1023u;  // operands start on 1024 bytes
   uint8_t* smem = reinterpret_cast<uint8_t*>(smem_raw) + pad;
-  WideBarriers& sh = *reinterpret_cast<WideBarriers*>(smem + kWideSums<N>);
+  WideBarriers& sh = *reinterpret_cast<WideBarriers*>(smem);
+  uint8_t* stage_b = smem + 1024;
+  uint4* ring = reinterpret_cast<uint4*>(stage_b + kWideStages * kWideStageBytes<N>) + threadIdx.x;
   // by shuffle: so the compiler knows a warp's role to be the same for all its lanes
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(~0u, tid >> 5, 0);
   const int rank = special<kRank>(), tile = special<kCluster>();
   const int c0 = rank * p.per, mine = max(0, min(p.per, p.chunks - c0));
-  const int stages = 2 * mine, groups = mine * (4 / GS);
+  constexpr int kGroups = 4 / GS, kUnits = kWideUnits<N>, kHalf = N / 2;
 
   if (warp == 0) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)),
@@ -150,13 +169,11 @@ __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (tid == 32) {
-    for (int s = 0; s < kWideStages; ++s) {
-      mbar_init(&sh.full[s], 8);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&sh.full[s], kWideWarps);
       mbar_init(&sh.empty[s], 1);
-    }
-    for (int b = 0; b < 2; ++b) {
-      mbar_init(&sh.sums[b], 1);
-      mbar_init(&sh.taken[b], 8);
+      mbar_init(&sh.sums[s], 1);
+      mbar_init(&sh.taken[s], kWideWarps);
     }
     sh.failed = 0;
     mbar_init_fence();
@@ -164,171 +181,200 @@ __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  constexpr uint32_t tmem = 0;  // all of it
   depend_on_last();
 
-  const float nan = __int_as_float(0x7FC00000);
-  float* sums = reinterpret_cast<float*>(smem);  // of the CTA, in the end
-  auto finish = [&](int r, int c, float v) {
-    const int ch = tile * kWideChannels + c;
-    if (ch >= p.m) return;
-    if (p.xs) v *= p.xs[r];
-    store1_any(p.y, p.ydtype, (int64_t)r * p.ldy + ch, v);
-  };
-  if (warp < 8) {
-    // scale and add: thread tid is channel tid of the tile
-    const int ch = min(tile * kWideChannels + tid, p.m - 1);
-    const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + (warp >> 2) * N;
-    auto fetch = [&](int k) { return p.scales[(int64_t)min(c0 * (4 / GS) + k, p.groups - 1) * p.m + ch]; };
-    // warp 0: the products of group k
-    auto issue = [&](int k) {
-      // fp32 sums of fp16 or bf16 products, M = 128, N, B K-major
-      constexpr uint32_t kWhat = 1u << 4 | (BF ? 1u : 0u) << 7 | (BF ? 1u : 0u) << 10 | (N / 8) << 17 | (128 / 16) << 24;
-      if (k >= 2) {
-        barrier_wait(&sh.taken[k & 1], (k >> 1) - 1 & 1, &sh.failed);
-        __syncwarp();
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      }
-      const uint32_t to = tmem + (k & 1) * 2 * N;
+  // this thread's lane of tensor memory, channel, and half: inputs 64 part .. + 63 of a
+  // chunk, rows kHalf part .. of the sums (tensor memory starts at 0: all of it is taken)
+  const int tile_half = warp >> 2 & 1, part = warp >> 3, of_tile = tile_half * 128 + (warp & 3) * 32 + lane;
+  const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+  const int ch = min(tile * kWideChannels + of_tile, p.m - 1);
+
+  // Codes: pieces idx % 4 of channel idx / 4 of the 32 that this warp shares with the one
+  // eight further, idx = 32 part + lane (+ 64); piece c of channel r lies at c ^ (r / 2 % 4).
+  // Rows: 8 inputs of row u / 16, u = tid + 512 i, for this thread alone.  Rows past the
+  // batch repeat its last one: a column of B meets one column of the sums.
+  const int idx = 32 * part + lane, base = tile * kWideChannels + tile_half * 128 + (warp & 3) * 32;
+  uint4* pair_ring = reinterpret_cast<uint4*>(stage_b + kWideStages * kWideStageBytes<N>) + (warp & 7) * 128;
+  const uint4* codes[2];
+  int code_at[2];
 #pragma unroll
-      for (int i = 0; i < 2 * GS; ++i) {  // 16 inputs each: 32 bytes further along the rows
-        const int s = (2 * GS * k + i) / 4, slot = s % kWideStages, q = (GS == 1 ? 2 * (k & 1) : 0) + i % 4;
-        if (q == 0) {
-          barrier_wait(&sh.full[slot], s / kWideStages & 1, &sh.failed);
-          __syncwarp();
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        }
-        const uint32_t a = tmem + kColumnsOfA<N> + slot * 64 + 8 * q;
-        const uint64_t b = operand_descriptor(smem_u32(smem) + slot * kWideStageBytes<N>) + 2 * q;
-        if (elect()) {
-          tensor_mma(to, a, b, kWhat, i > 0);
-          tensor_mma(to + N, a + 32, b, kWhat, i > 0);
-          if (q == 3) tensor_commit(&sh.empty[slot]);
-          if (i == 2 * GS - 1) tensor_commit(&sh.sums[k & 1]);
-        }
-        __syncwarp();
-      }
-    };
-    float acc[N];
+  for (int i = 0; i < 2; ++i) {
+    const int r = (idx + 64 * i) >> 2, c = idx & 3;
+    codes[i] = reinterpret_cast<const uint4*>(p.codes + (int64_t)min(base + r, p.m - 1) * p.pieces * 16);
+    code_at[i] = r * 4 + (c ^ (r >> 1 & 3));
+  }
+  const uint8_t* x[kUnits];
 #pragma unroll
-    for (int j = 0; j < N; ++j) acc[j] = 0.f;
-    uint16_t next = groups ? fetch(0) : 0;
-    if (warp == 0 && groups) issue(0);
-    for (int k = 0; k < groups; ++k) {
-      const uint16_t raw = next;
-      if (k + 1 < groups) next = fetch(k + 1);
-      if (warp == 0 && k + 1 < groups) issue(k + 1);
-      __syncwarp();
-      const float s = p.scale_bf16 ? __uint_as_float((uint32_t)raw << 16) : __half2float(__ushort_as_half(raw));
-      barrier_wait(&sh.sums[k & 1], k >> 1 & 1, &sh.failed);
-      __syncwarp();
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  for (int i = 0; i < kUnits; ++i)
+    x[i] = p.x + ((int64_t)min((tid + kWideThreads * i) >> 4, p.rows - 1) * p.ldx + c0 * kChunk + 8 * (tid & 15)) *
+                     (p.e4m3 ? 1 : 2);
+  const int whole = p.x_vec ? (p.n - c0 * kChunk) / kChunk : 0;  // chunks without a row's end
+  int to_slot = 0;
+  auto fetch = [&](int l) {
+    if (l < mine) {
+      const int slot_at = to_slot * (kWideRingBytes<N> / 16);
+      to_slot = to_slot + 1 == kWideRing ? 0 : to_slot + 1;
+      const int piece = min(4 * (c0 + l) + (idx & 3), p.pieces - 1);
 #pragma unroll
-      for (int h = 0; h < N / 32; ++h) {
-        float v[32];
-        tensor_load(from + (k & 1) * 2 * N + 32 * h, v);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) acc[32 * h + j] = __fmaf_rn(s, v[j], acc[32 * h + j]);
-      }
-      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) barrier_arrive(&sh.taken[k & 1]);
-    }
-    // the last sums are here, so no product runs any more and the stages' memory is free;
-    // nothing of this CTA is in flight when it ends
-    if (stages) barrier_wait(&sh.empty[(stages - 1) % kWideStages], (stages - 1) / kWideStages & 1, &sh.failed);
-    const bool failed = *static_cast<volatile int*>(&sh.failed);
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (j < p.rows) {
-        const float v = failed ? nan : acc[j];
-        if (p.split == 1) finish(j, tid, v);
-        else sums[j * kWideChannels + tid] = v;
-      }
-  } else {
-    // decode: thread d is channel d of the tile; and lay out the rows
-    const int d = tid - 256, ch = min(tile * kWideChannels + d, p.m - 1);
-    const uint4* codes = reinterpret_cast<const uint4*>(p.codes + (int64_t)ch * p.pieces * 16);
-    const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21) + kColumnsOfA<N> + (d >> 7) * 32;
-    const Magic<BF> magic;
-    constexpr int kUnits = N * 8 / 256;  // 16-byte pieces of B a thread lays out
-    // This thread's own places in the ring of raw stages: two pieces of codes, then its
-    // pieces of the rows (8 inputs of row u / 8, u = d + 256 i).  Rows past the batch repeat
-    // its last one: a column of B meets one column of the sums.
-    uint4* ring = reinterpret_cast<uint4*>(smem + kWideSums<N> + 256) + d;
-    const uint8_t* x[kUnits];
-#pragma unroll
-    for (int i = 0; i < kUnits; ++i)
-      x[i] = p.x + ((int64_t)min((d + 256 * i) >> 3, p.rows - 1) * p.ldx + c0 * kChunk + 8 * (d & 7)) * (p.e4m3 ? 1 : 2);
-    auto fetch = [&](int s) {
-      if (s < stages) {
-        uint4* to = ring + s % kWideRing * (2 + kUnits) * 256;
-        const int piece = 4 * c0 + 2 * s;
-        copy16(smem_u32(to), codes + min(piece, p.pieces - 1));
-        copy16(smem_u32(to + 256), codes + min(piece + 1, p.pieces - 1));
-        const int have = p.n - c0 * kChunk - s * kStageInputs - 8 * (d & 7);  // inputs from this piece on
+      for (int i = 0; i < 2; ++i) copy16(smem_u32(pair_ring + slot_at + code_at[i]), codes[i] + piece);
+      if (l < whole) {
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
-          uint4* slot = to + (2 + i) * 256;
-          if (p.x_vec && have >= 8) {
-            if (p.e4m3) copy8(smem_u32(slot), x[i] + s * kStageInputs);
-            else copy16(smem_u32(slot), x[i] + s * (2 * kStageInputs));
-          } else {
-            *slot = have > 0 ? load_inputs_one_by_one(x[i], p.e4m3, s * kStageInputs, have) : make_uint4(0, 0, 0, 0);
-          }
+          const uint32_t slot = smem_u32(ring + slot_at + (2 + i) * kWideThreads);
+          if (p.e4m3) copy8(slot, x[i] + l * kChunk);
+          else copy16(slot, x[i] + l * (2 * kChunk));
         }
+      } else {
+        const int have = p.n - (c0 + l) * kChunk - 8 * (tid & 15);  // inputs from this piece on
+#pragma unroll 1
+        for (int i = 0; i < kUnits; ++i)
+          ring[slot_at + (2 + i) * kWideThreads] =
+              have > 0 ? load_inputs_one_by_one(x[i], p.e4m3, l * kChunk, have) : make_uint4(0, 0, 0, 0);
       }
-      commit();
-    };
-    uint32_t zero = 0;
-    for (int s = 0; s < kWideRing - 1; ++s) fetch(s);
-    for (int s = 0; s < stages; ++s) {
-      const int slot = s % kWideStages;
-      if constexpr (ZEROS) {
-        // the group of the stage's first and second 32 inputs
-        const int g0 = (4 * c0 + 2 * s) / GS;
-        zero = p.zeros[(int64_t)min(g0, p.groups - 1) * p.m + ch];
-        if constexpr (GS == 1) zero |= (uint32_t)p.zeros[(int64_t)min(g0 + 1, p.groups - 1) * p.m + ch] << 8;
-        else zero *= 0x101u;
-      }
-      fetch(s + kWideRing - 1);
-      wait_group<kWideRing - 1>();  // this thread's own copies: nobody else reads them
-      const uint4* raw = ring + s % kWideRing * (2 + kUnits) * 256;
-      uint32_t a[32];
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        const uint4 v = raw[c / 4 * 256];
-        const uint32_t w = c % 4 == 0 ? v.x : c % 4 == 1 ? v.y : c % 4 == 2 ? v.z : v.w;
-        const uint2 z = zero_words<BF>(ZEROS ? zero >> (8 * (c / 4)) & 255u : 8u);
-        const uint2 lo = code_pairs<BF>(w, 0, magic, z), hi = code_pairs<BF>(w, 1, magic, z);
-        a[4 * c] = lo.x; a[4 * c + 1] = lo.y; a[4 * c + 2] = hi.x; a[4 * c + 3] = hi.y;
-      }
-      if (s >= kWideStages) {
-        barrier_wait(&sh.empty[slot], s / kWideStages - 1 & 1, &sh.failed);
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      }
-      __syncwarp();
-      tensor_store(lanes + slot * 64, a);
-      uint8_t* b = smem + slot * kWideStageBytes<N>;
-#pragma unroll
-      for (int i = 0; i < kUnits; ++i) {
-        const int u = d + 256 * i, r = u >> 3, c = u & 7;
-        const uint4 v = raw[(2 + i) * 256], h = p.e4m3 ? bytes_to_half(v) : v;
-        *reinterpret_cast<uint4*>(b + r * 128 + ((c ^ (r & 7)) << 4)) =
-            make_uint4(__byte_perm(h.x, h.z, 0x5410), __byte_perm(h.x, h.z, 0x7632), __byte_perm(h.y, h.w, 0x5410),
-                       __byte_perm(h.y, h.w, 0x7632));
-      }
-      fence_proxy_async_smem();
-      tensor_store_wait();
-      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) barrier_arrive(&sh.full[slot]);
     }
-    wait_group<0>();
+    commit();
+  };
+  for (int l = 0; l < kWideRing - 1; ++l) fetch(l);
+
+  // scales, and zero points of this thread's inputs, of a chunk's groups
+  uint32_t scale[kGroups], zero[GS == 1 ? 2 : 1];
+  const uint16_t* scales = p.scales + (int64_t)c0 * kGroups * p.m + ch;
+  auto fetch_scales = [&](int l) {
+#pragma unroll
+    for (int k = 0; k < kGroups; ++k)
+      scale[k] = scales[(int64_t)(GS == 4 ? l : min(l * kGroups + k, p.groups - 1 - c0 * kGroups)) * p.m];
+    if constexpr (ZEROS) {
+#pragma unroll
+      for (int k = 0; k < (GS == 1 ? 2 : 1); ++k)
+        zero[k] = p.zeros[(int64_t)min((4 * (c0 + l) + 2 * part + k) / GS, p.groups - 1) * p.m + ch];
+    }
+  };
+  if (mine) fetch_scales(0);
+
+  // warp 0: the products of group k, of chunk l
+  auto issue = [&](int l, int k) {
+    // fp32 sums of fp16 or bf16 products, M = 128, N, B K-major
+    constexpr uint32_t kWhat = 1u << 4 | (BF ? 1u : 0u) << 7 | (BF ? 1u : 0u) << 10 | (N / 8) << 17 | (128 / 16) << 24;
+    const int group = l * kGroups + k, stage = l & 1;
+    if (group >= 2) barrier_wait(&sh.taken[group & 1], (group >> 1) - 1 & 1, &sh.failed);
+    if (k == 0) barrier_wait(&sh.full[stage], l >> 1 & 1, &sh.failed);
+    __syncwarp();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t to = (group & 1) * 2 * N, a = kColumnsOfA<N> + stage * 128 + k * (16 * GS);
+    const uint64_t b = operand_descriptor(smem_u32(stage_b) + stage * kWideStageBytes<N>);
+    if (elect()) {
+#pragma unroll
+      for (int i = 0; i < 2 * GS; ++i) {  // 16 inputs each: 32 bytes further along the rows
+        const int q = 2 * GS * k + i;
+        const uint64_t bq = b + (q >> 2) * (N * 128 / 16) + 2 * (q & 3);
+        tensor_mma(to, a + 8 * i, bq, kWhat, i > 0);
+        tensor_mma(to + N, a + 64 + 8 * i, bq, kWhat, i > 0);
+      }
+      if (k == kGroups - 1) tensor_commit(&sh.empty[stage]);
+      tensor_commit(&sh.sums[group & 1]);
+    }
+    __syncwarp();
+  };
+  float acc[kHalf];
+#pragma unroll
+  for (int j = 0; j < kHalf; ++j) acc[j] = 0.f;
+  // this thread's sums of a group, scaled and added
+  auto take = [&](int group, uint32_t raw) {
+    const float s = p.scale_bf16 ? __uint_as_float(raw << 16) : __half2float(__ushort_as_half((unsigned short)raw));
+    barrier_wait(&sh.sums[group & 1], group >> 1 & 1, &sh.failed);
+    __syncwarp();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    float v[kHalf];
+    tensor_load(lanes + (group & 1) * 2 * N + tile_half * N + part * kHalf, v);
+#pragma unroll
+    for (int j = 0; j < kHalf; ++j) acc[j] = __fmaf_rn(s, v[j], acc[j]);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) barrier_arrive(&sh.taken[group & 1]);
+  };
+
+  const Magic<BF> magic;
+  uint32_t last = 0;  // the scale of the group before
+  int from_slot = 0;
+  for (int l = 0; l < mine; ++l) {
+    const int stage = l & 1;
+    uint32_t now[kGroups];
+#pragma unroll
+    for (int k = 0; k < kGroups; ++k) now[k] = scale[k];
+    wait_group<kWideRing - 2>();
+    // both warps' copies are there, and both have read the chunk before, whose place is next
+    asm volatile("barrier.sync %0, 64;" ::"r"(1 + (warp & 7)) : "memory");
+    fetch(l + kWideRing - 1);
+    const int slot_at = from_slot * (kWideRingBytes<N> / 16);
+    from_slot = from_slot + 1 == kWideRing ? 0 : from_slot + 1;
+    const uint4* raw = ring + slot_at;
+    uint4 word[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) word[c] = pair_ring[slot_at + lane * 4 + ((2 * part + c) ^ (lane >> 1 & 3))];
+    uint32_t a[32];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const uint4 v = word[c / 4];
+      const uint32_t w = c % 4 == 0 ? v.x : c % 4 == 1 ? v.y : c % 4 == 2 ? v.z : v.w;
+      const uint2 z = zero_words<BF>(ZEROS ? zero[GS == 1 ? c / 4 : 0] : 8u);
+      const uint2 lo = code_pairs<BF>(w, 0, magic, z), hi = code_pairs<BF>(w, 1, magic, z);
+      a[4 * c] = lo.x; a[4 * c + 1] = lo.y; a[4 * c + 2] = hi.x; a[4 * c + 3] = hi.y;
+    }
+    if (l + 1 < mine) fetch_scales(l + 1);
+    if (l >= kWideStages) barrier_wait(&sh.empty[stage], (l >> 1) - 1 & 1, &sh.failed);
+    __syncwarp();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    tensor_store(lanes + kColumnsOfA<N> + stage * 128 + tile_half * 64 + part * 32, a);
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      const int u = tid + kWideThreads * i, r = u >> 4, c = u & 15;
+      const uint4 v = raw[(2 + i) * kWideThreads], h = p.e4m3 ? bytes_to_half(v) : v;
+      *reinterpret_cast<uint4*>(stage_b + stage * kWideStageBytes<N> + (c >> 3) * (N * 128) + r * 128 +
+                                (((c ^ r) & 7) << 4)) =
+          make_uint4(__byte_perm(h.x, h.z, 0x5410), __byte_perm(h.x, h.z, 0x7632), __byte_perm(h.y, h.w, 0x5410),
+                     __byte_perm(h.y, h.w, 0x7632));
+    }
+    fence_proxy_async_smem();
+    tensor_store_wait();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) barrier_arrive(&sh.full[stage]);
+#pragma unroll
+    for (int k = 0; k < kGroups; ++k) {
+      if (warp == 0) issue(l, k);
+      if (l * kGroups + k > 0) take(l * kGroups + k - 1, k ? now[k - 1] : last);
+    }
+    last = now[kGroups - 1];
   }
-  __syncwarp();
-  if (p.split > 1) {
+  if (mine) {
+    take(mine * kGroups - 1, last);
+    // nothing of this CTA is in flight when it ends
+    barrier_wait(&sh.empty[(mine - 1) & 1], (mine - 1) >> 1 & 1, &sh.failed);
+  }
+  wait_group<0>();
+
+  const bool failed = *static_cast<volatile int*>(&sh.failed);
+  auto finish = [&](int r, int c, float v) {
+    const int j = tile * kWideChannels + c;
+    if (j >= p.m) return;
+    if (p.xs) v *= p.xs[r];
+    store1_any(p.y, p.ydtype, (int64_t)r * p.ldy + j, v);
+  };
+  if (failed) {
+#pragma unroll
+    for (int j = 0; j < kHalf; ++j) acc[j] = __int_as_float(0x7FC00000);
+  }
+  if (p.split == 1) {
+#pragma unroll
+    for (int j = 0; j < kHalf; ++j)
+      if (part * kHalf + j < p.rows) finish(part * kHalf + j, of_tile, acc[j]);
+  } else {
     cg::cluster_group cl = cg::this_cluster();
+    float* sums = reinterpret_cast<float*>(stage_b);
+    __syncthreads();  // stages and ring are free: every thread has its last sums
+#pragma unroll
+    for (int j = 0; j < kHalf; ++j)
+      if (part * kHalf + j < p.rows) sums[(part * kHalf + j) * kWideChannels + of_tile] = acc[j];
     cl.sync();
     for (int o = rank * kWideThreads + tid; o < p.rows * kWideChannels; o += p.split * kWideThreads) {
       float v = 0.f;
