@@ -571,12 +571,14 @@ kd_status kd_dequantise_4bit(const kd_weight4* w, kd_dtype out_dtype, void* out,
  *   x       device, x_dtype KD_F16, KD_BF16 or KD_E4M3; x_scale: rows fp32 (the e4m3
  *           rows' scales, as kd_rmsnorm leaves them), or NULL: 1.
  *   y       device, y_dtype KD_F32, KD_F16 or KD_BF16.
- * Meant for few rows (decoding): up to 32 rows share one pass over the weights, more rows
+ * Meant for few rows (decoding): up to 64 rows share one pass over the weights, more rows
  * take more passes.  Within a group the sum over integers code - zero is formed on the tensor
  * cores (exact products, fp32 sums); groups are added in fp32 with their scale, and the
  * whole is rounded once.  The order of the sums is fixed (deterministic results), and is
  * the same for all calls of at most eight rows: a row's bits do not depend on what shares
- * its batch.  An infinity or NaN in a row leaves nothing finite in that row alone.
+ * its batch.  An infinity or NaN in a row leaves nothing finite in that row alone.  (From
+ * 17 rows on every wait inside the kernel is bounded to about a second; one that expires
+ * gives NaN in the outputs of its channels.)
  * Rows of 16-byte aligned base and stride (8-byte for e4m3) take wide loads.
  * Errors: KD_ERR_INVALID_ARG (sizes, group, types, ld < n or ldy < m, pointers missing
  * with m > 0 and rows > 0, or unaligned), KD_ERR_UNSUPPORTED_N (n > 65536), KD_ERR_CUDA.

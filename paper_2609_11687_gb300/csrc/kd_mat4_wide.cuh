@@ -8,16 +8,17 @@
 // lane (through shared memory, which is then written and read once per stage by A's 32 KB,
 // 32000 x 4096 at 64 rows took 51 us instead of 48 when this was changed).
 //
-// A CTA owns 256 channels (two A tiles for each B, which halves the traffic of the rows) and
-// its share of the inputs, in chunks of 128.  Its 16 warps all do the same: a thread has one
+// A CTA owns 128 channels and its share of the inputs, in chunks of 128; two CTAs share an
+// SM, so that one computes while the other waits (one CTA of 256 channels and twice the warps:
+// 24 us instead of 14 at 32 rows of 4096 x 11008).  Its eight warps all do the same: a thread has one
 // channel (the warp's place among the lanes of tensor memory gives it) and one half of what
 // belongs to that channel.  Per chunk it turns 64 codes into 32 columns of its lane of A and
 // lays out its share of B; per group of inputs it reads its half of the group's sums from
 // tensor memory, scales and adds them in fp32 registers, while the next group's form in the
 // other of two accumulators.  One thread issues the products.  Codes and rows come through a
-// ring (cp.async); the two warps of 32 channels copy those together, four lanes a channel:
-// a lane for each channel's 64 bytes is 32 lines a load, and the lines a load touches are
-// what it costs.
+// ring (cp.async); the two warps of 32 channels copy their codes together, four lanes a
+// channel: a lane for each channel's 64 bytes is 32 lines a load, and the lines a load touches
+// are what it costs.
 //
 // Stages of A and B, and the accumulators, pass between threads and tensor cores by
 // mbarriers.  B is K-major with 128-byte swizzle: 16-byte piece c of row r lies at
@@ -35,11 +36,12 @@
 namespace kd {
 namespace mat4 {
 
-constexpr int kWideChannels = 256;
-constexpr int kWideThreads = 512;
+constexpr int kWideChannels = 128;
+constexpr int kWideThreads = 256;
 constexpr int kWideWarps = kWideThreads / 32;
 constexpr int kWideStages = 2;  // of A and B
-constexpr int kWideRing = 5;    // of codes and rows as they come
+template <int N>
+constexpr int kWideRing = N == 64 ? 3 : 5;  // chunks of codes and rows as they come
 template <int N>
 constexpr int kWideUnits = N * 16 / kWideThreads;  // 16-byte pieces of B a thread lays out
 template <int N>
@@ -48,16 +50,15 @@ template <int N>
 constexpr int kWideRingBytes = (2 + kWideUnits<N>) * kWideThreads * 16;  // of a chunk
 // The barriers (and what aligns B), B's stages, the ring; in the end the CTA's sums in their place.
 template <int N>
-constexpr size_t kWideSmem = 1024 + 1024 + kWideStages * kWideStageBytes<N> + kWideRing * kWideRingBytes<N>;
-static_assert(kWideSmem<64> <= 227 * 1024 && kWideSmem<32> >= 2048 + 32 * kWideChannels * 4 &&
-                  kWideSmem<64> >= 2048 + 64 * kWideChannels * 4,
-              "shared memory");
-// Columns of tensor memory, all 512 taken (one CTA an SM): two accumulators of two times 128
-// channels, N columns each; A's stages, 64 columns for each 128 channels.
-constexpr int kTensorColumns = 512;
+constexpr size_t kWideSmem = 1024 + 1024 + kWideStages * kWideStageBytes<N> + kWideRing<N> * kWideRingBytes<N>;
+static_assert(kWideSmem<64> <= 113 * 1024 && kWideSmem<32> <= 113 * 1024 &&
+                  kWideSmem<32> >= 2048 + 32 * kWideChannels * 4 && kWideSmem<64> >= 2048 + 64 * kWideChannels * 4,
+              "shared memory of two CTAs an SM");
+// Columns of tensor memory: two accumulators of N columns, A's stages of 64.  Half of all 512.
+constexpr int kTensorColumns = 256;
 template <int N>
-constexpr int kColumnsOfA = 4 * N;
-static_assert(kColumnsOfA<64> + kWideStages * 128 <= kTensorColumns, "tensor memory");
+constexpr int kColumnsOfA = 2 * N;
+static_assert(kColumnsOfA<64> + kWideStages * 64 <= kTensorColumns, "tensor memory");
 
 struct WideBarriers {
   uint64_t full[kWideStages], empty[kWideStages];  // a stage of A and B is laid out; its products are done
@@ -146,9 +147,9 @@ __device__ __forceinline__ void copy8(uint32_t dst, const void* src) {
 }
 
 // BF: bf16 rows; GS: groups of 32 GS inputs; N: rows of a pass at most (32, 64); ZEROS: zero
-// points by group.  Grid: one cluster of `split` CTAs for each 256 channels.
+// points by group.  Grid: one cluster of `split` CTAs for each 128 channels.
 template <bool BF, int GS, int N, bool ZEROS>
-__global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kWideThreads, 2) mat4_wide_kernel(const __grid_constant__ Params p) {
   namespace cg = cooperative_groups;
   extern __shared__ uint4 smem_raw[];
   const uint32_t pad = -smem_u32(smem_raw) & 1023u;  // operands start on 1024 bytes
@@ -160,7 +161,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(~0u, tid >> 5, 0);
   const int rank = special<kRank>(), tile = special<kCluster>();
   const int c0 = rank * p.per, mine = max(0, min(p.per, p.chunks - c0));
-  constexpr int kGroups = 4 / GS, kUnits = kWideUnits<N>, kHalf = N / 2;
+  constexpr int kGroups = 4 / GS, kUnits = kWideUnits<N>, kHalf = N / 2, kRing = kWideRing<N>;
 
   if (warp == 0) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)),
@@ -184,17 +185,17 @@ __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid
   depend_on_last();
 
   // this thread's lane of tensor memory, channel, and half: inputs 64 part .. + 63 of a
-  // chunk, rows kHalf part .. of the sums (tensor memory starts at 0: all of it is taken)
-  const int tile_half = warp >> 2 & 1, part = warp >> 3, of_tile = tile_half * 128 + (warp & 3) * 32 + lane;
-  const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+  // chunk, rows kHalf part .. of the sums
+  const int part = warp >> 2, of_tile = (warp & 3) * 32 + lane;
+  const uint32_t tensor = __shfl_sync(~0u, sh.tmem, 0), lanes = tensor + ((uint32_t)(warp & 3) << 21);
   const int ch = min(tile * kWideChannels + of_tile, p.m - 1);
 
   // Codes: pieces idx % 4 of channel idx / 4 of the 32 that this warp shares with the one
-  // eight further, idx = 32 part + lane (+ 64); piece c of channel r lies at c ^ (r / 2 % 4).
-  // Rows: 8 inputs of row u / 16, u = tid + 512 i, for this thread alone.  Rows past the
+  // four further, idx = 32 part + lane (+ 64); piece c of channel r lies at c ^ (r / 2 % 4).
+  // Rows: 8 inputs of row u / 16, u = tid + 256 i, for this thread alone.  Rows past the
   // batch repeat its last one: a column of B meets one column of the sums.
-  const int idx = 32 * part + lane, base = tile * kWideChannels + tile_half * 128 + (warp & 3) * 32;
-  uint4* pair_ring = reinterpret_cast<uint4*>(stage_b + kWideStages * kWideStageBytes<N>) + (warp & 7) * 128;
+  const int idx = 32 * part + lane, base = tile * kWideChannels + (warp & 3) * 32;
+  uint4* pair_ring = reinterpret_cast<uint4*>(stage_b + kWideStages * kWideStageBytes<N>) + (warp & 3) * 128;
   const uint4* codes[2];
   int code_at[2];
 #pragma unroll
@@ -213,7 +214,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid
   auto fetch = [&](int l) {
     if (l < mine) {
       const int slot_at = to_slot * (kWideRingBytes<N> / 16);
-      to_slot = to_slot + 1 == kWideRing ? 0 : to_slot + 1;
+      to_slot = to_slot + 1 == kRing ? 0 : to_slot + 1;
       const int piece = min(4 * (c0 + l) + (idx & 3), p.pieces - 1);
 #pragma unroll
       for (int i = 0; i < 2; ++i) copy16(smem_u32(pair_ring + slot_at + code_at[i]), codes[i] + piece);
@@ -234,7 +235,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid
     }
     commit();
   };
-  for (int l = 0; l < kWideRing - 1; ++l) fetch(l);
+  for (int l = 0; l < kRing - 1; ++l) fetch(l);
 
   // scales, and zero points of this thread's inputs, of a chunk's groups
   uint32_t scale[kGroups], zero[GS == 1 ? 2 : 1];
@@ -260,7 +261,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid
     if (k == 0) barrier_wait(&sh.full[stage], l >> 1 & 1, &sh.failed);
     __syncwarp();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const uint32_t to = (group & 1) * 2 * N, a = kColumnsOfA<N> + stage * 128 + k * (16 * GS);
+    const uint32_t to = tensor + (group & 1) * N, a = tensor + kColumnsOfA<N> + stage * 64 + k * (16 * GS);
     const uint64_t b = operand_descriptor(smem_u32(stage_b) + stage * kWideStageBytes<N>);
     if (elect()) {
 #pragma unroll
@@ -268,7 +269,6 @@ __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid
         const int q = 2 * GS * k + i;
         const uint64_t bq = b + (q >> 2) * (N * 128 / 16) + 2 * (q & 3);
         tensor_mma(to, a + 8 * i, bq, kWhat, i > 0);
-        tensor_mma(to + N, a + 64 + 8 * i, bq, kWhat, i > 0);
       }
       if (k == kGroups - 1) tensor_commit(&sh.empty[stage]);
       tensor_commit(&sh.sums[group & 1]);
@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid
     __syncwarp();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     float v[kHalf];
-    tensor_load(lanes + (group & 1) * 2 * N + tile_half * N + part * kHalf, v);
+    tensor_load(lanes + (group & 1) * N + part * kHalf, v);
 #pragma unroll
     for (int j = 0; j < kHalf; ++j) acc[j] = __fmaf_rn(s, v[j], acc[j]);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -301,12 +301,12 @@ __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid
     uint32_t now[kGroups];
 #pragma unroll
     for (int k = 0; k < kGroups; ++k) now[k] = scale[k];
-    wait_group<kWideRing - 2>();
+    wait_group<kRing - 2>();
     // both warps' copies are there, and both have read the chunk before, whose place is next
-    asm volatile("barrier.sync %0, 64;" ::"r"(1 + (warp & 7)) : "memory");
-    fetch(l + kWideRing - 1);
+    asm volatile("barrier.sync %0, 64;" ::"r"(1 + (warp & 3)) : "memory");
+    fetch(l + kRing - 1);
     const int slot_at = from_slot * (kWideRingBytes<N> / 16);
-    from_slot = from_slot + 1 == kWideRing ? 0 : from_slot + 1;
+    from_slot = from_slot + 1 == kRing ? 0 : from_slot + 1;
     const uint4* raw = ring + slot_at;
     uint4 word[2];
 #pragma unroll
@@ -324,7 +324,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) mat4_wide_kernel(const __grid
     if (l >= kWideStages) barrier_wait(&sh.empty[stage], (l >> 1) - 1 & 1, &sh.failed);
     __syncwarp();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    tensor_store(lanes + kColumnsOfA<N> + stage * 128 + tile_half * 64 + part * 32, a);
+    tensor_store(lanes + kColumnsOfA<N> + stage * 64 + part * 32, a);
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       const int u = tid + kWideThreads * i, r = u >> 4, c = u & 15;
