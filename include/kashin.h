@@ -554,9 +554,10 @@ typedef struct kd_weight4 {
  *   without zeros: s = max(hi / 7, -lo / 8), z = 8;
  *   with zeros:    lo' = min(lo, 0), hi' = max(hi, 0), s = (hi' - lo') / 15,
  *                  z = min(15, max(0, rint(-lo' / s)));
- * s is rounded to scale_dtype first, and the codes are rint(w / s) + z held to 0..15
- * (nearest, ties to even; all divisions fp32).  A group whose rounded scale is 0 gets
- * z = 0 (8 without zeros) and codes z.  A group with an infinity or NaN, or whose scale
+ * s is rounded up to scale_dtype first (so that no weight is further than half a step from
+ * its code's value), and the codes are rint(w / s) + z held to 0..15 (nearest, ties to
+ * even; all divisions fp32).  A group whose scale is 0 gets z = 0 (8 without zeros) and
+ * codes z.  A group with an infinity or NaN, or whose scale
  * does not fit the type, gets a NaN or infinite scale and codes z.
  * Errors: KD_ERR_INVALID_ARG (sizes, group, types, ld, pointers missing with m > 0 or
  * unaligned), KD_ERR_CUDA.  m == 0 enqueues nothing. */

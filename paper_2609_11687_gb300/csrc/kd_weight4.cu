@@ -56,8 +56,10 @@ __global__ void __launch_bounds__(256) quantise4_kernel(const __grid_constant__ 
       s = fmaxf(hi / 7.f, -lo / 8.f);
     }
     if (bad) s = __int_as_float(0x7FC00000);
-    // the scale as it is stored is the scale that the codes are for
-    s = p.scale_dtype == KD_F16 ? __half2float(__float2half_rn(s)) : __bfloat162float(__float2bfloat16_rn(s));
+    // The scale as it is stored is the scale that the codes are for.  It is rounded up: a scale
+    // rounded down leaves the group wider than its 15 steps, and the ends that the codes' range
+    // then cuts are off by up to 15 * 2^-8 of a step (bf16) more than the half step of all others.
+    s = p.scale_dtype == KD_F16 ? __half2float(__float2half_ru(s)) : __bfloat162float(__float2bfloat16_ru(s));
     const bool usable = isfinite(s) && s > 0.f;
     float z = p.zeros ? 0.f : 8.f;
     if (p.zeros && usable) z = fminf(15.f, fmaxf(0.f, rintf(-lo / s)));

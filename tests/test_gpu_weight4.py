@@ -171,6 +171,13 @@ def test_large_offsets(kd):
     assert torch.equal(out[-40:], d.half())
 
 
+def _round_up(s, dt):
+    """s (fp32, not negative) rounded to the next value of dt that is not below it."""
+    r = s.to(dt)
+    up = (r.view(torch.int16) + 1).view(dt)      # the next one: the same sign, one further
+    return torch.where(r.float() < s, up, r).float().numpy()
+
+
 def _quantise_host(w, group, zeros, sdt):
     """The definition, step by step in fp32 on the host."""
     m, n = w.shape
@@ -184,7 +191,7 @@ def _quantise_host(w, group, zeros, sdt):
             s = (hi - lo) / f(15)
         else:
             s = np.maximum(hi / f(7), -lo / f(8))
-        s = torch.from_numpy(s).to(sdt).float().numpy()
+        s = _round_up(torch.from_numpy(s), sdt)
         ok = np.isfinite(s) & (s > 0) & np.isfinite(v).all(1)
         d = np.where(ok, s, f(1))
         z = np.where(ok, np.clip(np.rint(-lo / d), 0, 15), 0) if zeros else np.full(m, 8)
@@ -213,6 +220,18 @@ def test_quantise_and_dequantise_bits(kd, group, zeros, dt, sdt, m, n):
     dense = scales[:, which] * (codes - zs[:, which]).astype(np.float32)
     for odt in (torch.float32, torch.float16, torch.bfloat16):
         assert torch.equal(kd.dequantise_4bit(q, odt).cpu(), torch.from_numpy(dense).to(odt))
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("sdt", [torch.bfloat16, torch.float16])
+def test_quantise_is_within_half_a_step(kd, zeros, sdt):
+    """Many groups of every scale: no weight is further than half a step from its code's value
+    (1e-5: the fp32 divisions' roundings), also where the codes end."""
+    g = torch.Generator(device="cuda").manual_seed(16)
+    w = torch.randn((512, 1024), generator=g, device="cuda") * 10 ** (3 * torch.rand((512, 1), generator=g, device="cuda") - 2)
+    q = kd.quantise_4bit(w, 32, zeros, scale_dtype=sdt)
+    step = q.scales.double().repeat_interleave(32, 1)
+    assert ((kd.dequantise_4bit(q).double() - w.double()).abs() <= step * (0.5 + 1e-5)).all()
 
 
 def test_quantise_special_and_strided(kd):
