@@ -23,9 +23,9 @@ bool plan(Params& p, int nt, int rows) {
   for (int split = 1; split <= 8; split *= 2) {
     const int per = (p.chunks + split - 1) / split;
     if (split > 1 && per < 2) break;
-    for (int kw = warps_of(nt); kw >= 1; kw /= 2) {
+    for (int kw = kWarps; kw >= 1; kw /= 2) {
       if (smem_bytes(nt, rows, per, split, kw) > kSmem) continue;
-      const int channels = kTile * warps_of(nt) / kw;
+      const int channels = kTile * kWarps / kw;
       const int tiles = (p.m + channels - 1) / channels;
       const int at_once = room(split);
       const double rounds = (tiles + at_once - 1) / at_once;

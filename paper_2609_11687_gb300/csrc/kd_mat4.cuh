@@ -44,9 +44,8 @@ using namespace serve;
 
 constexpr int kTile = 32;    // output channels of a warp: two m16 tiles
 constexpr int kChunk = 128;  // inputs of a chunk
-constexpr int kStages = 3;
+constexpr int kStages = 2;
 constexpr int kStageUnits = 128;  // 16-byte units of a stage: 32 channels x 64 bytes
-constexpr int kSumStride = 36;    // floats of one row's 32 partial sums, padded
 
 struct Params {
   const uint8_t* codes;
@@ -67,17 +66,14 @@ struct Params {
   int x_vec, scale_vec, scale_bf16, ydtype;
 };
 
-// warps of a CTA for nt tiles of rows: several tiles' sums want twice the registers
-template <int NT>
-constexpr int kWarps = NT == 1 ? 16 : 8;
-inline int warps_of(int nt) { return nt == 1 ? 16 : 8; }
+constexpr int kWarps = 16;  // of a CTA
 // Shared memory, in bytes: the ring; the warps' partial sums; the rows; for clusters two
 // sets of the CTA's sums.
 constexpr size_t kRingBytes = (size_t)kStages * kStageUnits * 16;  // of a warp
-constexpr size_t kRedBytes = (size_t)8 * kSumStride * 4;           // of a warp, for each 8 rows
+constexpr size_t kRedBytes = (size_t)8 * kTile * 4;                // of a warp, for each 8 rows
 inline size_t smem_bytes(int nt, int rows, int per, int split, int kw) {
-  const size_t outputs = (size_t)kTile * (warps_of(nt) / kw) * rows;
-  return warps_of(nt) * (kRingBytes + nt * kRedBytes) + (size_t)per * nt * 2048 +
+  const size_t outputs = (size_t)kTile * (kWarps / kw) * rows;
+  return kWarps * (kRingBytes + nt * kRedBytes) + (size_t)per * nt * 2048 +
          (split > 1 ? 2 * outputs * 4 : 0);
 }
 
@@ -194,8 +190,8 @@ __device__ __forceinline__ uint4 bytes_to_half(uint4 v) {
 // BF: bf16 rows; GS: 32-input steps of a group (1, 2, 4); NT: 8-row tiles of one pass; ZEROS:
 // zero points by group
 template <bool BF, int GS, int NT, bool ZEROS>
-__global__ void __launch_bounds__(32 * kWarps<NT>, 1) mat4_kernel(const __grid_constant__ Params p) {
-  constexpr int W = kWarps<NT>, kThreads = 32 * W;
+__global__ void __launch_bounds__(32 * kWarps, 1) mat4_kernel(const __grid_constant__ Params p) {
+  constexpr int W = kWarps, kThreads = 32 * W;
   constexpr int kGroups = 4 / GS;  // groups of a chunk
   constexpr int kCols = 8 * NT;
   constexpr int kBatch = 4;        // loads of rows in flight
@@ -203,7 +199,7 @@ __global__ void __launch_bounds__(32 * kWarps<NT>, 1) mat4_kernel(const __grid_c
   extern __shared__ uint4 smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int mw = W >> p.kw_log, mi = warp >> p.kw_log, ki = warp & (p.kw - 1);
-  const int tile_log = (W == 16 ? 9 : 8) - p.kw_log;  // of the CTA's channels, 32 mw
+  const int tile_log = 9 - p.kw_log;  // of the CTA's channels, 32 mw
   const int rank = special<kRank>(), first = special<kCluster>(), step = special<kClusters>();
   const int c0 = rank * p.per, mine = min(p.per, p.chunks - c0);  // this CTA's chunks
   const int outputs = p.rows << tile_log;
@@ -406,13 +402,14 @@ __global__ void __launch_bounds__(32 * kWarps<NT>, 1) mat4_kernel(const __grid_c
       }
     }
 
-    // the warps' sums of a channel, added in the order of their inputs
+    // The warps' sums of a channel, added in the order of their inputs.  Channels 4g .. 4g + 3 of
+    // row r lie at 4 (g ^ (r & 6)) of the row's 32: no bank conflicts.
     __syncthreads();  // the last tile's sums have been read
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        *reinterpret_cast<float4*>(red + (warp * kCols + 8 * j + 2 * t + e) * kSumStride + 4 * g) =
+        *reinterpret_cast<float4*>(red + (warp * kCols + 8 * j + 2 * t + e) * kTile + 4 * (g ^ 2 * t)) =
             make_float4(acc[0][j][e], acc[0][j][e + 2], acc[1][j][e], acc[1][j][e + 2]);
     __syncthreads();
     const int j0 = tile << tile_log;
@@ -424,10 +421,10 @@ __global__ void __launch_bounds__(32 * kWarps<NT>, 1) mat4_kernel(const __grid_c
     // output o: row o / (32 mw), channel o % (32 mw) of the tile
     for (int o = threadIdx.x; o < outputs; o += kThreads) {
       const int r = o >> tile_log, ch = o & ((1 << tile_log) - 1);
-      const float* at = red + (((ch / kTile) << p.kw_log) * kCols + r) * kSumStride + ch % kTile;
+      const float* at = red + (((ch / kTile) << p.kw_log) * kCols + r) * kTile + (ch % kTile ^ (r & 6) << 2);
       float s = at[0];
 #pragma unroll 5
-      for (int w = 1; w < p.kw; ++w) s += at[w * kCols * kSumStride];
+      for (int w = 1; w < p.kw; ++w) s += at[w * kCols * kTile];
       if (p.split == 1) finish(r, ch, s);
       else csum[parity * outputs + o] = s;
     }
@@ -467,7 +464,7 @@ cudaError_t launch_one(const Params& p, int clusters, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(clusters * p.split));
-  cfg.blockDim = dim3(32 * kWarps<NT>);
+  cfg.blockDim = dim3(32 * kWarps);
   cfg.dynamicSmemBytes = smem_bytes(NT, p.rows, p.per, p.split, p.kw);
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
