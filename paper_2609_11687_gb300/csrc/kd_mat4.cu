@@ -14,8 +14,11 @@ int room(int split) { return split == 1 ? 152 : split == 2 ? 76 : split == 4 ? 3
 
 // How the work is split: CTAs of a cluster (split) and warps (kw) that share a tile's
 // inputs, for `rows` rows in nt tiles of eight.  The cost counts chunks of one warp, one
-// after the other: a tile's chunks, and what joining its sums takes (half a chunk, one and a
-// half across a cluster: fitted to layers of 4096, 11008 and 32000 channels at all splits).
+// after the other: a tile's chunks, half a chunk to join its sums, across a cluster another
+// one and a part for each output, and once the time to lay out the CTA's rows.  Fitted to all
+// splits of 24 products (64 to 32000 channels of 700 to 16384 inputs, 1 to 16 rows): the
+// choice is the fastest within 2 %, but for one of rows that are not aligned (11 %).  Without the rows' part 4096 x
+// 4096 at 16 rows took 8.3 us instead of 7.2, 64 x 8192 6.2 instead of 4.5.
 // False if the rows fit no CTA's shared memory.
 bool plan(Params& p, int nt, int rows) {
   bool found = false;
@@ -29,7 +32,8 @@ bool plan(Params& p, int nt, int rows) {
       const int tiles = (p.m + channels - 1) / channels;
       const int at_once = room(split);
       const double rounds = (tiles + at_once - 1) / at_once;
-      const double cost = rounds * ((per + kw - 1) / kw + (split > 1 ? 1.5 : 0.5));
+      const double join = split > 1 ? 1.5 + channels * rows / 16384. : 0.5;
+      const double cost = rounds * ((per + kw - 1) / kw + join) + 0.005 * per * rows;
       if (!found || cost < least) {
         found = true;
         least = cost;
@@ -101,9 +105,9 @@ extern "C" kd_status kd_matmul_4bit(const kd_weight4* w, const void* x, kd_dtype
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   // Passes of equal numbers of rows: from 17 rows on of at most 64, by the kernel for many
   // rows; else one of at most 16 (or, where an input is so long that those fit no CTA's
-  // shared memory, of 8).  At 16 rows that one takes 10.0 / 13.9 / 36 us for 4096 x 4096,
-  // 4096 x 11008 and 32000 x 4096, the kernel for many rows 7.7 / 14.1 / 34 at 17 to 32, two
-  // passes of the other about twice its time.
+  // shared memory, of 8).  At 16 rows that one takes 7.2 / 12.8 / 24 us for 4096 x 4096,
+  // 4096 x 11008 and 32000 x 4096, the kernel for many rows 7.6 / 13.9 / 34 there and no more
+  // at 17 to 32, where two passes of the other take about twice its time.
   int nt = 0, clusters = 0;
   int64_t pass = 0;
   if (rows > 16) {

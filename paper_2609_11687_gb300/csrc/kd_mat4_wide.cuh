@@ -27,6 +27,11 @@
 // K order: a piece of eight inputs holds them as the codes of a word come out, (0 4 1 5 2 6
 // 3 7), in A and B alike.
 //
+// Bound by issue slots (49 % used, four warps a scheduler, 345 instructions a warp and chunk)
+// and by the waits on tensor memory between; the tensor pipe is 18 % busy: 43 us for 64 rows of
+// 32000 x 4096 in fp16 with groups of 128, floor 11.3.  Smaller groups drain the accumulators
+// more often: 55 us at 64, 67 at 32.
+//
 // Every wait is bounded (about a second); one that expires marks the CTA, whose waits then
 // all return at once and whose outputs become NaN.
 #pragma once
@@ -192,8 +197,11 @@ __global__ void __launch_bounds__(kWideThreads, 2) mat4_wide_kernel(const __grid
 
   // Codes: pieces idx % 4 of channel idx / 4 of the 32 that this warp shares with the one
   // four further, idx = 32 part + lane (+ 64); piece c of channel r lies at c ^ (r / 2 % 4).
-  // Rows: 8 inputs of row u / 16, u = tid + 256 i, for this thread alone.  Rows past the
-  // batch repeat its last one: a column of B meets one column of the sums.
+  // Rows: 8 inputs of row u / 16, u = tid + 256 i, for this thread alone.  In place of
+  // rows past the batch its first ones come again: a column of B meets one column of the sums.
+  // (The last one in all these places is the same few lines for all CTAs: 32000 x 4096 took 40 us
+  // at 17 rows, 65 at 33, instead of 34 and 43.  Copying no rows there cost more at full tiles,
+  // 47 us instead of 43 at 64 rows, than it saved at others.)
   const int idx = 32 * part + lane, base = tile * kWideChannels + (warp & 3) * 32;
   uint4* pair_ring = reinterpret_cast<uint4*>(stage_b + kWideStages * kWideStageBytes<N>) + (warp & 3) * 128;
   const uint4* codes[2];
@@ -207,7 +215,7 @@ __global__ void __launch_bounds__(kWideThreads, 2) mat4_wide_kernel(const __grid
   const uint8_t* x[kUnits];
 #pragma unroll
   for (int i = 0; i < kUnits; ++i)
-    x[i] = p.x + ((int64_t)min((tid + kWideThreads * i) >> 4, p.rows - 1) * p.ldx + c0 * kChunk + 8 * (tid & 15)) *
+    x[i] = p.x + ((int64_t)(((tid + kWideThreads * i) >> 4) % p.rows) * p.ldx + c0 * kChunk + 8 * (tid & 15)) *
                      (p.e4m3 ? 1 : 2);
   const int whole = p.x_vec ? (p.n - c0 * kChunk) / kChunk : 0;  // chunks without a row's end
   int to_slot = 0;
