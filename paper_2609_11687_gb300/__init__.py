@@ -4,4 +4,5 @@
 from ``csrc/`` (hand-written sm_103a CUDA).  Importing this package does not load
 the library; importing ``.kashin`` does, and fails loudly if it is missing.
 ``paper_2609_11687_gb300.synth`` draws the seeded synthetic weight matrices.
+``paper_2609_11687_gb300.score`` runs norm, 4-bit head and log probabilities together.
 """
