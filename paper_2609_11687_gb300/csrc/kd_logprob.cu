@@ -307,20 +307,23 @@ __device__ __noinline__ void collect(Shared& sh, const Row<DT>& r, int c, uint4 
   }
 }
 
-template <int DT>
-__global__ void __launch_bounds__(kT, 1280 / kT) logprob_kernel(const __grid_constant__ LogpParams p) {
+// SHARED: a cluster shares a row.  Registers: with many rows a fifth CTA of an SM helps more than
+// the registers that it costs (2048 x 32000 bf16 28 us instead of 31), with few the reverse (61 x
+// 65537 fp16 11.1 instead of 13.4).
+template <int DT, bool SHARED>
+__global__ void __launch_bounds__(kT, SHARED ? 4 : 5) logprob_kernel(const __grid_constant__ LogpParams p) {
   __shared__ Shared sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int rank = special<kRank>();
+  const int rank = SHARED ? special<kRank>() : 0;
   const int64_t step = special<kClusters>();
   const float low = __int_as_float(0xFF800000);
-  if (p.split > 1) cluster_arrive();
+  if constexpr (SHARED) cluster_arrive();
   depend_on_last();
 
   for (int64_t row = special<kCluster>(); row < p.rows; row += step) {
     const Row<DT> r(p, row);
     // this CTA's pieces [c0, c1); this thread's: c0 + tid, c0 + tid + kT, ...
-    const int per = (r.pieces + p.split - 1) >> p.split_log;
+    const int per = SHARED ? (r.pieces + p.split - 1) >> p.split_log : r.pieces;
     const int c0 = min(r.pieces, rank * per), c1 = min(r.pieces, c0 + per);
     // the first given token of this thread, on its way meanwhile
     const bool reads = rank == 0 && tid < 32 && tid < p.tokens;
@@ -493,7 +496,7 @@ __global__ void __launch_bounds__(kT, 1280 / kT) logprob_kernel(const __grid_con
       all.t += sh.sums[w].y;
     }
     if (ranked && p.top == 1 && tid == 0 && sh.first != 0xFFFFFFFFu) sh.best[0] = (Key)most << 32 | (0xFFFFFFFFu - sh.first);
-    if (p.split > 1) {
+    if constexpr (SHARED) {
       cg::cluster_group cl = cg::this_cluster();
       __syncwarp();
       cluster_wait();  // the first CTA runs: its shared memory may be written
@@ -554,7 +557,7 @@ __global__ void __launch_bounds__(kT, 1280 / kT) logprob_kernel(const __grid_con
         p.top_logprobs[row * p.top + lane] = ok ? logprob(value_of((uint32_t)(k >> 32))) : nan;
       }
     }
-    if (p.split > 1) return;  // a launch with clusters holds all rows at once
+    if constexpr (SHARED) return;  // a launch with clusters holds all rows at once
     __syncthreads();          // the shared values have been read
   }
 }
@@ -573,7 +576,8 @@ cudaError_t launch(const LogpParams& p, cudaStream_t s) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = p.split > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, logprob_kernel<DT>, p);
+  return p.split > 1 ? cudaLaunchKernelEx(&cfg, logprob_kernel<DT, true>, p)
+                     : cudaLaunchKernelEx(&cfg, logprob_kernel<DT, false>, p);
 }
 
 }  // namespace
