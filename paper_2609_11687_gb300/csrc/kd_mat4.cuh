@@ -201,7 +201,10 @@ __global__ void __launch_bounds__(32 * kWarps, 1) mat4_kernel(const __grid_const
   constexpr int W = kWarps, kThreads = 32 * W;
   constexpr int kGroups = 4 / GS;  // groups of a chunk
   constexpr int kCols = 8 * NT;
-  constexpr int kBatch = 4;        // loads of rows in flight
+  // Loads of rows in flight, first and then.  What a launch runs once costs the more the longer
+  // its code is, 0.1 us for each load, and a single row's first one is all that it needs: 4.1 us
+  // instead of 4.4 (four first ones) for 4096 x 4096.
+  constexpr int kFirst = 1, kBatch = 4;
   namespace cg = cooperative_groups;
   extern __shared__ uint4 smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
@@ -228,10 +231,10 @@ __global__ void __launch_bounds__(32 * kWarps, 1) mat4_kernel(const __grid_const
     return p.x_vec && k + 8 <= p.n ? load_inputs(p, at) : load_inputs_one_by_one(p.x, p.e4m3, at, p.n - k);
   };
   depend_on_last();
-  uint4 v0[kBatch];
-  int row0[kBatch], item0[kBatch];
+  uint4 v0[kFirst];
+  int row0[kFirst], item0[kFirst];
 #pragma unroll
-  for (int b = 0; b < kBatch; ++b) v0[b] = take(warp + b * W, row0[b], item0[b]);
+  for (int b = 0; b < kFirst; ++b) v0[b] = take(warp + b * W, row0[b], item0[b]);
 
   // The warp's ring of codes.  This lane copies piece t of channels 4g + i to row 8i + g of
   // a stage, at a place that lets a row's words be read 4, 8 or 16 bytes a lane without
@@ -309,10 +312,10 @@ __global__ void __launch_bounds__(32 * kWarps, 1) mat4_kernel(const __grid_const
                    __byte_perm(h.y, h.w, 0x7632));
   };
 #pragma unroll
-  for (int b = 0; b < kBatch; ++b)
+  for (int b = 0; b < kFirst; ++b)
     if (warp + b * W < turns) put(row0[b], item0[b], v0[b]);
 #pragma unroll 1
-  for (int turn0 = warp + kBatch * W; turn0 < turns; turn0 += kBatch * W) {
+  for (int turn0 = warp + kFirst * W; turn0 < turns; turn0 += kBatch * W) {
     uint4 v[kBatch];
     int row[kBatch], item[kBatch];
 #pragma unroll
