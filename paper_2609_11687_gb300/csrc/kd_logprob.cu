@@ -339,9 +339,17 @@ __global__ void __launch_bounds__(kT, SHARED ? 4 : 5) logprob_kernel(const __gri
     Pair s2 = pack(0.f, 0.f), t2 = s2;
     const Pair l2e = pack(kLog2e, kLog2e);
     uint4 a[kUnroll];
+    // pieces [from, upto) lie within the row
+    const int from = r.before > 0, upto = min(c1, (int)(((int64_t)r.before + r.vocab) / kPiece<DT>));
+    const uint4* pieces = reinterpret_cast<const uint4*>(r.x - r.before);
     for (int c = c0 + tid; c < c1; c += kUnroll * kT) {
+      if (c >= from && c + (kUnroll - 1) * kT < upto) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) a[u] = c + u * kT < c1 ? r.load(c + u * kT) : lowest_piece<DT>();
+        for (int u = 0; u < kUnroll; ++u) a[u] = pieces[c + u * kT];
+      } else {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) a[u] = c + u * kT < c1 ? r.load(c + u * kT) : lowest_piece<DT>();
+      }
       uint4 am = a[0];
 #pragma unroll
       for (int u = 1; u < kUnroll; ++u) am = max_piece<DT>(am, a[u]);
