@@ -20,8 +20,9 @@
 // Few rows: a cluster of CTAs shares a row, and its first CTA joins their sums and their
 // lists of alternatives.
 //
-// Bound by HBM for many rows (the exponential, one an entry, comes second), by latency for
-// few.
+// Bound by instructions for many rows (2048 x 32000 bf16: 28 us, 4.7 TB/s or 70 % of the
+// measured copy rate), by the latency of the phases after the pass for few (one row of 32000 fp32
+// with 20 alternatives: 6.5 us).
 #include <cooperative_groups.h>
 
 #include "kd_serve.cuh"

@@ -26,8 +26,8 @@
 // stages 32, their shared memory leaves room for half the rows only).
 //
 // Bound by the instructions that decode (the integer pipe 54 % busy, 58 % of all issue slots
-// used at 8 rows of 32000 x 4096): 3.5 TB/s there, 19.8 us for a floor of 10.1; one row of 11008
-// x 4096 8.2 us, of 4096 x 4096 4.4.
+// used at 8 rows of 32000 x 4096): 3.5 TB/s there, 19.9 us for a floor of 10.1; one row of 11008
+// x 4096 7.9 us, of 4096 x 4096 4.1.
 //
 // K order.  The product is a sum over inputs, so A and B may enumerate them in any common
 // order.  A group of GS x 32 inputs is 4 GS code words of a channel; the lanes with
