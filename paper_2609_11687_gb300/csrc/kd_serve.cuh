@@ -88,21 +88,7 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   }
 }
 
-// eight consecutive elements from a 16-byte boundary
-template <int DT>
-__device__ __forceinline__ void load8(const void* base, int64_t at, float (&v)[8]) {
-  if constexpr (DT == KD_F32) {
-    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at);
-    const float4 a = p[0], b = p[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  } else {
-    const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + at);
-    const float2 p0 = unpack2<DT>(a.x), p1 = unpack2<DT>(a.y), p2 = unpack2<DT>(a.z), p3 = unpack2<DT>(a.w);
-    v[0] = p0.x; v[1] = p0.y; v[2] = p1.x; v[3] = p1.y;
-    v[4] = p2.x; v[5] = p2.y; v[6] = p3.x; v[7] = p3.y;
-  }
-}
+// eight consecutive elements to a 16-byte boundary
 template <int DT>
 __device__ __forceinline__ void store8(void* base, int64_t at, const float (&v)[8]) {
   if constexpr (DT == KD_F32) {
