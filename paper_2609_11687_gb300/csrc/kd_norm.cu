@@ -5,15 +5,19 @@
 //     y = h rsqrt(mean(h^2) + eps) w              (optional output, rounded to its type)
 //     s = max|y| / 448,  q = e4m3(y / s)          (optional outputs; s = 1 where max|y| < 2^-100)
 //
-// One pass over the row: a thread keeps its elements of h and w in registers, and one
-// reduction over the row yields both sum(h^2) and max|h w| (max|y| is that times the
-// row's positive factor), so x and r are read once and nothing is read again.
+// One pass over the row: a thread keeps its elements of h and w in registers; a reduction
+// over the row yields sum(h^2), another one the largest of |y| as it is rounded (the factor
+// max|h w| from the first pass would save it, but its products overflow where y does not, and
+// its scale is not y's in the last place), so x and r are read once and nothing is read again.
+// q is the rounded quotient's own rounding; see Quotient for why few are divided.
 //
 // Bound by HBM for many rows, by latency for few.  A CTA walks rows: it keeps w, and loads
 // its next row before it reduces this one, so that loads are in flight all the time (a CTA
-// a row reached half of the bandwidth: most of its life is the reduction).  2048 x 4096 bf16 with
-// a residual, e4m3 and bf16 rows: 14.9 us, 75 % of the measured copy rate; one row 2.0 us, 333
-// unaligned rows of 5003 6.5 us.
+// a row reached half of the bandwidth: most of its life is the reductions).  2048 x 4096 bf16 with
+// a residual, e4m3 and bf16 rows: 15.2 us, 73 % of the measured copy rate (one IEEE division an
+// element: 17.2); one row 2.3 us, 333 unaligned rows of 5003 6.6 us.  Instances of two pieces a
+// thread spill (28 to 132 bytes, fp16 with its own weight type none): 64 registers are what 1024
+// threads, the longest rows, leave each.
 #include <cuda_fp8.h>
 
 #include "kd_serve.cuh"
@@ -44,6 +48,24 @@ __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
   const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
   return lo | (hi << 16);
 }
+
+// e4m3(v / scale) without a division for most: the reciprocal, 2^-21 to either side of which
+// the products lie below and above the quotient (they round three times, 3 2^-24, the
+// quotient once).  Where both round to the same byte so does all between them.
+struct Quotient {
+  float scale, below, above;
+  __device__ __forceinline__ explicit Quotient(float s) : scale(s) {
+    const float inv = 1.f / s;
+    below = inv * (1.f - 0x1p-21f);
+    above = inv * (1.f + 0x1p-21f);
+  }
+  __device__ __forceinline__ uint32_t four(float a, float b, float c, float d) const {
+    const uint32_t lo = e4m3x4(a * below, b * below, c * below, d * below);
+    const uint32_t hi = e4m3x4(a * above, b * above, c * above, d * above);
+    if (lo == hi) return lo;
+    return e4m3x4(a / scale, b / scale, c / scale, d / scale);
+  }
+};
 
 // eight elements as they come: 16 bytes of a 16-bit type, 32 of fp32; without VEC one by one
 template <int DT, bool VEC>
@@ -94,7 +116,8 @@ constexpr int kNormThreads = 1024;  // of a CTA at most: two pieces each cover t
 // elements; else the 8 elements of a piece lie blockDim.x apart (coalesced element loads).
 template <int DT, int WT, int C, bool VEC>
 __global__ void __launch_bounds__(kNormThreads) norm_kernel(const __grid_constant__ NormParams p) {
-  __shared__ float2 red[2][kNormThreads / 32];
+  __shared__ float sums[2][kNormThreads / 32];
+  __shared__ uint32_t tops[kNormThreads / 32];
   const int tid = threadIdx.x, T = blockDim.x, n = (int)p.n;
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
   auto index = [&](int c) { return VEC ? 8 * (c * T + tid) : 8 * c * T + tid; };
@@ -129,53 +152,69 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const __grid_constan
       }
     }
     if (row + step < p.rows) fetch(row + step);
-    float ss = 0.f, big = 0.f;
+    // the sum goes out here, not with y: there are stores in flight during the reductions
+    if (p.r_out && live) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        if constexpr (VEC) {
+          if (index(c) < n) store8<DT>(p.r_out, row * p.ldro + index(c), h[c]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (index(c) + e * T < n) store1<DT>(p.r_out, row * p.ldro + index(c) + e * T, h[c][e]);
+        }
+      }
+    }
+    float ss = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss = __fmaf_rn(h[c][e], h[c][e], ss);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) ss += __shfl_xor_sync(~0u, ss, o);
+    // the warps of a row are consecutive: slots of one row stay together
+    const int per = T >> 5, at = threadIdx.y * per;
+    if (T > 32) {
+      if ((tid & 31) == 0) sums[parity][at + (tid >> 5)] = ss;
+      __syncthreads();
+      ss = 0.f;
+      for (int k = 0; k < per; ++k) ss += sums[parity][at + k];
+    }
+    const float nan = __int_as_float(0x7FC00000);
+    // a row whose sum of squares is no finite number has no norm: NaN, not zeros
+    const float rstd = isfinite(ss) ? 1.f / sqrtf(ss / (float)n + p.eps) : nan;
+    uint32_t top = 0;  // the largest |y| as bits, whose order is the values' with NaN above all
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       float v[8];
       w[c].get(v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        ss = __fmaf_rn(h[c][e], h[c][e], ss);
-        big = max_nan(big, fabsf(h[c][e] * v[e]));
+        h[c][e] = h[c][e] * rstd * v[e];
+        top = max(top, __float_as_uint(h[c][e]) & 0x7FFFFFFFu);
       }
     }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-      ss += __shfl_xor_sync(~0u, ss, o);
-      big = max_nan(big, __shfl_xor_sync(~0u, big, o));
-    }
-    if (T > 32) {
-      // the warps of a row are consecutive: slots of one row stay together
-      const int per = T >> 5, at = threadIdx.y * per;
-      if ((tid & 31) == 0) red[parity][at + (tid >> 5)] = make_float2(ss, big);
-      __syncthreads();
-      ss = big = 0.f;
-      for (int k = 0; k < per; ++k) {
-        const float2 v = red[parity][at + k];
-        ss += v.x;
-        big = max_nan(big, v.y);
+    float scale = 1.f;
+    if (p.q) {
+      top = __reduce_max_sync(~0u, top);
+      if (T > 32) {
+        if ((tid & 31) == 0) tops[at + (tid >> 5)] = top;
+        __syncthreads();
+        top = __reduce_max_sync(~0u, (tid & 31) < per ? tops[at + (tid & 31)] : 0u);
       }
+      const float amax = __uint_as_float(top);
+      scale = amax < 0x1p-100f ? 1.f : amax / kE4M3Max;
     }
     if (!live) continue;
 
-    const float nan = __int_as_float(0x7FC00000);
-    // a row whose sum of squares is no finite number has no norm: NaN, not zeros
-    const float rstd = isfinite(ss) ? 1.f / sqrtf(ss / (float)n + p.eps) : nan;
-    const float amax = big * rstd;
-    const float scale = amax < 0x1p-100f ? 1.f : amax / kE4M3Max;
-    const float inv = 1.f / scale;
     if (p.scale && tid == 0) p.scale[row] = scale;
+    const Quotient quotient(scale);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      float y[8];
-      w[c].get(y);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = h[c][e] * rstd * y[e];
+      const float(&y)[8] = h[c];
       if constexpr (VEC) {
         const int i = index(c);
         if (i >= n) break;
-        if (p.r_out) store8<DT>(p.r_out, row * p.ldro + i, h[c]);
         if (p.y) {
           if (p.ydtype == KD_F32) store8<KD_F32>(p.y, row * p.ldy + i, y);
           else if (p.ydtype == KD_F16) store8<KD_F16>(p.y, row * p.ldy + i, y);
@@ -183,16 +222,19 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const __grid_constan
         }
         if (p.q)
           *reinterpret_cast<uint2*>(p.q + row * p.ldq + i) =
-              make_uint2(e4m3x4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv),
-                         e4m3x4(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
+              make_uint2(quotient.four(y[0], y[1], y[2], y[3]), quotient.four(y[4], y[5], y[6], y[7]));
       } else {
+        uint32_t q[2];
+        if (p.q) {
+          q[0] = quotient.four(y[0], y[1], y[2], y[3]);
+          q[1] = quotient.four(y[4], y[5], y[6], y[7]);
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int i = index(c) + e * T;
           if (i >= n) break;
-          if (p.r_out) store1<DT>(p.r_out, row * p.ldro + i, h[c][e]);
           if (p.y) store1_any(p.y, p.ydtype, row * p.ldy + i, y[e]);
-          if (p.q) p.q[row * p.ldq + i] = __nv_cvt_float_to_fp8(y[e] * inv, __NV_SATFINITE, __NV_E4M3);
+          if (p.q) p.q[row * p.ldq + i] = (uint8_t)(q[e / 4] >> (8 * (e % 4)));
         }
       }
     }
