@@ -924,10 +924,18 @@ def _vec(t, name, types, index, length):
 
 
 def _new(stream, shape, dtype, device):
-    """An output allocated here: the allocator learns of the stream that it is used on."""
-    t = _torch().empty(shape, dtype=dtype, device=device)
-    if stream is not None:
-        t.record_stream(stream)
+    """An output allocated here for work on ``stream`` (None: the current one).  The block comes
+    from that stream's own pool: one of the current stream's may have been freed with work
+    still pending there, which ``stream`` does not wait for.  The caller's stream is noted, so
+    that a result dropped there is not given out again before it has been read."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    current = torch.cuda.current_stream(device)
+    if current != stream:
+        t.record_stream(current)
     return t
 
 
