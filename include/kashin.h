@@ -581,8 +581,9 @@ kd_status kd_dequantise_4bit(const kd_weight4* w, kd_dtype out_dtype, void* out,
  * 17 rows on every wait inside the kernel is bounded to about a second; one that expires
  * gives NaN in the outputs of its channels.)
  * Rows of 16-byte aligned base and stride (8-byte for e4m3) take wide loads.
- * Errors: KD_ERR_INVALID_ARG (sizes, group, types, ld < n or ldy < m, pointers missing
- * with m > 0 and rows > 0, or unaligned), KD_ERR_UNSUPPORTED_N (n > 65536), KD_ERR_CUDA.
+ * Errors: KD_ERR_INVALID_ARG (sizes, m > 2^31 - 512, group, types, ld < n or ldy < m,
+ * pointers missing with m > 0 and rows > 0, or unaligned), KD_ERR_UNSUPPORTED_N (n >
+ * 65536), KD_ERR_CUDA.
  * m == 0 or rows == 0 enqueues nothing. */
 kd_status kd_matmul_4bit(const kd_weight4* w, const void* x, kd_dtype x_dtype, const float* x_scale, int64_t rows,
                          int64_t ldx, void* y, kd_dtype y_dtype, int64_t ldy, void* stream);

@@ -6,6 +6,8 @@ namespace mat4 {
 namespace {
 
 constexpr int64_t kMaxN = 65536;
+// channels are counted in 32 bits up to the end of the last tile, of 512 at most
+constexpr int64_t kMaxM = INT32_MAX - kTile * kWarps + 1;
 constexpr size_t kSmem = 227 * 1024;
 
 // CTAs of one launch that run at a time, one an SM: clusters of `split` on 152 SMs, less what
@@ -75,7 +77,7 @@ extern "C" kd_status kd_matmul_4bit(const kd_weight4* w, const void* x, kd_dtype
                                     void* stream) {
   using namespace kd;
   using namespace kd::mat4;
-  if (!weight4_sizes_ok(w) || rows < 0 || (x_dtype != KD_F16 && x_dtype != KD_BF16 && x_dtype != KD_E4M3) ||
+  if (!weight4_sizes_ok(w) || w->m > kMaxM || rows < 0 || (x_dtype != KD_F16 && x_dtype != KD_BF16 && x_dtype != KD_E4M3) ||
       !float_type(y_dtype) || ldx < w->n || ldy < w->m)
     return KD_ERR_INVALID_ARG;
   if (w->n > kMaxN) return KD_ERR_UNSUPPORTED_N;
