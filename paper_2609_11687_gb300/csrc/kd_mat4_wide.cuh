@@ -33,7 +33,8 @@
 // more often: 55 us at 64, 67 at 32.
 //
 // Every wait is bounded (about a second); one that expires marks the CTA, whose waits then
-// all return at once and whose outputs become NaN.
+// all return at once and whose outputs become NaN.  Before it gives back its memory such a CTA
+// waits once more, bounded again, for the products that it has in flight.
 #pragma once
 #include "kd_bulk.cuh"
 #include "kd_mat4.cuh"
@@ -68,6 +69,7 @@ static_assert(kColumnsOfA<64> + kWideStages * 64 <= kTensorColumns, "tensor memo
 struct WideBarriers {
   uint64_t full[kWideStages], empty[kWideStages];  // a stage of A and B is laid out; its products are done
   uint64_t sums[2], taken[2];  // an accumulator holds a group's sums; they have been read
+  uint64_t drained;            // after an expired wait: no product is in flight
   uint32_t tmem;
   int failed;
 };
@@ -181,6 +183,7 @@ __global__ void __launch_bounds__(kWideThreads, 2) mat4_wide_kernel(const __grid
       mbar_init(&sh.sums[s], 1);
       mbar_init(&sh.taken[s], kWideWarps);
     }
+    mbar_init(&sh.drained, 1);
     sh.failed = 0;
     mbar_init_fence();
   }
@@ -360,8 +363,15 @@ __global__ void __launch_bounds__(kWideThreads, 2) mat4_wide_kernel(const __grid
     barrier_wait(&sh.empty[(mine - 1) & 1], (mine - 1) >> 1 & 1, &sh.failed);
   }
   wait_group<0>();
-
+  __syncthreads();  // every wait is over: `failed` is final, and stages and ring are free
   const bool failed = *static_cast<volatile int*>(&sh.failed);
+  if (failed) {
+    // The stages' barriers are out of step with the products by now; this one is new.  Every
+    // product has been issued, by the lane that commits here.
+    if (warp == 0 && elect()) tensor_commit(&sh.drained);
+    mbar_wait_bounded(&sh.drained, 0);
+  }
+
   auto finish = [&](int r, int c, float v) {
     const int j = tile * kWideChannels + c;
     if (j >= p.m) return;
@@ -379,7 +389,6 @@ __global__ void __launch_bounds__(kWideThreads, 2) mat4_wide_kernel(const __grid
   } else {
     cg::cluster_group cl = cg::this_cluster();
     float* sums = reinterpret_cast<float*>(stage_b);
-    __syncthreads();  // stages and ring are free: every thread has its last sums
 #pragma unroll
     for (int j = 0; j < kHalf; ++j)
       if (part * kHalf + j < p.rows) sums[(part * kHalf + j) * kWideChannels + of_tile] = acc[j];
