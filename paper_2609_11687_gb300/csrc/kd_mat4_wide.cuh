@@ -170,12 +170,6 @@ __global__ void __launch_bounds__(kWideThreads, 2) mat4_wide_kernel(const __grid
   const int c0 = rank * p.per, mine = max(0, min(p.per, p.chunks - c0));
   constexpr int kGroups = 4 / GS, kUnits = kWideUnits<N>, kHalf = N / 2, kRing = kWideRing<N>;
 
-  if (warp == 0) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)),
-                 "r"(kTensorColumns)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
   if (tid == 32) {
     for (int s = 0; s < 2; ++s) {
       mbar_init(&sh.full[s], kWideWarps);
@@ -187,10 +181,17 @@ __global__ void __launch_bounds__(kWideThreads, 2) mat4_wide_kernel(const __grid
     sh.failed = 0;
     mbar_init_fence();
   }
+  wait_for_last();
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)),
+                 "r"(kTensorColumns)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  depend_on_last();
+  let_next_start();
 
   // this thread's lane of tensor memory, channel, and half: inputs 64 part .. + 63 of a
   // chunk, rows kHalf part .. of the sums

@@ -23,13 +23,18 @@ inline bool rows_aligned16(const void* p, int64_t ld, int64_t rows, int d) {
 // Programmatic dependent launch: a kernel launched with launch_early may be set up while the
 // one before it in the stream still runs; depend_on_last, before its first access to
 // global memory, waits for that one's end and results, and lets the next be set up in turn.
+// What a kernel takes of its SM but its launch (tensor memory) it takes between the two
+// (wait_for_last, let_next_start): taken earlier it may be what the kernel before still wants, taken
+// later the next one's CTAs may hold it.
 inline void launch_early(cudaLaunchAttribute& a) {
   a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   a.val.programmaticStreamSerializationAllowed = 1;
 }
+__device__ __forceinline__ void wait_for_last() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void depend_on_last() {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  wait_for_last();
+  let_next_start();
 }
 
 // this CTA's rank in its cluster, the cluster's index, the launch's clusters (CTAs without one
