@@ -573,7 +573,8 @@ kd_status kd_dequantise_4bit(const kd_weight4* w, kd_dtype out_dtype, void* out,
  *           rows' scales, as kd_rmsnorm leaves them), or NULL: 1.
  *   y       device, y_dtype KD_F32, KD_F16 or KD_BF16.
  * Meant for few rows (decoding): up to 64 rows share one pass over the weights, more rows
- * take more passes.  Within a group the sum over integers code - zero is formed on the tensor
+ * take more passes (and so do 9 to 16 rows of about 32768 inputs or more, eight rows a
+ * pass, if they are not aligned or there are fewer than 2560 channels).  Within a group the sum over integers code - zero is formed on the tensor
  * cores (exact products, fp32 sums); groups are added in fp32 with their scale, and the
  * whole is rounded once.  The order of the sums is fixed (deterministic results), and is
  * the same for all calls of at most eight rows: a row's bits do not depend on what shares

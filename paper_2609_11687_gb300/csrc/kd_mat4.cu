@@ -21,7 +21,7 @@ int room(int split) { return split == 1 ? 152 : split == 2 ? 76 : split == 4 ? 3
 // splits of 24 products (64 to 32000 channels of 700 to 16384 inputs, 1 to 16 rows): the
 // choice is the fastest within 2 %, but for one of rows that are not aligned (11 %).  Without the rows' part 4096 x
 // 4096 at 16 rows took 8.3 us instead of 7.2, 64 x 8192 6.2 instead of 4.5.
-// False if the rows fit no CTA's shared memory.
+// False if the rows fit no CTA's shared memory (eight rows always do).
 bool plan(Params& p, int nt, int rows) {
   bool found = false;
   double least = 0;
@@ -106,27 +106,34 @@ extern "C" kd_status kd_matmul_4bit(const kd_weight4* w, const void* x, kd_dtype
   const size_t wide = p.e4m3 ? 8 : 16;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   // Passes of equal numbers of rows: from 17 rows on of at most 64, by the kernel for many
-  // rows; else one of at most 16 (or, where an input is so long that those fit no CTA's
-  // shared memory, of 8).  At 16 rows that one takes 7.2 / 12.8 / 24 us for 4096 x 4096,
-  // 4096 x 11008 and 32000 x 4096, the kernel for many rows 7.6 / 13.9 / 34 there and no more
-  // at 17 to 32, where two passes of the other take about twice its time.
-  int nt = 0, clusters = 0;
-  int64_t pass = 0;
-  if (rows > 16) {
-    const int64_t passes = (rows + 63) / 64;
-    pass = (rows + passes - 1) / passes;
-    plan_wide(p);
-  } else {
-    nt = rows > 8 ? 2 : 1;
-    pass = rows;
-    // up to eight rows split the work alike, so that a row's sums have one order whatever
-    // else is in the batch
-    if (!plan(p, nt, nt == 1 ? 8 : (int)rows)) {
-      if (nt == 1 || !plan(p, nt = 1, 8)) return KD_ERR_UNSUPPORTED_N;
-      pass = 8;
-    }
+  // rows; else one by the kernel for few.  At 16 rows that one takes 7.2 / 12.8 / 24 us for
+  // 4096 x 4096, 4096 x 11008 and 32000 x 4096, the kernel for many rows 7.6 / 13.9 / 34 there and no
+  // more at 17 to 32, where two passes of the other take about twice its time.
+  // Where 9 to 16 rows of long inputs fit no CTA's shared memory (16 of 32768), the kernel for
+  // many rows takes them too, 35 us for 4096 channels of 32768 and 65 of 65536, where two passes
+  // of eight take 42 and 99; it has one cluster for 128 channels, and few of those leave SMs idle: 512
+  // channels take it 27 and 51 us, the two passes 16 and 25 (2500 channels 34 and 65, 37 and 62).  Each of
+  // its clusters reads the rows again, by elements where they are not aligned: 4096 channels of 39999
+  // then take it 121 us, the two passes 82.
+  constexpr int kManyChannels = 2560;
+  int nt = rows > 8 ? 2 : 1, clusters = 0;
+  int64_t pass = rows;
+  // up to eight rows split the work alike, so that a row's sums have one order whatever
+  // else is in the batch
+  bool few = rows <= 16 && plan(p, nt, nt == 1 ? 8 : (int)rows);
+  if (!few && rows <= 16 && (p.m < kManyChannels || !aligned(x, wide) || ldx * xb % (int64_t)wide != 0)) {
+    nt = 1;
+    pass = 8;
+    few = plan(p, nt, 8);
+  }
+  if (few) {
     p.turns_of_row_inv = 1.f / (float)((p.per * 16 + 31) / 32);
     clusters = p.tiles < room(p.split) ? p.tiles : room(p.split);
+  } else {
+    const int64_t passes = (rows + 63) / 64;
+    nt = 0;
+    pass = (rows + passes - 1) / passes;
+    plan_wide(p);
   }
   for (int64_t r0 = 0; r0 < rows; r0 += pass) {
     p.rows = (int)(rows - r0 < pass ? rows - r0 : pass);
