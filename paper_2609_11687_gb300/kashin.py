@@ -377,10 +377,29 @@ def _stream(stream) -> int:
     return s.cuda_stream
 
 
-class Workspace:
-    """Device scratch for one vector length (reusable across calls on one stream)."""
+def _new(stream, shape, dtype, device):
+    """An output allocated here for work on ``stream`` (None: the current one).  The block comes
+    from that stream's own pool: one of the current stream's may have been freed with work
+    still pending there, which ``stream`` does not wait for.  The caller's stream is noted, so
+    that a result dropped there is not given out again before it has been read."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if hasattr(stream, "cuda_stream") and not hasattr(stream, "device"):  # a holder of a bare handle
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    current = torch.cuda.current_stream(device)
+    if current != stream:
+        t.record_stream(current)
+    return t
 
-    def __init__(self, n: int, device="cuda", count: int = 1):
+
+class Workspace:
+    """Device scratch for one vector length (reusable across calls on one stream, ``stream`` or
+    the current one)."""
+
+    def __init__(self, n: int, device="cuda", count: int = 1, stream=None):
         torch = _torch()
         self.n = int(n)
         self.count = int(count)
@@ -389,7 +408,7 @@ class Workspace:
             raise KashinError(KD_ERR_UNSUPPORTED_N if kd_supported(self.n) else KD_ERR_CUDA,
                               f"kd_workspace_size({self.n})")
         self.nbytes = size
-        self.buf = torch.empty(size, dtype=torch.uint8, device=device)
+        self.buf = _new(stream, (size,), torch.uint8, device)
 
     @property
     def ptr(self) -> int:
@@ -432,17 +451,17 @@ def decompose(w, iters: int, sign_seed: int, layout: str = "rows", factors: bool
     dev = w.device
     words = (n + 15) // 16
     if out is None:
-        f32 = dict(dtype=torch.float32, device=dev)
+        def empty(shape, dtype=torch.float32):
+            return _new(stream, shape, dtype, dev)
         out = Decomposed(
-            codes_u=torch.empty((m, words), dtype=torch.int32, device=dev),
-            codes_v=torch.empty((m, words), dtype=torch.int32, device=dev),
-            centres_u=torch.empty((m, 4), **f32), centres_v=torch.empty((m, 4), **f32),
-            coeffs=torch.empty((m, 4), **f32) if coeffs else None,
-            u=torch.empty((m, n), **f32) if factors else None,
-            vhat=torch.empty((m, n), **f32) if factors else None,
-            resid=torch.empty((m, n), **f32) if factors else None,
-            trace=torch.empty((m, 4 * iters + 2 * kmeans_iters, n), dtype=torch.int8, device=dev) if trace else None)
-    ws = workspace if workspace is not None else Workspace(n, dev)
+            codes_u=empty((m, words), torch.int32), codes_v=empty((m, words), torch.int32),
+            centres_u=empty((m, 4)), centres_v=empty((m, 4)),
+            coeffs=empty((m, 4)) if coeffs else None,
+            u=empty((m, n)) if factors else None,
+            vhat=empty((m, n)) if factors else None,
+            resid=empty((m, n)) if factors else None,
+            trace=empty((m, 4 * iters + 2 * kmeans_iters, n), torch.int8) if trace else None)
+    ws = workspace if workspace is not None else Workspace(n, dev, stream=stream)
     st = kd_decompose(w.data_ptr(), _dtype_code(w.dtype), lay, n, m, ld, sign_seed, int(iters), int(kmeans_iters),
                       _ptr(out.codes_u), _ptr(out.codes_v), _ptr(out.centres_u), _ptr(out.centres_v),
                       _ptr(out.coeffs), _ptr(out.u), _ptr(out.vhat), _ptr(out.resid), _ptr(out.trace),
@@ -475,16 +494,17 @@ def decompose_batch(ws, iters: int, sign_seeds, layout: str = "rows", coeffs: bo
         if outs is not None:
             o = outs[i]
         else:
-            f32 = dict(dtype=torch.float32, device=w.device)
-            o = Decomposed(codes_u=torch.empty((m, (n + 15) // 16), dtype=torch.int32, device=w.device),
-                           codes_v=torch.empty((m, (n + 15) // 16), dtype=torch.int32, device=w.device),
-                           centres_u=torch.empty((m, 4), **f32), centres_v=torch.empty((m, 4), **f32),
-                           coeffs=torch.empty((m, 4), **f32) if coeffs else None,
+            def empty(shape, dtype=torch.float32):
+                return _new(stream, shape, dtype, w.device)
+            o = Decomposed(codes_u=empty((m, (n + 15) // 16), torch.int32),
+                           codes_v=empty((m, (n + 15) // 16), torch.int32),
+                           centres_u=empty((m, 4)), centres_v=empty((m, 4)),
+                           coeffs=empty((m, 4)) if coeffs else None,
                            u=None, vhat=None, resid=None, trace=None)
         arr[i] = KdMatrix(w.data_ptr(), m, _ld(w), int(sign_seeds[i]) & ((1 << 64) - 1),
                           _ptr(o.codes_u), _ptr(o.codes_v), _ptr(o.centres_u), _ptr(o.centres_v), _ptr(o.coeffs))
         res.append(o)
-    wsp = workspace if workspace is not None else Workspace(n, ws[0].device, count=len(ws))
+    wsp = workspace if workspace is not None else Workspace(n, ws[0].device, count=len(ws), stream=stream)
     st = kd_decompose_batch(ctypes.cast(arr, ctypes.c_void_p), len(ws), _dtype_code(dt), lay, n, int(iters),
                             int(kmeans_iters), wsp.ptr, wsp.nbytes, _stream(stream))
     if st != KD_OK:
@@ -509,7 +529,7 @@ def matmul_2bit(dec: "Decomposed", x, xp, out=None, stream=None):
     b, n = x.shape
     if (n + 15) // 16 != words:
         raise ValueError("x does not match the code planes' vector length")
-    y = out if out is not None else torch.empty((b, m), dtype=torch.float32, device=x.device)
+    y = out if out is not None else _new(stream, (b, m), torch.float32, x.device)
     st = kd_matmul_2bit(dec.codes_u.data_ptr(), dec.codes_v.data_ptr(), dec.centres_u.data_ptr(),
                         dec.centres_v.data_ptr(), n, m, x.data_ptr(), xp.data_ptr(), b, _ld(x), y.data_ptr(),
                         _ld(y), _stream(stream))
@@ -564,7 +584,7 @@ def matmul_2bit_f16_batch(decs, xs, xps, outs=None, stream=None):
         n = x.shape[1]
         if (n + 15) // 16 != words:
             raise ValueError("x does not match the code planes' vector length")
-        y = outs[i] if outs is not None else torch.empty((b, m), dtype=torch.float32, device=x.device)
+        y = outs[i] if outs is not None else _new(stream, (b, m), torch.float32, x.device)
         arr[i] = KdFoldMatF16(d.codes_u.data_ptr(), d.codes_v.data_ptr(), d.centres_u.data_ptr(),
                               d.centres_v.data_ptr(), x.data_ptr(), xp.data_ptr(), y.data_ptr(), n, m, _ld(x),
                               _ld(y))
@@ -597,7 +617,7 @@ def matmul_2bit_batch(decs, xs, xps, outs=None, stream=None):
         n = x.shape[1]
         if (n + 15) // 16 != words:
             raise ValueError("x does not match the code planes' vector length")
-        y = outs[i] if outs is not None else torch.empty((b, m), dtype=torch.float32, device=x.device)
+        y = outs[i] if outs is not None else _new(stream, (b, m), torch.float32, x.device)
         arr[i] = KdFoldMat(d.codes_u.data_ptr(), d.codes_v.data_ptr(), d.centres_u.data_ptr(), d.centres_v.data_ptr(),
                            x.data_ptr(), xp.data_ptr(), y.data_ptr(), n, m, _ld(x), _ld(y))
         res.append(y)
@@ -619,10 +639,10 @@ def apply_p_batch(xs, sign_seeds, outs=None, workspace: Optional[Workspace] = No
     for i, x in enumerate(xs):
         if x.dtype != torch.float32 or not x.is_contiguous() or x.dim() != 2 or x.shape[1] != n:
             raise ValueError("inputs must be contiguous fp32 (m, n) CUDA tensors of one n")
-        y = outs[i] if outs is not None else torch.empty_like(x)
+        y = outs[i] if outs is not None else _new(stream, x.shape, x.dtype, x.device)
         arr[i] = KdPMat(x.data_ptr(), y.data_ptr(), x.shape[0], int(sign_seeds[i]) & ((1 << 64) - 1))
         res.append(y)
-    ws = workspace if workspace is not None else Workspace(n, xs[0].device, count=len(xs))
+    ws = workspace if workspace is not None else Workspace(n, xs[0].device, count=len(xs), stream=stream)
     st = kd_apply_p_batch(ctypes.cast(arr, ctypes.c_void_p), len(xs), n, ws.ptr, ws.nbytes, _stream(stream))
     if st != KD_OK:
         raise KashinError(st, "kd_apply_p_batch")
@@ -642,7 +662,7 @@ def prepare_p(n: int, sign_seeds, workspace: Optional[Workspace] = None, device=
     into a workspace (returned) for apply_p_prepared."""
     if not 1 <= len(sign_seeds) <= KD_MAX_BATCH:
         raise ValueError(f"1..{KD_MAX_BATCH} sign seeds")
-    ws = workspace if workspace is not None else Workspace(n, device, count=len(sign_seeds))
+    ws = workspace if workspace is not None else Workspace(n, device, count=len(sign_seeds), stream=stream)
     seeds = (ctypes.c_uint64 * len(sign_seeds))(*[int(s) & ((1 << 64) - 1) for s in sign_seeds])
     st = kd_prepare_p(ctypes.cast(seeds, ctypes.c_void_p), len(sign_seeds), n, ws.ptr, ws.nbytes, _stream(stream))
     if st != KD_OK:
@@ -662,7 +682,7 @@ def apply_p_prepared(xs, workspace: Workspace, outs=None, stream=None):
     for i, x in enumerate(xs):
         if x.dtype != torch.float32 or not x.is_contiguous() or x.dim() != 2 or x.shape[1] != n:
             raise ValueError("inputs must be contiguous fp32 (m, n) CUDA tensors of one n")
-        y = outs[i] if outs is not None else torch.empty_like(x)
+        y = outs[i] if outs is not None else _new(stream, x.shape, x.dtype, x.device)
         arr[i] = KdPMat(x.data_ptr(), y.data_ptr(), x.shape[0], 0)
         res.append(y)
     st = kd_apply_p_prepared(ctypes.cast(arr, ctypes.c_void_p), len(xs), n, workspace.ptr, workspace.nbytes,
@@ -739,8 +759,8 @@ def apply_p(x, sign_seed: int, out=None, workspace: Optional[Workspace] = None, 
     if x.dtype != torch.float32 or not x.is_contiguous() or x.dim() != 2:
         raise ValueError("x must be a contiguous fp32 (m, n) CUDA tensor")
     m, n = x.shape
-    y = out if out is not None else torch.empty_like(x)
-    ws = workspace if workspace is not None else Workspace(n, x.device)
+    y = out if out is not None else _new(stream, x.shape, x.dtype, x.device)
+    ws = workspace if workspace is not None else Workspace(n, x.device, stream=stream)
     st = kd_apply_p(x.data_ptr(), y.data_ptr(), n, m, sign_seed, ws.ptr, ws.nbytes, _stream(stream))
     if st != KD_OK:
         raise KashinError(st, "kd_apply_p")
@@ -755,7 +775,7 @@ def dequantise(codes, centres, n: int, dtype=None, layout: str = "rows", out=Non
     m = codes.shape[0]
     lay = KD_VEC_ROWS if layout == "rows" else KD_VEC_COLUMNS
     if out is None:
-        out = torch.empty((m, n) if lay == KD_VEC_ROWS else (n, m), dtype=dtype, device=codes.device)
+        out = _new(stream, (m, n) if lay == KD_VEC_ROWS else (n, m), dtype, codes.device)
     st = kd_dequantise(codes.data_ptr(), centres.data_ptr(), n, m, _dtype_code(out.dtype), lay, out.data_ptr(),
                        _ld(out), _stream(stream))
     if st != KD_OK:
@@ -778,7 +798,7 @@ def dequantise_batch(planes, n: int, dtype=None, layout: str = "rows", outs=None
         if outs is not None:
             o = outs[i]
         else:
-            o = torch.empty((m, n) if lay == KD_VEC_ROWS else (n, m), dtype=dtype, device=codes.device)
+            o = _new(stream, (m, n) if lay == KD_VEC_ROWS else (n, m), dtype, codes.device)
         if o.dtype != dtype:
             raise ValueError("outputs must share one dtype")
         arr[i] = KdPlane(codes.data_ptr(), centres.data_ptr(), o.data_ptr(), m, _ld(o))
@@ -799,7 +819,7 @@ def rht(x, seed: int, inverse: bool = False, out=None, status=None, stream=None)
     if x.dim() != 2 or x.stride(1) != 1:
         raise ValueError("x must be a 2-D CUDA tensor with unit inner stride")
     m, n = x.shape
-    y = out if out is not None else torch.empty((m, n), dtype=torch.float32, device=x.device)
+    y = out if out is not None else _new(stream, (m, n), torch.float32, x.device)
     if y.dtype != torch.float32 or y.shape != x.shape or y.stride(1) != 1:
         raise ValueError("out must be an fp32 tensor of x's shape with unit inner stride")
     st = kd_rht(x.data_ptr(), _dtype_code(x.dtype), n, m, _ld(x), seed, 1 if inverse else 0, y.data_ptr(),
@@ -818,8 +838,8 @@ def reconstruct(dec: Decomposed, n: int, sign_seed: int, dtype=None, layout: str
     lay = KD_VEC_ROWS if layout == "rows" else KD_VEC_COLUMNS
     dev = dec.codes_u.device
     if out is None:
-        out = torch.empty((m, n) if lay == KD_VEC_ROWS else (n, m), dtype=dtype, device=dev)
-    ws = workspace if workspace is not None else Workspace(n, dev)
+        out = _new(stream, (m, n) if lay == KD_VEC_ROWS else (n, m), dtype, dev)
+    ws = workspace if workspace is not None else Workspace(n, dev, stream=stream)
     st = kd_reconstruct(dec.codes_u.data_ptr(), dec.codes_v.data_ptr(), dec.centres_u.data_ptr(),
                         dec.centres_v.data_ptr(), n, m, sign_seed, _dtype_code(out.dtype), lay, out.data_ptr(),
                         _ld(out), ws.ptr, ws.nbytes, _stream(stream))
@@ -842,14 +862,13 @@ def reconstruct_batch(decs, n: int, sign_seeds, dtype=None, layout: str = "rows"
     res = []
     for i, d in enumerate(decs):
         m = d.codes_u.shape[0]
-        o = outs[i] if outs is not None else torch.empty((m, n) if lay == KD_VEC_ROWS else (n, m), dtype=dtype,
-                                                         device=dev)
+        o = outs[i] if outs is not None else _new(stream, (m, n) if lay == KD_VEC_ROWS else (n, m), dtype, dev)
         if o.dtype != dtype:
             raise ValueError("outputs must share one dtype")
         arr[i] = KdRecMat(d.codes_u.data_ptr(), d.codes_v.data_ptr(), d.centres_u.data_ptr(), d.centres_v.data_ptr(),
                           int(sign_seeds[i]) & ((1 << 64) - 1), o.data_ptr(), m, _ld(o))
         res.append(o)
-    ws = workspace if workspace is not None else Workspace(n, dev, count=len(decs))
+    ws = workspace if workspace is not None else Workspace(n, dev, count=len(decs), stream=stream)
     st = kd_reconstruct_batch(ctypes.cast(arr, ctypes.c_void_p), len(decs), n, _dtype_code(dtype), lay, ws.ptr,
                               ws.nbytes, _stream(stream))
     if st != KD_OK:
@@ -921,22 +940,6 @@ def _vec(t, name, types, index, length):
         _refuse(t, name, types, index, (length,))
     if length > 1 and t.stride(0) != 1:
         raise ValueError(f"{name} must be contiguous")
-
-
-def _new(stream, shape, dtype, device):
-    """An output allocated here for work on ``stream`` (None: the current one).  The block comes
-    from that stream's own pool: one of the current stream's may have been freed with work
-    still pending there, which ``stream`` does not wait for.  The caller's stream is noted, so
-    that a result dropped there is not given out again before it has been read."""
-    torch = _torch()
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        t = torch.empty(shape, dtype=dtype, device=device)
-    current = torch.cuda.current_stream(device)
-    if current != stream:
-        t.record_stream(current)
-    return t
 
 
 def _call(what, fn, index, stream, *args):
