@@ -7,8 +7,9 @@ the log probabilities of the wanted tokens, the entropy and the likeliest altern
 
     python -m paper_2609_11687_gb300.score [--rows R] [--hidden N] [--vocab V]
 
-scores synthetic rows with the dense fp16 head, with the 4-bit head and with the same head
-decomposed to 2-bit planes (Kashin-DCT), and prints the perplexity of each.
+scores the same fp16 rows with the dense fp16 head, with the 4-bit head and with that head
+decomposed to 2-bit planes (Kashin-DCT; two planes, so four bits a weight as well), and the 4-bit
+head on 8-bit rows, and prints the perplexity of each.
 """
 
 from __future__ import annotations
@@ -21,18 +22,23 @@ from . import kashin as kd
 
 class OutputHead:
     """Final norm and 4-bit output head.  ``head``: a Weight4, or the dense (vocab, hidden)
-    matrix to quantise; ``norm``: the norm's weight (hidden,)."""
+    matrix to quantise; ``norm``: the norm's weight (hidden,).  ``eight_bits``: the normed rows
+    go to the head in e4m3 with a scale each; without it in the hidden rows' own 16-bit type."""
 
-    def __init__(self, norm, head, eps: float = 1e-5, group: int = 128, zeros: bool = False):
-        self.norm, self.eps = norm, eps
+    def __init__(self, norm, head, eps: float = 1e-5, group: int = 128, zeros: bool = False, eight_bits: bool = True):
+        self.norm, self.eps, self.eight_bits = norm, eps, eight_bits
         self.head = head if isinstance(head, kd.Weight4) else kd.quantise_4bit(head, group, zeros)
         if norm.shape != (self.head.n,):
             raise ValueError(f"the norm's weight must have the head's {self.head.n} inputs")
 
     def logits(self, x, residual=None, stream=None):
         """fp32 logits (rows, vocab) of the hidden rows ``x`` (plus ``residual``)."""
-        r = kd.rmsnorm(x, self.norm, self.eps, residual=residual, stream=stream)
-        return kd.matmul_4bit(self.head, r.q, scale=r.scale, stream=stream)
+        if self.eight_bits:
+            r = kd.rmsnorm(x, self.norm, self.eps, residual=residual, stream=stream)
+            return kd.matmul_4bit(self.head, r.q, scale=r.scale, stream=stream)
+        rows = kd.Normed(y=kd._new(stream, x.shape, x.dtype, x.device))
+        r = kd.rmsnorm(x, self.norm, self.eps, residual=residual, out=rows, stream=stream)
+        return kd.matmul_4bit(self.head, r.y, stream=stream)
 
     def score(self, x, ids, residual=None, top: int = 0, stream=None) -> kd.TokenLogprobs:
         """Log probabilities of ``ids`` (int64 (rows,) or (rows, tokens)) after the rows."""
@@ -69,14 +75,15 @@ def main(argv=None) -> dict:
     ids = torch.multinomial(dense.float().softmax(1), 1, generator=g)
     out = {"dense fp16": perplexity(kd.token_logprobs(dense, ids).logprobs)}
 
-    h4 = OutputHead(norm, head)
+    h4 = OutputHead(norm, head, eight_bits=False)
     out["4 bits"] = perplexity(h4.score(x, ids, residual).logprobs)
+    out["4 bits, 8-bit rows"] = perplexity(OutputHead(norm, h4.head).score(x, ids, residual).logprobs)
 
     d = kd.decompose(head, iters=16, sign_seed=1)
     xp = kd.apply_p(r.y.float(), 1).half()
     out["2-bit planes"] = perplexity(kd.token_logprobs(kd.matmul_2bit_f16(d, r.y, xp), ids).logprobs)
     for name, value in out.items():
-        print(f"{name:14s} perplexity {value:.3f}")
+        print(f"{name:18s} perplexity {value:.3f}")
     return out
 
 
