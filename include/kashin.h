@@ -495,9 +495,14 @@ kd_status kd_rht(const void* x, kd_dtype dtype, int64_t n, int64_t m, int64_t ld
 
 /* ---------------------------------------------------------------------------
  * Serving operators around the coded layers: the norm that makes a product's
- * activations, the product with 4-bit weights for layers that 2 bits do not carry (an
- * output head, sensitive projections), and the log probabilities that a model is scored
- * with.  They have no counterpart in the paper.  As everywhere, arguments are checked
+ * activations, the product with 4-bit weights, and the log probabilities that a model is
+ * scored with.  They have no counterpart in the paper.  4-bit weights cost the memory of a
+ * matrix's two 2-bit planes and lose about as much; they are for layers where the product's
+ * time counts (an output head: no P, and about a third of the planes' time), for weights
+ * that other quantisers have coded, and for comparisons with the planes.  Their rows'
+ * sums are fp32 in an order that is fixed for a call's sizes, types and alignment, but may
+ * change with them, the number of rows included (where a call promises more it says so).
+ * As everywhere, arguments are checked
  * first and nothing is enqueued on an error; no call allocates or needs a workspace.
  * Outputs must not overlap inputs or each other except where a call says so.
  * --------------------------------------------------------------------------- */
@@ -516,6 +521,8 @@ kd_status kd_rht(const void* x, kd_dtype dtype, int64_t n, int64_t m, int64_t ld
  *   q, scale       device, rows of n e4m3 bytes (row stride ldq bytes) and rows fp32.
  *   y              device, y_dtype any of KD_F32, KD_F16, KD_BF16.  y may be x itself
  *                  with the same dtype and ld.
+ * q and scale are those of the fp32 yv bit for bit.  h is normalised as it is, not as new_residual
+ * rounds it: a model that normalises the rounded sum differs in a 16-bit output's last place.
  * At least one of q and y is wanted (rows > 0).  A row whose sum of squares is not
  * finite (an infinity or NaN in it, or fp32/bf16 values past 1e19) gives NaN in y, q and
  * scale.  Rows of 16-byte aligned base and stride and n a multiple of 8 take 128-bit

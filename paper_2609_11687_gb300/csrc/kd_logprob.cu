@@ -20,9 +20,11 @@
 // Few rows: a cluster of CTAs shares a row, and its first CTA joins their sums and their
 // lists of alternatives.
 //
-// Bound by instructions for many rows (2048 x 32000 bf16: 28 us, 4.7 TB/s or 70 % of the
-// measured copy rate), by the latency of the phases after the pass for few (one row of 32000 fp32
-// with 20 alternatives: 6.5 us).
+// For many rows bound by memory and by the phases after a row's pass, during which its CTA
+// loads nothing (2048 x 32000 bf16: 28 us, 4.7 TB/s or 70 % of the measured copy rate; 63 % of the
+// issue slots used, warps wait for loads first, then at barriers); for few by the latency of
+// those phases (one row of 32000 fp32 with 20 alternatives 6.5 us; 61 masked rows of 65537 11.1 us, 40 %
+// of the slots used, warps wait at barriers first).
 #include <cooperative_groups.h>
 
 #include "kd_serve.cuh"

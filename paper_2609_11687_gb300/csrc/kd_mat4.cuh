@@ -25,9 +25,15 @@
 // warps of up to 177 registers at 9 to 16 rows: 36 us instead of 24 for 32000 x 4096; three
 // stages 32, their shared memory leaves room for half the rows only).
 //
-// Bound by the instructions that decode (the integer pipe 54 % busy, 58 % of all issue slots
-// used at 8 rows of 32000 x 4096): 3.5 TB/s there, 19.9 us for a floor of 10.1; one row of 11008
-// x 4096 7.9 us, of 4096 x 4096 4.1.
+// No unit is saturated: at 8 rows of 32000 x 4096 the SMs that have a CTA (125 of 152, two tiles
+// each) use 60 % of their issue slots and 55 % of the integer pipe, the tensor pipe 23 %, DRAM
+// 38 %.  A warp issues 341 instructions a chunk: 112 on the integer pipe (of about 157 there) and 64
+// subtractions decode, 16 are products, the rest are addresses, scales, copies and the loop.  3.5 TB/s
+// there, 19.9 us for a floor of 10.1; one row of 11008 x 4096 7.9 us, of 4096 x 4096 4.1.  At 16 e4m3
+// rows of 4096 x 11008 in groups of 64 (13.3 us) 597 instructions a chunk, 44 % of the slots used:
+// warps wait for memory and for each other.  The registers of sixteen warps (128 a thread)
+// make these instances spill: groups of 32 at 9 to 16 rows (60 to 100 bytes) and with zero points
+// below (20), groups of 64 (8, with zero points 76) and of 128 with zero points (8) at 9 to 16 fp16 rows.
 //
 // K order.  The product is a sum over inputs, so A and B may enumerate them in any common
 // order.  A group of GS x 32 inputs is 4 GS code words of a channel; the lanes with

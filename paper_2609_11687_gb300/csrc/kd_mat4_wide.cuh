@@ -27,10 +27,13 @@
 // K order: a piece of eight inputs holds them as the codes of a word come out, (0 4 1 5 2 6
 // 3 7), in A and B alike.
 //
-// Bound by issue slots (49 % used, four warps a scheduler, 345 instructions a warp and chunk)
-// and by the waits on tensor memory between; the tensor pipe is 18 % busy: 43 us for 64 rows of
-// 32000 x 4096 in fp16 with groups of 128, floor 11.3.  Smaller groups drain the accumulators
-// more often: 55 us at 64, 67 at 32.
+// No unit is saturated: 49 % of the issue slots are used (346 instructions a warp and chunk), the
+// integer pipe is 32 % busy, the tensor pipe 18 %, DRAM 19 %; a warp waits longest for memory (the
+// copies) and for shared and tensor memory, one step of a chunk after the other, and of 152 SMs 98 have two
+// CTAs and the others one: 43.3 us for 64 rows of 32000 x 4096 in fp16 with groups of 128, floor
+// 11.3.  Smaller groups drain the accumulators more often: 55 us at 64, 67 at 32.  Rows that are
+// not aligned are read by elements, again by each CTA: 175 us for 64 rows of 32000 x 4095, 92 for
+// 32, where the kernel for few rows takes 33 for each 16.
 //
 // Every wait is bounded (about a second); one that expires marks the CTA, whose waits then
 // all return at once and whose outputs become NaN.  Before it gives back its memory such a CTA

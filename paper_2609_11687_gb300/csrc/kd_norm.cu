@@ -15,9 +15,9 @@
 // its next row before it reduces this one, so that loads are in flight all the time (a CTA
 // a row reached half of the bandwidth: most of its life is the reductions).  2048 x 4096 bf16 with
 // a residual, e4m3 and bf16 rows: 15.2 us, 73 % of the measured copy rate (one IEEE division an
-// element: 17.2); one row 2.3 us, 333 unaligned rows of 5003 6.6 us.  Instances of two pieces a
-// thread spill (28 to 132 bytes, fp16 with its own weight type none): 64 registers are what 1024
-// threads, the longest rows, leave each.
+// element: 17.2); one row 2.3 us, 333 unaligned rows of 5003 6.6 us.  64 registers are what
+// 1024 threads, the longest rows, leave each: instances of two pieces a thread spill 28 to 48 bytes
+// (fp16 rows and weight none, fp32 112), unaligned ones 64 to 188 and of one piece 16 to 24.
 #include <cuda_fp8.h>
 
 #include "kd_serve.cuh"

@@ -1,7 +1,9 @@
 // 4-bit weights with group scales at load time: kd_quantise_4bit makes them,
-// kd_dequantise_4bit expands them.  32000 x 4096 takes 0.41 ms to quantise from fp16 (0.8 TB/s:
-// bound by instructions, IEEE divisions above all, which reproducible codes want) and 0.11 ms to
-// expand to fp16 or fp32 (3.1 and 5.4 TB/s).
+// kd_dequantise_4bit expands them.  32000 x 4096 takes 0.40 ms to quantise from fp16 (0.8 TB/s,
+// floor 0.049) and 0.10 to 0.11 ms to expand to 16 bits or fp32 (3.2 and 5.6 TB/s).  Both are bound
+// by instructions: 407 for a warp's 128 weights (84 % of the issue slots used, the integer pipe
+// 66 % busy; six of a lane's steps are IEEE divisions, which reproducible codes want) and 195 for a
+// warp's 256 (79 % and 59 %: a scale is looked up for each word).
 //
 // Quantisation: one warp takes 128 consecutive inputs of a channel, four per lane, so a
 // group of 32, 64 or 128 is 8, 16 or 32 lanes: its extremes come from that many lanes'

@@ -18,6 +18,10 @@ Two layers:
   tensor cores), each with a ``_batch`` form; and the serving operators around them,
   ``rmsnorm`` (residual addition, 8-bit output), ``quantise_4bit`` / ``dequantise_4bit`` /
   ``matmul_4bit`` (4-bit weights with group scales) and ``token_logprobs``.
+
+A wrapper's ``stream`` (the current one without it) is where its work goes and whose memory its
+own outputs and scratch are.  As with any work on a second stream the caller has the inputs
+ready there, and keeps them, and tensors given as ``out``, until that work is done.
 """
 
 from __future__ import annotations
@@ -1016,7 +1020,8 @@ class Weight4:
     row at bits 4 (i % 8) of word i // 8; ``scales`` fp16 or bf16 (m, ceil(n/group));
     ``zeros`` uint8 of that shape with values 0..15, or None for 8 everywhere.  The weight is
     ``scale * (code - zero)``.  ``codes`` is contiguous; scales and zeros are kept group by
-    group (a tensor in another order is laid out anew here, once)."""
+    group (a tensor in another order is laid out anew here, once, on the current stream: the
+    one given is not needed any more)."""
 
     __slots__ = ("codes", "scales", "zeros", "n", "m", "group", "device", "index", "desc", "ref")
 
