@@ -620,6 +620,119 @@ kd_status kd_token_logprobs(const void* logits, kd_dtype dtype, int64_t rows, in
                             const int64_t* ids, int64_t tokens, int top, float* logprobs, float* lse, float* entropy,
                             int64_t* top_ids, float* top_logprobs, void* stream);
 
+/* How the channels of a head that turn together lie: channels i and i + rot/2 of the first
+ * rot (KD_ROPE_HALF), or 2i and 2i + 1 (KD_ROPE_INTERLEAVED). */
+typedef enum { KD_ROPE_HALF = 0, KD_ROPE_INTERLEAVED = 1 } kd_rope_layout;
+
+/* The heads of one operand of kd_rope: channel c of head h of token t is element
+ * t*x_token + h*x_head + c of x; likewise of y, which may be x itself with the same strides
+ * (in place) and overlaps nothing else.
+ *   weight  device, d values of weight_dtype (the operand's or KD_F32): the heads are normed
+ *           with it; NULL: no norm. */
+typedef struct kd_heads {
+  const void* x;
+  void* y;
+  const void* weight;
+  int64_t heads;
+  int64_t x_token, x_head;
+  int64_t y_token, y_head;
+  int64_t weight_dtype;
+} kd_heads;
+
+/* Frequencies (radians for one step of position) as kd_rope takes them, on the host: the
+ * 64-bit fraction of a turn, turns_host[i] = frequencies[i] / (2 pi) * 2^64 modulo 2^64, to
+ * within 2^-52 of its value.  Errors: KD_ERR_INVALID_ARG (count < 0, null pointers with
+ * count > 0, a frequency that is not finite). */
+kd_status kd_rope_turns(const double* frequencies, int64_t count, uint64_t* turns_host);
+
+/* Head norm and rotary positions in one pass over queries and keys:
+ *   h = x rsqrt(mean(x^2) + eps) w     over the d channels of a head (with a weight)
+ *   y_a = amplitude (h_a cos - h_b sin),  y_b = amplitude (h_b cos + h_a sin)
+ * for the rot/2 pairs (a, b) of the first rot channels, the others as they are; the angle of
+ * pair i at position p is p turns[i] / 2^64 turns.  The 64-bit product wraps at whole turns, so
+ * no position is far: an angle is off by p times its frequency's error plus 2^-25 turns (fp32's).
+ *   q, k       operands (host structs; k may be NULL), of one dtype: KD_F32, KD_F16, KD_BF16.
+ *   positions  device int64, `tokens` of them; negative ones turn the other way.
+ *   turns      device, rot/2 values as kd_rope_turns makes them.
+ * 1 <= d <= 1024, rot even, 2 <= rot <= d, tokens x heads below 2^31.  fp32 arithmetic, rounded once; a head whose sum of
+ * squares is no finite number is NaN throughout (with a norm).
+ * Rows on 16-byte boundaries with rot a multiple of 32 bytes take wide loads.
+ * Errors: KD_ERR_INVALID_ARG (sizes, rot, layout, types, eps < 0 or NaN, amplitude not finite,
+ * strides below 0, overlapping heads of y, missing or unaligned pointers),
+ * KD_ERR_UNSUPPORTED_N (d), KD_ERR_CUDA.  tokens == 0 or no heads enqueues nothing. */
+kd_status kd_rope(const kd_heads* q, const kd_heads* k, kd_dtype dtype, int64_t tokens, int64_t d,
+                  const int64_t* positions, const uint64_t* turns, int64_t rot, kd_rope_layout layout,
+                  float amplitude, float eps, void* stream);
+
+/* Keys and values of 4-bit codes in pages of `page` tokens.  The row of a token and a key head
+ * is its d channels in groups of `group`, each with a step and a lowest value:
+ *   value[c] = low[c / group] + step[c / group] * code[c].
+ *   k_codes, v_codes    device, 16-byte aligned, pages x heads x page rows of 4 ceil(d/32) uint32:
+ *                       code c at bits 4(c % 8) of word c/8; the padding codes do not count.
+ *   k_scales, v_scales  device, 16-byte aligned, pages x heads x page rows of ceil(d/group) pairs
+ *                       of fp16: step, low.
+ *   page   a multiple of 16, at most 65536;  group  32, 64 or 128;  1 <= d <= 256. */
+typedef struct kd_cache4 {
+  uint32_t* k_codes;
+  uint16_t* k_scales;
+  uint32_t* v_codes;
+  uint16_t* v_scales;
+  int64_t pages;
+  int64_t heads;
+  int64_t page;
+  int64_t d;
+  int64_t group;
+} kd_cache4;
+
+/* Which tokens of which sequences a call is about: for sequence s of `seqs` the rows
+ * starts[s] .. starts[s+1] - 1 are its LAST tokens, in order, so that its final row is position
+ * lengths[s] - 1.
+ *   table    device int32, seqs rows of `wide` page numbers, row s at table + s*ld_table:
+ *            position p of the sequence is place p % page of page table[s][p / page].
+ *   lengths  device int32: tokens of each sequence, the rows of this call among them.
+ *   starts   device int32, seqs + 1 values that do not decrease; NULL: every sequence has `most`
+ *            rows.
+ *   most     rows of one sequence at most.
+ *   longest  the largest length, as far as the host knows it (at most wide * page): a hint for how
+ *            attention is split, not a limit.
+ * The contents are read on the device and checked there: a row of no sequence (behind the
+ * last one, or past `most` of its sequence) is neither read nor written; a position below
+ * 0 has no place; a page number outside 0 .. pages - 1, or one past the table, is a bad page. */
+typedef struct kd_sequences {
+  const int32_t* table;
+  const int32_t* lengths;
+  const int32_t* starts;
+  int64_t ld_table;
+  int64_t seqs;
+  int64_t wide;
+  int64_t most;
+  int64_t longest;
+} kd_sequences;
+
+/* Quantises rows of keys and values into the cache: row t of head h is d elements at
+ * k + t*k_token + h*k_head (likewise v), dtype KD_F32, KD_F16 or KD_BF16.  For each group, with
+ * lo and hi its extremes: low = lo rounded down to fp16; step = (hi - low) / 15 (fp32) rounded up to
+ * fp16; code = min(15, rint((x - low) / step)) (fp32, nearest, ties to even), 0 where step is 0: no
+ * element is further than half a step from its value.  A group with an infinity or NaN, or
+ * whose low or step does not fit fp16, reads back as NaN.
+ * Rows of positions below 0 and on bad pages are left out.  The pages that new tokens fall on
+ * belong to one sequence, once; two rows of one call for one place leave a mixture there.
+ *   tokens   rows of k and v.
+ * Errors: KD_ERR_INVALID_ARG (cache, sequences, tokens, type, strides below 0, missing or unaligned
+ * pointers; 2 tokens x heads above 2^31 - 1), KD_ERR_UNSUPPORTED_N (d), KD_ERR_CUDA.  Nothing to do
+ * enqueues nothing. */
+kd_status kd_cache_write_4bit(const kd_cache4* cache, const kd_sequences* seqs, int64_t tokens, const void* k,
+                              int64_t k_token, int64_t k_head, const void* v, int64_t v_token, int64_t v_head,
+                              kd_dtype dtype, void* stream);
+
+/* The rows of the sequences' tokens out of the cache, rounded to dtype (KD_F32, KD_F16,
+ * KD_BF16): row t of head h at k + t*k_token + h*k_head (likewise v; either may be NULL).  Rows of
+ * positions below 0 are 0, rows on bad pages NaN.  Errors as kd_cache_write_4bit, overlapping rows
+ * among them. */
+kd_status kd_cache_read_4bit(const kd_cache4* cache, const kd_sequences* seqs, int64_t tokens, void* k,
+                             int64_t k_token, int64_t k_head, void* v, int64_t v_token, int64_t v_head,
+                             kd_dtype dtype, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

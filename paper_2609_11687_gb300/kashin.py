@@ -17,7 +17,9 @@ Two layers:
   planes ``matmul_2bit`` (fp32) and ``matmul_2bit_f16`` (fp16 or bf16 activations,
   tensor cores), each with a ``_batch`` form; and the serving operators around them,
   ``rmsnorm`` (residual addition, 8-bit output), ``quantise_4bit`` / ``dequantise_4bit`` /
-  ``matmul_4bit`` (4-bit weights with group scales) and ``token_logprobs``.
+  ``matmul_4bit`` (4-bit weights with group scales) and ``token_logprobs``; and those of an
+  attention step, ``rope`` (head norms and rotary positions), ``cache_write_4bit`` and
+  ``cache_read_4bit`` (a paged cache of 4-bit keys and values).
 
 A wrapper's ``stream`` (the current one without it) is where its work goes and whose memory its
 own outputs and scratch are.  As with any work on a second stream the caller has the inputs
@@ -40,6 +42,7 @@ LIB_PATH = os.path.join(HERE, "libkashin.so")
 KD_OK, KD_ERR_INVALID_ARG, KD_ERR_UNSUPPORTED_N, KD_ERR_CUDA, KD_ERR_NONFINITE, KD_ERR_WORKSPACE, KD_ERR_TIMEOUT = range(7)
 KD_F32, KD_F16, KD_BF16, KD_E4M3 = 0, 1, 2, 3
 KD_VEC_ROWS, KD_VEC_COLUMNS = 0, 1
+KD_ROPE_HALF, KD_ROPE_INTERLEAVED = 0, 1
 
 EXPORTS = ("kd_status_string", "kd_version", "kd_supported", "kd_tuned", "kd_workspace_size", "kd_signs",
            "kd_decompose", "kd_apply_p", "kd_reconstruct", "kd_read_status", "kd_decompose_static",
@@ -49,7 +52,8 @@ EXPORTS = ("kd_status_string", "kd_version", "kd_supported", "kd_tuned", "kd_wor
            "kd_apply_p_batch", "kd_prepare_p", "kd_apply_p_prepared",
            "kd_rht_block", "kd_rht", "kd_dequantise", "kd_dequantise_batch", "kd_measure_fp32_peak",
            "kd_workspace_size_batch", "kd_decompose_batch", "kd_reconstruct_batch",
-           "kd_rmsnorm", "kd_quantise_4bit", "kd_dequantise_4bit", "kd_matmul_4bit", "kd_token_logprobs")
+           "kd_rmsnorm", "kd_quantise_4bit", "kd_dequantise_4bit", "kd_matmul_4bit", "kd_token_logprobs",
+           "kd_rope_turns", "kd_rope", "kd_cache_write_4bit", "kd_cache_read_4bit")
 KD_MAX_BATCH = 32
 KD_MAX_TOP = 32
 
@@ -104,6 +108,24 @@ class KdWeight4(ctypes.Structure):
     _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("zeros", ctypes.c_void_p),
                 ("n", ctypes.c_int64), ("m", ctypes.c_int64), ("group", ctypes.c_int32),
                 ("scale_dtype", ctypes.c_int32)]
+
+
+class KdHeads(ctypes.Structure):
+    """Mirror of kd_heads (include/kashin.h)."""
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("weight", ctypes.c_void_p)] + \
+               [(name, ctypes.c_int64) for name in ("heads", "x_token", "x_head", "y_token", "y_head", "weight_dtype")]
+
+
+class KdCache4(ctypes.Structure):
+    """Mirror of kd_cache4 (include/kashin.h)."""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("k_codes", "k_scales", "v_codes", "v_scales")] + \
+               [(name, ctypes.c_int64) for name in ("pages", "heads", "page", "d", "group")]
+
+
+class KdSequences(ctypes.Structure):
+    """Mirror of kd_sequences (include/kashin.h)."""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("table", "lengths", "starts")] + \
+               [(name, ctypes.c_int64) for name in ("ld_table", "seqs", "wide", "most", "longest")]
 
 
 def _load() -> ctypes.CDLL:
@@ -191,6 +213,15 @@ def _load() -> ctypes.CDLL:
     lib.kd_token_logprobs.argtypes = [c_vp, c_int, c_i64, c_i64, c_i64, c_vp, c_i64, c_int, c_vp, c_vp, c_vp, c_vp,
                                       c_vp, c_vp]
     lib.kd_token_logprobs.restype = c_int
+    lib.kd_rope_turns.argtypes = [c_vp, c_i64, c_vp]
+    lib.kd_rope_turns.restype = c_int
+    lib.kd_rope.argtypes = [c_vp, c_vp, c_int, c_i64, c_i64, c_vp, c_vp, c_i64, c_int, ctypes.c_float, ctypes.c_float,
+                            c_vp]
+    lib.kd_rope.restype = c_int
+    lib.kd_cache_write_4bit.argtypes = [c_vp, c_vp, c_i64, c_vp, c_i64, c_i64, c_vp, c_i64, c_i64, c_int, c_vp]
+    lib.kd_cache_write_4bit.restype = c_int
+    lib.kd_cache_read_4bit.argtypes = lib.kd_cache_write_4bit.argtypes
+    lib.kd_cache_read_4bit.restype = c_int
     return lib
 
 
@@ -346,6 +377,22 @@ def kd_token_logprobs(logits, dtype, rows, vocab, ld, ids, tokens, top, logprobs
                       stream) -> int:
     return lib.kd_token_logprobs(logits, dtype, rows, vocab, ld, ids, tokens, top, logprobs, lse, entropy, top_ids,
                                  top_logprobs, stream)
+
+
+def kd_rope_turns(frequencies, count, turns) -> int:
+    return lib.kd_rope_turns(frequencies, count, turns)
+
+
+def kd_rope(q, k, dtype, tokens, d, positions, turns, rot, layout, amplitude, eps, stream) -> int:
+    return lib.kd_rope(q, k, dtype, tokens, d, positions, turns, rot, layout, amplitude, eps, stream)
+
+
+def kd_cache_write_4bit(cache, seqs, tokens, k, k_token, k_head, v, v_token, v_head, dtype, stream) -> int:
+    return lib.kd_cache_write_4bit(cache, seqs, tokens, k, k_token, k_head, v, v_token, v_head, dtype, stream)
+
+
+def kd_cache_read_4bit(cache, seqs, tokens, k, k_token, k_head, v, v_token, v_head, dtype, stream) -> int:
+    return lib.kd_cache_read_4bit(cache, seqs, tokens, k, k_token, k_head, v, v_token, v_head, dtype, stream)
 
 
 # ---------------------------------------------------------------------------
@@ -1147,3 +1194,291 @@ def token_logprobs(logits, ids, top: int = 0, out: Optional[TokenLogprobs] = Non
           vocab, ld, ids.data_ptr(), tokens, top, out.logprobs.data_ptr(), None if lse is None else lse.data_ptr(),
           None if entropy is None else entropy.data_ptr(), out.top_ids.data_ptr(), out.top_logprobs.data_ptr())
     return out
+
+
+@dataclasses.dataclass(frozen=True)
+class Scaling:
+    """How a rotation trained on ``original`` positions is stretched by ``factor``:
+
+    * ``"linear"``: every frequency divided by it;
+    * ``"bands"``: pairs that turn at most ``low`` (1) times within ``original`` positions are, pairs
+      that turn at least ``high`` (4) times are not, those between in proportion to their turns;
+    * ``"ramp"``: the same between ``low`` (1) and ``high`` (32) turns, in proportion to the pair's
+      index, and the rotated part grows by ``amplitude`` (0.1 ln factor + 1)."""
+    kind: str
+    factor: float
+    original: int = 8192
+    low: float = 1.0
+    high: Optional[float] = None
+    amplitude: Optional[float] = None
+
+    def __post_init__(self):
+        if self.kind not in ("linear", "bands", "ramp"):
+            raise ValueError("kind must be linear, bands or ramp")
+        high = (4.0 if self.kind == "bands" else 32.0) if self.high is None else self.high
+        if not 0 < self.factor < np.inf or not 0 < self.low < high < np.inf or not 0 < self.original < np.inf:
+            raise ValueError("factor, original and 0 < low < high must be finite and positive")
+        object.__setattr__(self, "high", float(high))
+        if self.amplitude is None:
+            object.__setattr__(self, "amplitude", max(1.0, 0.1 * float(np.log(self.factor)) + 1.0) if self.kind == "ramp" else 1.0)
+
+
+def rotary_frequencies(rot: int, base: float = 10000.0, scaling: Optional[Scaling] = None) -> np.ndarray:
+    """Angles (radians, fp64) by which the rot/2 pairs turn for one step of position:
+    base^(-2i/rot), stretched as ``scaling`` says."""
+    if rot < 2 or rot % 2:
+        raise ValueError("rot must be even and at least 2")
+    if not 1 < base < np.inf:
+        raise ValueError("base must be finite and above 1")
+    i = np.arange(rot // 2, dtype=np.float64)
+    f = float(base) ** (-2.0 * i / rot)
+    if scaling is None:
+        return f
+    if scaling.kind == "linear":
+        return f / scaling.factor
+    if scaling.kind == "bands":
+        kept = np.clip((scaling.original * f / (2 * np.pi) - scaling.low) / (scaling.high - scaling.low), 0.0, 1.0)
+    else:
+        first, last = (rot * np.log(scaling.original / (turns * 2 * np.pi)) / (2 * np.log(base))
+                       for turns in (scaling.high, scaling.low))
+        first, last = max(np.floor(first), 0.0), min(np.ceil(last), rot - 1.0)
+        kept = 1.0 - np.clip((i - first) / max(last - first, 1e-3), 0.0, 1.0)
+    return f * kept + f / scaling.factor * (1.0 - kept)
+
+
+class Rotation:
+    """A model's rotary positions: ``rot`` channels of a head turn, in pairs rot/2 apart (layout
+    ``"half"``) or side by side (``"interleaved"``), by position times ``frequencies``
+    (``rotary_frequencies`` unless given).  The table is made here, once, on the host."""
+
+    __slots__ = ("rot", "layout", "frequencies", "amplitude", "turns", "index")
+
+    def __init__(self, rot: int, base: float = 10000.0, layout: str = "half", scaling: Optional[Scaling] = None,
+                 frequencies=None, amplitude: Optional[float] = None, device="cuda"):
+        torch = _torch()
+        if layout not in ("half", "interleaved"):
+            raise ValueError("layout must be half or interleaved")
+        if frequencies is None:
+            frequencies = rotary_frequencies(rot, base, scaling)
+        elif scaling is not None:
+            raise ValueError("frequencies are given as they are: no scaling with them")
+        frequencies = np.ascontiguousarray(frequencies, dtype=np.float64)
+        if frequencies.shape != (rot // 2,) or rot < 2 or rot % 2:
+            raise ValueError("rot must be even, with rot/2 frequencies")
+        turns = np.empty(rot // 2, dtype=np.uint64)
+        st = kd_rope_turns(frequencies.ctypes.data, rot // 2, turns.ctypes.data)
+        if st != KD_OK:
+            raise KashinError(st, "kd_rope_turns")
+        if amplitude is None:
+            amplitude = 1.0 if scaling is None else scaling.amplitude
+        self.rot, self.layout, self.frequencies, self.amplitude = int(rot), layout, frequencies, float(amplitude)
+        self.turns = torch.from_numpy(turns.view(np.int64)).to(device)
+        self.index = self.turns.get_device()
+
+
+def _ld3(t, name, types, index, shape=None):
+    """Strides over tokens and heads of a (tokens, heads, d) operand after its checks; what a
+    size of 1 leaves open is 0."""
+    size, stride = t.shape, t.stride()
+    if len(size) != 3:
+        raise ValueError(f"{name} must be (tokens, heads, channels)")
+    if t.dtype not in types:
+        raise ValueError(f"{name} has dtype {t.dtype}: one of {', '.join(map(str, types))} is wanted")
+    if not t.is_cuda or t.get_device() != index:
+        raise ValueError(f"{name} must be a CUDA tensor on " + ("one device with the others" if index < 0 else f"cuda:{index}"))
+    if shape is not None and tuple(size) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(size)}: {tuple(shape)} is wanted")
+    if size[2] > 1 and stride[2] != 1:
+        raise ValueError(f"{name} needs unit inner stride")
+    tokens, heads, d = size
+    return stride[0] if tokens > 1 else heads * d, stride[1] if heads > 1 else d
+
+
+def _row_strides(t, name):
+    """_ld3's of an output, whose rows must not overlap."""
+    tokens, heads, d = t.shape
+    a, b = t.stride()[:2]
+    if tokens > 1 and heads > 1:
+        apart = (b >= d and a >= (heads - 1) * b + d) or (a >= d and b >= (tokens - 1) * a + d)
+    else:
+        apart = (tokens <= 1 or a >= d) and (heads <= 1 or b >= d)
+    if not apart and t.numel():
+        raise ValueError(f"{name}'s rows must not overlap")
+
+
+def rope(q, k, positions, rotation: Rotation, q_norm=None, k_norm=None, eps: float = 1e-6, out=None, stream=None):
+    """Rotary positions of the heads of ``q`` and ``k`` (k may be None), after the norm of each
+    head where its weight is given (kd_rope); returns the pair.
+
+    ``q``, ``k``: (tokens, heads, d) CUDA tensors of one dtype (fp16, bf16, fp32) with unit inner
+    stride, views of a common projection's rows say; d <= 1024.  ``positions``: int64 (tokens,).
+    ``q_norm``, ``k_norm``: (d,) of that dtype or fp32.  ``out``: the pair of tensors to write, which
+    may be ``q`` and ``k`` themselves."""
+    floats, _, f32, _, _, _ = _serve()
+    index, dt = rotation.index, q.dtype
+    i64 = rotation.turns.dtype
+    if positions.shape != q.shape[:1] or positions.dtype != i64 or positions.get_device() != index \
+            or not positions.is_contiguous():
+        raise ValueError("positions must be a contiguous int64 tensor of q's tokens on the rotation's device")
+    out = (None, None) if out is None else out
+    done, descs, d = [], [], q.shape[-1]
+    for name, x, weight, y in (("q", q, q_norm, out[0]), ("k", k, k_norm, out[1])):
+        if x is None:
+            if weight is not None or y is not None:
+                raise ValueError(f"no {name}, but its weight or output")
+            done.append(None)
+            descs.append(None)
+            continue
+        xt, xh = _ld3(x, name, floats if x is q else (dt,), index)
+        if x.shape[0] != q.shape[0] or x.shape[2] != d:
+            raise ValueError("q and k must have the same tokens and channels")
+        if y is None:
+            y = _new(stream, x.shape, dt, x.device)
+        yt, yh = _ld3(y, f"out's {name}", (dt,), index, x.shape)
+        _row_strides(y, f"out's {name}")
+        if weight is not None:
+            _vec(weight, f"{name}_norm", (dt, f32), index, d)
+        descs.append(KdHeads(x.data_ptr(), y.data_ptr(), _ptr(weight), x.shape[1], xt, xh, yt, yh,
+                             0 if weight is None else floats[weight.dtype]))
+        done.append(y)
+    if rotation.rot > d:
+        raise ValueError(f"the rotation turns {rotation.rot} channels of {d}")
+    _call("kd_rope", lib.kd_rope, index, stream, ctypes.byref(descs[0]), None if k is None else ctypes.byref(descs[1]),
+          floats[dt], q.shape[0], d, positions.data_ptr(), rotation.turns.data_ptr(), rotation.rot,
+          KD_ROPE_HALF if rotation.layout == "half" else KD_ROPE_INTERLEAVED, rotation.amplitude, eps)
+    return done[0], done[1]
+
+
+class Cache4:
+    """Keys and values of 4-bit codes in pages (kd_cache4), for ``heads`` heads of ``d`` channels:
+    ``k_codes``, ``v_codes`` int32 (pages, heads, page, 4 ceil(d/32)), code c of a row at bits
+    4 (c % 8) of word c // 8; ``k_scales``, ``v_scales`` fp16 (pages, heads, page, ceil(d/group), 2),
+    a group's step and lowest value.  All contiguous; page a multiple of 16, d <= 256."""
+
+    __slots__ = ("k_codes", "k_scales", "v_codes", "v_scales", "pages", "heads", "page", "d", "group", "device", "index",
+                 "desc", "ref")
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales, *, d: int, group: int = 64):
+        torch = _torch()
+        if group not in (32, 64, 128):
+            raise ValueError("group must be 32, 64 or 128")
+        if not 1 <= d <= 256:
+            raise ValueError("d must be 1..256")
+        if k_codes.dim() != 4 or k_codes.shape[3] != (d + 31) // 32 * 4:
+            raise ValueError("codes must be int32 (pages, heads, page, 4 ceil(d/32))")
+        pages, heads, page, _ = k_codes.shape
+        if page % 16 or not 16 <= page <= 65536 or not 1 <= heads <= 65535:
+            raise ValueError("page must be a multiple of 16 up to 65536, and there must be 1..65535 heads")
+        codes, scales = (pages, heads, page, k_codes.shape[3]), (pages, heads, page, (d + group - 1) // group, 2)
+        operands = (k_codes, "k_codes", torch.int32, codes), (v_codes, "v_codes", torch.int32, codes), \
+            (k_scales, "k_scales", torch.float16, scales), (v_scales, "v_scales", torch.float16, scales)
+        for t, name, dtype, shape in operands:
+            if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous {dtype} {shape} tensor")
+        for t, *_ in operands:
+            if not t.is_cuda or t.device != k_codes.device:
+                raise ValueError("codes and scales must be CUDA tensors on one device")
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self.pages, self.heads, self.page, self.d, self.group = pages, heads, page, int(d), int(group)
+        self.device, self.index = k_codes.device, k_codes.get_device()
+        self.desc = KdCache4(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(), pages,
+                             heads, page, d, group)
+        self.ref = ctypes.addressof(self.desc)
+
+
+def new_cache_4bit(pages: int, heads: int, d: int, page: int = 64, group: int = 64, device="cuda") -> Cache4:
+    """A Cache4 whose places all hold 0."""
+    torch = _torch()
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128")
+    codes, scales = (pages, heads, page, (d + 31) // 32 * 4), (pages, heads, page, (d + group - 1) // group, 2)
+    return Cache4(torch.zeros(codes, dtype=torch.int32, device=device), torch.zeros(scales, dtype=torch.float16, device=device),
+                  torch.zeros(codes, dtype=torch.int32, device=device), torch.zeros(scales, dtype=torch.float16, device=device),
+                  d=d, group=group)
+
+
+class Sequences:
+    """The rows of a call (kd_sequences): for each sequence s the rows starts[s] .. starts[s+1] - 1
+    are its LAST tokens, in order, up to position lengths[s] - 1.
+
+    ``table`` int32 (sequences, wide): position p lies on page table[s, p // page]; ``lengths`` int32
+    (sequences,), the rows of the call counted; ``starts`` int32 (sequences + 1,), not decreasing,
+    or None: ``most`` rows each; ``most``: rows of a sequence at most; ``longest``: the largest
+    length as far as it is known here, by which attention is split (all that the table has room
+    for without it).  The tensors are kept and read on the device at each call: a step rewrites
+    them in place, a captured graph too.  Rows of no sequence are left as they are."""
+
+    __slots__ = ("table", "lengths", "starts", "most", "longest", "index", "desc", "ref")
+
+    def __init__(self, table, lengths, starts=None, *, most: int = 1, longest: Optional[int] = None):
+        torch = _torch()
+        if table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1) \
+                or (table.shape[0] > 1 and table.stride(0) < table.shape[1]):
+            raise ValueError("table must be (sequences, wide) with unit inner stride")
+        seqs, wide = table.shape
+        if lengths.shape != (seqs,) or not lengths.is_contiguous():
+            raise ValueError(f"lengths must be contiguous ({seqs},)")
+        if starts is not None and (starts.shape != (seqs + 1,) or not starts.is_contiguous()):
+            raise ValueError(f"starts must be contiguous ({seqs + 1},)")
+        for t, name in ((table, "table"), (lengths, "lengths"), (starts, "starts")):
+            if t is not None and t.dtype != torch.int32:
+                raise ValueError(f"{name} must be int32")
+            if t is not None and (not t.is_cuda or t.device != table.device):
+                raise ValueError("table, lengths and starts must be CUDA tensors on one device")
+        if not 0 <= most < 2 ** 31 or (longest is not None and longest < 0):
+            raise ValueError("most must be 0 .. 2^31 - 1 and longest not negative")
+        self.table, self.lengths, self.starts = table, lengths, starts
+        self.most, self.longest, self.index = int(most), None if longest is None else int(longest), table.get_device()
+        self.desc = KdSequences(table.data_ptr(), lengths.data_ptr(), _ptr(starts), _ld(table), seqs, wide, self.most,
+                                2 ** 62 if longest is None else self.longest)
+        self.ref = ctypes.addressof(self.desc)
+
+
+def _cache_rows(cache, seqs, k, v, types):
+    """Tokens and strides of keys and values that go to or come from the cache."""
+    if seqs.index != cache.index:
+        raise ValueError("the sequences must be on the cache's device")
+    strides, tokens = [], None
+    for which, t in (("k", k), ("v", v)):
+        if t is None:
+            strides.append((0, 0))
+            continue
+        strides.append(_ld3(t, which, types, cache.index))
+        if tokens is None:
+            tokens, types = t.shape[0], (t.dtype,)
+        if tuple(t.shape) != (tokens, cache.heads, cache.d):
+            raise ValueError(f"{which} has shape {tuple(t.shape)}: ({tokens}, {cache.heads}, {cache.d}) is wanted")
+    return tokens, strides
+
+
+def cache_write_4bit(cache: Cache4, k, v, seqs: Sequences, stream=None) -> None:
+    """Quantises the rows ``k`` and ``v`` (tokens, heads, d; fp16, bf16 or fp32) of the sequences'
+    last tokens into their places of the cache (kd_cache_write_4bit)."""
+    floats = _serve()[0]
+    tokens, ((kt, kh), (vt, vh)) = _cache_rows(cache, seqs, k, v, floats)
+    _call("kd_cache_write_4bit", lib.kd_cache_write_4bit, cache.index, stream, cache.ref, seqs.ref, tokens, k.data_ptr(), kt,
+          kh, v.data_ptr(), vt, vh, floats[k.dtype])
+
+
+def cache_read_4bit(cache: Cache4, seqs: Sequences, tokens: Optional[int] = None, dtype=None, out=None, stream=None):
+    """The rows of the sequences' last tokens out of the cache: the pair of ``out``, either of which
+    may be None, or new ones of ``tokens`` rows (every sequence's ``most`` without it and without
+    ``starts``) in ``dtype`` (fp16) (kd_cache_read_4bit)."""
+    floats = _serve()[0]
+    if out is None:
+        if tokens is None:
+            if seqs.starts is not None:
+                raise ValueError("tokens is wanted where the sequences have starts")
+            tokens = seqs.table.shape[0] * seqs.most
+        shape = (tokens, cache.heads, cache.d)
+        out = tuple(_new(stream, shape, dtype or _torch().float16, cache.device) for _ in range(2))
+    k, v = out
+    if k is None and v is None:
+        raise ValueError("out wants keys or values")
+    tokens, ((kt, kh), (vt, vh)) = _cache_rows(cache, seqs, k, v, floats)
+    for name, t in (("k", k), ("v", v)):
+        if t is not None:
+            _row_strides(t, f"out's {name}")
+    _call("kd_cache_read_4bit", lib.kd_cache_read_4bit, cache.index, stream, cache.ref, seqs.ref, tokens, _ptr(k), kt, kh,
+          _ptr(v), vt, vh, floats[(v if k is None else k).dtype])
+    return k, v
