@@ -733,6 +733,36 @@ kd_status kd_cache_read_4bit(const kd_cache4* cache, const kd_sequences* seqs, i
                              int64_t k_token, int64_t k_head, void* v, int64_t v_token, int64_t v_head,
                              kd_dtype dtype, void* stream);
 
+/* Bytes of device workspace that kd_attention_4bit needs for such a call (0 where none is, or
+ * where the call is refused).  Host only. */
+size_t kd_attention_4bit_workspace(const kd_cache4* cache, const kd_sequences* seqs, int64_t heads, int64_t window);
+
+/* Attention of the sequences' rows over the cache:
+ *   out[t][h] = sum_p w_p value[p],  w = softmax over p of scale * <q[t][h], key[p]>,
+ * with the keys and values of head h / (heads / cache heads), p over the row's sequence: with
+ * `causal` the positions up to the row's own, of which with window > 0 the last `window`; else all
+ * lengths[s] of them.
+ *   q, out   dtype KD_F16 or KD_BF16, head h of row t at q + t*q_token + h*q_head; `tokens` rows.
+ *   heads    a multiple of the cache's.
+ *   lse      optional, fp32 tokens x heads: ln sum_p exp(scale <q, key[p]>).
+ * A row that sees nothing: out 0, lse -infinity.  What a row does not see does not touch it,
+ * whatever is there.  A bad page that a row sees makes it NaN, and so do NaN there and in q.
+ * Meant for few rows of a sequence (decoding, drafted tokens): 16 rows times heads for each cache head
+ * share a pass over its codes, more take more passes.  Scores are exact products summed in fp32;
+ * the weights are rounded to fp16 as factors of a value's distance from the middle of its group, their
+ * sums are fp32; the whole is rounded once.  The order of all sums is fixed by the sizes and lengths
+ * (deterministic results).
+ *   workspace  device, 16-byte aligned, ws_bytes >= kd_attention_4bit_workspace(...); it must not
+ *              be shared by calls in flight on different streams.
+ * Errors: KD_ERR_INVALID_ARG (cache, sequences, heads, type, window < 0 or without causal, scale
+ * not finite, strides below 0, overlapping rows of out, missing or unaligned pointers, more than
+ * 2^31 - 1 blocks of work), KD_ERR_UNSUPPORTED_N (d), KD_ERR_WORKSPACE, KD_ERR_CUDA.  Nothing to
+ * do enqueues nothing. */
+kd_status kd_attention_4bit(const kd_cache4* cache, const kd_sequences* seqs, int64_t tokens, int64_t heads,
+                            const void* q, int64_t q_token, int64_t q_head, kd_dtype dtype, void* out,
+                            int64_t out_token, int64_t out_head, float* lse, float scale, int causal, int64_t window,
+                            void* workspace, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

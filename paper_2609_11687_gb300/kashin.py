@@ -19,7 +19,7 @@ Two layers:
   ``rmsnorm`` (residual addition, 8-bit output), ``quantise_4bit`` / ``dequantise_4bit`` /
   ``matmul_4bit`` (4-bit weights with group scales) and ``token_logprobs``; and those of an
   attention step, ``rope`` (head norms and rotary positions), ``cache_write_4bit`` and
-  ``cache_read_4bit`` (a paged cache of 4-bit keys and values).
+  ``cache_read_4bit`` (a paged cache of 4-bit keys and values) and ``attention_4bit`` over it.
 
 A wrapper's ``stream`` (the current one without it) is where its work goes and whose memory its
 own outputs and scratch are.  As with any work on a second stream the caller has the inputs
@@ -53,7 +53,8 @@ EXPORTS = ("kd_status_string", "kd_version", "kd_supported", "kd_tuned", "kd_wor
            "kd_rht_block", "kd_rht", "kd_dequantise", "kd_dequantise_batch", "kd_measure_fp32_peak",
            "kd_workspace_size_batch", "kd_decompose_batch", "kd_reconstruct_batch",
            "kd_rmsnorm", "kd_quantise_4bit", "kd_dequantise_4bit", "kd_matmul_4bit", "kd_token_logprobs",
-           "kd_rope_turns", "kd_rope", "kd_cache_write_4bit", "kd_cache_read_4bit")
+           "kd_rope_turns", "kd_rope", "kd_cache_write_4bit", "kd_cache_read_4bit",
+           "kd_attention_4bit_workspace", "kd_attention_4bit")
 KD_MAX_BATCH = 32
 KD_MAX_TOP = 32
 
@@ -222,6 +223,11 @@ def _load() -> ctypes.CDLL:
     lib.kd_cache_write_4bit.restype = c_int
     lib.kd_cache_read_4bit.argtypes = lib.kd_cache_write_4bit.argtypes
     lib.kd_cache_read_4bit.restype = c_int
+    lib.kd_attention_4bit_workspace.argtypes = [c_vp, c_vp, c_i64, c_i64]
+    lib.kd_attention_4bit_workspace.restype = c_sz
+    lib.kd_attention_4bit.argtypes = [c_vp, c_vp, c_i64, c_i64, c_vp, c_i64, c_i64, c_int, c_vp, c_i64, c_i64, c_vp,
+                                      ctypes.c_float, c_int, c_i64, c_vp, c_sz, c_vp]
+    lib.kd_attention_4bit.restype = c_int
     return lib
 
 
@@ -393,6 +399,16 @@ def kd_cache_write_4bit(cache, seqs, tokens, k, k_token, k_head, v, v_token, v_h
 
 def kd_cache_read_4bit(cache, seqs, tokens, k, k_token, k_head, v, v_token, v_head, dtype, stream) -> int:
     return lib.kd_cache_read_4bit(cache, seqs, tokens, k, k_token, k_head, v, v_token, v_head, dtype, stream)
+
+
+def kd_attention_4bit_workspace(cache, seqs, heads, window) -> int:
+    return int(lib.kd_attention_4bit_workspace(cache, seqs, heads, window))
+
+
+def kd_attention_4bit(cache, seqs, tokens, heads, q, q_token, q_head, dtype, out, out_token, out_head, lse, scale, causal,
+                      window, workspace, ws_bytes, stream) -> int:
+    return lib.kd_attention_4bit(cache, seqs, tokens, heads, q, q_token, q_head, dtype, out, out_token, out_head, lse,
+                                 scale, causal, window, workspace, ws_bytes, stream)
 
 
 # ---------------------------------------------------------------------------
@@ -1482,3 +1498,48 @@ def cache_read_4bit(cache: Cache4, seqs: Sequences, tokens: Optional[int] = None
     _call("kd_cache_read_4bit", lib.kd_cache_read_4bit, cache.index, stream, cache.ref, seqs.ref, tokens, _ptr(k), kt, kh,
           _ptr(v), vt, vh, floats[(v if k is None else k).dtype])
     return k, v
+
+
+def attention_4bit(cache: Cache4, q, seqs: Sequences, scale: Optional[float] = None, causal: bool = True, window: int = 0,
+                   out=None, lse=None, workspace=None, stream=None):
+    """Attention of the rows ``q`` (tokens, heads, d; fp16 or bf16), the sequences' last tokens,
+    over the cache (kd_attention_4bit); returns ``out``, of q's shape and type.
+
+    ``scale``: of the scores, d^-0.5 without it; ``causal``: a row sees the positions up to its
+    own, with ``window`` > 0 the last ``window`` of them, else its whole sequence; ``lse``: fp32
+    (tokens, heads), where the logarithm of the scores' sums goes; ``workspace``: a uint8 tensor of
+    at least ``attention_4bit_workspace`` bytes, for calls on one stream only (one is taken from
+    the stream's pool without it)."""
+    _, rows4, f32, e4m3, _, _ = _serve()
+    index, dt = cache.index, q.dtype
+    if dt == e4m3:
+        raise ValueError(f"q has dtype {dt}: torch.float16 or torch.bfloat16 is wanted")
+    qt, qh = _ld3(q, "q", rows4, index)
+    tokens, heads, d = q.shape
+    if d != cache.d or heads % cache.heads or not heads:
+        raise ValueError(f"q must have {cache.d} channels and a multiple of {cache.heads} heads")
+    if seqs.index != index:
+        raise ValueError("the sequences must be on the cache's device")
+    if out is None:
+        out = _new(stream, q.shape, dt, q.device)
+    ot, oh = _ld3(out, "out", (dt,), index, q.shape)
+    _row_strides(out, "out")
+    if lse is not None and (lse.dtype != f32 or lse.shape != q.shape[:2] or lse.get_device() != index or not lse.is_contiguous()):
+        raise ValueError(f"lse must be a contiguous torch.float32 {(tokens, heads)} tensor on the cache's device")
+    if window < 0 or (window and not causal):
+        raise ValueError("window must not be negative, and wants causal")
+    nbytes = lib.kd_attention_4bit_workspace(cache.ref, seqs.ref, heads, window)
+    if workspace is None:
+        if nbytes:
+            workspace = _new(stream, (nbytes,), _torch().uint8, q.device)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous, on the cache's device")
+    _call("kd_attention_4bit", lib.kd_attention_4bit, index, stream, cache.ref, seqs.ref, tokens, heads, q.data_ptr(), qt, qh,
+          rows4[dt], out.data_ptr(), ot, oh, _ptr(lse), d ** -0.5 if scale is None else scale, 1 if causal else 0, window,
+          _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
+    return out
+
+
+def attention_4bit_workspace(cache: Cache4, seqs: Sequences, heads: int, window: int = 0) -> int:
+    """Bytes of workspace that attention_4bit takes for rows of ``heads`` heads."""
+    return kd_attention_4bit_workspace(cache.ref, seqs.ref, heads, window)

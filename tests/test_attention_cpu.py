@@ -234,3 +234,38 @@ def test_cache_handles_refuse(kd):
     for bad in ((t[0], n), (t, n[:1]), (t, n.long()), (t.t().contiguous().t(), n), (t, n, n), (t, n, torch.zeros(3)), (t, n)):
         with pytest.raises(ValueError):
             kd.Sequences(*bad)
+
+
+def _attend(kd, cache={}, seqs={}, **more):
+    a = dict(tokens=2, heads=4, q=A, q_token=256, q_head=64, dtype=kd.KD_F16, out=A, out_token=256, out_head=64, lse=A, scale=0.125,
+             causal=1, window=0, workspace=A, ws_bytes=2 ** 40)
+    a.update(more)
+    c, s = _cache(kd, **cache), _sequences(kd, **seqs)
+    return kd.kd_attention_4bit(ctypes.addressof(c), ctypes.addressof(s), *a.values(), None)
+
+
+@pytest.mark.parametrize("bad", [dict(cache=b) for b in BAD_CACHE] + [dict(seqs=b) for b in BAD_SEQUENCES] + [
+    dict(tokens=-1), dict(tokens=2 ** 31), dict(heads=0), dict(heads=3), dict(heads=-2), dict(heads=2 ** 31), dict(dtype=0), dict(dtype=3),
+    dict(q=NULL), dict(out=NULL), dict(q=A + 1), dict(out=A + 1), dict(lse=A + 2), dict(q_token=-1), dict(q_head=-1), dict(out_token=-1),
+    dict(out_head=63), dict(out_token=255), dict(out_head=0), dict(scale=math.inf), dict(scale=math.nan), dict(window=-1),
+    dict(window=5, causal=0), dict(window=2 ** 31), dict(seqs=dict(most=2 ** 31 - 1)), dict(seqs=dict(seqs=2 ** 30, most=64))])
+def test_attention_refusals(kd, bad):
+    assert _attend(kd, **bad) == kd.KD_ERR_INVALID_ARG
+
+
+def test_attention_calls(kd):
+    for d in (0, 257):
+        assert _attend(kd, cache=dict(d=d)) == kd.KD_ERR_UNSUPPORTED_N
+    long = dict(longest=10 ** 6, wide=10 ** 6, ld_table=10 ** 6)
+    c, s = _cache(kd), _sequences(kd, **long)
+    size = kd.kd_attention_4bit_workspace(ctypes.addressof(c), ctypes.addressof(s), 4, 0)
+    assert size > 0 and size % 16 == 0
+    assert _attend(kd, seqs=long, workspace=NULL) == kd.KD_ERR_WORKSPACE
+    assert _attend(kd, seqs=long, ws_bytes=size - 1) == kd.KD_ERR_WORKSPACE
+    assert _attend(kd, seqs=long, workspace=A + 8) == kd.KD_ERR_WORKSPACE
+    assert kd.kd_attention_4bit_workspace(ctypes.addressof(c), ctypes.addressof(s), 3, 0) == 0
+    assert kd.kd_attention_4bit_workspace(None, None, 4, 0) == 0
+    none = dict(q=NULL, out=NULL, lse=NULL, workspace=NULL)
+    assert _attend(kd, tokens=0, **none) == kd.KD_OK
+    assert _attend(kd, seqs=dict(seqs=0, table=NULL, lengths=NULL), **none) == kd.KD_OK
+    assert _attend(kd, seqs=dict(most=0), **none) == kd.KD_OK
