@@ -46,7 +46,9 @@ namespace attn4 {
 using namespace cache4;
 
 constexpr int kWarps = 8;
-constexpr int kTile = 16;     // positions of one step of a warp
+constexpr int kTile = 16;     // positions of a tensor-core tile, all on one page
+constexpr int kTiles = 2;     // of one step of a warp
+constexpr int kChunk = kTiles * kWarps;  // tiles of one step of a CTA: what work is shared out in
 constexpr int kBatch = 256;   // tiles whose places are looked up at a time
 
 struct Params {
@@ -57,12 +59,21 @@ struct Params {
   int64_t q_token, q_head, out_token, out_head;
   int64_t tokens;
   int heads, shared;            // query heads; of one key head
-  int row_blocks, splits, per;  // of a sequence: blocks of rows; shares of positions, of at least `per` tiles
+  int row_blocks;               // of a sequence: blocks of rows
+  int whole;                    // a CTA has an item (sequence, key head, block of rows) to itself; else all CTAs equal shares
   int causal, window;
   int bf16, q_vec;
   float scale2;                 // scale log2 e
-  float* part;                  // partial sums [sequence][key head][row block][split][row][d], then (m, sum) pairs
-  float2* part_ml;
+  struct Cut* cuts;             // the item that each CTA leaves to the next ones
+  float2* part_ml;              // (m, sum) of each row of a CTA's first item and of its last, where they are cut
+  float* part;                  // and their sums [CTA][first, last][row][d]
+};
+
+// An item whose first chunks are the end of a CTA's share: the sums of its rows are in `slot` and in the first
+// places of the `more` CTAs that follow.
+struct Cut {
+  int64_t first;  // row of the sequence's first query token
+  int block, head, rows, slot, more, unused;
 };
 
 // The rows and positions of a block of rows: the same for the kernel that sums and the one that joins.
@@ -73,7 +84,7 @@ struct Work {
   int lo, hi;          // positions that some row sees
   int all_lo, all_hi;  // positions that every row sees
   int tile, tiles;     // of the positions lo .. hi
-  int per, splits;     // tiles of a share, shares that have any (at least one)
+  int chunks;          // of kChunk tiles; one for rows that see nothing, none for no rows
 };
 __device__ __forceinline__ int clamp_to(int64_t v, int most) { return (int)(v < 0 ? 0 : v > most ? most : v); }
 __device__ __forceinline__ Work work_of(const Params& p, int s, int block, int of_block) {
@@ -104,8 +115,7 @@ __device__ __forceinline__ Work work_of(const Params& p, int s, int block, int o
   w.hi = (int)min((int64_t)w.hi, (int64_t)p.c.wide * p.c.page);
   w.tile = w.lo / kTile;
   w.tiles = w.hi > w.lo ? (w.hi + kTile - 1) / kTile - w.tile : 0;
-  w.per = max(p.per, (w.tiles + p.splits - 1) / p.splits);  // lengths past the host's hint: longer shares
-  w.splits = w.tiles > w.per ? (w.tiles + w.per - 1) / w.per : 1;
+  w.chunks = w.rows == 0 ? 0 : max((w.tiles + kChunk - 1) / kChunk, 1);
   return w;
 }
 
@@ -130,6 +140,14 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// the same with sums that start from c0, c1 in every row
+__device__ __forceinline__ void mma_from(float (&d)[4], float c0, float c1, uint32_t a0, uint32_t a1, uint32_t a2,
+                                         uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%10, %11, %10, %11};\n"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+}
 // an 8 x 8 matrix of halves, a row to four lanes, turned
 __device__ __forceinline__ uint32_t turned(uint32_t v) {
   uint32_t r;
@@ -151,20 +169,23 @@ __device__ __forceinline__ float high_half(uint32_t w) { return __half2float(__u
 
 constexpr float kNone = -__builtin_inff();
 
-// NC: 32-channel pieces of a row (the next of 1, 2, 3, 4, 6, 8); GS: of a group; NT: blocks of eight rows
+// NC: 32-channel pieces of a row; GS: of a group; NT: blocks of eight rows
 template <int NC, int GS, int NT>
 struct Shape {
   static constexpr int kGroups = (NC + GS - 1) / GS;
   static constexpr int kRows = 8 * NT;
-  static constexpr int kStages = NC <= 4 ? 4 : 3;
+  static constexpr int kStages = NC <= 4 ? 2 : 2;
   static constexpr int kStride = 4 * (NC | 1);                       // words of a row of codes in the ring
-  static constexpr int kCodes = kTile * kStride, kScales = kTile * kGroups;  // words of a stage, keys or values
+  // words of a stage, keys or values
+  static constexpr int kCodes = kTiles * kTile * kStride, kScales = kTiles * kTile * kGroups;
   static constexpr int kStage = 2 * (kCodes + kScales);
   // a value's 64 channels at a time (four tiles of 16), or 32 (two) where those have one scale
   static constexpr int kUnits = GS == 1 ? NC : (NC + 1) / 2, kOfUnit = GS == 1 ? 2 : 4;
   static constexpr int kSums = 32 * NC + 4;                          // floats of a row of a warp's sums
+  static constexpr int kQueries = 64 * NC + 64;                      // bytes of a row of queries as operands
   static constexpr size_t kRing = (size_t)kWarps * kStages * kStage * 4, kJoin = (size_t)kWarps * kRows * kSums * 4;
-  static constexpr size_t kBytes = (kRing > kJoin ? kRing : kJoin) + kBatch * 8 + (size_t)kWarps * kRows * 8;
+  static constexpr size_t kBytes = (kRing > kJoin ? kRing : kJoin) + kBatch * 16 + (size_t)kWarps * kRows * 8 +
+                                    kRows * (kQueries + 4 * (kGroups + 1)) + 64;
 };
 
 // fp16 or bf16 bits as a float
@@ -175,105 +196,196 @@ __device__ __forceinline__ uint16_t narrow(const Params& p, float v) {
   return p.bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v)) : __half_as_ushort(__float2half_rn(v));
 }
 
+// The block's exclusive sum of v over its threads, and the total; scratch: kWarps words of shared memory.
+__device__ __forceinline__ int sum_before(int v, int* scratch, int& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int in = v;
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) {
+    const int up = __shfl_up_sync(~0u, in, o);
+    if (lane >= o) in += up;
+  }
+  if (lane == 31) scratch[warp] = in;
+  __syncthreads();
+  int before = in - v;
+  total = 0;
+#pragma unroll
+  for (int k = 0; k < kWarps; ++k) {
+    if (k < warp) before += scratch[k];
+    total += scratch[k];
+  }
+  __syncthreads();
+  return before;
+}
+
 template <int NC, int GS, int NT>
 __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4_kernel(const __grid_constant__ Params p) {
   using Z = Shape<NC, GS, NT>;
   constexpr int GN = Z::kGroups, ST = Z::kStages, S = Z::kStride;
   extern __shared__ uint4 smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g8 = lane >> 2, t4 = lane & 3;
-  int64_t* place = reinterpret_cast<int64_t*>(reinterpret_cast<char*>(smem) + (Z::kRing > Z::kJoin ? Z::kRing : Z::kJoin));
+  // shared memory: the ring, where sums are joined too; places; (m, sum) of the warps' rows; queries, their
+  // groups' sums and powers of two; a few words
+  char* after = reinterpret_cast<char*>(smem) + (Z::kRing > Z::kJoin ? Z::kRing : Z::kJoin);
+  longlong2* place = reinterpret_cast<longlong2*>(after);
   float2* ml = reinterpret_cast<float2*>(place + kBatch);
+  char* queries = reinterpret_cast<char*>(ml + kWarps * Z::kRows);
+  float* query_sums = reinterpret_cast<float*>(queries + Z::kRows * Z::kQueries);
+  int* words = reinterpret_cast<int*>(query_sums + Z::kRows * (GN + 1));
   depend_on_last();
 
-  int at = blockIdx.x;
-  const int block = at % p.row_blocks;
-  at /= p.row_blocks;
-  const int split = at % p.splits;
-  at /= p.splits;
-  const int head = at % p.c.heads, s = at / p.c.heads;
-  const Work w = work_of(p, s, block, Z::kRows);
-  if (w.rows == 0 || split >= w.splits) return;
-  const int first_tile = w.tile + split * w.per, tiles = min(w.per, w.tiles - split * w.per);
+  // This CTA's share: `left` chunks from chunk `chunk` of item (s, head, block) on.
+  int s, head, block, chunk = 0, left;
+  if (p.whole) {
+    int at = blockIdx.x;
+    block = at % p.row_blocks;
+    at /= p.row_blocks;
+    head = at % p.c.heads;
+    s = at / p.c.heads;
+    left = INT32_MAX;
+  } else {
+    const int each = (p.c.seqs + 32 * kWarps - 1) / (32 * kWarps), s0 = threadIdx.x * each, s1 = min(s0 + each, p.c.seqs);
+    auto of_head = [&](int s) {
+      int n = 0;
+      for (int b = 0; b < p.row_blocks; ++b) {
+        const int of = work_of(p, s, b, Z::kRows).chunks;
+        if (of == 0) break;  // no rows from here on
+        n += of;
+      }
+      return n;
+    };
+    int mine = 0, total;
+    for (int i = s0; i < s1; ++i) mine += of_head(i);
+    mine *= p.c.heads;
+    int before = sum_before(mine, words, total);
+    const int per = (int)(((int64_t)total + gridDim.x - 1) / gridDim.x);
+    const int64_t from = (int64_t)blockIdx.x * per;
+    left = (int)min((int64_t)per, total - from);
+    if (threadIdx.x == 0) p.cuts[blockIdx.x].more = 0;
+    if (left <= 0) return;
+    if (from >= before && from < (int64_t)before + mine) {
+      int i = s0, of = of_head(i);
+      while (from >= (int64_t)before + of * p.c.heads) {
+        before += of * p.c.heads;
+        of = of_head(++i);
+      }
+      int in = (int)(from - before), b = 0;
+      const int h = in / of;
+      in -= h * of;
+      for (int n; in >= (n = work_of(p, i, b, Z::kRows).chunks); ++b) in -= n;
+      words[8] = i;
+      words[9] = h;
+      words[10] = b;
+      words[11] = in;
+    }
+    __syncthreads();
+    s = words[8];
+    head = words[9];
+    block = words[10];
+    chunk = words[11];
+  }
+  const int share = left;
+  constexpr int row_bytes = 16 * NC, scale_bytes = 4 * GN;
+  // the ring: this lane's pieces of a tile
+  uint32_t* ring = reinterpret_cast<uint32_t*>(smem) + warp * ST * Z::kStage;
+  const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+  constexpr int pieces = kTile * NC;  // 16-byte pieces of a tile's keys
+  uint32_t to[(NC + 1) / 2];
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(to) / 4); ++i) {
+    const int n = lane + 32 * i, row = n / NC;
+    to[i] = (uint32_t)(row * S * 4 + (n - row * NC) * 16);
+  }
 
-  // Where a batch's tiles lie: the first row's number for this head, -1 on a bad page.
+  for (;;) {
+  const Work w = work_of(p, s, block, Z::kRows);
+  const int n_chunks = min(w.chunks - chunk, left);
+  if (n_chunks > 0) {
+  const bool cut = n_chunks < w.chunks;  // only a part of the item
+  const int first_tile = w.tile + chunk * kChunk, tiles = min(n_chunks * kChunk, w.tiles - chunk * kChunk);
+  const int share_hi = min(w.hi, (first_tile + tiles) * kTile);  // where the part's positions end
+
+  // Where a batch's tiles lie, in bytes of codes and scales from the cache's first row: -1 on a bad page.
   auto look_up = [&](int b0, int n) {
     for (int i = threadIdx.x; i < n; i += 32 * kWarps) {
-      const int64_t row = row_of(p.c, s, (int64_t)(first_tile + b0 + i) * kTile);
-      place[i] = row < 0 ? -1 : row + (int64_t)head * p.c.page;
+      const int64_t first = row_of(p.c, s, (int64_t)(first_tile + b0 + i) * kTile), row = first + (int64_t)head * p.c.page;
+      place[i] = first < 0 ? make_longlong2(-1, 0) : make_longlong2(row * row_bytes, row * scale_bytes);
     }
   };
   look_up(0, min(tiles, kBatch));
 
-  // The rows: this lane has row 8 nt + g8 and of each piece the eight channels of word t4.
+  // The rows as operands, a warp a row: fp16 in eights of channels 0 4 1 5 2 6 3 7, the odd ones over 16, with
+  // the row's power of two and its sums over groups.
   const int r0 = block * Z::kRows;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = 8 * nt + warp, token = (r0 + r) / p.shared;
+    const int64_t t = w.first + token;
+    const bool live = r < w.rows && t >= 0 && t < p.tokens;
+    const uint16_t* q = p.q + (live ? t * p.q_token + (int64_t)(head * p.shared + (r0 + r) - token * p.shared) * p.q_head : 0);
+    // lane l has channels 8 l .. 8 l + 7 (of 256)
+    uint32_t raw[4] = {0, 0, 0, 0};
+    if (live && 8 * lane < p.c.d) {
+      if (p.q_vec) {
+        const uint4 u = *reinterpret_cast<const uint4*>(q + 8 * lane);
+        raw[0] = u.x; raw[1] = u.y; raw[2] = u.z; raw[3] = u.w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (8 * lane + e < p.c.d) raw[e / 2] |= (uint32_t)q[8 * lane + e] << (16 * (e % 2));
+      }
+    }
+    float v[8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = wide(p, raw[e / 2] >> (16 * (e % 2)) & 0xFFFFu);
+      top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+    }
+    top = __reduce_max_sync(~0u, top);
+    // 2^e <= max |q| < 2^(e + 1); an infinity or NaN stays what it is under any factor
+    const int e2 = top >> 23 == 255 || top == 0 ? 0 : max((int)(top >> 23) - 127, -100);
+    const float up = __uint_as_float((uint32_t)(14 - e2 + 127) << 23);
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] *= up;
+      sum += v[e];
+      if (e % 2) v[e] *= 0.0625f;
+    }
+    if (lane < 4 * NC)
+      *reinterpret_cast<uint4*>(queries + r * Z::kQueries + 16 * lane) =
+          make_uint4(pack2<KD_F16>(v[0], v[4]), pack2<KD_F16>(v[1], v[5]), pack2<KD_F16>(v[2], v[6]), pack2<KD_F16>(v[3], v[7]));
+    // four lanes a piece of 32 channels
+#pragma unroll
+    for (int o = 1; o < 4 * GS && o < 32; o *= 2) sum += __shfl_xor_sync(~0u, sum, o);
+    if (lane % (4 * GS) == 0 && lane / (4 * GS) < GN) query_sums[r * (GN + 1) + lane / (4 * GS)] = sum * 0x1p-14f;
+    if (lane == 0) query_sums[r * (GN + 1) + GN] = __uint_as_float((uint32_t)(e2 + 127) << 23) * p.scale2;
+  }
+  __syncthreads();
   uint32_t qb[2 * NC][NT][2];
   // of columns 2 t4, 2 t4 + 1: power of two of the row, and its sums over groups, both times scale log2 e
   float qs[GN][NT][2], qe[NT][2], q8[GN][NT][2];  // q8: where the sums over a group's codes start
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int r = 8 * nt + g8, token = (r0 + r) / p.shared;
-    const int64_t t = w.first + token;
-    const bool live = r < w.rows && t >= 0 && t < p.tokens;
-    const uint16_t* q = p.q + (live ? t * p.q_token + (int64_t)(head * p.shared + (r0 + r) - token * p.shared) * p.q_head : 0);
-    uint32_t raw[NC][4];  // pairs of channels
-    uint32_t top = 0;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      const int ch = 32 * c + 8 * t4;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) raw[c][e] = 0;
-      if (live) {
-        if (p.q_vec) {
-          if (ch < p.c.d) {
-            const uint4 u = *reinterpret_cast<const uint4*>(q + ch);
-            raw[c][0] = u.x; raw[c][1] = u.y; raw[c][2] = u.z; raw[c][3] = u.w;
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (ch + e < p.c.d) raw[c][e / 2] |= (uint32_t)q[ch + e] << (16 * (e % 2));
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        top = max(top, __float_as_uint(wide(p, raw[c][e / 2] >> (16 * (e % 2)) & 0xFFFFu)) & 0x7FFFFFFFu);
+      const uint4 u = *reinterpret_cast<const uint4*>(queries + (8 * nt + g8) * Z::kQueries + 16 * (4 * c + t4));
+      qb[2 * c][nt][0] = u.x;
+      qb[2 * c][nt][1] = u.y;
+      qb[2 * c + 1][nt][0] = u.z;
+      qb[2 * c + 1][nt][1] = u.w;
     }
-    top = max(top, __shfl_xor_sync(~0u, top, 1));
-    top = max(top, __shfl_xor_sync(~0u, top, 2));
-    // 2^e <= max |q| < 2^(e + 1); an infinity or NaN stays what it is under any factor
-    const int e2 = top >> 23 == 255 || top == 0 ? 0 : max((int)(top >> 23) - 127, -100);
-    const float up = __uint_as_float((uint32_t)(14 - e2 + 127) << 23);
-    float sum[GN];
 #pragma unroll
-    for (int g = 0; g < GN; ++g) sum[g] = 0.f;
+    for (int j = 0; j < 2; ++j) {
+      const float* of_column = query_sums + (8 * nt + 2 * t4 + j) * (GN + 1);
+      const float down = of_column[GN];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      float v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v[e] = wide(p, raw[c][e / 2] >> (16 * (e % 2)) & 0xFFFFu);
-        v[e] *= up;
-        sum[c / GS] += v[e];
-        if (e % 2) v[e] *= 0.0625f;
+      for (int g = 0; g < GN; ++g) {
+        qs[g][nt][j] = of_column[g] * down;
+        q8[g][nt][j] = of_column[g] * -0x1p-7f;  // 8 times 2^14 / 2^24
       }
-      qb[2 * c][nt][0] = pack2<KD_F16>(v[0], v[4]);
-      qb[2 * c][nt][1] = pack2<KD_F16>(v[1], v[5]);
-      qb[2 * c + 1][nt][0] = pack2<KD_F16>(v[2], v[6]);
-      qb[2 * c + 1][nt][1] = pack2<KD_F16>(v[3], v[7]);
-    }
-    const float down = __uint_as_float((uint32_t)(e2 + 127) << 23) * p.scale2;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) qe[nt][j] = __shfl_sync(~0u, down, 4 * (2 * t4 + j));
-#pragma unroll
-    for (int g = 0; g < GN; ++g) {
-      sum[g] += __shfl_xor_sync(~0u, sum[g], 1);
-      sum[g] += __shfl_xor_sync(~0u, sum[g], 2);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float of_column = __shfl_sync(~0u, sum[g] * 0x1p-14f, 4 * (2 * t4 + j));
-        qs[g][nt][j] = of_column * qe[nt][j];
-        q8[g][nt][j] = of_column * -0x1p-7f;  // 8 times 2^14 / 2^24
-      }
+      qe[nt][j] = down * 1024.f;  // codes' 2^24 less q's 2^14
     }
   }
   // what the columns' rows see: positions from sees_lo on, below sees_hi
@@ -284,41 +396,37 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
     for (int j = 0; j < 2; ++j) {
       const int r = 8 * nt + 2 * t4 + j;
       const int64_t pos = w.before + (r0 + r) / p.shared;
-      sees_hi[nt][j] = r >= w.rows ? 0 : p.causal ? clamp_to(pos + 1, w.length) : w.length;
+      sees_hi[nt][j] = r >= w.rows ? 0 : min(share_hi, p.causal ? clamp_to(pos + 1, w.length) : w.length);
       sees_lo[nt][j] = p.window ? clamp_to(pos + 1 - p.window, w.length) : 0;
     }
 
-  // the ring: this lane's pieces of a stage
-  uint32_t* ring = reinterpret_cast<uint32_t*>(smem) + warp * ST * Z::kStage;
-  const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
-  const int pieces = kTile * p.c.chunks;  // 16-byte pieces of a tile's keys
-  uint32_t to[(NC + 1) / 2];
+  const char* src[4] = {reinterpret_cast<const char*>(p.c.codes[0]) + lane * 16, reinterpret_cast<const char*>(p.c.codes[1]) + lane * 16,
+                        reinterpret_cast<const char*>(p.c.scales[0]) + lane * 16, reinterpret_cast<const char*>(p.c.scales[1]) + lane * 16};
+  auto issue = [&](int first, int n, int stage) {  // tiles first, first + 1 of the batch's n
 #pragma unroll
-  for (int i = 0; i < (int)(sizeof(to) / 4); ++i) {
-    const int n = lane + 32 * i, row = n / p.c.chunks;
-    to[i] = (uint32_t)(row * S * 4 + (n - row * p.c.chunks) * 16);
-  }
-  const int row_bytes = 16 * p.c.chunks, scale_bytes = 4 * p.c.groups;
-  auto issue = [&](int i, int stage) {
-    const int64_t row = max(place[i], (int64_t)0);
-    const uint32_t base = ring_at + stage * (Z::kStage * 4);
-    const char* k = reinterpret_cast<const char*>(p.c.codes[0]) + row * row_bytes + lane * 16;
-    const char* v = reinterpret_cast<const char*>(p.c.codes[1]) + row * row_bytes + lane * 16;
+    for (int i = 0; i < kTiles; ++i) {
+      if (first + i >= n) break;
+      const longlong2 from = place[first + i];
+      const int64_t code = max((int64_t)from.x, (int64_t)0), scale = from.y;
+      const uint32_t codes = ring_at + stage * (Z::kStage * 4) + i * kTile * S * 4;
 #pragma unroll
-    for (int n = 0; n < (int)(sizeof(to) / 4); ++n)
-      if (lane + 32 * n < pieces) {
-        copy16(base + to[n], k + 512 * n);
-        copy16(base + Z::kCodes * 4 + to[n], v + 512 * n);
+      for (int k = 0; k < (int)(sizeof(to) / 4); ++k)
+        if (lane + 32 * k < pieces) {
+          copy16(codes + to[k], src[0] + code + 512 * k);
+          copy16(codes + Z::kCodes * 4 + to[k], src[1] + code + 512 * k);
+        }
+      if (lane < 4 * GN) {
+        const uint32_t scales = ring_at + stage * (Z::kStage * 4) + 2 * Z::kCodes * 4 + i * kTile * scale_bytes + lane * 16;
+        copy16(scales, src[2] + scale);
+        copy16(scales + Z::kScales * 4, src[3] + scale);
       }
-    if (lane < 4 * p.c.groups) {
-      copy16(base + 2 * Z::kCodes * 4 + lane * 16, reinterpret_cast<const char*>(p.c.scales[0]) + row * scale_bytes + lane * 16);
-      copy16(base + (2 * Z::kCodes + Z::kScales) * 4 + lane * 16,
-             reinterpret_cast<const char*>(p.c.scales[1]) + row * scale_bytes + lane * 16);
     }
   };
 
   float acc[Z::kUnits * Z::kOfUnit][NT][4];
-  float mids[GN][NT][2], m[NT][2], sum[NT][2];
+  // of the columns: sums of weights times middles and of weights, m (0 before the first), and how far above it
+  // a score may lie (nothing may, before the first)
+  float mids[GN][NT][2], sum[NT][2], m[NT][2], room[NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -327,97 +435,107 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
       for (int e = 0; e < 4; ++e) acc[i][nt][e] = 0.f;
 #pragma unroll
     for (int g = 0; g < GN; ++g) mids[g][nt][0] = mids[g][nt][1] = 0.f;
-    m[nt][0] = m[nt][1] = kNone;
+    m[nt][0] = m[nt][1] = 0.f;
+    room[nt][0] = room[nt][1] = kNone;
     sum[nt][0] = sum[nt][1] = 0.f;
   }
-  uint32_t step_cap = 0;  // fp16 bits: no step so far lies above
-  float step_up = 1.f;    // the power of two of the values' weights: step_cap becomes 2^5 .. 2^6
+  float step_cap = 0.f;  // no step so far lies above
+  float step_up = 1.f;   // the power of two of the values' weights: step_cap becomes 2^6
 
-  // One tile.  EDGE: some row does not see all of it, or its page is bad.
-  auto tile = [&](auto edge, const uint32_t* stage, int position, bool bad) {
+  // One step.  EDGE: some row does not see all of it, or a page is bad.
+  auto step = [&](auto edge, const uint32_t* stage, int position, bool bad0, bool bad1) {
     constexpr bool EDGE = decltype(edge)::value;
     const uint32_t* ks = stage;
     const uint32_t* vs = stage + Z::kCodes;
     const uint32_t* kp = stage + 2 * Z::kCodes;
     const uint32_t* vp = kp + Z::kScales;
-    float x[NT][4], part[NT][4];
+    float x[kTiles][NT][4];  // scores less m
+    bool seen[kTiles][NT][4];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int i = 0; i < kTiles; ++i) {
+      float part[NT][4], mid[NT][4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[nt][e] = 0.f;
-        part[nt][e] = q8[0][nt][e & 1];
-      }
-    float mid[NT][4];
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+        for (int e = 0; e < 4; ++e) {
+          x[i][nt][e] = 0.f;
+          mid[nt][e] = -m[nt][e & 1];
+        }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) mid[nt][e] = 0.f;
+      for (int c = 0; c < NC; ++c) {
+        uint32_t a = ks[(kTile * i + g8) * S + 4 * c + t4], b = ks[(kTile * i + g8 + 8) * S + 4 * c + t4];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      uint32_t a = ks[g8 * S + 4 * c + t4], b = ks[(g8 + 8) * S + 4 * c + t4];
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          mma(part[nt], a & 0x000F000Fu, b & 0x000F000Fu, a & 0x00F000F0u, b & 0x00F000F0u, qb[2 * c + h][nt][0], qb[2 * c + h][nt][1]);
-        a >>= 8;
-        b >>= 8;
-      }
-      if ((c + 1) % GS == 0 || c == NC - 1) {
-        // a piece past the row's last group meets q of 0: any group's scale will do
-        const int g = min(c / GS, p.c.groups - 1);
-        const uint32_t u = kp[g8 * p.c.groups + g], v = kp[(g8 + 8) * p.c.groups + g];
-        const float s0 = low_half(u), m0 = __fmaf_rn(8.f, s0, high_half(u));
-        const float s1 = low_half(v), m1 = __fmaf_rn(8.f, s1, high_half(v));
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x[nt][e] = __fmaf_rn(e < 2 ? s0 : s1, part[nt][e], x[nt][e]);
-            mid[nt][e] = __fmaf_rn(e < 2 ? m0 : m1, qs[c / GS][nt][e & 1], mid[nt][e]);
-            part[nt][e] = q8[c / GS + 1 < GN ? c / GS + 1 : 0][nt][e & 1];
+          for (int nt = 0; nt < NT; ++nt) {
+            const uint32_t a0 = a & 0x000F000Fu, a1 = b & 0x000F000Fu, a2 = a & 0x00F000F0u, a3 = b & 0x00F000F0u;
+            if (c % GS == 0 && h == 0)
+              mma_from(part[nt], q8[c / GS][nt][0], q8[c / GS][nt][1], a0, a1, a2, a3, qb[2 * c][nt][0], qb[2 * c][nt][1]);
+            else mma(part[nt], a0, a1, a2, a3, qb[2 * c + h][nt][0], qb[2 * c + h][nt][1]);
           }
-      }
-    }
-    bool seen[NT][4];
-    bool grow = false;
+          a >>= 8;
+          b >>= 8;
+        }
+        if ((c + 1) % GS == 0 || c == NC - 1) {
+          const uint32_t* at = kp + (kTile * i + g8) * GN + c / GS;
+          const uint32_t u = at[0], v = at[8 * GN];
+          const float s0 = low_half(u), m0 = __fmaf_rn(8.f, s0, high_half(u));
+          const float s1 = low_half(v), m1 = __fmaf_rn(8.f, s1, high_half(v));
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[nt][e] = __fmaf_rn(x[nt][e] * 1024.f, qe[nt][e & 1], mid[nt][e]);  // codes' 2^24 less q's 2^14
-        if constexpr (EDGE) {
-          const int pos = position + g8 + 8 * (e >> 1);
-          seen[nt][e] = pos < sees_hi[nt][e & 1] && pos >= sees_lo[nt][e & 1];
-          x[nt][e] = !seen[nt][e] ? kNone : bad ? __int_as_float(0x7FC00000) : x[nt][e];
+            for (int e = 0; e < 4; ++e) {
+              x[i][nt][e] = __fmaf_rn(e < 2 ? s0 : s1, part[nt][e], x[i][nt][e]);
+              mid[nt][e] = __fmaf_rn(e < 2 ? m0 : m1, qs[c / GS][nt][e & 1], mid[nt][e]);
+            }
         }
       }
 #pragma unroll
-      for (int j = 0; j < 2; ++j) grow |= fmaxf(x[nt][j], x[nt][j + 2]) > m[nt][j] + 8.f;
-    }
-    uint32_t vscale[GN][2];
-    uint32_t top = 0;
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int g = 0; g < GN; ++g)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        vscale[g][i] = vp[(g8 + 8 * i) * p.c.groups + min(g, p.c.groups - 1)];
-        uint32_t bits = vscale[g][i] & 0xFFFFu;
-        if constexpr (EDGE) {  // a position that no row sees may hold anything
-          const int pos = position + g8 + 8 * i;
-          if (pos >= w.hi || pos < w.lo) bits = 0;
+        for (int e = 0; e < 4; ++e) {
+          x[i][nt][e] = __fmaf_rn(x[i][nt][e], qe[nt][e & 1], mid[nt][e]);
+          if constexpr (EDGE) {
+            const int pos = position + kTile * i + g8 + 8 * (e >> 1);
+            seen[i][nt][e] = pos < sees_hi[nt][e & 1] && pos >= sees_lo[nt][e & 1];
+            x[i][nt][e] = !seen[i][nt][e] ? kNone : (i ? bad1 : bad0) ? __int_as_float(0x7FC00000) : x[i][nt][e];
+          }
         }
-        if (bits <= 0x7BFFu) top = max(top, bits);
+    }
+    uint32_t vscale[kTiles][GN][2];
+    __half2 tops = __half2half2(__ushort_as_half(0));  // the larger step, in the low half
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int g = 0; g < GN; ++g)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          uint32_t v = vp[(kTile * i + g8 + 8 * k) * GN + g];
+          if constexpr (EDGE) {  // a position that no row sees may hold anything
+            const int pos = position + kTile * i + g8 + 8 * k;
+            if (pos >= share_hi || pos < w.lo) v = 0;
+          }
+          vscale[i][g][k] = v;
+          tops = __hmax2(tops, *reinterpret_cast<const __half2*>(&v));
+        }
+    float top = __low2float(tops);
+    bool grow = top > step_cap;
+    float most[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        most[nt][j] = fmaxf(fmaxf(x[0][nt][j], x[0][nt][j + 2]), fmaxf(x[1][nt][j], x[1][nt][j + 2]));
+        grow |= most[nt][j] > room[nt][j];
       }
-    if (__any_sync(~0u, grow || top > step_cap)) {
+    if (__any_sync(~0u, grow)) {
       float by_step = 1.f;
-      top = __reduce_max_sync(~0u, top);
+      top = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top)));  // not negative: ordered as bits
       if (top > step_cap) {
-        // 2^e <= step < 2^(e + 1) at most e = top's exponent, for subnormal ones the lowest normal
-        const int e2 = max((int)(top >> 10) - 15, -14);
+        // 2^e <= top < 2^(e + 1); an infinite one leaves nothing finite in any case
+        const int e2 = min((int)(__float_as_uint(top) >> 23) - 127, 15);
         const float up = __uint_as_float((uint32_t)(5 - e2 + 127) << 23);
-        step_cap = min((uint32_t)(e2 + 15) << 10 | 0x3FFu, 0x7BFFu);
+        step_cap = top > 65504.f ? top : __uint_as_float((uint32_t)(e2 + 128) << 23);
         by_step = up / step_up;
         step_up = up;
       }
@@ -425,17 +543,25 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          float to = fmaxf(x[nt][j], x[nt][j + 2]);
+          float to = most[nt][j];
           to = fmaxf(to, __shfl_xor_sync(~0u, to, 4));
           to = fmaxf(to, __shfl_xor_sync(~0u, to, 8));
           to = fmaxf(to, __shfl_xor_sync(~0u, to, 16));
-          to = fmaxf(to, m[nt][j]);
-          const float f = m[nt][j] == kNone ? 0.f : exp2_of(m[nt][j] - to);
-          m[nt][j] = to;
+          const bool fresh = room[nt][j] == kNone;
+          if (!fresh) to = fmaxf(to, 0.f);
+          if (to == kNone) continue;  // nothing seen yet; the sums are 0
+          // m moves up by `to`; a first one by whatever it is
+          const float f = fresh ? 0.f : exp2_of(-to), fs = f * by_step;
+          m[nt][j] += to;
+          room[nt][j] = 8.f;
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i) {
+            x[i][nt][j] -= to;
+            x[i][nt][j + 2] -= to;
+          }
           sum[nt][j] *= f;
 #pragma unroll
           for (int g = 0; g < GN; ++g) mids[g][nt][j] *= f;
-          const float fs = f * by_step;
 #pragma unroll
           for (int i = 0; i < Z::kUnits * Z::kOfUnit; ++i) {
             acc[i][nt][j] *= fs;
@@ -443,61 +569,78 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
           }
         }
     }
-    float wt[NT][4];
+    // weights, and the operands of the values
+    uint32_t bw[kTiles][GN][NT][2];
+    float all[GN][NT][4];  // of each column, in every row: 2^-24 of the step's weights as they are rounded
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int i = 0; i < kTiles; ++i) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float top_of = m[nt][e & 1];
-        wt[nt][e] = exp2_of(x[nt][e] - (top_of == kNone ? 0.f : top_of));
-        sum[nt][e & 1] += wt[nt][e];
-      }
-    // the values
-    uint32_t bw[GN][NT][2];
-#pragma unroll
-    for (int g = 0; g < GN; ++g) {
-      float up[2], mid[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float step = low_half(vscale[g][i]);
-        mid[i] = __fmaf_rn(8.f, step, high_half(vscale[g][i]));
-        up[i] = step * step_up;
-      }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float b[4];
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          b[e] = wt[nt][e] * up[e >> 1];
-          float add = wt[nt][e] * mid[e >> 1];
-          if constexpr (EDGE) {  // whatever stands where a row does not see: 0
-            if (!seen[nt][e]) b[e] = add = 0.f;
-          }
-          mids[g][nt][e & 1] += add;
+          x[i][nt][e] = exp2_of(x[i][nt][e]);
+          sum[nt][e & 1] += x[i][nt][e];
         }
-        bw[g][nt][0] = turned(pack2<KD_F16>(b[0], b[1]));
-        bw[g][nt][1] = turned(pack2<KD_F16>(b[2], b[3]));
+#pragma unroll
+      for (int g = 0; g < GN; ++g) {
+        float up[2], mid[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const float step = low_half(vscale[i][g][k]);
+          mid[k] = __fmaf_rn(8.f, step, high_half(vscale[i][g][k]));
+          up[k] = step * step_up;
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float b[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            b[e] = x[i][nt][e] * up[e >> 1];
+            if constexpr (EDGE) {  // whatever stands where a row does not see: 0
+              if (!seen[i][nt][e]) b[e] = 0.f;
+              else mids[g][nt][e & 1] = __fmaf_rn(x[i][nt][e], mid[e >> 1], mids[g][nt][e & 1]);
+            } else {
+              mids[g][nt][e & 1] = __fmaf_rn(x[i][nt][e], mid[e >> 1], mids[g][nt][e & 1]);
+            }
+          }
+          bw[i][g][nt][0] = turned(pack2<KD_F16>(b[0], b[1]));
+          bw[i][g][nt][1] = turned(pack2<KD_F16>(b[2], b[3]));
+          constexpr uint32_t one = 0x00010001u;
+          if (i == 0) mma_from(all[g][nt], 0.f, 0.f, one, one, one, one, bw[i][g][nt][0], bw[i][g][nt][1]);
+          else mma(all[g][nt], one, one, one, one, bw[i][g][nt][0], bw[i][g][nt][1]);
+        }
       }
     }
 #pragma unroll
     for (int u = 0; u < Z::kUnits; ++u) {
       const int g = GS == 1 ? u : 2 * u / GS;
-      // the words of positions 2 t4, 2 t4 + 1, and of the same 8 on
-      const int word = GS == 1 ? 4 * u + (g8 >> 1) : min(8 * u + g8, 4 * NC - 1);
-      const uint32_t* at = vs + 2 * t4 * S + word;
-      const uint32_t w0 = at[0], w1 = at[S], w2 = at[8 * S], w3 = at[9 * S];
 #pragma unroll
-      for (int half = 0; half < (GS == 1 ? 1 : 2); ++half) {
-        const uint32_t pick = GS == 1 ? (g8 & 1 ? 0x7632u : 0x5410u) : half ? 0x7632u : 0x5410u;
-        uint32_t a = __byte_perm(w0, w1, pick), b = __byte_perm(w2, w3, pick);
+      for (int k = 0; k < Z::kOfUnit; ++k)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t a0 = minus2(a & 0x000F000Fu, 0x00080008u), a1 = minus2(a & 0x00F000F0u, 0x00800080u);
-          const uint32_t a2 = minus2(b & 0x000F000Fu, 0x00080008u), a3 = minus2(b & 0x00F000F0u, 0x00800080u);
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) mma(acc[u * Z::kOfUnit + 2 * half + i][nt], a0, a1, a2, a3, bw[g][nt][0], bw[g][nt][1]);
-          a >>= 8;
-          b >>= 8;
+          for (int e = 0; e < 4; ++e) acc[u * Z::kOfUnit + k][nt][e] = __fmaf_rn(all[g][nt][e & 1], e < 2 ? -8.f : -136.f, acc[u * Z::kOfUnit + k][nt][e]);
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) {
+        // the words of positions 2 t4, 2 t4 + 1, and of the same 8 on
+        const int word = GS == 1 ? 4 * u + (g8 >> 1) : min(8 * u + g8, 4 * NC - 1);
+        const uint32_t* at = vs + (kTile * i + 2 * t4) * S + word;
+        const uint32_t w0 = at[0], w1 = at[S], w2 = at[8 * S], w3 = at[9 * S];
+#pragma unroll
+        for (int half = 0; half < (GS == 1 ? 1 : 2); ++half) {
+          const uint32_t pick = GS == 1 ? (g8 & 1 ? 0x7632u : 0x5410u) : half ? 0x7632u : 0x5410u;
+          uint32_t a = __byte_perm(w0, w1, pick), b = __byte_perm(w2, w3, pick);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            if (k) {  // the upper bytes down
+              a = __byte_perm(a, 0, 0x4341);
+              b = __byte_perm(b, 0, 0x4341);
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              mma(acc[u * Z::kOfUnit + 2 * half + k][nt], a & 0x000F000Fu, k ? a : a & 0x00FF00FFu, b & 0x000F000Fu, k ? b : b & 0x00FF00FFu,
+                  bw[i][g][nt][0], bw[i][g][nt][1]);
+          }
         }
       }
     }
@@ -510,22 +653,26 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
       look_up(b0, n);
     }
     __syncthreads();
-    const int mine = (n - warp + kWarps - 1) / kWarps;
+    // this warp's steps: tiles kTiles * warp on, kTiles * kWarps apart
+    constexpr int kApart = kTiles * kWarps;
+    int fetch = kTiles * warp;
 #pragma unroll
-    for (int i = 0; i < ST - 1; ++i) {
-      if (i < mine) issue(warp + i * kWarps, i);
+    for (int i = 0; i < ST - 1; ++i, fetch += kApart) {
+      issue(fetch, n, i);
       commit();
     }
     int stage = 0, next = ST - 1;
-    for (int i = 0; i < mine; ++i) {
-      if (i + ST - 1 < mine) issue(warp + (i + ST - 1) * kWarps, next);
+    for (int nth = kTiles * warp; nth < n; nth += kApart, fetch += kApart) {
+      issue(fetch, n, next);
       commit();
       wait_group<ST - 1>();
       __syncwarp();  // the lanes' copies are each other's
-      const int nth = warp + i * kWarps, position = (first_tile + b0 + nth) * kTile;
-      const bool bad = place[nth] < 0;
-      if (bad || position < w.all_lo || position + kTile > w.all_hi) tile(std::true_type{}, ring + stage * Z::kStage, position, bad);
-      else tile(std::false_type{}, ring + stage * Z::kStage, position, false);
+      const int position = (first_tile + b0 + nth) * kTile;
+      const bool bad0 = place[nth].x < 0, bad1 = nth + 1 < n && place[nth + 1].x < 0;
+      const uint32_t* at = ring + stage * Z::kStage;
+      if (bad0 || bad1 || position < w.all_lo || position + kTiles * kTile > min(w.all_hi, share_hi))
+        step(std::true_type{}, at, position, bad0, bad1);
+      else step(std::false_type{}, at, position, false, false);
       __syncwarp();
       stage = stage + 1 == ST ? 0 : stage + 1;
       next = next + 1 == ST ? 0 : next + 1;
@@ -548,7 +695,7 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
 #pragma unroll
         for (int g = 0; g < GN; ++g) mids[g][nt][j] += __shfl_xor_sync(~0u, mids[g][nt][j], o);
       }
-      if (g8 == 0) ml[warp * Z::kRows + r] = make_float2(m[nt][j], sum[nt][j]);
+      if (g8 == 0) ml[warp * Z::kRows + r] = make_float2(room[nt][j] == kNone ? kNone : m[nt][j], sum[nt][j]);
       float* to = sums + (warp * Z::kRows + r) * Z::kSums;
 #pragma unroll
       for (int u = 0; u < Z::kUnits; ++u) {
@@ -558,13 +705,14 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
           const int ch = GS == 1 ? 32 * u + 4 * g8 + 2 * i : 64 * u + 8 * g8 + 2 * i;
           if (ch < 32 * NC) {
             to[ch] = __fmaf_rn(acc[u * Z::kOfUnit + i][nt][j], back, mids[g][nt][j]);
-            to[ch + 1] = __fmaf_rn(acc[u * Z::kOfUnit + i][nt][j + 2], back * 0.0625f, mids[g][nt][j]);
+            to[ch + 1] = __fmaf_rn(acc[u * Z::kOfUnit + i][nt][j + 2] - acc[u * Z::kOfUnit + i][nt][j], back * 0.0625f, mids[g][nt][j]);
           }
         }
       }
     }
   __syncthreads();
-  const int64_t item = ((int64_t)s * p.c.heads + head) * p.row_blocks + block;
+  // the part's place for partial sums: the share's first item, or its last
+  const int64_t slot = 2 * (int64_t)blockIdx.x + (left == share ? 0 : 1);
   for (int r = warp; r < w.rows; r += kWarps) {
     const int token = (r0 + r) / p.shared, h = head * p.shared + (r0 + r) - token * p.shared;
     const int64_t t = w.first + token;
@@ -580,20 +728,39 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
     }
     if (past_table(p, w, token)) total = __int_as_float(0x7FC00000);
     const bool none = total == 0.f;
-    const float over = w.splits > 1 ? 1.f : none ? 0.f : 1.f / total;
+    const float over = cut ? 1.f : none ? 0.f : 1.f / total;
     for (int ch = lane; ch < p.c.d; ch += 32) {
       float o = 0.f;
 #pragma unroll
       for (int k = 0; k < kWarps; ++k) o = __fmaf_rn(sums[(k * Z::kRows + r) * Z::kSums + ch], f[k], o);
       o *= over;
       if (total != total) o = total;
-      if (w.splits > 1) p.part[((item * p.splits + split) * Z::kRows + r) * p.c.d + ch] = o;
+      if (cut) p.part[(slot * Z::kRows + r) * p.c.d + ch] = o;
       else p.out[t * p.out_token + h * p.out_head + ch] = narrow(p, o);
     }
     if (lane == 0) {
-      if (w.splits > 1) p.part_ml[(item * p.splits + split) * Z::kRows + r] = make_float2(top, total);
+      if (cut) p.part_ml[slot * Z::kRows + r] = make_float2(top, total);
       else if (p.lse) p.lse[t * p.heads + h] = none ? kNone : (top + log2f(total)) * 0.693147180559945f;
     }
+  }
+  if (cut && chunk == 0 && threadIdx.x == 0) {
+    // the item goes on in the CTAs that follow
+    const int rest = w.chunks - n_chunks;
+    p.cuts[blockIdx.x] = Cut{w.first, block, head, w.rows, (int)slot, (rest + share - 1) / share, 0};
+  }
+  left -= n_chunks;
+  }
+  if (p.whole || left <= 0) return;
+  // the next item
+  chunk = 0;
+  if (w.rows == 0 || ++block == p.row_blocks) {
+    block = 0;
+    if (++head == p.c.heads) {
+      head = 0;
+      ++s;
+    }
+  }
+  __syncthreads();  // the sums are read before the ring is written again
   }
 }
 
@@ -609,14 +776,14 @@ cudaError_t allow_shared_memory(Kernel kernel, std::atomic<uint64_t>& ready) {
 }
 
 template <int NC, int GS, int NT>
-cudaError_t launch_one(const Params& p, cudaStream_t s) {
+cudaError_t launch_one(const Params& p, int grid, cudaStream_t s) {
   static_assert(Shape<NC, GS, NT>::kBytes <= 227 * 1024, "shared memory");
   auto kernel = attn4_kernel<NC, GS, NT>;
   static std::atomic<uint64_t> ready{0};
   const cudaError_t e = allow_shared_memory(kernel, ready);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((int64_t)p.c.seqs * p.c.heads * p.row_blocks * p.splits));
+  cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(32 * kWarps);
   cfg.dynamicSmemBytes = Shape<NC, GS, NT>::kBytes;
   cfg.stream = s;
@@ -628,19 +795,19 @@ cudaError_t launch_one(const Params& p, cudaStream_t s) {
 }
 // gs: 32-channel pieces of a group; nt: blocks of eight rows
 template <int NC, int NT>
-cudaError_t launch(const Params& p, int gs, cudaStream_t s) {
+cudaError_t launch(const Params& p, int gs, int grid, cudaStream_t s) {
   if constexpr (NC > 2)
-    if (gs == 4) return launch_one<NC, 4, NT>(p, s);
+    if (gs == 4) return launch_one<NC, 4, NT>(p, grid, s);
   if constexpr (NC > 1)
-    if (gs >= 2) return launch_one<NC, 2, NT>(p, s);
-  return launch_one<NC, 1, NT>(p, s);
+    if (gs >= 2) return launch_one<NC, 2, NT>(p, grid, s);
+  return launch_one<NC, 1, NT>(p, grid, s);
 }
 
-cudaError_t launch_small(const Params& p, int nc, int gs, int nt, cudaStream_t s);  // up to 64 channels
-cudaError_t launch_96(const Params& p, int gs, int nt, cudaStream_t s);
-cudaError_t launch_128(const Params& p, int gs, int nt, cudaStream_t s);
-cudaError_t launch_192(const Params& p, int gs, cudaStream_t s);
-cudaError_t launch_256(const Params& p, int gs, cudaStream_t s);
+cudaError_t launch_small(const Params& p, int nc, int gs, int nt, int grid, cudaStream_t s);  // up to 64 channels
+cudaError_t launch_96(const Params& p, int gs, int nt, int grid, cudaStream_t s);
+cudaError_t launch_128(const Params& p, int gs, int nt, int grid, cudaStream_t s);
+cudaError_t launch_192(const Params& p, int nc, int gs, int grid, cudaStream_t s);  // 129 to 192
+cudaError_t launch_256(const Params& p, int nc, int gs, int grid, cudaStream_t s);  // 193 to 256
 
 }  // namespace attn4
 }  // namespace kd
