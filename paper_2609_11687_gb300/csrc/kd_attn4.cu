@@ -9,41 +9,75 @@ namespace kd {
 namespace attn4 {
 namespace {
 
-constexpr int kJoinWarps = 8;
+constexpr int kJoinThreads = 256;
 
-// A block of warps for each CTA's cut item, a warp a row: the parts' sums, weighted by their maxima, in order.
-__global__ void __launch_bounds__(32 * kJoinWarps) attn4_join_kernel(const __grid_constant__ Params p, int of_block) {
+// A block for each CTA's cut item.  First the parts' weights, from their maxima, for all rows; then a thread has four
+// channels of a row and adds the parts in order, its loads independent of each other.
+__global__ void __launch_bounds__(kJoinThreads) attn4_join_kernel(const __grid_constant__ Params p, int of_block) {
+  extern __shared__ float weights[];  // [part][row], then a row's maxima and sums
   depend_on_last();
   const Cut c = p.cuts[blockIdx.x];
   if (c.more == 0) return;
-  const int lane = threadIdx.x & 31;
-  for (int r = threadIdx.x >> 5; r < c.rows; r += kJoinWarps) {
+  const int parts = c.more + 1, lane = threadIdx.x & 31;
+  float* totals = weights + (gridDim.x + 1) * of_block;
+  // part k's rows: the item's first place, then the first ones of the CTAs that follow
+  auto first_row = [&](int k) { return (int64_t)(k ? 2 * ((int)blockIdx.x + k) : c.slot) * of_block; };
+  for (int r = threadIdx.x >> 5; r < c.rows; r += kJoinThreads / 32) {
+    float top = kNone;
+    for (int k = lane; k < parts; k += 32) top = fmaxf(top, p.part_ml[first_row(k) + r].x);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    float total = 0.f;
+    for (int k = lane; k < parts; k += 32) {
+      const float2 v = p.part_ml[first_row(k) + r];
+      const float f = v.x == kNone ? 0.f : exp2_of(v.x - top);
+      total += v.x == kNone ? v.y : v.y * f;
+      weights[k * of_block + r] = f;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
+    if (lane == 0) {
+      totals[r] = total;
+      const int in = c.block * of_block + r, token = token_of(p, in);
+      const int64_t t = c.first + token;
+      if (p.lse && t >= 0 && t < p.tokens)
+        p.lse[t * p.heads + c.head * p.shared + in - token * p.shared] =
+            total == 0.f ? kNone : (top + log2f(total)) * 0.693147180559945f;
+    }
+  }
+  __syncthreads();
+  const int quads = (p.c.d + 3) / 4;
+  for (int i = threadIdx.x; i < c.rows * quads; i += kJoinThreads) {
+    const int r = i / quads, ch = 4 * (i - r * quads);
     const int in = c.block * of_block + r, token = in / p.shared, h = c.head * p.shared + in - token * p.shared;
     const int64_t t = c.first + token;
     if (t < 0 || t >= p.tokens) continue;
-    // part k's row: the item's first place, then the first ones of the CTAs that follow
-    auto row = [&](int k) { return (int64_t)(k ? 2 * ((int)blockIdx.x + k) : c.slot) * of_block + r; };
-    float top = kNone;
-    for (int k = lane; k <= c.more; k += 32) top = fmaxf(top, p.part_ml[row(k)].x);
+    float o[4] = {0.f, 0.f, 0.f, 0.f};
+    const float* from = p.part + (int64_t)r * p.part_row + ch;
+    const int64_t apart = (int64_t)of_block * p.part_row;  // of two places
+    constexpr int kAhead = 8;
+    for (int k0 = 0; k0 < parts; k0 += kAhead) {
+      float4 v[kAhead];
 #pragma unroll
-    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-    float total = 0.f, o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll 4
-    for (int k = 0; k <= c.more; ++k) {
-      const float2 v = p.part_ml[row(k)];
-      const float f = v.x == kNone ? 0.f : exp2_of(v.x - top);
-      total += v.x == kNone ? v.y : v.y * f;
+      for (int k = 0; k < kAhead; ++k) {
+        const int n = min(k0 + k, parts - 1);
+        v[k] = *reinterpret_cast<const float4*>(from + apart * (n ? 2 * ((int)blockIdx.x + n) : c.slot));
+      }
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (lane + 32 * i < p.c.d) o[i] = __fmaf_rn(p.part[row(k) * p.c.d + lane + 32 * i], f, o[i]);
+      for (int k = 0; k < kAhead; ++k) {
+        const float f = k0 + k < parts ? weights[(k0 + k) * of_block + r] : 0.f;
+        if (k0 + k >= parts) continue;
+        o[0] = __fmaf_rn(v[k].x, f, o[0]);
+        o[1] = __fmaf_rn(v[k].y, f, o[1]);
+        o[2] = __fmaf_rn(v[k].z, f, o[2]);
+        o[3] = __fmaf_rn(v[k].w, f, o[3]);
+      }
     }
-    const bool none = total == 0.f;
-    const float over = none ? 0.f : 1.f / total;
+    const float total = totals[r], over = total == 0.f ? 0.f : 1.f / total;
+    uint16_t* out = p.out + t * p.out_token + h * p.out_head + ch;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (lane + 32 * i < p.c.d)
-        p.out[t * p.out_token + h * p.out_head + lane + 32 * i] = narrow(p, total != total ? total : o[i] * over);
-    if (lane == 0 && p.lse) p.lse[t * p.heads + h] = none ? kNone : (top + log2f(total)) * 0.693147180559945f;
+    for (int e = 0; e < 4; ++e)
+      if (ch + e < p.c.d) out[e] = narrow(p, total != total ? total : o[e] * over);
   }
 }
 
@@ -67,18 +101,18 @@ bool plan(const kd_cache4* c, const kd_sequences* s, int64_t heads, int64_t wind
   const int64_t items = s->seqs * c->heads;
   // chunks of positions of all items together, were all as long as the table has room for
   auto chunks_of = [&](int64_t positions) { return std::max<int64_t>(1, (positions + kTile * kChunk - 1) / (kTile * kChunk) + 1); };
-  const int64_t room = std::min(s->wide * c->page, (int64_t)INT32_MAX);
+  const int64_t room = std::min(s->wide * c->page, (int64_t)INT32_MAX - kTile);
   if (blocks > INT32_MAX || items > INT32_MAX || (blocks && items > INT32_MAX / blocks) ||
       (blocks && items * blocks > INT32_MAX / chunks_of(room)))
     return false;
   pl.row_blocks = (int)blocks;
   int64_t longest = std::min(s->longest, room);
   if (window > 0) longest = std::min(longest, window + 8 * pl.nt + kTile);
-  const int64_t all = items * blocks, places = 152 * (pl.nt == 1 && pl.nc <= 4 ? 2 : 1);
+  const int64_t all = items * blocks, places = 152 * (pl.nt == 1 && pl.nc <= 4 ? 4 : 2);
   pl.whole = longest <= 2 * kTile * kChunk;
   pl.grid = (int)(pl.whole ? all : std::min(places, all * chunks_of(longest)));
   pl.workspace = 0;
-  if (!pl.whole) pl.workspace = (size_t)pl.grid * (sizeof(Cut) + 2 * (8 * pl.nt) * (8 + 4 * (size_t)c->d));
+  if (!pl.whole) pl.workspace = (size_t)pl.grid * (sizeof(Cut) + 2 * (8 * pl.nt) * (8 + 4 * (size_t)((c->d + 3) / 4 * 4)));
   pl.workspace = (pl.workspace + 15) / 16 * 16;
   return true;
 }
@@ -141,8 +175,13 @@ extern "C" kd_status kd_attention_4bit(const kd_cache4* cache, const kd_sequence
   p.shared = (int)(heads / cache->heads);
   p.row_blocks = pl.row_blocks;
   p.whole = pl.whole;
+  p.part_row = (int)((cache->d + 3) / 4 * 4);
   p.causal = causal != 0;
   p.window = (int)window;
+  p.room = (int)std::min(seqs->wide * cache->page, (int64_t)INT32_MAX - kTile);
+  p.page_log = -1;
+  for (int log = 0; log <= 12; ++log)
+    if (cache->page == (int64_t)kTile << log) p.page_log = log;
   p.bf16 = dtype == KD_BF16;
   p.q_vec = cache->d % 8 == 0 && aligned(q, 16) && (tokens == 1 || q_token % 8 == 0) && (heads == 1 || q_head % 8 == 0);
   p.scale2 = scale * 1.4426950408889634f;
@@ -160,7 +199,8 @@ extern "C" kd_status kd_attention_4bit(const kd_cache4* cache, const kd_sequence
   if (e == cudaSuccess && !pl.whole) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)pl.grid);
-    cfg.blockDim = dim3(32 * kJoinWarps);
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.dynamicSmemBytes = (size_t)(pl.grid + 2) * (8 * pl.nt) * sizeof(float);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     launch_early(attr[0]);

@@ -45,7 +45,7 @@ namespace attn4 {
 
 using namespace cache4;
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 4;
 constexpr int kTile = 16;     // positions of a tensor-core tile, all on one page
 constexpr int kTiles = 2;     // of one step of a warp
 constexpr int kChunk = kTiles * kWarps;  // tiles of one step of a CTA: what work is shared out in
@@ -62,11 +62,14 @@ struct Params {
   int row_blocks;               // of a sequence: blocks of rows
   int whole;                    // a CTA has an item (sequence, key head, block of rows) to itself; else all CTAs equal shares
   int causal, window;
+  int room;                     // positions that the table has room for
+  int page_log;                 // of a page's tiles, where that is a power of two, else -1
   int bf16, q_vec;
   float scale2;                 // scale log2 e
   struct Cut* cuts;             // the item that each CTA leaves to the next ones
   float2* part_ml;              // (m, sum) of each row of a CTA's first item and of its last, where they are cut
-  float* part;                  // and their sums [CTA][first, last][row][d]
+  float* part;                  // and their sums [CTA][first, last][row][part_row]
+  int part_row;                 // d, up to a multiple of 4
 };
 
 // An item whose first chunks are the end of a CTA's share: the sums of its rows are in `slot` and in the first
@@ -79,31 +82,35 @@ struct Cut {
 // The rows and positions of a block of rows: the same for the kernel that sums and the one that joins.
 struct Work {
   int64_t first;       // row of the sequence's first query token
-  int64_t before;      // position of that token
+  int before;          // position of that token
   int length, rows;    // rows: tokens times heads, from the block's first on
   int lo, hi;          // positions that some row sees
   int all_lo, all_hi;  // positions that every row sees
   int tile, tiles;     // of the positions lo .. hi
   int chunks;          // of kChunk tiles; one for rows that see nothing, none for no rows
 };
-__device__ __forceinline__ int clamp_to(int64_t v, int most) { return (int)(v < 0 ? 0 : v > most ? most : v); }
+__device__ __forceinline__ int clamp_to(int v, int most) { return max(0, min(v, most)); }
+// token of a row, of its sequence's
+__device__ __forceinline__ int token_of(const Params& p, int row) {
+  return p.shared == 1 ? row : (int)((unsigned)row / (unsigned)p.shared);
+}
 __device__ __forceinline__ Work work_of(const Params& p, int s, int block, int of_block) {
   Work w;
-  int64_t count = p.c.most;
+  const int length = p.c.lengths[s];
+  int count = p.c.most;
   w.first = (int64_t)s * p.c.most;
   if (p.c.starts) {
     w.first = p.c.starts[s];
-    count = (int64_t)p.c.starts[s + 1] - w.first;
+    count = (int)max((int64_t)0, min((int64_t)p.c.starts[s + 1] - w.first, (int64_t)INT32_MAX));
   }
-  const int64_t tokens = min(count, (int64_t)p.c.most);
-  w.length = max(p.c.lengths[s], 0);
-  w.before = (int64_t)p.c.lengths[s] - count;
-  const int64_t r0 = (int64_t)block * of_block, rows = tokens * p.shared - r0;
-  w.rows = (int)max((int64_t)0, min(rows, (int64_t)of_block));
-  const int64_t a = w.before + r0 / p.shared, b = w.before + (r0 + w.rows - 1) / p.shared;  // first, last position
+  w.length = max(length, 0);
+  w.before = w.length - count;
+  const int r0 = block * of_block, rows = min(count, p.c.most) * p.shared;  // the host has checked their range
+  w.rows = clamp_to(rows - r0, of_block);
   w.lo = w.all_lo = 0;
   w.hi = w.all_hi = w.length;
   if (p.causal) {
+    const int a = w.before + token_of(p, r0), b = w.before + token_of(p, max(r0 + w.rows - 1, r0));  // first, last position
     w.hi = clamp_to(b + 1, w.length);
     w.all_hi = clamp_to(a + 1, w.length);
     if (p.window) {
@@ -112,7 +119,7 @@ __device__ __forceinline__ Work work_of(const Params& p, int s, int block, int o
     }
   }
   // positions past the table's room have no page: none is visited, and rows that see one are NaN
-  w.hi = (int)min((int64_t)w.hi, (int64_t)p.c.wide * p.c.page);
+  w.hi = min(w.hi, p.room);
   w.tile = w.lo / kTile;
   w.tiles = w.hi > w.lo ? (w.hi + kTile - 1) / kTile - w.tile : 0;
   w.chunks = w.rows == 0 ? 0 : max((w.tiles + kChunk - 1) / kChunk, 1);
@@ -121,8 +128,15 @@ __device__ __forceinline__ Work work_of(const Params& p, int s, int block, int o
 
 // does the row of a token, `nth` of its sequence's, see positions past the table's room?
 __device__ __forceinline__ bool past_table(const Params& p, const Work& w, int nth) {
-  const int64_t end = p.causal ? min(w.before + nth + 1, (int64_t)w.length) : w.length;
-  return end > (int64_t)p.c.wide * p.c.page;
+  return (p.causal ? min(w.before + nth + 1, w.length) : w.length) > p.room;
+}
+
+// The first row's number of a tile (of 16 positions on one page) for the first key head, -1 on a bad page.
+__device__ __forceinline__ int64_t tile_row(const Params& p, int s, int tile) {
+  const unsigned of_page = (unsigned)p.c.page / kTile, nth = p.page_log >= 0 ? (unsigned)tile >> p.page_log : (unsigned)tile / of_page;
+  const int page = p.c.table[s * p.c.ld_table + nth];  // tiles lie within the table's room
+  if ((unsigned)page >= (unsigned)p.c.pages) return -1;
+  return (int64_t)page * p.c.heads * p.c.page + (int)(tile - nth * of_page) * kTile;
 }
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
@@ -140,15 +154,52 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// the same with sums that start from c0, c1 in every row
-__device__ __forceinline__ void mma_from(float (&d)[4], float c0, float c1, uint32_t a0, uint32_t a1, uint32_t a2,
-                                         uint32_t a3, uint32_t b0, uint32_t b1) {
+// the same with sums that start from 0
+__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                          uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-      "{%10, %11, %10, %11};\n"
+      "{%10, %10, %10, %10};\n"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-// an 8 x 8 matrix of halves, a row to four lanes, turned
+// Matrices of 8 rows of 16 bytes, as 16-bit units: to a lane units 2 t4, 2 t4 + 1 of row g8, or (TURN) unit g8 of
+// rows 2 t4, 2 t4 + 1.  Lane l gives the address of row l % 8 of matrix l / 8.
+template <bool TURN>
+__device__ __forceinline__ void load_matrices(uint32_t (&d)[4], uint32_t at) {
+  if constexpr (TURN)
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3]) : "r"(at) : "memory");
+  else
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3]) : "r"(at) : "memory");
+}
+template <bool TURN>
+__device__ __forceinline__ void load_two_matrices(uint32_t (&d)[4], uint32_t at) {
+  if constexpr (TURN)
+    asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0, %1}, [%2];" : "=r"(d[0]), "=r"(d[1]) : "r"(at) : "memory");
+  else asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0, %1}, [%2];" : "=r"(d[0]), "=r"(d[1]) : "r"(at) : "memory");
+}
+// two fp32 operations in one
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{.reg .b64 a, b, c, d; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; mov.b64 c, {%6, %7}; fma.rn.f32x2 d, a, b, c; "
+      "mov.b64 {%0, %1}, d;}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{.reg .b64 a, b, d; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; mul.rn.f32x2 d, a, b; mov.b64 {%0, %1}, d;}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{.reg .b64 a, b, d; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; add.rn.f32x2 d, a, b; mov.b64 {%0, %1}, d;}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+// an 8 x 8 matrix of halves, a row to four lanes, turned// an 8 x 8 matrix of halves, a row to four lanes, turned
 __device__ __forceinline__ uint32_t turned(uint32_t v) {
   uint32_t r;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
@@ -179,8 +230,7 @@ struct Shape {
   // words of a stage, keys or values
   static constexpr int kCodes = kTiles * kTile * kStride, kScales = kTiles * kTile * kGroups;
   static constexpr int kStage = 2 * (kCodes + kScales);
-  // a value's 64 channels at a time (four tiles of 16), or 32 (two) where those have one scale
-  static constexpr int kUnits = GS == 1 ? NC : (NC + 1) / 2, kOfUnit = GS == 1 ? 2 : 4;
+  static constexpr int kSumTiles = 2 * NC;                           // tiles of 16 channels of the values' sums
   static constexpr int kSums = 32 * NC + 4;                          // floats of a row of a warp's sums
   static constexpr int kQueries = 64 * NC + 64;                      // bytes of a row of queries as operands
   static constexpr size_t kRing = (size_t)kWarps * kStages * kStage * 4, kJoin = (size_t)kWarps * kRows * kSums * 4;
@@ -219,7 +269,7 @@ __device__ __forceinline__ int sum_before(int v, int* scratch, int& total) {
 }
 
 template <int NC, int GS, int NT>
-__global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 4 : 2) attn4_kernel(const __grid_constant__ Params p) {
   using Z = Shape<NC, GS, NT>;
   constexpr int GN = Z::kGroups, ST = Z::kStages, S = Z::kStride;
   extern __shared__ uint4 smem[];
@@ -307,19 +357,22 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
 
   // Where a batch's tiles lie, in bytes of codes and scales from the cache's first row: -1 on a bad page.
   auto look_up = [&](int b0, int n) {
+    bool bad = false;
     for (int i = threadIdx.x; i < n; i += 32 * kWarps) {
-      const int64_t first = row_of(p.c, s, (int64_t)(first_tile + b0 + i) * kTile), row = first + (int64_t)head * p.c.page;
+      const int64_t first = tile_row(p, s, first_tile + b0 + i), row = first + (int64_t)head * p.c.page;
       place[i] = first < 0 ? make_longlong2(-1, 0) : make_longlong2(row * row_bytes, row * scale_bytes);
+      bad |= first < 0;
     }
+    return bad;
   };
-  look_up(0, min(tiles, kBatch));
+  bool bad_pages = look_up(0, min(tiles, kBatch));
 
   // The rows as operands, a warp a row: fp16 in eights of channels 0 4 1 5 2 6 3 7, the odd ones over 16, with
   // the row's power of two and its sums over groups.
   const int r0 = block * Z::kRows;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int r = 8 * nt + warp, token = (r0 + r) / p.shared;
+  for (int r = warp; r < Z::kRows; r += kWarps) {
+    const int token = token_of(p, r0 + r);
     const int64_t t = w.first + token;
     const bool live = r < w.rows && t >= 0 && t < p.tokens;
     const uint16_t* q = p.q + (live ? t * p.q_token + (int64_t)(head * p.shared + (r0 + r) - token * p.shared) * p.q_head : 0);
@@ -365,7 +418,7 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
   __syncthreads();
   uint32_t qb[2 * NC][NT][2];
   // of columns 2 t4, 2 t4 + 1: power of two of the row, and its sums over groups, both times scale log2 e
-  float qs[GN][NT][2], qe[NT][2], q8[GN][NT][2];  // q8: where the sums over a group's codes start
+  float qs[GN][NT][2], qe[NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -381,10 +434,7 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
       const float* of_column = query_sums + (8 * nt + 2 * t4 + j) * (GN + 1);
       const float down = of_column[GN];
 #pragma unroll
-      for (int g = 0; g < GN; ++g) {
-        qs[g][nt][j] = of_column[g] * down;
-        q8[g][nt][j] = of_column[g] * -0x1p-7f;  // 8 times 2^14 / 2^24
-      }
+      for (int g = 0; g < GN; ++g) qs[g][nt][j] = of_column[g] * down;
       qe[nt][j] = down * 1024.f;  // codes' 2^24 less q's 2^14
     }
   }
@@ -395,7 +445,7 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int r = 8 * nt + 2 * t4 + j;
-      const int64_t pos = w.before + (r0 + r) / p.shared;
+      const int pos = w.before + token_of(p, r0 + r);
       sees_hi[nt][j] = r >= w.rows ? 0 : min(share_hi, p.causal ? clamp_to(pos + 1, w.length) : w.length);
       sees_lo[nt][j] = p.window ? clamp_to(pos + 1 - p.window, w.length) : 0;
     }
@@ -423,82 +473,90 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
     }
   };
 
-  float acc[Z::kUnits * Z::kOfUnit][NT][4];
-  // of the columns: sums of weights times middles and of weights, m (0 before the first), and how far above it
-  // a score may lie (nothing may, before the first)
-  float mids[GN][NT][2], sum[NT][2], m[NT][2], room[NT][2];
+  float acc[Z::kSumTiles][NT][4];
+  // of the columns: sums of weights times middles and of weights (of the positions g8 and g8 + 8 of the tiles
+  // apart), m (0 before the first), and how far above it a score may lie (nothing may, before the first)
+  float2 mids[GN][NT][2], sum[NT][2];
+  float m[NT][2], room[NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-    for (int i = 0; i < Z::kUnits * Z::kOfUnit; ++i)
+    for (int i = 0; i < Z::kSumTiles; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[i][nt][e] = 0.f;
 #pragma unroll
-    for (int g = 0; g < GN; ++g) mids[g][nt][0] = mids[g][nt][1] = 0.f;
+    for (int g = 0; g < GN; ++g) mids[g][nt][0] = mids[g][nt][1] = make_float2(0.f, 0.f);
     m[nt][0] = m[nt][1] = 0.f;
     room[nt][0] = room[nt][1] = kNone;
-    sum[nt][0] = sum[nt][1] = 0.f;
+    sum[nt][0] = sum[nt][1] = make_float2(0.f, 0.f);
   }
   float step_cap = 0.f;  // no step so far lies above
   float step_up = 1.f;   // the power of two of the values' weights: step_cap becomes 2^6
 
   // One step.  EDGE: some row does not see all of it, or a page is bad.
-  auto step = [&](auto edge, const uint32_t* stage, int position, bool bad0, bool bad1) {
+  const uint32_t matrix_at = (lane & 15) * S * 4 + (lane >> 4) * 16;  // this lane's row of four matrices
+  auto step = [&](auto edge, int stage, int position, bool bad0, bool bad1) {
     constexpr bool EDGE = decltype(edge)::value;
-    const uint32_t* ks = stage;
-    const uint32_t* vs = stage + Z::kCodes;
-    const uint32_t* kp = stage + 2 * Z::kCodes;
+    const uint32_t codes = ring_at + stage * (Z::kStage * 4) + matrix_at;
+    const uint32_t* kp = ring + stage * Z::kStage + 2 * Z::kCodes + g8 * GN;
     const uint32_t* vp = kp + Z::kScales;
     float x[kTiles][NT][4];  // scores less m
     bool seen[kTiles][NT][4];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
-      float part[NT][4], mid[NT][4];
+      float part[NT][4], low[NT][4];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           x[i][nt][e] = 0.f;
-          mid[nt][e] = -m[nt][e & 1];
+          low[nt][e] = -m[nt][e & 1];
         }
+      uint32_t w[4];  // positions g8, g8 + 8 of one piece, and of the next
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        uint32_t a = ks[(kTile * i + g8) * S + 4 * c + t4], b = ks[(kTile * i + g8 + 8) * S + 4 * c + t4];
+        if (c % 2 == 0) {
+          if (c + 1 < NC) load_matrices<false>(w, codes + i * kTile * S * 4 + c * 16);
+          else load_two_matrices<false>(w, codes + i * kTile * S * 4 + c * 16);
+        }
+        uint32_t a = w[c % 2 * 2], b = w[c % 2 * 2 + 1];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
+          const uint32_t a0 = a & 0x000F000Fu, a1 = b & 0x000F000Fu, a2 = a & 0x00F000F0u, a3 = b & 0x00F000F0u;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            const uint32_t a0 = a & 0x000F000Fu, a1 = b & 0x000F000Fu, a2 = a & 0x00F000F0u, a3 = b & 0x00F000F0u;
-            if (c % GS == 0 && h == 0)
-              mma_from(part[nt], q8[c / GS][nt][0], q8[c / GS][nt][1], a0, a1, a2, a3, qb[2 * c][nt][0], qb[2 * c][nt][1]);
+            if (c % GS == 0 && h == 0) mma_first(part[nt], a0, a1, a2, a3, qb[2 * c][nt][0], qb[2 * c][nt][1]);
             else mma(part[nt], a0, a1, a2, a3, qb[2 * c + h][nt][0], qb[2 * c + h][nt][1]);
           }
           a >>= 8;
           b >>= 8;
         }
         if ((c + 1) % GS == 0 || c == NC - 1) {
-          const uint32_t* at = kp + (kTile * i + g8) * GN + c / GS;
-          const uint32_t u = at[0], v = at[8 * GN];
-          const float s0 = low_half(u), m0 = __fmaf_rn(8.f, s0, high_half(u));
-          const float s1 = low_half(v), m1 = __fmaf_rn(8.f, s1, high_half(v));
+          const uint32_t u = kp[i * kTile * GN + c / GS], v = kp[(i * kTile + 8) * GN + c / GS];
+          const float s0 = low_half(u), l0 = high_half(u), s1 = low_half(v), l1 = high_half(v);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               x[i][nt][e] = __fmaf_rn(e < 2 ? s0 : s1, part[nt][e], x[i][nt][e]);
-              mid[nt][e] = __fmaf_rn(e < 2 ? m0 : m1, qs[c / GS][nt][e & 1], mid[nt][e]);
+              low[nt][e] = __fmaf_rn(e < 2 ? l0 : l1, qs[c / GS][nt][e & 1], low[nt][e]);
             }
         }
       }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[i][nt][e] = __fmaf_rn(x[i][nt][e], qe[nt][e & 1], mid[nt][e]);
+        for (int e = 0; e < 4; e += 2) {
+          const float2 of = fma2(make_float2(x[i][nt][e], x[i][nt][e + 1]), make_float2(qe[nt][0], qe[nt][1]), make_float2(low[nt][e], low[nt][e + 1]));
+          x[i][nt][e] = of.x;
+          x[i][nt][e + 1] = of.y;
           if constexpr (EDGE) {
-            const int pos = position + kTile * i + g8 + 8 * (e >> 1);
-            seen[i][nt][e] = pos < sees_hi[nt][e & 1] && pos >= sees_lo[nt][e & 1];
-            x[i][nt][e] = !seen[i][nt][e] ? kNone : (i ? bad1 : bad0) ? __int_as_float(0x7FC00000) : x[i][nt][e];
+            const int pos = position + kTile * i + g8 + 4 * e;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              seen[i][nt][e + j] = pos < sees_hi[nt][j] && pos >= sees_lo[nt][j];
+              x[i][nt][e + j] = !seen[i][nt][e + j] ? kNone : (i ? bad1 : bad0) ? __int_as_float(0x7FC00000) : x[i][nt][e + j];
+            }
           }
         }
     }
@@ -507,10 +565,10 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-      for (int g = 0; g < GN; ++g)
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          uint32_t v = vp[(kTile * i + g8 + 8 * k) * GN + g];
+        for (int g = 0; g < GN; ++g) {
+          uint32_t v = vp[(kTile * i + 8 * k) * GN + g];
           if constexpr (EDGE) {  // a position that no row sees may hold anything
             const int pos = position + kTile * i + g8 + 8 * k;
             if (pos >= share_hi || pos < w.lo) v = 0;
@@ -552,6 +610,7 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
           if (to == kNone) continue;  // nothing seen yet; the sums are 0
           // m moves up by `to`; a first one by whatever it is
           const float f = fresh ? 0.f : exp2_of(-to), fs = f * by_step;
+          const float2 ff = make_float2(f, f);
           m[nt][j] += to;
           room[nt][j] = 8.f;
 #pragma unroll
@@ -559,11 +618,11 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
             x[i][nt][j] -= to;
             x[i][nt][j + 2] -= to;
           }
-          sum[nt][j] *= f;
+          sum[nt][j] = mul2(sum[nt][j], ff);
 #pragma unroll
-          for (int g = 0; g < GN; ++g) mids[g][nt][j] *= f;
+          for (int g = 0; g < GN; ++g) mids[g][nt][j] = mul2(mids[g][nt][j], ff);
 #pragma unroll
-          for (int i = 0; i < Z::kUnits * Z::kOfUnit; ++i) {
+          for (int i = 0; i < Z::kSumTiles; ++i) {
             acc[i][nt][j] *= fs;
             acc[i][nt][j + 2] *= fs;
           }
@@ -574,73 +633,77 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
     float all[GN][NT][4];  // of each column, in every row: 2^-24 of the step's weights as they are rounded
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
+      float2 wt[NT][2];  // of a column, positions g8 and g8 + 8
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[i][nt][e] = exp2_of(x[i][nt][e]);
-          sum[nt][e & 1] += x[i][nt][e];
+        for (int j = 0; j < 2; ++j) {
+          wt[nt][j] = make_float2(exp2_of(x[i][nt][j]), exp2_of(x[i][nt][j + 2]));
+          sum[nt][j] = add2(sum[nt][j], wt[nt][j]);
         }
 #pragma unroll
       for (int g = 0; g < GN; ++g) {
-        float up[2], mid[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const float step = low_half(vscale[i][g][k]);
-          mid[k] = __fmaf_rn(8.f, step, high_half(vscale[i][g][k]));
-          up[k] = step * step_up;
-        }
+        const float2 step = make_float2(low_half(vscale[i][g][0]), low_half(vscale[i][g][1]));
+        const float2 mid = fma2(make_float2(8.f, 8.f), step, make_float2(high_half(vscale[i][g][0]), high_half(vscale[i][g][1])));
+        const float2 up = mul2(step, make_float2(step_up, step_up));
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          float b[4];
+          float2 b[2];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            b[e] = x[i][nt][e] * up[e >> 1];
+          for (int j = 0; j < 2; ++j) {
+            b[j] = mul2(wt[nt][j], up);
             if constexpr (EDGE) {  // whatever stands where a row does not see: 0
-              if (!seen[i][nt][e]) b[e] = 0.f;
-              else mids[g][nt][e & 1] = __fmaf_rn(x[i][nt][e], mid[e >> 1], mids[g][nt][e & 1]);
+              b[j].x = seen[i][nt][j] ? b[j].x : 0.f;
+              b[j].y = seen[i][nt][j + 2] ? b[j].y : 0.f;
+              const float2 of = make_float2(seen[i][nt][j] ? mid.x : 0.f, seen[i][nt][j + 2] ? mid.y : 0.f);
+              mids[g][nt][j] = fma2(wt[nt][j], of, mids[g][nt][j]);
             } else {
-              mids[g][nt][e & 1] = __fmaf_rn(x[i][nt][e], mid[e >> 1], mids[g][nt][e & 1]);
+              mids[g][nt][j] = fma2(wt[nt][j], mid, mids[g][nt][j]);
             }
           }
-          bw[i][g][nt][0] = turned(pack2<KD_F16>(b[0], b[1]));
-          bw[i][g][nt][1] = turned(pack2<KD_F16>(b[2], b[3]));
+          bw[i][g][nt][0] = turned(pack2<KD_F16>(b[0].x, b[1].x));
+          bw[i][g][nt][1] = turned(pack2<KD_F16>(b[0].y, b[1].y));
           constexpr uint32_t one = 0x00010001u;
-          if (i == 0) mma_from(all[g][nt], 0.f, 0.f, one, one, one, one, bw[i][g][nt][0], bw[i][g][nt][1]);
+          if (i == 0) mma_first(all[g][nt], one, one, one, one, bw[i][g][nt][0], bw[i][g][nt][1]);
           else mma(all[g][nt], one, one, one, one, bw[i][g][nt][0], bw[i][g][nt][1]);
         }
       }
     }
 #pragma unroll
-    for (int u = 0; u < Z::kUnits; ++u) {
-      const int g = GS == 1 ? u : 2 * u / GS;
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int k = 0; k < Z::kOfUnit; ++k)
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
+          float(&d)[4] = acc[2 * c + k][nt];
+          const float2 eight = make_float2(all[c / GS][nt][0], all[c / GS][nt][1]);
+          const float2 even = fma2(eight, make_float2(-8.f, -8.f), make_float2(d[0], d[1]));
+          const float2 both = fma2(eight, make_float2(-136.f, -136.f), make_float2(d[2], d[3]));
+          d[0] = even.x;
+          d[1] = even.y;
+          d[2] = both.x;
+          d[3] = both.y;
+        }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[u * Z::kOfUnit + k][nt][e] = __fmaf_rn(all[g][nt][e & 1], e < 2 ? -8.f : -136.f, acc[u * Z::kOfUnit + k][nt][e]);
+    for (int i = 0; i < kTiles; ++i) {
+      uint32_t w[4];  // positions 2 t4, 2 t4 + 1, and the same 8 on, of one piece; of the next
 #pragma unroll
-      for (int i = 0; i < kTiles; ++i) {
-        // the words of positions 2 t4, 2 t4 + 1, and of the same 8 on
-        const int word = GS == 1 ? 4 * u + (g8 >> 1) : min(8 * u + g8, 4 * NC - 1);
-        const uint32_t* at = vs + (kTile * i + 2 * t4) * S + word;
-        const uint32_t w0 = at[0], w1 = at[S], w2 = at[8 * S], w3 = at[9 * S];
+      for (int c = 0; c < NC; ++c) {
+        if (c % 2 == 0) {
+          if (c + 1 < NC) load_matrices<true>(w, codes + Z::kCodes * 4 + i * kTile * S * 4 + c * 16);
+          else load_two_matrices<true>(w, codes + Z::kCodes * 4 + i * kTile * S * 4 + c * 16);
+        }
+        uint32_t a = w[c % 2 * 2], b = w[c % 2 * 2 + 1];
 #pragma unroll
-        for (int half = 0; half < (GS == 1 ? 1 : 2); ++half) {
-          const uint32_t pick = GS == 1 ? (g8 & 1 ? 0x7632u : 0x5410u) : half ? 0x7632u : 0x5410u;
-          uint32_t a = __byte_perm(w0, w1, pick), b = __byte_perm(w2, w3, pick);
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            if (k) {  // the upper bytes down
-              a = __byte_perm(a, 0, 0x4341);
-              b = __byte_perm(b, 0, 0x4341);
-            }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-              mma(acc[u * Z::kOfUnit + 2 * half + k][nt], a & 0x000F000Fu, k ? a : a & 0x00FF00FFu, b & 0x000F000Fu, k ? b : b & 0x00FF00FFu,
-                  bw[i][g][nt][0], bw[i][g][nt][1]);
+        for (int k = 0; k < 2; ++k) {
+          if (k) {  // the upper bytes down
+            a = __byte_perm(a, 0, 0x4341);
+            b = __byte_perm(b, 0, 0x4341);
           }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            mma(acc[2 * c + k][nt], a & 0x000F000Fu, k ? a : a & 0x00FF00FFu, b & 0x000F000Fu, k ? b : b & 0x00FF00FFu,
+                bw[i][c / GS][nt][0], bw[i][c / GS][nt][1]);
         }
       }
     }
@@ -650,9 +713,9 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
     const int n = min(kBatch, tiles - b0);
     if (b0) {
       __syncthreads();  // no warp still reads the last batch's places
-      look_up(b0, n);
+      bad_pages = look_up(b0, n);
     }
-    __syncthreads();
+    bad_pages = __syncthreads_or(bad_pages);
     // this warp's steps: tiles kTiles * warp on, kTiles * kWarps apart
     constexpr int kApart = kTiles * kWarps;
     int fetch = kTiles * warp;
@@ -668,11 +731,9 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
       wait_group<ST - 1>();
       __syncwarp();  // the lanes' copies are each other's
       const int position = (first_tile + b0 + nth) * kTile;
-      const bool bad0 = place[nth].x < 0, bad1 = nth + 1 < n && place[nth + 1].x < 0;
-      const uint32_t* at = ring + stage * Z::kStage;
-      if (bad0 || bad1 || position < w.all_lo || position + kTiles * kTile > min(w.all_hi, share_hi))
-        step(std::true_type{}, at, position, bad0, bad1);
-      else step(std::false_type{}, at, position, false, false);
+      if (bad_pages || position < w.all_lo || position + kTiles * kTile > min(w.all_hi, share_hi))
+        step(std::true_type{}, stage, position, place[nth].x < 0, nth + 1 < n && place[nth + 1].x < 0);
+      else step(std::false_type{}, stage, position, false, false);
       __syncwarp();
       stage = stage + 1 == ST ? 0 : stage + 1;
       next = next + 1 == ST ? 0 : next + 1;
@@ -689,32 +750,31 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int r = 8 * nt + 2 * t4 + j;
+      float total = sum[nt][j].x + sum[nt][j].y, of[GN];
+#pragma unroll
+      for (int g = 0; g < GN; ++g) of[g] = mids[g][nt][j].x + mids[g][nt][j].y;
 #pragma unroll
       for (int o = 4; o < 32; o *= 2) {
-        sum[nt][j] += __shfl_xor_sync(~0u, sum[nt][j], o);
+        total += __shfl_xor_sync(~0u, total, o);
 #pragma unroll
-        for (int g = 0; g < GN; ++g) mids[g][nt][j] += __shfl_xor_sync(~0u, mids[g][nt][j], o);
+        for (int g = 0; g < GN; ++g) of[g] += __shfl_xor_sync(~0u, of[g], o);
       }
-      if (g8 == 0) ml[warp * Z::kRows + r] = make_float2(room[nt][j] == kNone ? kNone : m[nt][j], sum[nt][j]);
-      float* to = sums + (warp * Z::kRows + r) * Z::kSums;
+      if (g8 == 0) ml[warp * Z::kRows + r] = make_float2(room[nt][j] == kNone ? kNone : m[nt][j], total);
+      float* to = sums + (warp * Z::kRows + r) * Z::kSums + 4 * g8;
 #pragma unroll
-      for (int u = 0; u < Z::kUnits; ++u) {
-        const int g = GS == 1 ? u : 2 * u / GS;
-#pragma unroll
-        for (int i = 0; i < Z::kOfUnit; ++i) {
-          const int ch = GS == 1 ? 32 * u + 4 * g8 + 2 * i : 64 * u + 8 * g8 + 2 * i;
-          if (ch < 32 * NC) {
-            to[ch] = __fmaf_rn(acc[u * Z::kOfUnit + i][nt][j], back, mids[g][nt][j]);
-            to[ch + 1] = __fmaf_rn(acc[u * Z::kOfUnit + i][nt][j + 2] - acc[u * Z::kOfUnit + i][nt][j], back * 0.0625f, mids[g][nt][j]);
-          }
-        }
+      for (int c = 0; c < NC; ++c) {  // even channels, and these plus 16 times the odd ones
+        const float(&d0)[4] = acc[2 * c][nt];
+        const float(&d1)[4] = acc[2 * c + 1][nt];
+        *reinterpret_cast<float4*>(to + 32 * c) =
+            make_float4(__fmaf_rn(d0[j], back, of[c / GS]), __fmaf_rn(d0[j + 2] - d0[j], back * 0.0625f, of[c / GS]),
+                        __fmaf_rn(d1[j], back, of[c / GS]), __fmaf_rn(d1[j + 2] - d1[j], back * 0.0625f, of[c / GS]));
       }
     }
   __syncthreads();
   // the part's place for partial sums: the share's first item, or its last
   const int64_t slot = 2 * (int64_t)blockIdx.x + (left == share ? 0 : 1);
   for (int r = warp; r < w.rows; r += kWarps) {
-    const int token = (r0 + r) / p.shared, h = head * p.shared + (r0 + r) - token * p.shared;
+    const int token = token_of(p, r0 + r), h = head * p.shared + (r0 + r) - token * p.shared;
     const int64_t t = w.first + token;
     if (t < 0 || t >= p.tokens) continue;
     float top = kNone, total = 0.f, f[kWarps];
@@ -735,7 +795,7 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 2 : 1) attn4
       for (int k = 0; k < kWarps; ++k) o = __fmaf_rn(sums[(k * Z::kRows + r) * Z::kSums + ch], f[k], o);
       o *= over;
       if (total != total) o = total;
-      if (cut) p.part[(slot * Z::kRows + r) * p.c.d + ch] = o;
+      if (cut) p.part[(slot * Z::kRows + r) * p.part_row + ch] = o;
       else p.out[t * p.out_token + h * p.out_head + ch] = narrow(p, o);
     }
     if (lane == 0) {
