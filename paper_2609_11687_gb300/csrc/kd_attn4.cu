@@ -11,79 +11,85 @@ namespace {
 
 constexpr int kJoinThreads = 256;
 
-// A block for each CTA's cut item.  First the parts' weights, from their maxima, for all rows; then a thread has four
-// channels of a row and adds the parts in order, its loads independent of each other.
-__global__ void __launch_bounds__(kJoinThreads) attn4_join_kernel(const __grid_constant__ Params p, int of_block) {
-  extern __shared__ float weights[];  // [part][row], then a row's maxima and sums
+// A block for each CTA's cut item, eight rows and 128 channels at a time: a warp takes every eighth part with a
+// running maximum of each row, all its loads independent of each other; then the warps' sums are joined in
+// their order.
+__global__ void __launch_bounds__(kJoinThreads) attn4_join_kernel(const __grid_constant__ Params p) {
+  constexpr int kJoinWarps = kJoinThreads / 32;
+  __shared__ float4 sums[kJoinWarps][kRows][32];
+  __shared__ float2 ml[kJoinWarps][kRows];
   depend_on_last();
   const Cut c = p.cuts[blockIdx.x];
   if (c.more == 0) return;
-  const int parts = c.more + 1, lane = threadIdx.x & 31;
-  float* totals = weights + (gridDim.x + 1) * of_block;
-  // part k's rows: the item's first place, then the first ones of the CTAs that follow
-  auto first_row = [&](int k) { return (int64_t)(k ? 2 * ((int)blockIdx.x + k) : c.slot) * of_block; };
-  for (int r = threadIdx.x >> 5; r < c.rows; r += kJoinThreads / 32) {
-    float top = kNone;
-    for (int k = lane; k < parts; k += 32) top = fmaxf(top, p.part_ml[first_row(k) + r].x);
+  const int parts = c.more + 1, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int c0 = 0; c0 < p.part_row; c0 += 128) {
+      const bool has = c0 + 4 * lane < p.part_row;
+      float4 o[kRows];
+      float2 at[kRows];
 #pragma unroll
-    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-    float total = 0.f;
-    for (int k = lane; k < parts; k += 32) {
-      const float2 v = p.part_ml[first_row(k) + r];
-      const float f = v.x == kNone ? 0.f : exp2_of(v.x - top);
-      total += v.x == kNone ? v.y : v.y * f;
-      weights[k * of_block + r] = f;
-    }
+      for (int r = 0; r < kRows; ++r) {
+        o[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+        at[r] = make_float2(kNone, 0.f);
+      }
+      for (int k = warp; k < parts; k += kJoinWarps) {
+        // the part's rows: in the item's first place, or the first one of a CTA that follows
+        const int64_t row = (int64_t)(k ? 2 * ((int)blockIdx.x + k) : c.slot) * kRows;
+        float4 v[kRows];
+        float2 n[kRows];
 #pragma unroll
-    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
-    if (lane == 0) {
-      totals[r] = total;
-      const int in = c.block * of_block + r, token = token_of(p, in);
+        for (int r = 0; r < kRows; ++r)
+          if (r < c.rows) {
+            n[r] = p.part_ml[row + r];
+            v[r] = has ? *reinterpret_cast<const float4*>(p.part + (row + r) * p.part_row + c0 + 4 * lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+          if (r < c.rows) {
+            const float top = fmaxf(at[r].x, n[r].x);
+            const float f = at[r].x == kNone ? 0.f : exp2_of(at[r].x - top), g = n[r].x == kNone ? 0.f : exp2_of(n[r].x - top);
+            at[r].y = __fmaf_rn(at[r].y, at[r].x == kNone ? 1.f : f, n[r].y * (n[r].x == kNone ? 1.f : g));  // without a maximum: 0, or NaN
+            at[r].x = top;
+            o[r].x = __fmaf_rn(v[r].x, g, o[r].x * f);
+            o[r].y = __fmaf_rn(v[r].y, g, o[r].y * f);
+            o[r].z = __fmaf_rn(v[r].z, g, o[r].z * f);
+            o[r].w = __fmaf_rn(v[r].w, g, o[r].w * f);
+          }
+      }
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        sums[warp][r][lane] = o[r];
+        if (lane == 0) ml[warp][r] = at[r];
+      }
+      __syncthreads();
+      const int r = warp;  // a row of a warp
+      const int in = c.block * kRows + r, token = token_of(p, in), h = c.head * p.shared + in - token * p.shared;
       const int64_t t = c.first + token;
-      if (p.lse && t >= 0 && t < p.tokens)
-        p.lse[t * p.heads + c.head * p.shared + in - token * p.shared] =
-            total == 0.f ? kNone : (top + log2f(total)) * 0.693147180559945f;
-    }
-  }
-  __syncthreads();
-  const int quads = (p.c.d + 3) / 4;
-  for (int i = threadIdx.x; i < c.rows * quads; i += kJoinThreads) {
-    const int r = i / quads, ch = 4 * (i - r * quads);
-    const int in = c.block * of_block + r, token = in / p.shared, h = c.head * p.shared + in - token * p.shared;
-    const int64_t t = c.first + token;
-    if (t < 0 || t >= p.tokens) continue;
-    float o[4] = {0.f, 0.f, 0.f, 0.f};
-    const float* from = p.part + (int64_t)r * p.part_row + ch;
-    const int64_t apart = (int64_t)of_block * p.part_row;  // of two places
-    constexpr int kAhead = 8;
-    for (int k0 = 0; k0 < parts; k0 += kAhead) {
-      float4 v[kAhead];
+      if (r < c.rows && t >= 0 && t < p.tokens) {
+        float top = kNone, total = 0.f;
+        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const int n = min(k0 + k, parts - 1);
-        v[k] = *reinterpret_cast<const float4*>(from + apart * (n ? 2 * ((int)blockIdx.x + n) : c.slot));
+        for (int k = 0; k < kJoinWarps; ++k) top = fmaxf(top, ml[k][r].x);
+#pragma unroll
+        for (int k = 0; k < kJoinWarps; ++k) {
+          const float2 n = ml[k][r];
+          const float f = n.x == kNone ? 0.f : exp2_of(n.x - top);
+          total += n.y * (n.x == kNone ? 1.f : f);
+          const float4 v = sums[k][r][lane];
+          y.x = __fmaf_rn(v.x, f, y.x);
+          y.y = __fmaf_rn(v.y, f, y.y);
+          y.z = __fmaf_rn(v.z, f, y.z);
+          y.w = __fmaf_rn(v.w, f, y.w);
+        }
+        if (has) put(p, p.out + t * p.out_token + h * p.out_head, c0 + 4 * lane, y, total);
+        if (lane == 0 && c0 == 0) put_lse(p, t * p.heads + h, top, total);
       }
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const float f = k0 + k < parts ? weights[(k0 + k) * of_block + r] : 0.f;
-        if (k0 + k >= parts) continue;
-        o[0] = __fmaf_rn(v[k].x, f, o[0]);
-        o[1] = __fmaf_rn(v[k].y, f, o[1]);
-        o[2] = __fmaf_rn(v[k].z, f, o[2]);
-        o[3] = __fmaf_rn(v[k].w, f, o[3]);
-      }
+      __syncthreads();
     }
-    const float total = totals[r], over = total == 0.f ? 0.f : 1.f / total;
-    uint16_t* out = p.out + t * p.out_token + h * p.out_head + ch;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (ch + e < p.c.d) out[e] = narrow(p, total != total ? total : o[e] * over);
-  }
 }
 
 struct Plan {
-  int nc, gs, nt;  // of the kernel: 32-channel pieces, of a group; blocks of eight rows
-  int row_blocks, whole;
+  int nc, gs;  // of the kernel: 32-channel pieces, of a group
+  int row_blocks, team;
   int grid;          // CTAs
   size_t workspace;  // bytes
 };
@@ -96,8 +102,7 @@ bool plan(const kd_cache4* c, const kd_sequences* s, int64_t heads, int64_t wind
   const int chunks = (int)((c->d + 31) / 32);
   pl.nc = chunks;
   pl.gs = (int)(c->group / 32);
-  pl.nt = s->most * shared > 8 && pl.nc <= 4 ? 2 : 1;
-  const int64_t blocks = (s->most * shared + 8 * pl.nt - 1) / (8 * pl.nt);
+  const int64_t blocks = (s->most * shared + kRows - 1) / kRows;
   const int64_t items = s->seqs * c->heads;
   // chunks of positions of all items together, were all as long as the table has room for
   auto chunks_of = [&](int64_t positions) { return std::max<int64_t>(1, (positions + kTile * kChunk - 1) / (kTile * kChunk) + 1); };
@@ -107,12 +112,23 @@ bool plan(const kd_cache4* c, const kd_sequences* s, int64_t heads, int64_t wind
     return false;
   pl.row_blocks = (int)blocks;
   int64_t longest = std::min(s->longest, room);
-  if (window > 0) longest = std::min(longest, window + 8 * pl.nt + kTile);
-  const int64_t all = items * blocks, places = 152 * (pl.nt == 1 && pl.nc <= 4 ? 4 : 2);
-  pl.whole = longest <= 2 * kTile * kChunk;
-  pl.grid = (int)(pl.whole ? all : std::min(places, all * chunks_of(longest)));
+  if (window > 0) longest = std::min(longest, window + kRows + kTile);
+  const int64_t all = items * blocks, places = 152 * (pl.nc <= 4 ? 4 : 2);
+  const double chunks_each = (double)((longest + kTile * kChunk - 1) / (kTile * kChunk));
+  // us: a CTA's step by how many share an SM, and a tile of equal shares
+  pl.team = 0;
+  double least = 13 + (all < 64 ? 4 : 0) + 0.8 * 0.0036 * all * chunks_each;
+  for (int team = 1; team <= 8 && team <= chunks_each; team *= 2) {
+    const double rounds = std::ceil((double)all * team / places), on_sm = std::min((double)all * team, (double)places) / 152;
+    const double cost = 4.5 + (team > 1 ? 1.2 : 0) + rounds * std::ceil(chunks_each / team) * std::max(0.86, 0.5 + 0.38 * on_sm);
+    if (cost < least) {
+      least = cost;
+      pl.team = team;
+    }
+  }
+  pl.grid = (int)(pl.team ? all * pl.team : std::min(places, all * chunks_of(longest)));
   pl.workspace = 0;
-  if (!pl.whole) pl.workspace = (size_t)pl.grid * (sizeof(Cut) + 2 * (8 * pl.nt) * (8 + 4 * (size_t)((c->d + 3) / 4 * 4)));
+  if (!pl.team) pl.workspace = (size_t)pl.grid * (sizeof(Cut) + 2 * kRows * (8 + 4 * (size_t)((c->d + 3) / 4 * 4)));
   pl.workspace = (pl.workspace + 15) / 16 * 16;
   return true;
 }
@@ -174,7 +190,7 @@ extern "C" kd_status kd_attention_4bit(const kd_cache4* cache, const kd_sequence
   p.heads = (int)heads;
   p.shared = (int)(heads / cache->heads);
   p.row_blocks = pl.row_blocks;
-  p.whole = pl.whole;
+  p.team = pl.team;
   p.part_row = (int)((cache->d + 3) / 4 * 4);
   p.causal = causal != 0;
   p.window = (int)window;
@@ -184,29 +200,26 @@ extern "C" kd_status kd_attention_4bit(const kd_cache4* cache, const kd_sequence
     if (cache->page == (int64_t)kTile << log) p.page_log = log;
   p.bf16 = dtype == KD_BF16;
   p.q_vec = cache->d % 8 == 0 && aligned(q, 16) && (tokens == 1 || q_token % 8 == 0) && (heads == 1 || q_head % 8 == 0);
+  p.out_vec = cache->d % 4 == 0 && aligned(out, 8) && (tokens == 1 || out_token % 4 == 0) && (heads == 1 || out_head % 4 == 0);
   p.scale2 = scale * 1.4426950408889634f;
-  if (!pl.whole) {
+  if (!pl.team) {
     p.cuts = static_cast<Cut*>(workspace);
     p.part_ml = reinterpret_cast<float2*>(p.cuts + pl.grid);
-    p.part = reinterpret_cast<float*>(p.part_ml + (int64_t)pl.grid * 2 * (8 * pl.nt));
+    p.part = reinterpret_cast<float*>(p.part_ml + (int64_t)pl.grid * 2 * kRows);
   }
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t e = pl.nc <= 2   ? launch_small(p, pl.nc, pl.gs, pl.nt, pl.grid, s)
-                  : pl.nc == 3 ? launch_96(p, pl.gs, pl.nt, pl.grid, s)
-                  : pl.nc == 4 ? launch_128(p, pl.gs, pl.nt, pl.grid, s)
-                  : pl.nc <= 6 ? launch_192(p, pl.nc, pl.gs, pl.grid, s)
-                               : launch_256(p, pl.nc, pl.gs, pl.grid, s);
-  if (e == cudaSuccess && !pl.whole) {
+  auto launch = pl.team ? (pl.nc <= 4 ? launch_team_128 : launch_team_256) : (pl.nc <= 4 ? launch_shares_128 : launch_shares_256);
+  cudaError_t e = launch(p, pl.nc, pl.gs, pl.grid, s);
+  if (e == cudaSuccess && !pl.team) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)pl.grid);
     cfg.blockDim = dim3(kJoinThreads);
-    cfg.dynamicSmemBytes = (size_t)(pl.grid + 2) * (8 * pl.nt) * sizeof(float);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     launch_early(attr[0]);
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, attn4_join_kernel, p, 8 * pl.nt);
+    e = cudaLaunchKernelEx(&cfg, attn4_join_kernel, p);
   }
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? KD_OK : KD_ERR_CUDA;
 }

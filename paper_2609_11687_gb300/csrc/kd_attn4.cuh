@@ -36,6 +36,8 @@
 // number of 16-byte pieces apart there, so that reads for both products are free of bank conflicts.  Where
 // sequences are few their positions are split over CTAs and joined by a second launch.
 #pragma once
+#include <cooperative_groups.h>
+
 #include <atomic>
 
 #include "kd_cache4.cuh"
@@ -46,6 +48,7 @@ namespace attn4 {
 using namespace cache4;
 
 constexpr int kWarps = 4;
+constexpr int kRows = 8;      // of a block: columns of a tensor-core tile
 constexpr int kTile = 16;     // positions of a tensor-core tile, all on one page
 constexpr int kTiles = 2;     // of one step of a warp
 constexpr int kChunk = kTiles * kWarps;  // tiles of one step of a CTA: what work is shared out in
@@ -60,11 +63,12 @@ struct Params {
   int64_t tokens;
   int heads, shared;            // query heads; of one key head
   int row_blocks;               // of a sequence: blocks of rows
-  int whole;                    // a CTA has an item (sequence, key head, block of rows) to itself; else all CTAs equal shares
+  int team;                     // CTAs of a cluster that has an item (sequence, key head, block of rows) to itself;
+                                // 0: all CTAs have equal shares of all of them
   int causal, window;
   int room;                     // positions that the table has room for
   int page_log;                 // of a page's tiles, where that is a power of two, else -1
-  int bf16, q_vec;
+  int bf16, q_vec, out_vec;
   float scale2;                 // scale log2 e
   struct Cut* cuts;             // the item that each CTA leaves to the next ones
   float2* part_ml;              // (m, sum) of each row of a CTA's first item and of its last, where they are cut
@@ -220,11 +224,11 @@ __device__ __forceinline__ float high_half(uint32_t w) { return __half2float(__u
 
 constexpr float kNone = -__builtin_inff();
 
-// NC: 32-channel pieces of a row; GS: of a group; NT: blocks of eight rows
-template <int NC, int GS, int NT>
+// NC: 32-channel pieces of a row; GS: of a group
+template <int NC, int GS>
 struct Shape {
   static constexpr int kGroups = (NC + GS - 1) / GS;
-  static constexpr int kRows = 8 * NT;
+  static constexpr int kRows = attn4::kRows;
   static constexpr int kStages = NC <= 4 ? 2 : 2;
   static constexpr int kStride = 4 * (NC | 1);                       // words of a row of codes in the ring
   // words of a stage, keys or values
@@ -268,9 +272,68 @@ __device__ __forceinline__ int sum_before(int v, int* scratch, int& total) {
   return before;
 }
 
-template <int NC, int GS, int NT>
-__global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 4 : 2) attn4_kernel(const __grid_constant__ Params p) {
-  using Z = Shape<NC, GS, NT>;
+// four channels of a row from ch on, over the row's total (0: nothing was seen)
+__device__ __forceinline__ void put(const Params& p, uint16_t* out, int ch, float4 v, float total) {
+  const float over = total == 0.f ? 0.f : 1.f / total;
+  const float of[4] = {v.x * over, v.y * over, v.z * over, v.w * over};
+  uint16_t bits[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) bits[e] = narrow(p, total != total ? total : of[e]);
+  if (p.out_vec) {
+    *reinterpret_cast<uint2*>(out + ch) = make_uint2(bits[0] | (uint32_t)bits[1] << 16, bits[2] | (uint32_t)bits[3] << 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (ch + e < p.c.d) out[ch + e] = bits[e];
+  }
+}
+__device__ __forceinline__ void put_lse(const Params& p, int64_t at, float top, float total) {
+  if (p.lse) p.lse[at] = total == 0.f ? kNone : (top + log2f(total)) * 0.693147180559945f;
+}
+
+// Joins the parts of a cluster's CTAs, which lie in the first rows of their `sums` and `ml` (where a CTA has any),
+// in the order of their ranks; a row is one CTA's.
+template <class Z>
+__device__ __forceinline__ void join_team(const Params& p, const Work& w, int head, int block, bool any, float* sums, float2* ml) {
+  namespace cg = cooperative_groups;
+  cg::cluster_group cl = cg::this_cluster();
+  if (!any)
+    for (int r = threadIdx.x; r < Z::kRows; r += 32 * kWarps) ml[r] = make_float2(kNone, 0.f);
+  cl.sync();
+  const int rank = special<kRank>(), quads = p.part_row / 4;
+  for (int i = threadIdx.x;; i += 32 * kWarps) {
+    const int nth = i / quads, r = rank + nth * p.team, ch = 4 * (i - nth * quads);
+    if (r >= w.rows) break;
+    const int in = block * Z::kRows + r, token = token_of(p, in), h = head * p.shared + in - token * p.shared;
+    const int64_t t = w.first + token;
+    if (t < 0 || t >= p.tokens) continue;
+    float top = kNone, total = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = 0; k < p.team; ++k) top = fmaxf(top, cl.map_shared_rank(ml, k)[r].x);
+    for (int k = 0; k < p.team; ++k) {
+      const float2 n = cl.map_shared_rank(ml, k)[r];
+      if (n.x == kNone) {  // no sums there, or NaN
+        total += n.y;
+        continue;
+      }
+      const float f = exp2_of(n.x - top);
+      total += n.y * f;
+      const float4 v = *reinterpret_cast<const float4*>(cl.map_shared_rank(sums, k) + r * Z::kSums + ch);
+      o.x = __fmaf_rn(v.x, f, o.x);
+      o.y = __fmaf_rn(v.y, f, o.y);
+      o.z = __fmaf_rn(v.z, f, o.z);
+      o.w = __fmaf_rn(v.w, f, o.w);
+    }
+    put(p, p.out + t * p.out_token + h * p.out_head, ch, o, total);
+    if (ch == 0) put_lse(p, t * p.heads + h, top, total);
+  }
+  cl.sync();  // no CTA leaves while its sums are read
+}
+
+// TEAM: a cluster of p.team CTAs has an item to itself; else all CTAs have equal shares of all of them
+template <int NC, int GS, bool TEAM>
+__global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(const __grid_constant__ Params p) {
+  using Z = Shape<NC, GS>;
   constexpr int GN = Z::kGroups, ST = Z::kStages, S = Z::kStride;
   extern __shared__ uint4 smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g8 = lane >> 2, t4 = lane & 3;
@@ -286,8 +349,8 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 4 : 2) attn4
 
   // This CTA's share: `left` chunks from chunk `chunk` of item (s, head, block) on.
   int s, head, block, chunk = 0, left;
-  if (p.whole) {
-    int at = blockIdx.x;
+  if constexpr (TEAM) {
+    int at = special<kCluster>();
     block = at % p.row_blocks;
     at /= p.row_blocks;
     head = at % p.c.heads;
@@ -349,9 +412,15 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 4 : 2) attn4
 
   for (;;) {
   const Work w = work_of(p, s, block, Z::kRows);
+  if constexpr (TEAM) {
+    if (w.rows == 0) return;
+    left = (w.chunks + p.team - 1) / p.team;
+    chunk = special<kRank>() * left;
+  }
   const int n_chunks = min(w.chunks - chunk, left);
+  // only a part of the item; in a cluster the same for all its CTAs, of which all or none take part in the join
+  const bool cut = (TEAM ? left : n_chunks) < w.chunks;
   if (n_chunks > 0) {
-  const bool cut = n_chunks < w.chunks;  // only a part of the item
   const int first_tile = w.tile + chunk * kChunk, tiles = min(n_chunks * kChunk, w.tiles - chunk * kChunk);
   const int share_hi = min(w.hi, (first_tile + tiles) * kTile);  // where the part's positions end
 
@@ -416,38 +485,35 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 4 : 2) attn4
     if (lane == 0) query_sums[r * (GN + 1) + GN] = __uint_as_float((uint32_t)(e2 + 127) << 23) * p.scale2;
   }
   __syncthreads();
-  uint32_t qb[2 * NC][NT][2];
+  uint32_t qb[2 * NC][2];
   // of columns 2 t4, 2 t4 + 1: power of two of the row, and its sums over groups, both times scale log2 e
-  float qs[GN][NT][2], qe[NT][2];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
+  float qs[GN][2], qe[2];
+  {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      const uint4 u = *reinterpret_cast<const uint4*>(queries + (8 * nt + g8) * Z::kQueries + 16 * (4 * c + t4));
-      qb[2 * c][nt][0] = u.x;
-      qb[2 * c][nt][1] = u.y;
-      qb[2 * c + 1][nt][0] = u.z;
-      qb[2 * c + 1][nt][1] = u.w;
+      const uint4 u = *reinterpret_cast<const uint4*>(queries + (g8) * Z::kQueries + 16 * (4 * c + t4));
+      qb[2 * c][0] = u.x;
+      qb[2 * c][1] = u.y;
+      qb[2 * c + 1][0] = u.z;
+      qb[2 * c + 1][1] = u.w;
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const float* of_column = query_sums + (8 * nt + 2 * t4 + j) * (GN + 1);
+      const float* of_column = query_sums + (2 * t4 + j) * (GN + 1);
       const float down = of_column[GN];
 #pragma unroll
-      for (int g = 0; g < GN; ++g) qs[g][nt][j] = of_column[g] * down;
-      qe[nt][j] = down * 1024.f;  // codes' 2^24 less q's 2^14
+      for (int g = 0; g < GN; ++g) qs[g][j] = of_column[g] * down;
+      qe[j] = down * 1024.f;  // codes' 2^24 less q's 2^14
     }
   }
   // what the columns' rows see: positions from sees_lo on, below sees_hi
-  int sees_lo[NT][2], sees_hi[NT][2];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
+  int sees_lo[2], sees_hi[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int r = 8 * nt + 2 * t4 + j;
+      const int r = 2 * t4 + j;
       const int pos = w.before + token_of(p, r0 + r);
-      sees_hi[nt][j] = r >= w.rows ? 0 : min(share_hi, p.causal ? clamp_to(pos + 1, w.length) : w.length);
-      sees_lo[nt][j] = p.window ? clamp_to(pos + 1 - p.window, w.length) : 0;
+      sees_hi[j] = r >= w.rows ? 0 : min(share_hi, p.causal ? clamp_to(pos + 1, w.length) : w.length);
+      sees_lo[j] = p.window ? clamp_to(pos + 1 - p.window, w.length) : 0;
     }
 
   const char* src[4] = {reinterpret_cast<const char*>(p.c.codes[0]) + lane * 16, reinterpret_cast<const char*>(p.c.codes[1]) + lane * 16,
@@ -473,22 +539,21 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 4 : 2) attn4
     }
   };
 
-  float acc[Z::kSumTiles][NT][4];
+  float acc[Z::kSumTiles][4];
   // of the columns: sums of weights times middles and of weights (of the positions g8 and g8 + 8 of the tiles
   // apart), m (0 before the first), and how far above it a score may lie (nothing may, before the first)
-  float2 mids[GN][NT][2], sum[NT][2];
-  float m[NT][2], room[NT][2];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
+  float2 mids[GN][2], sum[2];
+  float m[2], room[2];
+  {
 #pragma unroll
     for (int i = 0; i < Z::kSumTiles; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[i][nt][e] = 0.f;
+      for (int e = 0; e < 4; ++e) acc[i][e] = 0.f;
 #pragma unroll
-    for (int g = 0; g < GN; ++g) mids[g][nt][0] = mids[g][nt][1] = make_float2(0.f, 0.f);
-    m[nt][0] = m[nt][1] = 0.f;
-    room[nt][0] = room[nt][1] = kNone;
-    sum[nt][0] = sum[nt][1] = make_float2(0.f, 0.f);
+    for (int g = 0; g < GN; ++g) mids[g][0] = mids[g][1] = make_float2(0.f, 0.f);
+    m[0] = m[1] = 0.f;
+    room[0] = room[1] = kNone;
+    sum[0] = sum[1] = make_float2(0.f, 0.f);
   }
   float step_cap = 0.f;  // no step so far lies above
   float step_up = 1.f;   // the power of two of the values' weights: step_cap becomes 2^6
@@ -500,17 +565,15 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 4 : 2) attn4
     const uint32_t codes = ring_at + stage * (Z::kStage * 4) + matrix_at;
     const uint32_t* kp = ring + stage * Z::kStage + 2 * Z::kCodes + g8 * GN;
     const uint32_t* vp = kp + Z::kScales;
-    float x[kTiles][NT][4];  // scores less m
-    bool seen[kTiles][NT][4];
+    float x[kTiles][4];  // scores less m
+    bool seen[kTiles][4];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
-      float part[NT][4], low[NT][4];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      float part[4], low[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          x[i][nt][e] = 0.f;
-          low[nt][e] = -m[nt][e & 1];
+          x[i][e] = 0.f;
+          low[e] = -m[e & 1];
         }
       uint32_t w[4];  // positions g8, g8 + 8 of one piece, and of the next
 #pragma unroll
@@ -523,10 +586,9 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 4 : 2) attn4
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const uint32_t a0 = a & 0x000F000Fu, a1 = b & 0x000F000Fu, a2 = a & 0x00F000F0u, a3 = b & 0x00F000F0u;
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            if (c % GS == 0 && h == 0) mma_first(part[nt], a0, a1, a2, a3, qb[2 * c][nt][0], qb[2 * c][nt][1]);
-            else mma(part[nt], a0, a1, a2, a3, qb[2 * c + h][nt][0], qb[2 * c + h][nt][1]);
+          {
+            if (c % GS == 0 && h == 0) mma_first(part, a0, a1, a2, a3, qb[2 * c][0], qb[2 * c][1]);
+            else mma(part, a0, a1, a2, a3, qb[2 * c + h][0], qb[2 * c + h][1]);
           }
           a >>= 8;
           b >>= 8;
@@ -535,27 +597,23 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 4 : 2) attn4
           const uint32_t u = kp[i * kTile * GN + c / GS], v = kp[(i * kTile + 8) * GN + c / GS];
           const float s0 = low_half(u), l0 = high_half(u), s1 = low_half(v), l1 = high_half(v);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
             for (int e = 0; e < 4; ++e) {
-              x[i][nt][e] = __fmaf_rn(e < 2 ? s0 : s1, part[nt][e], x[i][nt][e]);
-              low[nt][e] = __fmaf_rn(e < 2 ? l0 : l1, qs[c / GS][nt][e & 1], low[nt][e]);
+              x[i][e] = __fmaf_rn(e < 2 ? s0 : s1, part[e], x[i][e]);
+              low[e] = __fmaf_rn(e < 2 ? l0 : l1, qs[c / GS][e & 1], low[e]);
             }
         }
       }
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
         for (int e = 0; e < 4; e += 2) {
-          const float2 of = fma2(make_float2(x[i][nt][e], x[i][nt][e + 1]), make_float2(qe[nt][0], qe[nt][1]), make_float2(low[nt][e], low[nt][e + 1]));
-          x[i][nt][e] = of.x;
-          x[i][nt][e + 1] = of.y;
+          const float2 of = fma2(make_float2(x[i][e], x[i][e + 1]), make_float2(qe[0], qe[1]), make_float2(low[e], low[e + 1]));
+          x[i][e] = of.x;
+          x[i][e + 1] = of.y;
           if constexpr (EDGE) {
             const int pos = position + kTile * i + g8 + 4 * e;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              seen[i][nt][e + j] = pos < sees_hi[nt][j] && pos >= sees_lo[nt][j];
-              x[i][nt][e + j] = !seen[i][nt][e + j] ? kNone : (i ? bad1 : bad0) ? __int_as_float(0x7FC00000) : x[i][nt][e + j];
+              seen[i][e + j] = pos < sees_hi[j] && pos >= sees_lo[j];
+              x[i][e + j] = !seen[i][e + j] ? kNone : (i ? bad1 : bad0) ? __int_as_float(0x7FC00000) : x[i][e + j];
             }
           }
         }
@@ -578,13 +636,11 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 4 : 2) attn4
         }
     float top = __low2float(tops);
     bool grow = top > step_cap;
-    float most[NT][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    float most[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        most[nt][j] = fmaxf(fmaxf(x[0][nt][j], x[0][nt][j + 2]), fmaxf(x[1][nt][j], x[1][nt][j + 2]));
-        grow |= most[nt][j] > room[nt][j];
+        most[j] = fmaxf(fmaxf(x[0][j], x[0][j + 2]), fmaxf(x[1][j], x[1][j + 2]));
+        grow |= most[j] > room[j];
       }
     if (__any_sync(~0u, grow)) {
       float by_step = 1.f;
@@ -598,74 +654,69 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 4 : 2) attn4
         step_up = up;
       }
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
         for (int j = 0; j < 2; ++j) {
-          float to = most[nt][j];
+          float to = most[j];
           to = fmaxf(to, __shfl_xor_sync(~0u, to, 4));
           to = fmaxf(to, __shfl_xor_sync(~0u, to, 8));
           to = fmaxf(to, __shfl_xor_sync(~0u, to, 16));
-          const bool fresh = room[nt][j] == kNone;
+          const bool fresh = room[j] == kNone;
           if (!fresh) to = fmaxf(to, 0.f);
           if (to == kNone) continue;  // nothing seen yet; the sums are 0
           // m moves up by `to`; a first one by whatever it is
           const float f = fresh ? 0.f : exp2_of(-to), fs = f * by_step;
           const float2 ff = make_float2(f, f);
-          m[nt][j] += to;
-          room[nt][j] = 8.f;
+          m[j] += to;
+          room[j] = 8.f;
 #pragma unroll
           for (int i = 0; i < kTiles; ++i) {
-            x[i][nt][j] -= to;
-            x[i][nt][j + 2] -= to;
+            x[i][j] -= to;
+            x[i][j + 2] -= to;
           }
-          sum[nt][j] = mul2(sum[nt][j], ff);
+          sum[j] = mul2(sum[j], ff);
 #pragma unroll
-          for (int g = 0; g < GN; ++g) mids[g][nt][j] = mul2(mids[g][nt][j], ff);
+          for (int g = 0; g < GN; ++g) mids[g][j] = mul2(mids[g][j], ff);
 #pragma unroll
           for (int i = 0; i < Z::kSumTiles; ++i) {
-            acc[i][nt][j] *= fs;
-            acc[i][nt][j + 2] *= fs;
+            acc[i][j] *= fs;
+            acc[i][j + 2] *= fs;
           }
         }
     }
     // weights, and the operands of the values
-    uint32_t bw[kTiles][GN][NT][2];
-    float all[GN][NT][4];  // of each column, in every row: 2^-24 of the step's weights as they are rounded
+    uint32_t bw[kTiles][GN][2];
+    float all[GN][4];  // of each column, in every row: 2^-24 of the step's weights as they are rounded
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
-      float2 wt[NT][2];  // of a column, positions g8 and g8 + 8
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      float2 wt[2];  // of a column, positions g8 and g8 + 8
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          wt[nt][j] = make_float2(exp2_of(x[i][nt][j]), exp2_of(x[i][nt][j + 2]));
-          sum[nt][j] = add2(sum[nt][j], wt[nt][j]);
+          wt[j] = make_float2(exp2_of(x[i][j]), exp2_of(x[i][j + 2]));
+          sum[j] = add2(sum[j], wt[j]);
         }
 #pragma unroll
       for (int g = 0; g < GN; ++g) {
         const float2 step = make_float2(low_half(vscale[i][g][0]), low_half(vscale[i][g][1]));
         const float2 mid = fma2(make_float2(8.f, 8.f), step, make_float2(high_half(vscale[i][g][0]), high_half(vscale[i][g][1])));
         const float2 up = mul2(step, make_float2(step_up, step_up));
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        {
           float2 b[2];
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            b[j] = mul2(wt[nt][j], up);
+            b[j] = mul2(wt[j], up);
             if constexpr (EDGE) {  // whatever stands where a row does not see: 0
-              b[j].x = seen[i][nt][j] ? b[j].x : 0.f;
-              b[j].y = seen[i][nt][j + 2] ? b[j].y : 0.f;
-              const float2 of = make_float2(seen[i][nt][j] ? mid.x : 0.f, seen[i][nt][j + 2] ? mid.y : 0.f);
-              mids[g][nt][j] = fma2(wt[nt][j], of, mids[g][nt][j]);
+              b[j].x = seen[i][j] ? b[j].x : 0.f;
+              b[j].y = seen[i][j + 2] ? b[j].y : 0.f;
+              const float2 of = make_float2(seen[i][j] ? mid.x : 0.f, seen[i][j + 2] ? mid.y : 0.f);
+              mids[g][j] = fma2(wt[j], of, mids[g][j]);
             } else {
-              mids[g][nt][j] = fma2(wt[nt][j], mid, mids[g][nt][j]);
+              mids[g][j] = fma2(wt[j], mid, mids[g][j]);
             }
           }
-          bw[i][g][nt][0] = turned(pack2<KD_F16>(b[0].x, b[1].x));
-          bw[i][g][nt][1] = turned(pack2<KD_F16>(b[0].y, b[1].y));
+          bw[i][g][0] = turned(pack2<KD_F16>(b[0].x, b[1].x));
+          bw[i][g][1] = turned(pack2<KD_F16>(b[0].y, b[1].y));
           constexpr uint32_t one = 0x00010001u;
-          if (i == 0) mma_first(all[g][nt], one, one, one, one, bw[i][g][nt][0], bw[i][g][nt][1]);
-          else mma(all[g][nt], one, one, one, one, bw[i][g][nt][0], bw[i][g][nt][1]);
+          if (i == 0) mma_first(all[g], one, one, one, one, bw[i][g][0], bw[i][g][1]);
+          else mma(all[g], one, one, one, one, bw[i][g][0], bw[i][g][1]);
         }
       }
     }
@@ -673,10 +724,9 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 4 : 2) attn4
     for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float(&d)[4] = acc[2 * c + k][nt];
-          const float2 eight = make_float2(all[c / GS][nt][0], all[c / GS][nt][1]);
+        {
+          float(&d)[4] = acc[2 * c + k];
+          const float2 eight = make_float2(all[c / GS][0], all[c / GS][1]);
           const float2 even = fma2(eight, make_float2(-8.f, -8.f), make_float2(d[0], d[1]));
           const float2 both = fma2(eight, make_float2(-136.f, -136.f), make_float2(d[2], d[3]));
           d[0] = even.x;
@@ -700,10 +750,8 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 4 : 2) attn4
             a = __byte_perm(a, 0, 0x4341);
             b = __byte_perm(b, 0, 0x4341);
           }
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-            mma(acc[2 * c + k][nt], a & 0x000F000Fu, k ? a : a & 0x00FF00FFu, b & 0x000F000Fu, k ? b : b & 0x00FF00FFu,
-                bw[i][c / GS][nt][0], bw[i][c / GS][nt][1]);
+            mma(acc[2 * c + k], a & 0x000F000Fu, k ? a : a & 0x00FF00FFu, b & 0x000F000Fu, k ? b : b & 0x00FF00FFu,
+                bw[i][c / GS][0], bw[i][c / GS][1]);
         }
       }
     }
@@ -746,25 +794,23 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 4 : 2) attn4
   float* sums = reinterpret_cast<float*>(smem);
   const float back = 0x1p24f / step_up;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int r = 8 * nt + 2 * t4 + j;
-      float total = sum[nt][j].x + sum[nt][j].y, of[GN];
+      const int r = 2 * t4 + j;
+      float total = sum[j].x + sum[j].y, of[GN];
 #pragma unroll
-      for (int g = 0; g < GN; ++g) of[g] = mids[g][nt][j].x + mids[g][nt][j].y;
+      for (int g = 0; g < GN; ++g) of[g] = mids[g][j].x + mids[g][j].y;
 #pragma unroll
       for (int o = 4; o < 32; o *= 2) {
         total += __shfl_xor_sync(~0u, total, o);
 #pragma unroll
         for (int g = 0; g < GN; ++g) of[g] += __shfl_xor_sync(~0u, of[g], o);
       }
-      if (g8 == 0) ml[warp * Z::kRows + r] = make_float2(room[nt][j] == kNone ? kNone : m[nt][j], total);
+      if (g8 == 0) ml[warp * Z::kRows + r] = make_float2(room[j] == kNone ? kNone : m[j], total);
       float* to = sums + (warp * Z::kRows + r) * Z::kSums + 4 * g8;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {  // even channels, and these plus 16 times the odd ones
-        const float(&d0)[4] = acc[2 * c][nt];
-        const float(&d1)[4] = acc[2 * c + 1][nt];
+        const float(&d0)[4] = acc[2 * c];
+        const float(&d1)[4] = acc[2 * c + 1];
         *reinterpret_cast<float4*>(to + 32 * c) =
             make_float4(__fmaf_rn(d0[j], back, of[c / GS]), __fmaf_rn(d0[j + 2] - d0[j], back * 0.0625f, of[c / GS]),
                         __fmaf_rn(d1[j], back, of[c / GS]), __fmaf_rn(d1[j + 2] - d1[j], back * 0.0625f, of[c / GS]));
@@ -787,30 +833,39 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 && NT == 1 ? 4 : 2) attn4
       total += v.x == kNone ? v.y : v.y * f[k];  // a warp without a maximum has summed nothing, or NaN
     }
     if (past_table(p, w, token)) total = __int_as_float(0x7FC00000);
-    const bool none = total == 0.f;
-    const float over = cut ? 1.f : none ? 0.f : 1.f / total;
-    for (int ch = lane; ch < p.c.d; ch += 32) {
-      float o = 0.f;
+    for (int ch = 4 * lane; ch < p.part_row; ch += 128) {
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int k = 0; k < kWarps; ++k) o = __fmaf_rn(sums[(k * Z::kRows + r) * Z::kSums + ch], f[k], o);
-      o *= over;
-      if (total != total) o = total;
-      if (cut) p.part[(slot * Z::kRows + r) * p.part_row + ch] = o;
-      else p.out[t * p.out_token + h * p.out_head + ch] = narrow(p, o);
+      for (int k = 0; k < kWarps; ++k) {
+        const float4 v = *reinterpret_cast<const float4*>(sums + (k * Z::kRows + r) * Z::kSums + ch);
+        o.x = __fmaf_rn(v.x, f[k], o.x);
+        o.y = __fmaf_rn(v.y, f[k], o.y);
+        o.z = __fmaf_rn(v.z, f[k], o.z);
+        o.w = __fmaf_rn(v.w, f[k], o.w);
+      }
+      if (!cut) put(p, p.out + t * p.out_token + h * p.out_head, ch, o, total);
+      else if (TEAM) *reinterpret_cast<float4*>(sums + r * Z::kSums + ch) = o;
+      else *reinterpret_cast<float4*>(p.part + (slot * Z::kRows + r) * p.part_row + ch) = o;
     }
+    __syncwarp();  // all lanes have read the warps' sums
     if (lane == 0) {
-      if (cut) p.part_ml[slot * Z::kRows + r] = make_float2(top, total);
-      else if (p.lse) p.lse[t * p.heads + h] = none ? kNone : (top + log2f(total)) * 0.693147180559945f;
+      if (!cut) put_lse(p, t * p.heads + h, top, total);
+      else if (TEAM) ml[r] = make_float2(top, total);
+      else p.part_ml[slot * Z::kRows + r] = make_float2(top, total);
     }
   }
-  if (cut && chunk == 0 && threadIdx.x == 0) {
+  if (cut && !TEAM && chunk == 0 && threadIdx.x == 0) {
     // the item goes on in the CTAs that follow
     const int rest = w.chunks - n_chunks;
     p.cuts[blockIdx.x] = Cut{w.first, block, head, w.rows, (int)slot, (rest + share - 1) / share, 0};
   }
   left -= n_chunks;
   }
-  if (p.whole || left <= 0) return;
+  if constexpr (TEAM) {
+    if (cut) join_team<Z>(p, w, head, block, n_chunks > 0, reinterpret_cast<float*>(smem), ml);
+    return;
+  }
+  if (left <= 0) return;
   // the next item
   chunk = 0;
   if (w.rows == 0 || ++block == p.row_blocks) {
@@ -835,39 +890,42 @@ cudaError_t allow_shared_memory(Kernel kernel, std::atomic<uint64_t>& ready) {
   return e;
 }
 
-template <int NC, int GS, int NT>
+template <int NC, int GS, bool TEAM>
 cudaError_t launch_one(const Params& p, int grid, cudaStream_t s) {
-  static_assert(Shape<NC, GS, NT>::kBytes <= 227 * 1024, "shared memory");
-  auto kernel = attn4_kernel<NC, GS, NT>;
+  static_assert(Shape<NC, GS>::kBytes <= 227 * 1024, "shared memory");
+  auto kernel = attn4_kernel<NC, GS, TEAM>;
   static std::atomic<uint64_t> ready{0};
   const cudaError_t e = allow_shared_memory(kernel, ready);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(32 * kWarps);
-  cfg.dynamicSmemBytes = Shape<NC, GS, NT>::kBytes;
+  cfg.dynamicSmemBytes = Shape<NC, GS>::kBytes;
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   launch_early(attr[0]);
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)p.team;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = p.team > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, p);
 }
-// gs: 32-channel pieces of a group; nt: blocks of eight rows
-template <int NC, int NT>
+// gs: 32-channel pieces of a group
+template <int NC, bool TEAM>
 cudaError_t launch(const Params& p, int gs, int grid, cudaStream_t s) {
   if constexpr (NC > 2)
-    if (gs == 4) return launch_one<NC, 4, NT>(p, grid, s);
+    if (gs == 4) return launch_one<NC, 4, TEAM>(p, grid, s);
   if constexpr (NC > 1)
-    if (gs >= 2) return launch_one<NC, 2, NT>(p, grid, s);
-  return launch_one<NC, 1, NT>(p, grid, s);
+    if (gs >= 2) return launch_one<NC, 2, TEAM>(p, grid, s);
+  return launch_one<NC, 1, TEAM>(p, grid, s);
 }
 
-cudaError_t launch_small(const Params& p, int nc, int gs, int nt, int grid, cudaStream_t s);  // up to 64 channels
-cudaError_t launch_96(const Params& p, int gs, int nt, int grid, cudaStream_t s);
-cudaError_t launch_128(const Params& p, int gs, int nt, int grid, cudaStream_t s);
-cudaError_t launch_192(const Params& p, int nc, int gs, int grid, cudaStream_t s);  // 129 to 192
-cudaError_t launch_256(const Params& p, int nc, int gs, int grid, cudaStream_t s);  // 193 to 256
+// nc: 32-channel pieces of a row, 1 to 4 and 5 to 8
+cudaError_t launch_team_128(const Params& p, int nc, int gs, int grid, cudaStream_t s);
+cudaError_t launch_team_256(const Params& p, int nc, int gs, int grid, cudaStream_t s);
+cudaError_t launch_shares_128(const Params& p, int nc, int gs, int grid, cudaStream_t s);
+cudaError_t launch_shares_256(const Params& p, int nc, int gs, int grid, cudaStream_t s);
 
 }  // namespace attn4
 }  // namespace kd

@@ -32,7 +32,7 @@ def kd():
 
 
 class Case:
-    def __init__(self, kd, lengths, counts, hq, hk, d, page=16, group=64, dt=F16, uniform=False, spare=0, seed=0, longest=None, steps=1.0):
+    def __init__(self, kd, lengths, counts, hq, hk, d, page=16, group=64, dt=F16, uniform=False, spare=0, seed=0, longest=None, steps=1.0, room=0):
         g = torch.Generator(device="cuda").manual_seed(seed + 7 * d + len(lengths))
         self.lengths, self.counts, self.hq, self.hk, self.d, self.page, self.group = lengths, counts, hq, hk, d, page, group
         seqs, wide = len(lengths), max(1, -(-max(max(lengths), 1) // page))
@@ -47,6 +47,9 @@ class Case:
             scales[..., 0] = step
             scales[..., 1] = step * (torch.randn(step.shape, generator=g, device="cuda") - 7.5)
         table = torch.randperm(pages, generator=g, device="cuda")[:seqs * wide].view(seqs, wide).int()
+        if room:  # a table for sequences of that length, of which no page is there yet
+            table = torch.cat((table, torch.full((seqs, room // page - wide), -1, dtype=torch.int32, device="cuda")), 1)
+            longest = room
         self.starts = np.concatenate(([0], np.cumsum(counts))).astype(int)
         most = max(counts)
         i32 = dict(dtype=torch.int32, device="cuda")
@@ -99,7 +102,7 @@ class Case:
             o = torch.einsum("nhgl,lhd->nhgd", w, v)
             t = eps * o.abs() * 1.001 + 2.0 ** -11 * torch.einsum("nhgl,lhd->nhgd", w, (v - v0).abs()) \
                 + (2 * delta + 2.0 ** -20) * torch.einsum("nhgl,lhd->nhgd", w, v.abs() + v0.abs() + 7.5 * vstep) \
-                + seen.sum(1)[:, None, None, None] * 2.0 ** -27 * vstep.amax() / z + 2.0 ** -25
+                + seen.sum(1)[:, None, None, None] * 2.0 ** -27 * vstep.amax() / torch.where(none, torch.ones_like(z), z) + 2.0 ** -25
             out[rows], tol[rows] = o.reshape(n, self.hq, self.d), t.reshape(n, self.hq, self.d)
             ls = torch.where(none, top, top + z.log())[..., 0]
             lse[rows] = ls.reshape(n, self.hq)
@@ -133,6 +136,23 @@ class Case:
                                      (1, 32), (200, 128), (100, 32), (250, 64), (129, 128)])
 def test_heads_and_groups(kd, d, group, dt):
     Case(kd, [1, 17, 100, 0, 333], [1, 1, 1, 1, 1], 4, 2, d, group=group, dt=dt).check(kd)
+
+
+@pytest.mark.parametrize("d,group", [(128, 32), (128, 64), (128, 128), (64, 32), (64, 64), (32, 32), (96, 32), (96, 64), (96, 128),
+                                     (160, 32), (160, 64), (160, 128), (192, 32), (192, 64), (192, 128), (224, 32), (224, 64), (224, 128),
+                                     (256, 32), (256, 64), (256, 128)])
+def test_equal_shares(kd, d, group):
+    """Lengths that may be long (the host knows the table's room only): equal shares of all positions for
+    every CTA, of which one here has several items, another a part of one."""
+    rng = np.random.RandomState(d)
+    lengths = rng.randint(0, 900, 40).tolist() + [0, 5000, 1, 3]
+    c = Case(kd, lengths, [1] * 20 + [2, 0] * 12, 6, 2, d, group=group, dt=BF16, spare=1, room=100000)
+    assert kd.attention_4bit_workspace(c.cache, c.seqs, 6) > 0
+    first = c.check(kd)
+    again = c.run(kd)
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    c.check(kd, window=300)
+    c.check(kd, causal=False)
 
 
 @pytest.mark.parametrize("hq,hk,most", [(1, 1, 1), (8, 1, 1), (9, 1, 1), (16, 1, 1), (17, 1, 1), (32, 8, 1), (32, 32, 1), (40, 8, 1), (7, 7, 3),
@@ -178,10 +198,12 @@ def test_positions_below_zero(kd):
 
 
 @pytest.mark.parametrize("lengths,hq,hk,d,group", [([40000], 8, 2, 128, 64), ([70001], 4, 1, 64, 32), ([20000, 1, 0, 7777], 8, 1, 128, 128),
-                                                   ([9000] * 3, 40, 1, 96, 64), ([30000], 2, 2, 256, 128)])
+                                                   ([9000] * 3, 40, 1, 96, 64), ([30000], 2, 2, 256, 128),
+                                                           ([25000] * 3, 40, 1, 96, 64), ([3000] * 90, 8, 4, 64, 64)])
 def test_long_sequences_in_shares(kd, lengths, hq, hk, d, group):
     c = Case(kd, lengths, [1] * len(lengths), hq, hk, d, page=64, group=group, dt=BF16)
-    assert kd.attention_4bit_workspace(c.cache, c.seqs, hq) > 0
+    if lengths == [40000]:  # equal shares for all CTAs, joined by a second launch
+        assert kd.attention_4bit_workspace(c.cache, c.seqs, hq) > 0
     first = c.check(kd)
     again = c.run(kd)
     assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
@@ -354,7 +376,7 @@ def test_rows_past_most_and_bad_starts(kd):
 
 
 def test_workspaces_streams_and_graphs(kd):
-    c = Case(kd, [9000, 5000], [1, 1], 8, 2, 128, page=64, dt=BF16)
+    c = Case(kd, [40000, 5000], [1, 1], 8, 2, 128, page=64, dt=BF16)
     want = c.check(kd)
     size = kd.attention_4bit_workspace(c.cache, c.seqs, 8)
     ws = torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda")
@@ -378,7 +400,7 @@ def test_workspaces_streams_and_graphs(kd):
         with torch.cuda.graph(g):
             out = kd.attention_4bit(c.cache, c.q, c.seqs, workspace=ws)
         graphs.append((g, out))
-    for length in (8999, 64, 1):
+    for length in (39999, 64, 1):
         c.seqs.lengths.fill_(length)
         c.q.copy_(torch.randn_like(c.q))
         for g, out in graphs:
