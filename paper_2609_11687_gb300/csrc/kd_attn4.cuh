@@ -434,34 +434,69 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
     }
     return bad;
   };
-  bool bad_pages = look_up(0, min(tiles, kBatch));
+  const char* src[4] = {reinterpret_cast<const char*>(p.c.codes[0]) + lane * 16, reinterpret_cast<const char*>(p.c.codes[1]) + lane * 16,
+                        reinterpret_cast<const char*>(p.c.scales[0]) + lane * 16, reinterpret_cast<const char*>(p.c.scales[1]) + lane * 16};
+  auto issue = [&](int first, int n, int stage) {  // tiles first, first + 1 of the batch's n
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+      if (first + i >= n) break;
+      const longlong2 from = place[first + i];
+      const int64_t code = max((int64_t)from.x, (int64_t)0), scale = from.y;
+      const uint32_t codes = ring_at + stage * (Z::kStage * 4) + i * kTile * S * 4;
+#pragma unroll
+      for (int k = 0; k < (int)(sizeof(to) / 4); ++k)
+        if (lane + 32 * k < pieces) {
+          copy16(codes + to[k], src[0] + code + 512 * k);
+          copy16(codes + Z::kCodes * 4 + to[k], src[1] + code + 512 * k);
+        }
+      if (lane < 4 * GN) {
+        const uint32_t scales = ring_at + stage * (Z::kStage * 4) + 2 * Z::kCodes * 4 + i * kTile * scale_bytes + lane * 16;
+        copy16(scales, src[2] + scale);
+        copy16(scales + Z::kScales * 4, src[3] + scale);
+      }
+    }
+  };
 
   // The rows as operands, a warp a row: fp16 in eights of channels 0 4 1 5 2 6 3 7, the odd ones over 16, with
   // the row's power of two and its sums over groups.
   const int r0 = block * Z::kRows;
+  constexpr int kOfWarp = Z::kRows / kWarps;
+  uint32_t raw[kOfWarp][4];  // lane l has channels 8 l .. 8 l + 7 (of 256)
 #pragma unroll
-  for (int r = warp; r < Z::kRows; r += kWarps) {
-    const int token = token_of(p, r0 + r);
+  for (int i = 0; i < kOfWarp; ++i) {
+    const int r = warp + i * kWarps, token = token_of(p, r0 + r);
     const int64_t t = w.first + token;
-    const bool live = r < w.rows && t >= 0 && t < p.tokens;
-    const uint16_t* q = p.q + (live ? t * p.q_token + (int64_t)(head * p.shared + (r0 + r) - token * p.shared) * p.q_head : 0);
-    // lane l has channels 8 l .. 8 l + 7 (of 256)
-    uint32_t raw[4] = {0, 0, 0, 0};
-    if (live && 8 * lane < p.c.d) {
+    raw[i][0] = raw[i][1] = raw[i][2] = raw[i][3] = 0;
+    if (r < w.rows && t >= 0 && t < p.tokens && 8 * lane < p.c.d) {
+      const uint16_t* q = p.q + t * p.q_token + (int64_t)(head * p.shared + (r0 + r) - token * p.shared) * p.q_head + 8 * lane;
       if (p.q_vec) {
-        const uint4 u = *reinterpret_cast<const uint4*>(q + 8 * lane);
-        raw[0] = u.x; raw[1] = u.y; raw[2] = u.z; raw[3] = u.w;
+        const uint4 u = *reinterpret_cast<const uint4*>(q);
+        raw[i][0] = u.x; raw[i][1] = u.y; raw[i][2] = u.z; raw[i][3] = u.w;
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (8 * lane + e < p.c.d) raw[e / 2] |= (uint32_t)q[8 * lane + e] << (16 * (e % 2));
+          if (8 * lane + e < p.c.d) raw[i][e / 2] |= (uint32_t)q[e] << (16 * (e % 2));
       }
     }
+  }
+  // the first batch's copies go out before the rows are worked on
+  bool bad_pages = __syncthreads_or(look_up(0, min(tiles, kBatch)));
+  auto prefetch = [&](int n) {
+#pragma unroll
+    for (int i = 0; i < ST - 1; ++i) {
+      issue(kTiles * warp + i * kChunk, n, i);
+      commit();
+    }
+  };
+  prefetch(min(tiles, kBatch));
+#pragma unroll
+  for (int i = 0; i < kOfWarp; ++i) {
+    const int r = warp + i * kWarps;
     float v[8];
     uint32_t top = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      v[e] = wide(p, raw[e / 2] >> (16 * (e % 2)) & 0xFFFFu);
+      v[e] = wide(p, raw[i][e / 2] >> (16 * (e % 2)) & 0xFFFFu);
       top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
     }
     top = __reduce_max_sync(~0u, top);
@@ -515,29 +550,6 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
       sees_hi[j] = r >= w.rows ? 0 : min(share_hi, p.causal ? clamp_to(pos + 1, w.length) : w.length);
       sees_lo[j] = p.window ? clamp_to(pos + 1 - p.window, w.length) : 0;
     }
-
-  const char* src[4] = {reinterpret_cast<const char*>(p.c.codes[0]) + lane * 16, reinterpret_cast<const char*>(p.c.codes[1]) + lane * 16,
-                        reinterpret_cast<const char*>(p.c.scales[0]) + lane * 16, reinterpret_cast<const char*>(p.c.scales[1]) + lane * 16};
-  auto issue = [&](int first, int n, int stage) {  // tiles first, first + 1 of the batch's n
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-      if (first + i >= n) break;
-      const longlong2 from = place[first + i];
-      const int64_t code = max((int64_t)from.x, (int64_t)0), scale = from.y;
-      const uint32_t codes = ring_at + stage * (Z::kStage * 4) + i * kTile * S * 4;
-#pragma unroll
-      for (int k = 0; k < (int)(sizeof(to) / 4); ++k)
-        if (lane + 32 * k < pieces) {
-          copy16(codes + to[k], src[0] + code + 512 * k);
-          copy16(codes + Z::kCodes * 4 + to[k], src[1] + code + 512 * k);
-        }
-      if (lane < 4 * GN) {
-        const uint32_t scales = ring_at + stage * (Z::kStage * 4) + 2 * Z::kCodes * 4 + i * kTile * scale_bytes + lane * 16;
-        copy16(scales, src[2] + scale);
-        copy16(scales + Z::kScales * 4, src[3] + scale);
-      }
-    }
-  };
 
   float acc[Z::kSumTiles][4];
   // of the columns: sums of weights times middles and of weights (of the positions g8 and g8 + 8 of the tiles
@@ -761,19 +773,13 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
     const int n = min(kBatch, tiles - b0);
     if (b0) {
       __syncthreads();  // no warp still reads the last batch's places
-      bad_pages = look_up(b0, n);
+      bad_pages = __syncthreads_or(look_up(b0, n));
+      prefetch(n);
     }
-    bad_pages = __syncthreads_or(bad_pages);
-    // this warp's steps: tiles kTiles * warp on, kTiles * kWarps apart
-    constexpr int kApart = kTiles * kWarps;
-    int fetch = kTiles * warp;
-#pragma unroll
-    for (int i = 0; i < ST - 1; ++i, fetch += kApart) {
-      issue(fetch, n, i);
-      commit();
-    }
+    // this warp's steps: tiles kTiles * warp on, kChunk apart
+    int fetch = kTiles * warp + (ST - 1) * kChunk;
     int stage = 0, next = ST - 1;
-    for (int nth = kTiles * warp; nth < n; nth += kApart, fetch += kApart) {
+    for (int nth = kTiles * warp; nth < n; nth += kChunk, fetch += kChunk) {
       issue(fetch, n, next);
       commit();
       wait_group<ST - 1>();
