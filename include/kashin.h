@@ -696,7 +696,7 @@ typedef struct kd_cache4 {
  *   longest  the largest length, as far as the host knows it (at most wide * page): a hint for how
  *            attention is split, not a limit.
  * The contents are read on the device and checked there: a row of no sequence (behind the
- * last one, or past `most` of its sequence) is neither read nor written; a position below
+ * last one, or past `most` of its sequence) has no effect and is not written; a position below
  * 0 has no place; a page number outside 0 .. pages - 1, or one past the table, is a bad page. */
 typedef struct kd_sequences {
   const int32_t* table;

@@ -5,7 +5,9 @@
 //     code = rint((x - low) / step),  value = low + step * code
 //
 // Rounding the two outwards keeps every code within 0..15 without clamping and every element within
-// half a step of its value.  All divisions are IEEE's: codes are reproducible bit for bit.
+// half a step of its value.  Codes are those of IEEE divisions, reproducible bit for bit: the product with the
+// reciprocal is off by less than 2^-18 (three roundings of at most 15.5), so only where it lies that close to a
+// half does the division itself decide.
 //
 // Mapping.  A lane has eight channels: one word of codes.  4, 8, 16 or 32 lanes have a row (of a
 // token, a head, and of keys or values), and reduce the extremes of a group among its 4 to 16 lanes
@@ -53,103 +55,162 @@ __device__ __forceinline__ void load8(const void* base, int64_t at, int c, int d
   }
 }
 
-struct Place {  // a warp's token
-  int token, first, last;  // its rounds
-  int64_t position, row;   // below 0: none; a bad page
+struct Share {  // a warp's token and its rounds of the token's rows
+  int token, first, last;
 };
-__device__ __forceinline__ bool place_of(const RowParams& p, Place& w) {
+__device__ __forceinline__ bool share_of(const RowParams& p, Share& w) {
   const int task = blockIdx.x * kCacheWarps + (threadIdx.x >> 5);
-  if (task >= p.tasks) return false;
   w.token = task / p.parts;
   w.first = (task - w.token * p.parts) * p.per;
   w.last = min(w.first + p.per, p.rounds);
+  return task < p.tasks;
+}
+// The token's place: its position (below 0: none) and the first head's row there (-1 on a bad page); false where
+// it is of no sequence.
+__device__ __forceinline__ bool place_of(const RowParams& p, int token, int64_t& position, int64_t& row) {
   int before;
-  const int s = sequence_of(p.c, w.token, before);
+  const int s = sequence_of(p.c, token, before);
   if (s < 0) return false;
-  w.position = (int64_t)p.c.lengths[s] - before;
-  w.row = w.position < 0 ? -1 : row_of(p.c, s, w.position);
+  position = (int64_t)p.c.lengths[s] - before;
+  row = position < 0 ? -1 : row_of(p.c, s, position);
   return true;
 }
 
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(32 * kCacheWarps) cache_write_kernel(const __grid_constant__ RowParams p) {
   depend_on_last();
-  Place w;
-  if (!place_of(p, w) || w.row < 0) return;
+  Share w;
+  if (!share_of(p, w)) return;
   const int lane = threadIdx.x & 31, word = lane & ((1 << p.lanes_log) - 1), nth = lane >> p.lanes_log;
   const int d = p.c.d, of_group = p.c.group / 8;
-  for (int round = w.first; round < w.last; ++round) {
-    const int item = (round << (5 - p.lanes_log)) + nth;
-    const bool live = item < 2 * p.c.heads;
-    const int side = live && item >= p.c.heads, h = live ? item - side * p.c.heads : 0;
-    const int have = live ? d - 8 * word : 0;  // elements from the lane's first on
-    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (have > 0) load8<DT, VEC>(p.in[side], w.token * p.token[side] + h * p.head[side], 8 * word, d, v);
-    const float inf = __int_as_float(0x7F800000);
-    float lo = inf, minus_hi = inf;  // of -x: one kind of maximum does for both
+  constexpr int kAhead = DT == KD_F32 ? 1 : 2;  // rounds whose loads are in flight together
+  float ahead[kAhead][8];
+  auto fetch = [&](int first) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < have) {
-        lo = -max_nan(-lo, -v[e]);
-        minus_hi = -max_nan(-minus_hi, v[e]);
-      }
-    for (int o = min(of_group, 1 << p.lanes_log) >> 1; o; o >>= 1) {
-      lo = -max_nan(-lo, -__shfl_xor_sync(~0u, lo, o));
-      minus_hi = -max_nan(-minus_hi, -__shfl_xor_sync(~0u, minus_hi, o));
+    for (int i = 0; i < kAhead; ++i) {
+      const int item = ((first + i) << (5 - p.lanes_log)) + nth, side = item >= p.c.heads, h = item - side * p.c.heads;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ahead[i][e] = 0.f;
+      if (first + i < w.last && item < 2 * p.c.heads && 8 * word < d)
+        load8<DT, VEC>(p.in[side], w.token * p.token[side] + h * p.head[side], 8 * word, d, ahead[i]);
     }
-    __half low = __float2half_rd(lo), step = __float2half_ru((-minus_hi - __half2float(low)) / 15.f);
-    float flow = __half2float(low), fstep = __half2float(step);
-    const bool fine = isfinite(flow) && isfinite(fstep);
-    if (!fine) low = step = __ushort_as_half(0x7FFF);
-    uint32_t codes = 0;
-    if (fine && fstep > 0.f) {
+  };
+  fetch(w.first);  // while the place is looked for
+  int64_t position, place;
+  if (!place_of(p, w.token, position, place) || place < 0) return;
+  for (int first = w.first; first < w.last; first += kAhead) {
+    if (first != w.first) fetch(first);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (first + i >= w.last) break;
+      const int item = ((first + i) << (5 - p.lanes_log)) + nth;
+      const bool live = item < 2 * p.c.heads;
+      const int side = live && item >= p.c.heads, h = live ? item - side * p.c.heads : 0;
+      const int have = live ? d - 8 * word : 0;  // elements from the lane's first on
+      const float(&v)[8] = ahead[i];
+      const float inf = __int_as_float(0x7F800000);
+      float lo = inf, minus_hi = inf;  // of -x: one kind of maximum does for both
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (e < have) codes |= (uint32_t)min(__float2int_rn((v[e] - flow) / fstep), 15) << (4 * e);
+        if (e < have) {
+          lo = -max_nan(-lo, -v[e]);
+          minus_hi = -max_nan(-minus_hi, v[e]);
+        }
+      for (int o = min(of_group, 1 << p.lanes_log) >> 1; o; o >>= 1) {
+        lo = -max_nan(-lo, -__shfl_xor_sync(~0u, lo, o));
+        minus_hi = -max_nan(-minus_hi, -__shfl_xor_sync(~0u, minus_hi, o));
+      }
+      __half low = __float2half_rd(lo), step = __float2half_ru((-minus_hi - __half2float(low)) / 15.f);
+      const float flow = __half2float(low), fstep = __half2float(step);
+      const bool fine = isfinite(flow) && isfinite(fstep);
+      if (!fine) low = step = __ushort_as_half(0x7FFF);
+      uint32_t codes = 0;
+      if (fine && fstep > 0.f) {
+        const float inverse = 1.f / fstep;
+        // rounded by adding 1.5 2^23, whose last digit is 1; the code is then in the low bits
+        constexpr float kRound = 12582912.f;
+        bool near = !(inverse < 0x1p100f);  // a reciprocal out of range decides nothing
+        uint32_t c[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float q = (v[e] - flow) * inverse, r = q + kRound;
+          c[e] = __float_as_uint(r) & 31u;
+          near |= fabsf(q - (r - kRound)) > 0.5f - 0x1p-17f;
+        }
+        if (near) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) c[e] = (uint32_t)__float2int_rn((v[e] - flow) / fstep);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < have) codes |= min(c[e], 15u) << (4 * e);
+      }
+      if (!live) continue;
+      const int64_t row = place + (int64_t)h * p.c.page;
+      if (word < 4 * p.c.chunks) p.c.codes[side][row * (4 * p.c.chunks) + word] = codes;
+      if (have > 0 && word % of_group == 0)
+        p.c.scales[side][row * p.c.groups + word / of_group] =
+            (uint32_t)__half_as_ushort(step) | (uint32_t)__half_as_ushort(low) << 16;
     }
-    if (!live) continue;
-    const int64_t row = w.row + (int64_t)h * p.c.page;
-    if (word < 4 * p.c.chunks) p.c.codes[side][row * (4 * p.c.chunks) + word] = codes;
-    if (have > 0 && word % of_group == 0)
-      p.c.scales[side][row * p.c.groups + word / of_group] =
-          (uint32_t)__half_as_ushort(step) | (uint32_t)__half_as_ushort(low) << 16;
   }
 }
 
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(32 * kCacheWarps) cache_read_kernel(const __grid_constant__ RowParams p) {
   depend_on_last();
-  Place w;
-  if (!place_of(p, w)) return;
+  Share w;
+  int64_t position, place;
+  if (!share_of(p, w) || !place_of(p, w.token, position, place)) return;
   const int lane = threadIdx.x & 31, word = lane & ((1 << p.lanes_log) - 1), nth = lane >> p.lanes_log;
   const int c = 8 * word, of_group = p.c.group / 8;
   if (c >= p.c.d) return;
-#pragma unroll 2
-  for (int round = w.first; round < w.last; ++round) {
-    const int item = (round << (5 - p.lanes_log)) + nth;
-    if (item >= p.sides * p.c.heads) break;
-    const int which = item >= p.c.heads, h = item - which * p.c.heads, side = p.first_side + which;
-    float v[8];
-    if (w.row < 0) {  // no place: 0; a bad page: NaN
-      const float fill = w.position < 0 ? 0.f : __int_as_float(0x7FC00000);
+  const int heads = p.c.heads, items = p.sides * heads;
+  const int64_t code_at = place * (4 * p.c.chunks) + word, scale_at = place * p.c.groups + word / of_group;
+  constexpr int kAhead = 4;  // rounds whose loads are in flight together
+  for (int first = w.first; first < w.last; first += kAhead) {
+    uint32_t codes[kAhead], scale[kAhead];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = fill;
-    } else {
-      const int64_t row = w.row + (int64_t)h * p.c.page;
-      const uint32_t codes = p.c.codes[side][row * (4 * p.c.chunks) + word];
-      const uint32_t scale = p.c.scales[side][row * p.c.groups + word / of_group];
-      const float step = __half2float(__ushort_as_half((unsigned short)scale));
-      const float low = __half2float(__ushort_as_half((unsigned short)(scale >> 16)));
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = low + step * (float)(codes >> (4 * e) & 15);  // the product is exact
+    for (int i = 0; i < kAhead; ++i) {
+      const int item = ((first + i) << (5 - p.lanes_log)) + nth;
+      if (first + i >= w.last || item >= items || place < 0) continue;
+      const int which = item >= heads, side = p.first_side + which;
+      const int64_t rows = (int64_t)(item - which * heads) * p.c.page;
+      codes[i] = p.c.codes[side][code_at + rows * (4 * p.c.chunks)];
+      scale[i] = p.c.scales[side][scale_at + rows * p.c.groups];
     }
-    const int64_t at = w.token * p.token[which] + h * p.head[which] + c;
-    if constexpr (VEC) {
-      store8<DT>(p.out[which], at, v);
-    } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (c + e < p.c.d) store1<DT>(p.out[which], at + e, v[e]);
+    for (int i = 0; i < kAhead; ++i) {
+      const int item = ((first + i) << (5 - p.lanes_log)) + nth;
+      if (first + i >= w.last || item >= items) break;
+      const int which = item >= heads, h = item - which * heads;
+      float v[8];
+      if (place < 0) {  // no place: 0; a bad page: NaN
+        const float fill = position < 0 ? 0.f : __int_as_float(0x7FC00000);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = fill;
+      } else {
+        // codes e and e + 4 as halves 1024 + c (in the low bits) or 64 + c (four bits higher), less that
+        const float step = __half2float(__ushort_as_half((unsigned short)scale[i]));
+        const float low = __half2float(__ushort_as_half((unsigned short)(scale[i] >> 16)));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t u = codes[i] >> (e & 2 ? 8 : 0);
+          const uint32_t bits = e & 1 ? (u & 0x00F000F0u) | 0x54005400u : (u & 0x000F000Fu) | 0x64006400u;
+          const uint32_t less = e & 1 ? 0x54005400u : 0x64006400u;
+          const float2 c2 = __half22float2(__hsub2(*reinterpret_cast<const __half2*>(&bits), *reinterpret_cast<const __half2*>(&less)));
+          const float2 of = fma2(make_float2(step, step), c2, make_float2(low, low));  // exact products: one rounding
+          v[e] = of.x;
+          v[e + 4] = of.y;
+        }
+      }
+      const int64_t at = w.token * p.token[which] + h * p.head[which] + c;
+      if constexpr (VEC) {
+        store8<DT>(p.out[which], at, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c + e < p.c.d) store1<DT>(p.out[which], at + e, v[e]);
+      }
     }
   }
 }
@@ -161,9 +222,11 @@ cudaError_t launch(Kernel kernel, RowParams& p, cudaStream_t s) {
   while ((1 << p.lanes_log) < 4 * p.c.chunks) ++p.lanes_log;
   const int of_warp = 32 >> p.lanes_log;
   p.rounds = (p.sides * p.c.heads + of_warp - 1) / of_warp;
-  // few tokens: a warp for each round of rows; many: several rounds share the search for their place
-  const int64_t share = (int64_t)p.tokens * p.rounds / (152 * 32);
-  p.per = (int)(share < 1 ? 1 : share > p.rounds ? p.rounds : share);
+  // as many parts of a token's rounds as all fit the GPU in two turns (64 warps an SM), at least one: the warps of
+  // one token each look for its place
+  const int64_t share = 152 * 64 / p.tokens;
+  p.parts = (int)(share < 1 ? 1 : share > p.rounds ? p.rounds : share);
+  p.per = (p.rounds + p.parts - 1) / p.parts;
   p.parts = (p.rounds + p.per - 1) / p.per;
   p.tasks = (int)((int64_t)p.tokens * p.parts);
   cudaLaunchConfig_t cfg = {};

@@ -86,17 +86,22 @@ __device__ __forceinline__ int sequence_of(const Pages& p, int t, int& before) {
   for (;;) {
     const int stride = (hi - lo + 31) / 32;
     const int64_t at = lo + (int64_t)lane * stride;
-    const int found = __popc(__ballot_sync(~0u, at < hi && p.starts[at] <= t));
+    const int start = at < hi ? p.starts[at] : 0;
+    const int found = __popc(__ballot_sync(~0u, at < hi && start <= t));
     if (found == 0) return -1;
     lo += (found - 1) * stride;
-    if (stride == 1) break;
+    if (stride == 1) {
+      if (lo >= p.seqs) return -1;
+      // the sequence's start and end are what these lanes have, but for the end in the last one
+      const int64_t first = __shfl_sync(~0u, start, found - 1);
+      int64_t end = __shfl_sync(~0u, start, found & 31);
+      if (lo + 1 >= hi) end = p.starts[lo + 1];
+      if (t < first || t >= end || t - first >= p.most) return -1;  // starts that decrease, rows past `most`
+      before = (int)(end - t);
+      return lo;
+    }
     hi = (int)min((int64_t)lo + stride, (int64_t)hi);
   }
-  if (lo >= p.seqs) return -1;
-  const int64_t first = p.starts[lo], end = p.starts[lo + 1];
-  if (t < first || t >= end || t - first >= p.most) return -1;  // starts that decrease, rows past `most`
-  before = (int)(end - t);
-  return lo;
 }
 
 }  // namespace cache4

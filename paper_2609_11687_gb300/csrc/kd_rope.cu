@@ -55,31 +55,35 @@ __device__ __forceinline__ float2 turn_of(const RopeParams& p, int64_t position,
 }
 
 template <int DT>
-struct Vec16 {  // 16 bytes as they come
-  static constexpr int V = DT == KD_F32 ? 4 : 8;
-  static __device__ __forceinline__ void get(uint4 u, float (&f)[V]) {
+struct Vec16 {  // 16 bytes as they come, as P pairs of floats
+  static constexpr int V = DT == KD_F32 ? 4 : 8, P = V / 2;
+  static __device__ __forceinline__ void get(uint4 u, float2 (&f)[P]) {
     if constexpr (DT == KD_F32) {
-      f[0] = __uint_as_float(u.x); f[1] = __uint_as_float(u.y); f[2] = __uint_as_float(u.z); f[3] = __uint_as_float(u.w);
+      f[0] = make_float2(__uint_as_float(u.x), __uint_as_float(u.y));
+      f[1] = make_float2(__uint_as_float(u.z), __uint_as_float(u.w));
     } else {
-      const float2 a = unpack2<DT>(u.x), b = unpack2<DT>(u.y), c = unpack2<DT>(u.z), d = unpack2<DT>(u.w);
-      f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y; f[4] = c.x; f[5] = c.y; f[6] = d.x; f[7] = d.y;
+      f[0] = unpack2<DT>(u.x);
+      f[1] = unpack2<DT>(u.y);
+      f[2] = unpack2<DT>(u.z);
+      f[3] = unpack2<DT>(u.w);
     }
   }
-  static __device__ __forceinline__ uint4 put(const float (&f)[V]) {
+  static __device__ __forceinline__ uint4 put(const float2 (&f)[P]) {
     if constexpr (DT == KD_F32)
-      return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-    else return make_uint4(pack2<DT>(f[0], f[1]), pack2<DT>(f[2], f[3]), pack2<DT>(f[4], f[5]), pack2<DT>(f[6], f[7]));
+      return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
+    else return make_uint4(pack2<DT>(f[0].x, f[0].y), pack2<DT>(f[1].x, f[1].y), pack2<DT>(f[2].x, f[2].y), pack2<DT>(f[3].x, f[3].y));
   }
 };
 
 // consecutive weights from channel c on
-template <int DT, int V>
-__device__ __forceinline__ void load_weights(const RopeSide& s, int c, float (&w)[V]) {
+template <int DT, int P>
+__device__ __forceinline__ void load_weights(const RopeSide& s, int c, float2 (&w)[P]) {
   if (s.wt == KD_F32) {
 #pragma unroll
-    for (int e = 0; e < V; e += 4) {
-      const float4 f = *reinterpret_cast<const float4*>(static_cast<const float*>(s.w) + c + e);
-      w[e] = f.x; w[e + 1] = f.y; w[e + 2] = f.z; w[e + 3] = f.w;
+    for (int e = 0; e < P; e += 2) {
+      const float4 f = *reinterpret_cast<const float4*>(static_cast<const float*>(s.w) + c + 2 * e);
+      w[e] = make_float2(f.x, f.y);
+      w[e + 1] = make_float2(f.z, f.w);
     }
   } else {
     Vec16<DT>::get(*reinterpret_cast<const uint4*>(static_cast<const typename Elem<DT>::type*>(s.w) + c), w);
@@ -92,7 +96,7 @@ __device__ __forceinline__ float inverse_root(float sum, const RopeParams& p) {
 
 template <int DT>
 __global__ void __launch_bounds__(32 * kRopeWarps) rope_kernel(const __grid_constant__ RopeParams p) {
-  constexpr int V = Vec16<DT>::V;
+  constexpr int V = Vec16<DT>::V, P = V / 2;
   using T = typename Elem<DT>::type;
   extern __shared__ float2 turns_of_warp[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -125,53 +129,64 @@ __global__ void __launch_bounds__(32 * kRopeWarps) rope_kernel(const __grid_cons
   const int64_t position = p.positions[token];
   for (int i = lane; i < p.rot / 2; i += 32) table[i] = turn_of(p, position, i);
   __syncwarp();
-  float2 turn[V];  // of the slot's pairs
+  // of the slot's pairs, two at a time
+  float2 sine[P], cosine[P], minus_sine[P];
   if (slot < rotated) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) turn[e] = table[V * slot + e];
+    for (int e = 0; e < P; ++e) {
+      const float2 u = table[V * slot + 2 * e], v = table[V * slot + 2 * e + 1];
+      sine[e] = make_float2(u.x, v.x);
+      minus_sine[e] = make_float2(-u.x, -v.x);
+      cosine[e] = make_float2(u.y, v.y);
+    }
   }
 
   for (int round = first; round < last; ++round) {
-    float fa[V], fb[V];
+    float2 fa[P], fb[P];
     Vec16<DT>::get(va, fa);
     Vec16<DT>::get(vb, fb);
     if (round + 1 < last) fetch(round + 1);
     const int h = (round << heads_log) + nth;
     const RopeSide& s = p.side[h >= p.side[0].heads];
     if (p.side[0].w || p.side[1].w) {
-      float ss = 0.f;
+      float2 sums = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int e = 0; e < V; ++e) ss = __fmaf_rn(fa[e], fa[e], __fmaf_rn(fb[e], fb[e], ss));
+      for (int e = 0; e < P; ++e) sums = fma2(fa[e], fa[e], fma2(fb[e], fb[e], sums));
+      float ss = sums.x + sums.y;
       for (int o = 1 << p.lanes_log >> 1; o; o >>= 1) ss += __shfl_xor_sync(~0u, ss, o);
       if (h < heads && s.w) {
         const float r = inverse_root(ss, p);
-        float w[V];
+        const float2 rr = make_float2(r, r);
+        float2 w[P];
         if (has_a) {
-          load_weights<DT, V>(s, a, w);
+          load_weights<DT, P>(s, a, w);
 #pragma unroll
-          for (int e = 0; e < V; ++e) fa[e] = fa[e] * r * w[e];
+          for (int e = 0; e < P; ++e) fa[e] = mul2(mul2(fa[e], rr), w[e]);
         }
         if (has_b) {
-          load_weights<DT, V>(s, b, w);
+          load_weights<DT, P>(s, b, w);
 #pragma unroll
-          for (int e = 0; e < V; ++e) fb[e] = fb[e] * r * w[e];
+          for (int e = 0; e < P; ++e) fb[e] = mul2(mul2(fb[e], rr), w[e]);
         }
       }
     }
     if (slot < rotated) {
-      auto rotate = [](float& u, float& v, float2 t) {
-        const float x = u, y = v;
-        u = __fmaf_rn(x, t.y, -(y * t.x));
-        v = __fmaf_rn(y, t.y, x * t.x);
-      };
       if (p.half) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) rotate(fa[e], fb[e], turn[e]);
-      } else {
+        for (int e = 0; e < P; ++e) {
+          const float2 x = fa[e], y = fb[e];
+          fa[e] = fma2(y, minus_sine[e], mul2(x, cosine[e]));
+          fb[e] = fma2(x, sine[e], mul2(y, cosine[e]));
+        }
+      } else {  // pair i of the slot is its i-th float2; its turn is half of turn pair i / 2
+        auto turn = [&](float2 v, int i) {
+          const float sn = i % 2 ? sine[i / 2].y : sine[i / 2].x, cs = i % 2 ? cosine[i / 2].y : cosine[i / 2].x;
+          return make_float2(__fmaf_rn(v.y, -sn, v.x * cs), __fmaf_rn(v.x, sn, v.y * cs));
+        };
 #pragma unroll
-        for (int e = 0; e < V / 2; ++e) {
-          rotate(fa[2 * e], fa[2 * e + 1], turn[e]);
-          rotate(fb[2 * e], fb[2 * e + 1], turn[V / 2 + e]);
+        for (int e = 0; e < P; ++e) {
+          fa[e] = turn(fa[e], e);
+          fb[e] = turn(fb[e], P + e);
         }
       }
     }
@@ -243,9 +258,11 @@ cudaError_t launch(RopeParams p, int64_t tokens, bool vec, cudaStream_t s) {
   p.lanes_log = 0;
   while (vec && (1 << p.lanes_log) < slots) ++p.lanes_log;
   const int rounds = vec ? (heads + (32 >> p.lanes_log) - 1) >> (5 - p.lanes_log) : heads;
-  // few tokens: a warp for each round of heads; many: several rounds a warp, which share the sines
-  const int64_t share = tokens * rounds / (152 * 24);
-  p.per = (int)(share < 1 ? 1 : share > rounds ? rounds : share);
+  // as many parts of a token's rounds as all fit the GPU at a time (28 warps an SM), at least one: 2048 tokens of
+  // ten rounds take 10.5 us in two parts, 13 in one, three or more
+  const int64_t share = 152 * 28 / tokens;
+  p.parts = (int)(share < 1 ? 1 : share > rounds ? rounds : share);
+  p.per = (rounds + p.parts - 1) / p.parts;
   p.parts = (rounds + p.per - 1) / p.per;
   p.tasks = (int)(tokens * p.parts);
   cudaLaunchConfig_t cfg = {};
