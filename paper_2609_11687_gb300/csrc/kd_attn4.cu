@@ -195,9 +195,6 @@ extern "C" kd_status kd_attention_4bit(const kd_cache4* cache, const kd_sequence
   p.causal = causal != 0;
   p.window = (int)window;
   p.room = (int)std::min(seqs->wide * cache->page, (int64_t)INT32_MAX - kTile);
-  p.page_log = -1;
-  for (int log = 0; log <= 12; ++log)
-    if (cache->page == (int64_t)kTile << log) p.page_log = log;
   p.bf16 = dtype == KD_BF16;
   p.q_vec = cache->d % 8 == 0 && aligned(q, 16) && (tokens == 1 || q_token % 8 == 0) && (heads == 1 || q_head % 8 == 0);
   p.out_vec = cache->d % 4 == 0 && aligned(out, 8) && (tokens == 1 || out_token % 4 == 0) && (heads == 1 || out_head % 4 == 0);

@@ -67,7 +67,6 @@ struct Params {
                                 // 0: all CTAs have equal shares of all of them
   int causal, window;
   int room;                     // positions that the table has room for
-  int page_log;                 // of a page's tiles, where that is a power of two, else -1
   int bf16, q_vec, out_vec;
   float scale2;                 // scale log2 e
   struct Cut* cuts;             // the item that each CTA leaves to the next ones
@@ -137,7 +136,7 @@ __device__ __forceinline__ bool past_table(const Params& p, const Work& w, int n
 
 // The first row's number of a tile (of 16 positions on one page) for the first key head, -1 on a bad page.
 __device__ __forceinline__ int64_t tile_row(const Params& p, int s, int tile) {
-  const unsigned of_page = (unsigned)p.c.page / kTile, nth = p.page_log >= 0 ? (unsigned)tile >> p.page_log : (unsigned)tile / of_page;
+  const unsigned of_page = (unsigned)p.c.page / kTile, nth = p.c.page_log >= 0 ? (unsigned)tile >> (p.c.page_log - 4) : (unsigned)tile / of_page;
   const int page = p.c.table[s * p.c.ld_table + nth];  // tiles lie within the table's room
   if ((unsigned)page >= (unsigned)p.c.pages) return -1;
   return (int64_t)page * p.c.heads * p.c.page + (int)(tile - nth * of_page) * kTile;

@@ -72,7 +72,7 @@ __device__ __forceinline__ bool place_of(const RowParams& p, int token, int64_t&
   const int s = sequence_of(p.c, token, before);
   if (s < 0) return false;
   position = (int64_t)p.c.lengths[s] - before;
-  row = position < 0 ? -1 : row_of(p.c, s, position);
+  row = position < 0 ? -1 : row_of(p.c, s, (int)position);  // positions are less than a length
   return true;
 }
 
@@ -109,18 +109,20 @@ __global__ void __launch_bounds__(32 * kCacheWarps) cache_write_kernel(const __g
       const int have = live ? d - 8 * word : 0;  // elements from the lane's first on
       const float(&v)[8] = ahead[i];
       const float inf = __int_as_float(0x7F800000);
-      float lo = inf, minus_hi = inf;  // of -x: one kind of maximum does for both
+      float lo = inf, hi = -inf;
+      if (have > 0) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < have) {
-          lo = -max_nan(-lo, -v[e]);
-          minus_hi = -max_nan(-minus_hi, v[e]);
-        }
-      for (int o = min(of_group, 1 << p.lanes_log) >> 1; o; o >>= 1) {
-        lo = -max_nan(-lo, -__shfl_xor_sync(~0u, lo, o));
-        minus_hi = -max_nan(-minus_hi, -__shfl_xor_sync(~0u, minus_hi, o));
+        for (int e = 0; e < 8; ++e)
+          if (VEC || e < have) {
+            lo = min_nan(lo, v[e]);
+            hi = max_nan(hi, v[e]);
+          }
       }
-      __half low = __float2half_rd(lo), step = __float2half_ru((-minus_hi - __half2float(low)) / 15.f);
+      for (int o = min(of_group, 1 << p.lanes_log) >> 1; o; o >>= 1) {
+        lo = min_nan(lo, __shfl_xor_sync(~0u, lo, o));
+        hi = max_nan(hi, __shfl_xor_sync(~0u, hi, o));
+      }
+      __half low = __float2half_rd(lo), step = __float2half_ru((hi - __half2float(low)) / 15.f);
       const float flow = __half2float(low), fstep = __half2float(step);
       const bool fine = isfinite(flow) && isfinite(fstep);
       if (!fine) low = step = __ushort_as_half(0x7FFF);
@@ -129,21 +131,24 @@ __global__ void __launch_bounds__(32 * kCacheWarps) cache_write_kernel(const __g
         const float inverse = 1.f / fstep;
         // rounded by adding 1.5 2^23, whose last digit is 1; the code is then in the low bits
         constexpr float kRound = 12582912.f;
-        bool near = !(inverse < 0x1p100f);  // a reciprocal out of range decides nothing
         uint32_t c[8];
+        float off = inverse < 0x1p100f ? 0.f : 1.f;  // a reciprocal out of range decides nothing
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float q = (v[e] - flow) * inverse, r = q + kRound;
-          c[e] = __float_as_uint(r) & 31u;
-          near |= fabsf(q - (r - kRound)) > 0.5f - 0x1p-17f;
+        for (int e = 0; e < 8; e += 2) {
+          const float2 q = mul2(add2(make_float2(v[e], v[e + 1]), make_float2(-flow, -flow)), make_float2(inverse, inverse));
+          const float2 r = add2(q, make_float2(kRound, kRound));
+          const float2 from = add2(q, make_float2(kRound - r.x, kRound - r.y));
+          c[e] = __float_as_uint(r.x) & 15u;
+          c[e + 1] = __float_as_uint(r.y) & 15u;
+          off = fmaxf(off, fmaxf(fabsf(from.x), fabsf(from.y)));
         }
-        if (near) {
+        if (off > 0.5f - 0x1p-17f) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) c[e] = (uint32_t)__float2int_rn((v[e] - flow) / fstep);
+          for (int e = 0; e < 8; ++e) c[e] = (uint32_t)__float2int_rn((v[e] - flow) / fstep) & 15u;
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e < have) codes |= min(c[e], 15u) << (4 * e);
+        for (int e = 7; e >= 0; --e) codes = codes * 16u + c[e];
+        if (have < (VEC ? 1 : 8)) codes &= have <= 0 ? 0u : (1u << (4 * have)) - 1u;
       }
       if (!live) continue;
       const int64_t row = place + (int64_t)h * p.c.page;

@@ -37,6 +37,7 @@ struct Pages {
   int64_t ld_table;
   int seqs, wide, most;
   int pages, heads, page;
+  int page_log;                  // of page, where it is a power of two, else -1
   int d, group, groups, chunks;  // of a row: channels, of one scale, scales, 32-channel pieces of codes
 };
 inline Pages pages_of(const kd_cache4* c, const kd_sequences* s) {
@@ -55,6 +56,9 @@ inline Pages pages_of(const kd_cache4* c, const kd_sequences* s) {
   p.pages = (int)c->pages;
   p.heads = (int)c->heads;
   p.page = (int)c->page;
+  p.page_log = -1;
+  for (int log = 4; log <= 16; ++log)
+    if (c->page == (int64_t)1 << log) p.page_log = log;
   p.d = (int)c->d;
   p.group = (int)c->group;
   p.groups = (int)((c->d + c->group - 1) / c->group);
@@ -62,14 +66,14 @@ inline Pages pages_of(const kd_cache4* c, const kd_sequences* s) {
   return p;
 }
 
-// The row of the first key head at a position of sequence s, -1 on a bad page.  Rows are counted
-// in 64 bits: a cache may have more than 2^31.
-__device__ __forceinline__ int64_t row_of(const Pages& p, int s, int64_t position) {
-  const int64_t nth = position / p.page;
-  if (nth >= p.wide) return -1;
+// The first key head's row at a position of sequence s, -1 on a bad page.  Rows are counted in 64 bits: a cache may
+// have more than 2^31.
+__device__ __forceinline__ int64_t row_of(const Pages& p, int s, int position) {
+  const unsigned nth = p.page_log >= 0 ? (unsigned)position >> p.page_log : (unsigned)position / (unsigned)p.page;
+  if (nth >= (unsigned)p.wide) return -1;
   const int page = p.table[s * p.ld_table + nth];
   if ((unsigned)page >= (unsigned)p.pages) return -1;
-  return (int64_t)page * p.heads * p.page + (position - nth * p.page);
+  return (int64_t)page * p.heads * p.page + (int)((unsigned)position - nth * (unsigned)p.page);
 }
 
 // Row t's sequence, -1 for none, found by the whole warp: the last s with starts[s] <= t, 32 ways
