@@ -9,88 +9,91 @@ namespace kd {
 namespace attn4 {
 namespace {
 
-constexpr int kJoinThreads = 256;
+// A block for an item and 32 of its channels: eight lanes have a part, so that a warp has four and the block up to 32 of
+// them in flight; four rows at a time, each with a running maximum, joined over lanes and warps in a fixed order.
+constexpr int kJoinWarps = 8, kJoinRows = 4;  // warps at most
 
-// A block for each CTA's cut item, eight rows and 128 channels at a time: a warp takes every eighth part with a
-// running maximum of each row, all its loads independent of each other; then the warps' sums are joined in
-// their order.
-__global__ void __launch_bounds__(kJoinThreads) attn4_join_kernel(const __grid_constant__ Params p) {
-  constexpr int kJoinWarps = kJoinThreads / 32;
-  __shared__ float4 sums[kJoinWarps][kRows][32];
-  __shared__ float2 ml[kJoinWarps][kRows];
+struct Sum {  // of one row: maximum, weights, four channels
+  float m, l;
+  float4 o;
+  __device__ __forceinline__ void add(const Sum& b) {
+    const float top = fmaxf(m, b.m);
+    // without a maximum a part has summed nothing, or NaN, which its weights' sum says
+    const float f = m == kNone ? 0.f : exp2_of(m - top), g = b.m == kNone ? 0.f : exp2_of(b.m - top);
+    l = l * (m == kNone ? 1.f : f) + b.l * (b.m == kNone ? 1.f : g);
+    m = top;
+    o.x = __fmaf_rn(b.o.x, g, o.x * f);
+    o.y = __fmaf_rn(b.o.y, g, o.y * f);
+    o.z = __fmaf_rn(b.o.z, g, o.z * f);
+    o.w = __fmaf_rn(b.o.w, g, o.w * f);
+  }
+};
+
+__global__ void __launch_bounds__(32 * kJoinWarps) attn4_join_kernel(const __grid_constant__ Params p) {
+  __shared__ Sum sums[kJoinWarps][kJoinRows][8];
   depend_on_last();
-  const Cut c = p.cuts[blockIdx.x];
-  if (c.more == 0) return;
-  const int parts = c.more + 1, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int c0 = 0; c0 < p.part_row; c0 += 128) {
-      const bool has = c0 + 4 * lane < p.part_row;
-      float4 o[kRows];
-      float2 at[kRows];
+  const int64_t item = blockIdx.x;
+  const int block = (int)(item % p.row_blocks), head = (int)(item / p.row_blocks % p.c.heads);
+  const int s = (int)(item / p.row_blocks / p.c.heads);
+  const Work w = work_of(p, s, block, kRows);
+  const Cut c = p.cuts[item];
+  if (w.chunks == 0 || c.more == 0) return;  // an item without rows has nothing in `cuts`
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int nth = lane >> 3, ch = 32 * blockIdx.y + 4 * (lane & 7);
+  const bool has = ch < p.part_row;
+  for (int r0 = 0; r0 < w.rows; r0 += kJoinRows) {
+    Sum sum[kJoinRows];
 #pragma unroll
-      for (int r = 0; r < kRows; ++r) {
-        o[r] = make_float4(0.f, 0.f, 0.f, 0.f);
-        at[r] = make_float2(kNone, 0.f);
-      }
-      for (int k = warp; k < parts; k += kJoinWarps) {
-        // the part's rows: in the item's first place, or the first one of a CTA that follows
-        const int64_t row = (int64_t)(k ? 2 * ((int)blockIdx.x + k) : c.slot) * kRows;
-        float4 v[kRows];
-        float2 n[kRows];
+    for (int r = 0; r < kJoinRows; ++r) sum[r] = Sum{kNone, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    for (int k = 4 * warp + nth; k <= c.more; k += 4 * warps) {
+      const int64_t row = (int64_t)(k ? 2 * (c.owner + k) : c.slot) * kRows + r0;
+      Sum part[kJoinRows];
 #pragma unroll
-        for (int r = 0; r < kRows; ++r)
-          if (r < c.rows) {
-            n[r] = p.part_ml[row + r];
-            v[r] = has ? *reinterpret_cast<const float4*>(p.part + (row + r) * p.part_row + c0 + 4 * lane) : make_float4(0.f, 0.f, 0.f, 0.f);
-          }
-#pragma unroll
-        for (int r = 0; r < kRows; ++r)
-          if (r < c.rows) {
-            const float top = fmaxf(at[r].x, n[r].x);
-            const float f = at[r].x == kNone ? 0.f : exp2_of(at[r].x - top), g = n[r].x == kNone ? 0.f : exp2_of(n[r].x - top);
-            at[r].y = __fmaf_rn(at[r].y, at[r].x == kNone ? 1.f : f, n[r].y * (n[r].x == kNone ? 1.f : g));  // without a maximum: 0, or NaN
-            at[r].x = top;
-            o[r].x = __fmaf_rn(v[r].x, g, o[r].x * f);
-            o[r].y = __fmaf_rn(v[r].y, g, o[r].y * f);
-            o[r].z = __fmaf_rn(v[r].z, g, o[r].z * f);
-            o[r].w = __fmaf_rn(v[r].w, g, o[r].w * f);
-          }
-      }
-#pragma unroll
-      for (int r = 0; r < kRows; ++r) {
-        sums[warp][r][lane] = o[r];
-        if (lane == 0) ml[warp][r] = at[r];
-      }
-      __syncthreads();
-      const int r = warp;  // a row of a warp
-      const int in = c.block * kRows + r, token = token_of(p, in), h = c.head * p.shared + in - token * p.shared;
-      const int64_t t = c.first + token;
-      if (r < c.rows && t >= 0 && t < p.tokens) {
-        float top = kNone, total = 0.f;
-        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < kJoinWarps; ++k) top = fmaxf(top, ml[k][r].x);
-#pragma unroll
-        for (int k = 0; k < kJoinWarps; ++k) {
-          const float2 n = ml[k][r];
-          const float f = n.x == kNone ? 0.f : exp2_of(n.x - top);
-          total += n.y * (n.x == kNone ? 1.f : f);
-          const float4 v = sums[k][r][lane];
-          y.x = __fmaf_rn(v.x, f, y.x);
-          y.y = __fmaf_rn(v.y, f, y.y);
-          y.z = __fmaf_rn(v.z, f, y.z);
-          y.w = __fmaf_rn(v.w, f, y.w);
+      for (int r = 0; r < kJoinRows; ++r) {
+        part[r] = Sum{kNone, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+        if (r0 + r < w.rows) {
+          const float2 ml = p.part_ml[row + r];
+          part[r].m = ml.x;
+          part[r].l = ml.y;
+          if (has) part[r].o = *reinterpret_cast<const float4*>(p.part + (row + r) * p.part_row + ch);
         }
-        if (has) put(p, p.out + t * p.out_token + h * p.out_head, c0 + 4 * lane, y, total);
-        if (lane == 0 && c0 == 0) put_lse(p, t * p.heads + h, top, total);
       }
-      __syncthreads();
+#pragma unroll
+      for (int r = 0; r < kJoinRows; ++r) sum[r].add(part[r]);
     }
+#pragma unroll
+    for (int r = 0; r < kJoinRows; ++r) {
+#pragma unroll
+      for (int o = 8; o < 32; o *= 2) {
+        Sum other;
+        other.m = __shfl_xor_sync(~0u, sum[r].m, o);
+        other.l = __shfl_xor_sync(~0u, sum[r].l, o);
+        other.o.x = __shfl_xor_sync(~0u, sum[r].o.x, o);
+        other.o.y = __shfl_xor_sync(~0u, sum[r].o.y, o);
+        other.o.z = __shfl_xor_sync(~0u, sum[r].o.z, o);
+        other.o.w = __shfl_xor_sync(~0u, sum[r].o.w, o);
+        sum[r].add(other);
+      }
+      if (lane < 8) sums[warp][r][lane] = sum[r];
+    }
+    __syncthreads();
+    const int r = threadIdx.x >> 3, in = block * kRows + r0 + r, token = token_of(p, in), h = head * p.shared + in - token * p.shared;
+    const int64_t t = w.first + token;
+    if (r < kJoinRows && r0 + r < w.rows && t >= 0 && t < p.tokens) {
+      Sum all = sums[0][r][lane & 7];
+      for (int k = 1; k < warps; ++k) all.add(sums[k][r][lane & 7]);
+      if (has) put(p, p.out + t * p.out_token + h * p.out_head, ch, all.o, all.l);
+      if (ch == 0) put_lse(p, t * p.heads + h, all.m, all.l);
+    }
+    __syncthreads();
+  }
 }
 
 struct Plan {
   int nc, gs;  // of the kernel: 32-channel pieces, of a group
   int row_blocks, team;
   int grid;          // CTAs
+  int64_t items;
   size_t workspace;  // bytes
 };
 
@@ -111,13 +114,14 @@ bool plan(const kd_cache4* c, const kd_sequences* s, int64_t heads, int64_t wind
       (blocks && items * blocks > INT32_MAX / chunks_of(room)))
     return false;
   pl.row_blocks = (int)blocks;
+  pl.items = items * blocks;
   int64_t longest = std::min(s->longest, room);
   if (window > 0) longest = std::min(longest, window + kRows + kTile);
   const int64_t all = items * blocks, places = 152 * (pl.nc <= 4 ? 4 : 2);
   const double chunks_each = (double)((longest + kTile * kChunk - 1) / (kTile * kChunk));
   // us: a CTA's step by how many share an SM, and a tile of equal shares
   pl.team = 0;
-  double least = 13 + (all < 64 ? 4 : 0) + 0.8 * 0.0036 * all * chunks_each;
+  double least = 10 + 0.003 * all * chunks_each;
   for (int team = 1; team <= 8 && team <= chunks_each; team *= 2) {
     const double rounds = std::ceil((double)all * team / places), on_sm = std::min((double)all * team, (double)places) / 152;
     const double cost = 4.5 + (team > 1 ? 1.2 : 0) + rounds * std::ceil(chunks_each / team) * std::max(0.86, 0.5 + 0.38 * on_sm);
@@ -128,7 +132,7 @@ bool plan(const kd_cache4* c, const kd_sequences* s, int64_t heads, int64_t wind
   }
   pl.grid = (int)(pl.team ? all * pl.team : std::min(places, all * chunks_of(longest)));
   pl.workspace = 0;
-  if (!pl.team) pl.workspace = (size_t)pl.grid * (sizeof(Cut) + 2 * kRows * (8 + 4 * (size_t)((c->d + 3) / 4 * 4)));
+  if (!pl.team) pl.workspace = (size_t)all * sizeof(Cut) + (size_t)pl.grid * 2 * kRows * (8 + 4 * (size_t)((c->d + 3) / 4 * 4));
   pl.workspace = (pl.workspace + 15) / 16 * 16;
   return true;
 }
@@ -201,21 +205,21 @@ extern "C" kd_status kd_attention_4bit(const kd_cache4* cache, const kd_sequence
   p.scale2 = scale * 1.4426950408889634f;
   if (!pl.team) {
     p.cuts = static_cast<Cut*>(workspace);
-    p.part_ml = reinterpret_cast<float2*>(p.cuts + pl.grid);
+    p.part_ml = reinterpret_cast<float2*>(p.cuts + pl.items);
     p.part = reinterpret_cast<float*>(p.part_ml + (int64_t)pl.grid * 2 * kRows);
   }
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  auto launch = pl.team ? (pl.nc <= 4 ? launch_team_128 : launch_team_256) : (pl.nc <= 4 ? launch_shares_128 : launch_shares_256);
+  static constexpr Launch* kLaunch[2][2][2] = {{{launch_shares_128, launch_shares_128_pack}, {launch_shares_256, launch_shares_256_pack}},
+                                               {{launch_team_128, launch_team_128_pack}, {launch_team_256, launch_team_256_pack}}};
+  Launch* launch = kLaunch[pl.team > 0][pl.nc > 4][seqs->most * p.shared <= 4];
   cudaError_t e = launch(p, pl.nc, pl.gs, pl.grid, s);
   if (e == cudaSuccess && !pl.team) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)pl.grid);
-    cfg.blockDim = dim3(kJoinThreads);
+    cfg.gridDim = dim3((unsigned)pl.items, (unsigned)((cache->d + 31) / 32));
+    const int64_t warps = (pl.grid / pl.items + 2 + 3) / 4;  // four parts of an item each
+    cfg.blockDim = dim3(32 * (unsigned)std::min<int64_t>(warps, kJoinWarps));
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    launch_early(attr[0]);
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    // not early: its blocks would wait on the SMs whose shares end first, and be joined there (15 us more)
     e = cudaLaunchKernelEx(&cfg, attn4_join_kernel, p);
   }
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? KD_OK : KD_ERR_CUDA;

@@ -69,17 +69,15 @@ struct Params {
   int room;                     // positions that the table has room for
   int bf16, q_vec, out_vec;
   float scale2;                 // scale log2 e
-  struct Cut* cuts;             // the item that each CTA leaves to the next ones
+  struct Cut* cuts;             // of each item: where its parts are, in equal shares
   float2* part_ml;              // (m, sum) of each row of a CTA's first item and of its last, where they are cut
   float* part;                  // and their sums [CTA][first, last][row][part_row]
   int part_row;                 // d, up to a multiple of 4
 };
 
-// An item whose first chunks are the end of a CTA's share: the sums of its rows are in `slot` and in the first
-// places of the `more` CTAs that follow.
+// An item's parts: in place `slot` (two a CTA), then in the first places of the `more` CTAs that follow `owner`.
 struct Cut {
-  int64_t first;  // row of the sequence's first query token
-  int block, head, rows, slot, more, unused;
+  int owner, slot, more, unused;
 };
 
 // The rows and positions of a block of rows: the same for the kernel that sums and the one that joins.
@@ -218,7 +216,7 @@ struct Shape {
   static constexpr int kQueries = 64 * NC + 64;                      // bytes of a row of queries as operands
   static constexpr size_t kRing = (size_t)kWarps * kStages * kStage * 4, kJoin = (size_t)kWarps * kRows * kSums * 4;
   static constexpr size_t kBytes = (kRing > kJoin ? kRing : kJoin) + kBatch * 16 + (size_t)kWarps * kRows * 8 +
-                                    kRows * (kQueries + 4 * (kGroups + 1)) + 64;
+                                    kRows * (kQueries + 4 * (kGroups + 1));
 };
 
 // fp16 or bf16 bits as a float
@@ -229,26 +227,53 @@ __device__ __forceinline__ uint16_t narrow(const Params& p, float v) {
   return p.bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v)) : __half_as_ushort(__float2half_rn(v));
 }
 
-// The block's exclusive sum of v over its threads, and the total; scratch: kWarps words of shared memory.
-__device__ __forceinline__ int sum_before(int v, int* scratch, int& total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int in = v;
+// The item (s, head, block) and its chunk that chunk `from` of all falls on, and all chunks' number; the whole warp
+// looks, 32 sequences at a time.
+struct Start {
+  int s, head, block, chunk, total;
+};
+__device__ __forceinline__ int chunks_of_head(const Params& p, int s) {
+  int n = 0;
+  if (s < p.c.seqs)
+    for (int b = 0; b < p.row_blocks; ++b) {
+      const int of = work_of(p, s, b, kRows).chunks;
+      if (of == 0) break;  // no rows from here on
+      n += of;
+    }
+  return n;
+}
+__device__ __forceinline__ Start start_of(const Params& p, int blocks, int block, int& per) {
+  const int lane = threadIdx.x & 31;
+  Start at{-1, 0, 0, 0, 0};
+  int first = chunks_of_head(p, lane);  // of the first 32 sequences, which are often all
+  int total = first;
+#pragma unroll 4
+  for (int s = 32 + lane; s - lane < p.c.seqs; s += 32) total += chunks_of_head(p, s);
+  at.total = __reduce_add_sync(~0u, total) * p.c.heads;
+  per = (at.total + blocks - 1) / blocks;  // blocks are fewer than chunks fit 31 bits
+  const int64_t from64 = (int64_t)block * per;
+  if (from64 >= at.total) return at;
+  int from = (int)from64;
+  for (int s0 = 0;; s0 += 32) {
+    const int mine = (s0 ? chunks_of_head(p, s0 + lane) : first) * p.c.heads;
+    int in = mine;
 #pragma unroll
-  for (int o = 1; o < 32; o *= 2) {
-    const int up = __shfl_up_sync(~0u, in, o);
-    if (lane >= o) in += up;
+    for (int o = 1; o < 32; o *= 2) {
+      const int up = __shfl_up_sync(~0u, in, o);
+      if (lane >= o) in += up;
+    }
+    const unsigned past = __ballot_sync(~0u, from < in);
+    if (past) {
+      const int which = __ffs(past) - 1, before = __shfl_sync(~0u, in - mine, which), of = __shfl_sync(~0u, mine, which) / p.c.heads;
+      at.s = s0 + which;
+      at.chunk = from - before;
+      at.head = at.chunk / of;
+      at.chunk -= at.head * of;
+      for (int n; at.chunk >= (n = work_of(p, at.s, at.block, kRows).chunks); ++at.block) at.chunk -= n;
+      return at;
+    }
+    from -= __shfl_sync(~0u, in, 31);
   }
-  if (lane == 31) scratch[warp] = in;
-  __syncthreads();
-  int before = in - v;
-  total = 0;
-#pragma unroll
-  for (int k = 0; k < kWarps; ++k) {
-    if (k < warp) before += scratch[k];
-    total += scratch[k];
-  }
-  __syncthreads();
-  return before;
 }
 
 // four channels of a row from ch on, over the row's total (0: nothing was seen)
@@ -310,20 +335,23 @@ __device__ __forceinline__ void join_team(const Params& p, const Work& w, int he
 }
 
 // TEAM: a cluster of p.team CTAs has an item to itself; else all CTAs have equal shares of all of them
-template <int NC, int GS, bool TEAM>
+// PACK: blocks have at most four rows, and the two tiles of a step four columns each: what follows the key
+// products is done once for both
+template <int NC, int GS, bool TEAM, bool PACK>
 __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(const __grid_constant__ Params p) {
   using Z = Shape<NC, GS>;
   constexpr int GN = Z::kGroups, ST = Z::kStages, S = Z::kStride;
+  // rows; and sets of elements of a step: a tile's, or those of both tiles together
+  constexpr int kColumns = PACK ? 4 : 8, kSets = PACK ? 1 : kTiles;
   extern __shared__ uint4 smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g8 = lane >> 2, t4 = lane & 3;
   // shared memory: the ring, where sums are joined too; places; (m, sum) of the warps' rows; queries, their
-  // groups' sums and powers of two; a few words
+  // groups' sums and powers of two
   char* after = reinterpret_cast<char*>(smem) + (Z::kRing > Z::kJoin ? Z::kRing : Z::kJoin);
   longlong2* place = reinterpret_cast<longlong2*>(after);
   float2* ml = reinterpret_cast<float2*>(place + kBatch);
   char* queries = reinterpret_cast<char*>(ml + kWarps * Z::kRows);
   float* query_sums = reinterpret_cast<float*>(queries + Z::kRows * Z::kQueries);
-  int* words = reinterpret_cast<int*>(query_sums + Z::kRows * (GN + 1));
   depend_on_last();
 
   // This CTA's share: `left` chunks from chunk `chunk` of item (s, head, block) on.
@@ -336,45 +364,14 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
     s = at / p.c.heads;
     left = INT32_MAX;
   } else {
-    const int each = (p.c.seqs + 32 * kWarps - 1) / (32 * kWarps), s0 = threadIdx.x * each, s1 = min(s0 + each, p.c.seqs);
-    auto of_head = [&](int s) {
-      int n = 0;
-      for (int b = 0; b < p.row_blocks; ++b) {
-        const int of = work_of(p, s, b, Z::kRows).chunks;
-        if (of == 0) break;  // no rows from here on
-        n += of;
-      }
-      return n;
-    };
-    int mine = 0, total;
-    for (int i = s0; i < s1; ++i) mine += of_head(i);
-    mine *= p.c.heads;
-    int before = sum_before(mine, words, total);
-    const int per = (int)(((int64_t)total + gridDim.x - 1) / gridDim.x);
-    const int64_t from = (int64_t)blockIdx.x * per;
-    left = (int)min((int64_t)per, total - from);
-    if (threadIdx.x == 0) p.cuts[blockIdx.x].more = 0;
-    if (left <= 0) return;
-    if (from >= before && from < (int64_t)before + mine) {
-      int i = s0, of = of_head(i);
-      while (from >= (int64_t)before + of * p.c.heads) {
-        before += of * p.c.heads;
-        of = of_head(++i);
-      }
-      int in = (int)(from - before), b = 0;
-      const int h = in / of;
-      in -= h * of;
-      for (int n; in >= (n = work_of(p, i, b, Z::kRows).chunks); ++b) in -= n;
-      words[8] = i;
-      words[9] = h;
-      words[10] = b;
-      words[11] = in;
-    }
-    __syncthreads();
-    s = words[8];
-    head = words[9];
-    block = words[10];
-    chunk = words[11];
+    int per;
+    const Start at = start_of(p, gridDim.x, blockIdx.x, per);
+    if (at.s < 0) return;
+    left = min(per, at.total - (int)blockIdx.x * per);
+    s = at.s;
+    head = at.head;
+    block = at.block;
+    chunk = at.chunk;
   }
   const int share = left;
   constexpr int row_bytes = 16 * NC, scale_bytes = 4 * GN;
@@ -505,7 +502,7 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
   {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      const uint4 u = *reinterpret_cast<const uint4*>(queries + (g8) * Z::kQueries + 16 * (4 * c + t4));
+      const uint4 u = *reinterpret_cast<const uint4*>(queries + g8 % kColumns * Z::kQueries + 16 * (4 * c + t4));
       qb[2 * c][0] = u.x;
       qb[2 * c][1] = u.y;
       qb[2 * c + 1][0] = u.z;
@@ -513,7 +510,7 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const float* of_column = query_sums + (2 * t4 + j) * (GN + 1);
+      const float* of_column = query_sums + (2 * t4 + j) % kColumns * (GN + 1);
       const float down = of_column[GN];
 #pragma unroll
       for (int g = 0; g < GN; ++g) qs[g][j] = of_column[g] * down;
@@ -523,12 +520,11 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
   // what the columns' rows see: positions from sees_lo on, below sees_hi
   int sees_lo[2], sees_hi[2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int r = 2 * t4 + j;
-      const int pos = w.before + token_of(p, r0 + r);
-      sees_hi[j] = r >= w.rows ? 0 : min(share_hi, p.causal ? clamp_to(pos + 1, w.length) : w.length);
-      sees_lo[j] = p.window ? clamp_to(pos + 1 - p.window, w.length) : 0;
-    }
+  for (int j = 0; j < 2; ++j) {
+    const int r = (2 * t4 + j) % kColumns, pos = w.before + token_of(p, r0 + r);
+    sees_hi[j] = r >= w.rows ? 0 : min(share_hi, p.causal ? clamp_to(pos + 1, w.length) : w.length);
+    sees_lo[j] = p.window ? clamp_to(pos + 1 - p.window, w.length) : 0;
+  }
 
   float acc[Z::kSumTiles][4];
   // of the columns: sums of weights times middles and of weights (of the positions g8 and g8 + 8 of the tiles
@@ -551,75 +547,79 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
 
   // One step.  EDGE: some row does not see all of it, or a page is bad.
   const uint32_t matrix_at = (lane & 15) * S * 4 + (lane >> 4) * 16;  // this lane's row of four matrices
+  const int own = PACK ? t4 >> 1 : 0;  // whose elements are the lane's of a set: the second tile's, in the upper columns
   auto step = [&](auto edge, int stage, int position, bool bad0, bool bad1) {
     constexpr bool EDGE = decltype(edge)::value;
     const uint32_t codes = ring_at + stage * (Z::kStage * 4) + matrix_at;
-    const uint32_t* kp = ring + stage * Z::kStage + 2 * Z::kCodes + g8 * GN;
+    const uint32_t* kp = ring + stage * Z::kStage + 2 * Z::kCodes + (kTile * own + g8) * GN;
     const uint32_t* vp = kp + Z::kScales;
-    float x[kTiles][4];  // scores less m
-    bool seen[kTiles][4];
+    float x[kSets][4];  // scores less m
+    bool seen[kSets][4];
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-      float part[4], low[4];
+    for (int i = 0; i < kSets; ++i) {
+      float part[kTiles][4], low[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[i][e] = 0.f;
-          low[e] = -m[e & 1];
-        }
-      uint32_t w[4];  // positions g8, g8 + 8 of one piece, and of the next
+      for (int e = 0; e < 4; ++e) {
+        x[i][e] = 0.f;
+        low[e] = -m[e & 1];
+      }
+      uint32_t w[kTiles][4];  // positions g8, g8 + 8 of one piece, and of the next
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        if (c % 2 == 0) {
-          if (c + 1 < NC) load_matrices<false>(w, codes + i * kTile * S * 4 + c * 16);
-          else load_two_matrices<false>(w, codes + i * kTile * S * 4 + c * 16);
-        }
-        uint32_t a = w[c % 2 * 2], b = w[c % 2 * 2 + 1];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t a0 = a & 0x000F000Fu, a1 = b & 0x000F000Fu, a2 = a & 0x00F000F0u, a3 = b & 0x00F000F0u;
-          {
-            if (c % GS == 0 && h == 0) mma_first(part, a0, a1, a2, a3, qb[2 * c][0], qb[2 * c][1]);
-            else mma(part, a0, a1, a2, a3, qb[2 * c + h][0], qb[2 * c + h][1]);
+        for (int n = 0; n < (PACK ? kTiles : 1); ++n) {
+          const int of = PACK ? n : i;  // the tile
+          if (c % 2 == 0) {
+            if (c + 1 < NC) load_matrices<false>(w[n], codes + of * kTile * S * 4 + c * 16);
+            else load_two_matrices<false>(w[n], codes + of * kTile * S * 4 + c * 16);
           }
-          a >>= 8;
-          b >>= 8;
+          uint32_t a = w[n][c % 2 * 2], b = w[n][c % 2 * 2 + 1];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t a0 = a & 0x000F000Fu, a1 = b & 0x000F000Fu, a2 = a & 0x00F000F0u, a3 = b & 0x00F000F0u;
+            if (c % GS == 0 && h == 0) mma_first(part[n], a0, a1, a2, a3, qb[2 * c][0], qb[2 * c][1]);
+            else mma(part[n], a0, a1, a2, a3, qb[2 * c + h][0], qb[2 * c + h][1]);
+            a >>= 8;
+            b >>= 8;
+          }
         }
         if ((c + 1) % GS == 0 || c == NC - 1) {
           const uint32_t u = kp[i * kTile * GN + c / GS], v = kp[(i * kTile + 8) * GN + c / GS];
           const float s0 = low_half(u), l0 = high_half(u), s1 = low_half(v), l1 = high_half(v);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              x[i][e] = __fmaf_rn(e < 2 ? s0 : s1, part[e], x[i][e]);
-              low[e] = __fmaf_rn(e < 2 ? l0 : l1, qs[c / GS][e & 1], low[e]);
-            }
+          for (int e = 0; e < 4; ++e) {
+            x[i][e] = __fmaf_rn(e < 2 ? s0 : s1, PACK && own ? part[1][e] : part[0][e], x[i][e]);
+            low[e] = __fmaf_rn(e < 2 ? l0 : l1, qs[c / GS][e & 1], low[e]);
+          }
         }
       }
 #pragma unroll
-        for (int e = 0; e < 4; e += 2) {
-          const float2 of = fma2(make_float2(x[i][e], x[i][e + 1]), make_float2(qe[0], qe[1]), make_float2(low[e], low[e + 1]));
-          x[i][e] = of.x;
-          x[i][e + 1] = of.y;
-          if constexpr (EDGE) {
-            const int pos = position + kTile * i + g8 + 4 * e;
+      for (int e = 0; e < 4; e += 2) {
+        const float2 of = fma2(make_float2(x[i][e], x[i][e + 1]), make_float2(qe[0], qe[1]), make_float2(low[e], low[e + 1]));
+        x[i][e] = of.x;
+        x[i][e + 1] = of.y;
+        if constexpr (EDGE) {
+          const int pos = position + kTile * (i + own) + g8 + 4 * e;
+          const bool bad = i + own ? bad1 : bad0;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              seen[i][e + j] = pos < sees_hi[j] && pos >= sees_lo[j];
-              x[i][e + j] = !seen[i][e + j] ? kNone : (i ? bad1 : bad0) ? __int_as_float(0x7FC00000) : x[i][e + j];
-            }
+          for (int j = 0; j < 2; ++j) {
+            seen[i][e + j] = pos < sees_hi[j] && pos >= sees_lo[j];
+            x[i][e + j] = !seen[i][e + j] ? kNone : bad ? __int_as_float(0x7FC00000) : x[i][e + j];
           }
         }
+      }
     }
-    uint32_t vscale[kTiles][GN][2];
+    uint32_t vscale[kSets][GN][2];
     __half2 tops = __half2half2(__ushort_as_half(0));  // the larger step, in the low half
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i)
+    for (int i = 0; i < kSets; ++i)
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int g = 0; g < GN; ++g) {
           uint32_t v = vp[(kTile * i + 8 * k) * GN + g];
           if constexpr (EDGE) {  // a position that no row sees may hold anything
-            const int pos = position + kTile * i + g8 + 8 * k;
+            const int pos = position + kTile * (i + own) + g8 + 8 * k;
             if (pos >= share_hi || pos < w.lo) v = 0;
           }
           vscale[i][g][k] = v;
@@ -630,7 +630,8 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
     float most[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        most[j] = fmaxf(fmaxf(x[0][j], x[0][j + 2]), fmaxf(x[1][j], x[1][j + 2]));
+        most[j] = fmaxf(x[0][j], x[0][j + 2]);
+      if (kSets == 2) most[j] = fmaxf(most[j], fmaxf(x[kSets - 1][j], x[kSets - 1][j + 2]));
         grow |= most[j] > room[j];
       }
     if (__any_sync(~0u, grow)) {
@@ -659,7 +660,7 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
           m[j] += to;
           room[j] = 8.f;
 #pragma unroll
-          for (int i = 0; i < kTiles; ++i) {
+          for (int i = 0; i < kSets; ++i) {
             x[i][j] -= to;
             x[i][j + 2] -= to;
           }
@@ -677,7 +678,7 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
     uint32_t bw[kTiles][GN][2];
     float all[GN][4];  // of each column, in every row: 2^-24 of the step's weights as they are rounded
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
+    for (int i = 0; i < kSets; ++i) {
       float2 wt[2];  // of a column, positions g8 and g8 + 8
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -703,11 +704,19 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
               mids[g][j] = fma2(wt[j], mid, mids[g][j]);
             }
           }
-          bw[i][g][0] = turned(pack2<KD_F16>(b[0].x, b[1].x));
-          bw[i][g][1] = turned(pack2<KD_F16>(b[0].y, b[1].y));
+          const uint32_t b0 = turned(pack2<KD_F16>(b[0].x, b[1].x)), b1 = turned(pack2<KD_F16>(b[0].y, b[1].y));
           constexpr uint32_t one = 0x00010001u;
-          if (i == 0) mma_first(all[g], one, one, one, one, bw[i][g][0], bw[i][g][1]);
-          else mma(all[g], one, one, one, one, bw[i][g][0], bw[i][g][1]);
+          if (i == 0) mma_first(all[g], one, one, one, one, b0, b1);
+          else mma(all[g], one, one, one, one, b0, b1);
+          if constexpr (PACK) {  // each tile's operand has its own columns only
+            bw[0][g][0] = g8 < 4 ? b0 : 0u;
+            bw[0][g][1] = g8 < 4 ? b1 : 0u;
+            bw[1][g][0] = g8 < 4 ? 0u : b0;
+            bw[1][g][1] = g8 < 4 ? 0u : b1;
+          } else {
+            bw[i][g][0] = b0;
+            bw[i][g][1] = b1;
+          }
         }
       }
     }
@@ -808,21 +817,23 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
     const int token = token_of(p, r0 + r), h = head * p.shared + (r0 + r) - token * p.shared;
     const int64_t t = w.first + token;
     if (t < 0 || t >= p.tokens) continue;
-    float top = kNone, total = 0.f, f[kWarps];
+    // the parts of a row: each warp's, of one tile and the other where they have columns of their own
+    constexpr int kParts = PACK ? 2 * kWarps : kWarps, kApart = PACK ? 4 : Z::kRows;
+    float top = kNone, total = 0.f, f[kParts];
 #pragma unroll
-    for (int k = 0; k < kWarps; ++k) top = fmaxf(top, ml[k * Z::kRows + r].x);
+    for (int k = 0; k < kParts; ++k) top = fmaxf(top, ml[k * kApart + r].x);
 #pragma unroll
-    for (int k = 0; k < kWarps; ++k) {
-      const float2 v = ml[k * Z::kRows + r];
+    for (int k = 0; k < kParts; ++k) {
+      const float2 v = ml[k * kApart + r];
       f[k] = v.x == kNone ? 0.f : exp2_of(v.x - top);
-      total += v.x == kNone ? v.y : v.y * f[k];  // a warp without a maximum has summed nothing, or NaN
+      total += v.x == kNone ? v.y : v.y * f[k];  // a part without a maximum has summed nothing, or NaN
     }
     if (past_table(p, w, token)) total = __int_as_float(0x7FC00000);
     for (int ch = 4 * lane; ch < p.part_row; ch += 128) {
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int k = 0; k < kWarps; ++k) {
-        const float4 v = *reinterpret_cast<const float4*>(sums + (k * Z::kRows + r) * Z::kSums + ch);
+      for (int k = 0; k < kParts; ++k) {
+        const float4 v = *reinterpret_cast<const float4*>(sums + (k * kApart + r) * Z::kSums + ch);
         o.x = __fmaf_rn(v.x, f[k], o.x);
         o.y = __fmaf_rn(v.y, f[k], o.y);
         o.z = __fmaf_rn(v.z, f[k], o.z);
@@ -839,11 +850,8 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
       else p.part_ml[slot * Z::kRows + r] = make_float2(top, total);
     }
   }
-  if (cut && !TEAM && chunk == 0 && threadIdx.x == 0) {
-    // the item goes on in the CTAs that follow
-    const int rest = w.chunks - n_chunks;
-    p.cuts[blockIdx.x] = Cut{w.first, block, head, w.rows, (int)slot, (rest + share - 1) / share, 0};
-  }
+  if (!TEAM && chunk == 0 && threadIdx.x == 0)  // what is left of the item is the CTAs' that follow
+    p.cuts[((int64_t)s * p.c.heads + head) * p.row_blocks + block] = Cut{(int)blockIdx.x, (int)slot, (w.chunks - n_chunks + share - 1) / share, 0};
   left -= n_chunks;
   }
   if constexpr (TEAM) {
@@ -875,10 +883,10 @@ cudaError_t allow_shared_memory(Kernel kernel, std::atomic<uint64_t>& ready) {
   return e;
 }
 
-template <int NC, int GS, bool TEAM>
+template <int NC, int GS, bool TEAM, bool PACK>
 cudaError_t launch_one(const Params& p, int grid, cudaStream_t s) {
   static_assert(Shape<NC, GS>::kBytes <= 227 * 1024, "shared memory");
-  auto kernel = attn4_kernel<NC, GS, TEAM>;
+  auto kernel = attn4_kernel<NC, GS, TEAM, PACK>;
   static std::atomic<uint64_t> ready{0};
   const cudaError_t e = allow_shared_memory(kernel, ready);
   if (e != cudaSuccess) return e;
@@ -897,20 +905,20 @@ cudaError_t launch_one(const Params& p, int grid, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 // gs: 32-channel pieces of a group
-template <int NC, bool TEAM>
+template <int NC, bool TEAM, bool PACK>
 cudaError_t launch(const Params& p, int gs, int grid, cudaStream_t s) {
   if constexpr (NC > 2)
-    if (gs == 4) return launch_one<NC, 4, TEAM>(p, grid, s);
+    if (gs == 4) return launch_one<NC, 4, TEAM, PACK>(p, grid, s);
   if constexpr (NC > 1)
-    if (gs >= 2) return launch_one<NC, 2, TEAM>(p, grid, s);
-  return launch_one<NC, 1, TEAM>(p, grid, s);
+    if (gs >= 2) return launch_one<NC, 2, TEAM, PACK>(p, grid, s);
+  return launch_one<NC, 1, TEAM, PACK>(p, grid, s);
 }
 
-// nc: 32-channel pieces of a row, 1 to 4 and 5 to 8
-cudaError_t launch_team_128(const Params& p, int nc, int gs, int grid, cudaStream_t s);
-cudaError_t launch_team_256(const Params& p, int nc, int gs, int grid, cudaStream_t s);
-cudaError_t launch_shares_128(const Params& p, int nc, int gs, int grid, cudaStream_t s);
-cudaError_t launch_shares_256(const Params& p, int nc, int gs, int grid, cudaStream_t s);
+// Of one translation unit each: with NC = 1 to 4 or 5 to 8, clusters or equal shares, blocks of eight rows or of
+// four.  nc: 32-channel pieces of a row
+using Launch = cudaError_t(const Params& p, int nc, int gs, int grid, cudaStream_t s);
+Launch launch_team_128, launch_team_256, launch_shares_128, launch_shares_256;
+Launch launch_team_128_pack, launch_team_256_pack, launch_shares_128_pack, launch_shares_256_pack;
 
 }  // namespace attn4
 }  // namespace kd

@@ -1,9 +1,9 @@
-// kd_attention_4bit's kernels for heads of up to 128 channels, an item to a cluster.
+// kd_attention_4bit's kernels for heads of up to 128 channels, an item to a cluster, blocks of eight rows.
 #include "kd_attn4.cuh"
 
 cudaError_t kd::attn4::launch_team_128(const Params& p, int nc, int gs, int grid, cudaStream_t s) {
-  return nc == 1   ? launch<1, true>(p, gs, grid, s)
-         : nc == 2 ? launch<2, true>(p, gs, grid, s)
-         : nc == 3 ? launch<3, true>(p, gs, grid, s)
-                   : launch<4, true>(p, gs, grid, s);
+  return nc == 1   ? launch<1, true, false>(p, gs, grid, s)
+         : nc == 2 ? launch<2, true, false>(p, gs, grid, s)
+         : nc == 3 ? launch<3, true, false>(p, gs, grid, s)
+                   : launch<4, true, false>(p, gs, grid, s);
 }

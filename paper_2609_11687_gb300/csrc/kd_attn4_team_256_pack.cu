@@ -1,0 +1,9 @@
+// kd_attention_4bit's kernels for heads of 129 to 256 channels, an item to a cluster, blocks of four rows.
+#include "kd_attn4.cuh"
+
+cudaError_t kd::attn4::launch_team_256_pack(const Params& p, int nc, int gs, int grid, cudaStream_t s) {
+  return nc == 5   ? launch<5, true, true>(p, gs, grid, s)
+         : nc == 6 ? launch<6, true, true>(p, gs, grid, s)
+         : nc == 7 ? launch<7, true, true>(p, gs, grid, s)
+                   : launch<8, true, true>(p, gs, grid, s);
+}

@@ -136,17 +136,19 @@ class Case:
                                      (1, 32), (200, 128), (100, 32), (250, 64), (129, 128)])
 def test_heads_and_groups(kd, d, group, dt):
     Case(kd, [1, 17, 100, 0, 333], [1, 1, 1, 1, 1], 4, 2, d, group=group, dt=dt).check(kd)
+    Case(kd, [1, 17, 100, 0, 333], [1, 3, 2, 1, 5], 4, 2, d, group=group, dt=dt).check(kd)
 
 
 @pytest.mark.parametrize("d,group", [(128, 32), (128, 64), (128, 128), (64, 32), (64, 64), (32, 32), (96, 32), (96, 64), (96, 128),
                                      (160, 32), (160, 64), (160, 128), (192, 32), (192, 64), (192, 128), (224, 32), (224, 64), (224, 128),
                                      (256, 32), (256, 64), (256, 128)])
-def test_equal_shares(kd, d, group):
+@pytest.mark.parametrize("drafted", [0, 1])
+def test_equal_shares(kd, d, group, drafted):
     """Lengths that may be long (the host knows the table's room only): equal shares of all positions for
     every CTA, of which one here has several items, another a part of one."""
     rng = np.random.RandomState(d)
     lengths = rng.randint(0, 900, 40).tolist() + [0, 5000, 1, 3]
-    c = Case(kd, lengths, [1] * 20 + [2, 0] * 12, 6, 2, d, group=group, dt=BF16, spare=1, room=100000)
+    c = Case(kd, lengths, [1] * 20 + [1 + drafted, 0] * 12, 6, 2, d, group=group, dt=BF16, spare=1, room=100000)
     assert kd.attention_4bit_workspace(c.cache, c.seqs, 6) > 0
     first = c.check(kd)
     again = c.run(kd)
