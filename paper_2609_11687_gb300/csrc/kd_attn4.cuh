@@ -433,8 +433,8 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
     }
   };
 
-  // The rows as operands, a warp a row: fp16 in eights of channels 0 4 1 5 2 6 3 7, the odd ones over 16, with
-  // the row's power of two and its sums over groups.
+  // The rows as operands, a warp a row: fp16 in eights of channels 0 4 1 5 2 6 3 7, with the
+  // row's power of two and its sums over groups.
   const int r0 = block * Z::kRows;
   constexpr int kOfWarp = Z::kRows / kWarps;
   uint32_t raw[kOfWarp][4];  // lane l has channels 8 l .. 8 l + 7 (of 256)
@@ -484,7 +484,6 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
     for (int e = 0; e < 8; ++e) {
       v[e] *= up;
       sum += v[e];
-      if (e % 2) v[e] *= 0.0625f;
     }
     if (lane < 4 * NC)
       *reinterpret_cast<uint4*>(queries + r * Z::kQueries + 16 * lane) =
@@ -514,7 +513,7 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
       const float down = of_column[GN];
 #pragma unroll
       for (int g = 0; g < GN; ++g) qs[g][j] = of_column[g] * down;
-      qe[j] = down * 1024.f;  // codes' 2^24 less q's 2^14
+      qe[j] = down * 64.f;  // codes' 2^20 less q's 2^14
     }
   }
   // what the columns' rows see: positions from sees_lo on, below sees_hi
@@ -573,14 +572,14 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
             if (c + 1 < NC) load_matrices<false>(w[n], codes + of * kTile * S * 4 + c * 16);
             else load_two_matrices<false>(w[n], codes + of * kTile * S * 4 + c * 16);
           }
-          uint32_t a = w[n][c % 2 * 2], b = w[n][c % 2 * 2 + 1];
+          const uint32_t a = w[n][c % 2 * 2], b = w[n][c % 2 * 2 + 1];
+          constexpr uint32_t mask = 0x00F000F0u;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const uint32_t a0 = a & 0x000F000Fu, a1 = b & 0x000F000Fu, a2 = a & 0x00F000F0u, a3 = b & 0x00F000F0u;
+            const uint32_t a0 = (h ? a >> 4 : a << 4) & mask, a1 = (h ? b >> 4 : b << 4) & mask;
+            const uint32_t a2 = (h ? a >> 8 : a) & mask, a3 = (h ? b >> 8 : b) & mask;
             if (c % GS == 0 && h == 0) mma_first(part[n], a0, a1, a2, a3, qb[2 * c][0], qb[2 * c][1]);
             else mma(part[n], a0, a1, a2, a3, qb[2 * c + h][0], qb[2 * c + h][1]);
-            a >>= 8;
-            b >>= 8;
           }
         }
         if ((c + 1) % GS == 0 || c == NC - 1) {
@@ -676,7 +675,7 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
     }
     // weights, and the operands of the values
     uint32_t bw[kTiles][GN][2];
-    float all[GN][4];  // of each column, in every row: 2^-24 of the step's weights as they are rounded
+    float all[GN][4];  // of each column, in every row: the step's weights as they are rounded
 #pragma unroll
     for (int i = 0; i < kSets; ++i) {
       float2 wt[2];  // of a column, positions g8 and g8 + 8
@@ -705,7 +704,7 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
             }
           }
           const uint32_t b0 = turned(pack2<KD_F16>(b[0].x, b[1].x)), b1 = turned(pack2<KD_F16>(b[0].y, b[1].y));
-          constexpr uint32_t one = 0x00010001u;
+          constexpr uint32_t one = 0x3C003C00u;
           if (i == 0) mma_first(all[g], one, one, one, one, b0, b1);
           else mma(all[g], one, one, one, one, b0, b1);
           if constexpr (PACK) {  // each tile's operand has its own columns only
@@ -727,8 +726,8 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
         {
           float(&d)[4] = acc[2 * c + k];
           const float2 eight = make_float2(all[c / GS][0], all[c / GS][1]);
-          const float2 even = fma2(eight, make_float2(-8.f, -8.f), make_float2(d[0], d[1]));
-          const float2 both = fma2(eight, make_float2(-136.f, -136.f), make_float2(d[2], d[3]));
+          const float2 even = fma2(eight, make_float2(-8.f * 0x1p-24f, -8.f * 0x1p-24f), make_float2(d[0], d[1]));
+          const float2 both = fma2(eight, make_float2(-136.f * 0x1p-24f, -136.f * 0x1p-24f), make_float2(d[2], d[3]));
           d[0] = even.x;
           d[1] = even.y;
           d[2] = both.x;
