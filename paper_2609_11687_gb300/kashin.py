@@ -32,6 +32,7 @@ import ctypes
 import dataclasses
 import functools
 import os
+import struct
 from typing import Optional
 
 import numpy as np
@@ -1267,7 +1268,7 @@ class Rotation:
     ``"half"``) or side by side (``"interleaved"``), by position times ``frequencies``
     (``rotary_frequencies`` unless given).  The table is made here, once, on the host."""
 
-    __slots__ = ("rot", "layout", "frequencies", "amplitude", "turns", "index")
+    __slots__ = ("rot", "layout", "frequencies", "amplitude", "turns", "index", "table", "half")
 
     def __init__(self, rot: int, base: float = 10000.0, layout: str = "half", scaling: Optional[Scaling] = None,
                  frequencies=None, amplitude: Optional[float] = None, device="cuda"):
@@ -1289,37 +1290,48 @@ class Rotation:
             amplitude = 1.0 if scaling is None else scaling.amplitude
         self.rot, self.layout, self.frequencies, self.amplitude = int(rot), layout, frequencies, float(amplitude)
         self.turns = torch.from_numpy(turns.view(np.int64)).to(device)
-        self.index = self.turns.get_device()
+        self.index, self.table = self.turns.get_device(), self.turns.data_ptr()
+        self.half = KD_ROPE_HALF if layout == "half" else KD_ROPE_INTERLEAVED
 
 
-def _ld3(t, name, types, index, shape=None):
-    """Strides over tokens and heads of a (tokens, heads, d) operand after its checks; what a
-    size of 1 leaves open is 0."""
-    size, stride = t.shape, t.stride()
-    if len(size) != 3:
+def _refuse3(t, name, types, index, shape):
+    """Says what is wrong with one (tokens, heads, channels) operand."""
+    if len(t.shape) != 3:
         raise ValueError(f"{name} must be (tokens, heads, channels)")
     if t.dtype not in types:
         raise ValueError(f"{name} has dtype {t.dtype}: one of {', '.join(map(str, types))} is wanted")
     if not t.is_cuda or t.get_device() != index:
         raise ValueError(f"{name} must be a CUDA tensor on " + ("one device with the others" if index < 0 else f"cuda:{index}"))
-    if shape is not None and tuple(size) != tuple(shape):
-        raise ValueError(f"{name} has shape {tuple(size)}: {tuple(shape)} is wanted")
-    if size[2] > 1 and stride[2] != 1:
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}: {tuple(shape)} is wanted")
+    if t.shape[2] > 1 and t.stride(2) != 1:
         raise ValueError(f"{name} needs unit inner stride")
+    raise ValueError(f"{name}'s rows must not overlap")
+
+
+def _ld3(t, name, types, index, shape=None, out=False):
+    """Strides over tokens and heads of a (tokens, heads, d) operand after its checks: a CUDA tensor of
+    one of ``types`` on device ``index``, of ``shape``, with unit inner stride and, of an output, rows that do
+    not overlap.  What a size of 1 leaves open is as if the rows were dense."""
+    size, stride = t.shape, t.stride()
+    if len(size) != 3 or t.dtype not in types or t.get_device() != index or index < 0 \
+            or (shape is not None and size != shape):
+        _refuse3(t, name, types, index, shape)
     tokens, heads, d = size
-    return stride[0] if tokens > 1 else heads * d, stride[1] if heads > 1 else d
+    a, b, c = stride
+    if d > 1 and c != 1:
+        _refuse3(t, name, types, index, shape)
+    if tokens <= 1:
+        a = heads * d
+    if heads <= 1:
+        b = d
+    if out and not ((b >= d and a >= (heads - 1) * b + d) or (a >= d and b >= (tokens - 1) * a + d)
+                    or (tokens <= 1 and b >= d) or (heads <= 1 and a >= d)) and t.numel():
+        _refuse3(t, name, types, index, shape)
+    return a, b
 
 
-def _row_strides(t, name):
-    """_ld3's of an output, whose rows must not overlap."""
-    tokens, heads, d = t.shape
-    a, b = t.stride()[:2]
-    if tokens > 1 and heads > 1:
-        apart = (b >= d and a >= (heads - 1) * b + d) or (a >= d and b >= (tokens - 1) * a + d)
-    else:
-        apart = (tokens <= 1 or a >= d) and (heads <= 1 or b >= d)
-    if not apart and t.numel():
-        raise ValueError(f"{name}'s rows must not overlap")
+_pack_heads = struct.Struct("9q").pack  # a kd_heads
 
 
 def rope(q, k, positions, rotation: Rotation, q_norm=None, k_norm=None, eps: float = 1e-6, out=None, stream=None):
@@ -1331,38 +1343,40 @@ def rope(q, k, positions, rotation: Rotation, q_norm=None, k_norm=None, eps: flo
     ``q_norm``, ``k_norm``: (d,) of that dtype or fp32.  ``out``: the pair of tensors to write, which
     may be ``q`` and ``k`` themselves."""
     floats, _, f32, _, _, _ = _serve()
-    index, dt = rotation.index, q.dtype
-    i64 = rotation.turns.dtype
-    if positions.shape != q.shape[:1] or positions.dtype != i64 or positions.get_device() != index \
+    index, dt, shape = rotation.index, q.dtype, q.shape
+    if positions.shape != shape[:1] or positions.dtype != rotation.turns.dtype or positions.get_device() != index \
             or not positions.is_contiguous():
         raise ValueError("positions must be a contiguous int64 tensor of q's tokens on the rotation's device")
-    out = (None, None) if out is None else out
-    done, descs, d = [], [], q.shape[-1]
-    for name, x, weight, y in (("q", q, q_norm, out[0]), ("k", k, k_norm, out[1])):
-        if x is None:
-            if weight is not None or y is not None:
-                raise ValueError(f"no {name}, but its weight or output")
-            done.append(None)
-            descs.append(None)
-            continue
-        xt, xh = _ld3(x, name, floats if x is q else (dt,), index)
-        if x.shape[0] != q.shape[0] or x.shape[2] != d:
-            raise ValueError("q and k must have the same tokens and channels")
-        if y is None:
-            y = _new(stream, x.shape, dt, x.device)
-        yt, yh = _ld3(y, f"out's {name}", (dt,), index, x.shape)
-        _row_strides(y, f"out's {name}")
-        if weight is not None:
-            _vec(weight, f"{name}_norm", (dt, f32), index, d)
-        descs.append(KdHeads(x.data_ptr(), y.data_ptr(), _ptr(weight), x.shape[1], xt, xh, yt, yh,
-                             0 if weight is None else floats[weight.dtype]))
-        done.append(y)
+    yq, yk = (None, None) if out is None else out
+    qt, qh = _ld3(q, "q", floats, index)
+    tokens, heads, d = shape
     if rotation.rot > d:
         raise ValueError(f"the rotation turns {rotation.rot} channels of {d}")
-    _call("kd_rope", lib.kd_rope, index, stream, ctypes.byref(descs[0]), None if k is None else ctypes.byref(descs[1]),
-          floats[dt], q.shape[0], d, positions.data_ptr(), rotation.turns.data_ptr(), rotation.rot,
-          KD_ROPE_HALF if rotation.layout == "half" else KD_ROPE_INTERLEAVED, rotation.amplitude, eps)
-    return done[0], done[1]
+    if yq is None:
+        yq = _new(stream, shape, dt, q.device)
+    ot, oh = _ld3(yq, "out's q", (dt,), index, shape, True)
+    weight = wt = 0
+    if q_norm is not None:
+        _vec(q_norm, "q_norm", (dt, f32), index, d)
+        weight, wt = q_norm.data_ptr(), floats[q_norm.dtype]
+    sides = [_pack_heads(q.data_ptr(), yq.data_ptr(), weight, heads, qt, qh, ot, oh, wt), None]
+    if k is not None:
+        kt, kh = _ld3(k, "k", (dt,), index)
+        if k.shape[0] != tokens or k.shape[2] != d:
+            raise ValueError("q and k must have the same tokens and channels")
+        if yk is None:
+            yk = _new(stream, k.shape, dt, k.device)
+        ot, oh = _ld3(yk, "out's k", (dt,), index, k.shape, True)
+        weight = wt = 0
+        if k_norm is not None:
+            _vec(k_norm, "k_norm", (dt, f32), index, d)
+            weight, wt = k_norm.data_ptr(), floats[k_norm.dtype]
+        sides[1] = _pack_heads(k.data_ptr(), yk.data_ptr(), weight, k.shape[1], kt, kh, ot, oh, wt)
+    elif k_norm is not None or yk is not None:
+        raise ValueError("no k, but its weight or output")
+    _call("kd_rope", lib.kd_rope, index, stream, sides[0], sides[1], floats[dt], tokens, d, positions.data_ptr(),
+          rotation.table, rotation.rot, rotation.half, rotation.amplitude, eps)
+    return yq, yk
 
 
 class Cache4:
@@ -1450,37 +1464,26 @@ class Sequences:
         self.ref = ctypes.addressof(self.desc)
 
 
-def _cache_rows(cache, seqs, k, v, types):
-    """Tokens and strides of keys and values that go to or come from the cache."""
-    if seqs.index != cache.index:
-        raise ValueError("the sequences must be on the cache's device")
-    strides, tokens = [], None
-    for which, t in (("k", k), ("v", v)):
-        if t is None:
-            strides.append((0, 0))
-            continue
-        strides.append(_ld3(t, which, types, cache.index))
-        if tokens is None:
-            tokens, types = t.shape[0], (t.dtype,)
-        if tuple(t.shape) != (tokens, cache.heads, cache.d):
-            raise ValueError(f"{which} has shape {tuple(t.shape)}: ({tokens}, {cache.heads}, {cache.d}) is wanted")
-    return tokens, strides
-
-
 def cache_write_4bit(cache: Cache4, k, v, seqs: Sequences, stream=None) -> None:
     """Quantises the rows ``k`` and ``v`` (tokens, heads, d; fp16, bf16 or fp32) of the sequences'
     last tokens into their places of the cache (kd_cache_write_4bit)."""
-    floats = _serve()[0]
-    tokens, ((kt, kh), (vt, vh)) = _cache_rows(cache, seqs, k, v, floats)
-    _call("kd_cache_write_4bit", lib.kd_cache_write_4bit, cache.index, stream, cache.ref, seqs.ref, tokens, k.data_ptr(), kt,
-          kh, v.data_ptr(), vt, vh, floats[k.dtype])
+    floats, index, dt = _serve()[0], cache.index, k.dtype
+    kt, kh = _ld3(k, "k", floats, index)
+    vt, vh = _ld3(v, "v", (dt,), index, k.shape)
+    tokens, heads, d = k.shape
+    if heads != cache.heads or d != cache.d:
+        raise ValueError(f"k has shape {tuple(k.shape)}: ({tokens}, {cache.heads}, {cache.d}) is wanted")
+    if seqs.index != index:
+        raise ValueError("the sequences must be on the cache's device")
+    _call("kd_cache_write_4bit", lib.kd_cache_write_4bit, index, stream, cache.ref, seqs.ref, tokens, k.data_ptr(), kt,
+          kh, v.data_ptr(), vt, vh, floats[dt])
 
 
 def cache_read_4bit(cache: Cache4, seqs: Sequences, tokens: Optional[int] = None, dtype=None, out=None, stream=None):
     """The rows of the sequences' last tokens out of the cache: the pair of ``out``, either of which
     may be None, or new ones of ``tokens`` rows (every sequence's ``most`` without it and without
     ``starts``) in ``dtype`` (fp16) (kd_cache_read_4bit)."""
-    floats = _serve()[0]
+    floats, index = _serve()[0], cache.index
     if out is None:
         if tokens is None:
             if seqs.starts is not None:
@@ -1489,14 +1492,22 @@ def cache_read_4bit(cache: Cache4, seqs: Sequences, tokens: Optional[int] = None
         shape = (tokens, cache.heads, cache.d)
         out = tuple(_new(stream, shape, dtype or _torch().float16, cache.device) for _ in range(2))
     k, v = out
-    if k is None and v is None:
+    first = v if k is None else k
+    if first is None:
         raise ValueError("out wants keys or values")
-    tokens, ((kt, kh), (vt, vh)) = _cache_rows(cache, seqs, k, v, floats)
-    for name, t in (("k", k), ("v", v)):
-        if t is not None:
-            _row_strides(t, f"out's {name}")
-    _call("kd_cache_read_4bit", lib.kd_cache_read_4bit, cache.index, stream, cache.ref, seqs.ref, tokens, _ptr(k), kt, kh,
-          _ptr(v), vt, vh, floats[(v if k is None else k).dtype])
+    if seqs.index != index:
+        raise ValueError("the sequences must be on the cache's device")
+    shape, dt = first.shape, first.dtype
+    kt = kh = vt = vh = 0
+    k_ptr = v_ptr = None
+    if k is not None:
+        (kt, kh), k_ptr = _ld3(k, "out's k", floats, index, None, True), k.data_ptr()
+    if v is not None:
+        (vt, vh), v_ptr = _ld3(v, "out's v", floats if k is None else (dt,), index, shape, True), v.data_ptr()
+    if shape[1] != cache.heads or shape[2] != cache.d:
+        raise ValueError(f"out has shape {tuple(shape)}: ({shape[0]}, {cache.heads}, {cache.d}) is wanted")
+    _call("kd_cache_read_4bit", lib.kd_cache_read_4bit, index, stream, cache.ref, seqs.ref, shape[0], k_ptr, kt, kh, v_ptr,
+          vt, vh, floats[dt])
     return k, v
 
 
@@ -1522,8 +1533,7 @@ def attention_4bit(cache: Cache4, q, seqs: Sequences, scale: Optional[float] = N
         raise ValueError("the sequences must be on the cache's device")
     if out is None:
         out = _new(stream, q.shape, dt, q.device)
-    ot, oh = _ld3(out, "out", (dt,), index, q.shape)
-    _row_strides(out, "out")
+    ot, oh = _ld3(out, "out", (dt,), index, q.shape, True)
     if lse is not None and (lse.dtype != f32 or lse.shape != q.shape[:2] or lse.get_device() != index or not lse.is_contiguous()):
         raise ValueError(f"lse must be a contiguous torch.float32 {(tokens, heads)} tensor on the cache's device")
     if window < 0 or (window and not causal):
