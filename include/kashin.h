@@ -693,8 +693,8 @@ typedef struct kd_cache4 {
  *   starts   device int32, seqs + 1 values that do not decrease; NULL: every sequence has `most`
  *            rows.
  *   most     rows of one sequence at most.
- *   longest  the largest length, as far as the host knows it (at most wide * page): a hint for how
- *            attention is split, not a limit.
+ *   longest  the largest length, as far as the host knows it: a hint for how attention is split, not
+ *            a limit.
  * The contents are read on the device and checked there: a row of no sequence (behind the
  * last one, or past `most` of its sequence) has no effect and is not written; a position below
  * 0 has no place; a page number outside 0 .. pages - 1, or one past the table, is a bad page. */
@@ -747,11 +747,11 @@ size_t kd_attention_4bit_workspace(const kd_cache4* cache, const kd_sequences* s
  *   lse      optional, fp32 tokens x heads: ln sum_p exp(scale <q, key[p]>).
  * A row that sees nothing: out 0, lse -infinity.  What a row does not see does not touch it,
  * whatever is there.  A bad page that a row sees makes it NaN, and so do NaN there and in q.
- * Meant for few rows of a sequence (decoding, drafted tokens): 16 rows times heads for each cache head
- * share a pass over its codes, more take more passes.  Scores are exact products summed in fp32;
- * the weights are rounded to fp16 as factors of a value's distance from the middle of its group, their
- * sums are fp32; the whole is rounded once.  The order of all sums is fixed by the sizes and lengths
- * (deterministic results).
+ * Meant for few rows of a sequence (decoding, drafted tokens): eight rows times heads for each cache
+ * head share a pass over its codes, more take more passes (for a long prompt kd_cache_read_4bit and a
+ * dense product are the shorter way).  Scores are exact products summed in fp32; the weights are rounded to
+ * fp16 as factors of a value's distance from the middle of its group, their sums are fp32; the whole is
+ * rounded once.  The order of all sums is fixed by the sizes and lengths (deterministic results).
  *   workspace  device, 16-byte aligned, ws_bytes >= kd_attention_4bit_workspace(...); it must not
  *              be shared by calls in flight on different streams.
  * Errors: KD_ERR_INVALID_ARG (cache, sequences, heads, type, window < 0 or without causal, scale

@@ -97,8 +97,20 @@ struct Plan {
   size_t workspace;  // bytes
 };
 
-// How the work is cut: into items (sequence, key head, block of rows) where those are short, else into equal
-// shares of all of it, however long each sequence is, as many as CTAs fit the GPU at a time.
+// How the work is cut: a cluster for each item (sequence, key head, block of rows), or equal shares of all of it.
+// Clusters need no search and no second launch, but are done when the longest is; equal shares take all SMs
+// whatever the lengths.  The rule estimates both in microseconds from the longest length that the host knows:
+//   a cluster of t CTAs: 4.5, 1.2 for its join, and for each round of CTAs that fit the GPU its steps of 128 positions
+//   at 0.86 where a CTA has an SM to itself, up to 2 where four share it;
+//   equal shares: 10, and 3 ns for each such step of all items (HBM's rate).
+// Measured for heads of 128 channels, groups of 64, four rows, clusters of 1 / 2 / 4 / 8 and equal shares:
+//     8 items of  1024 positions   10.4 / 9.4 / 7.8 / 7.4,   8.7
+//     8 items of  8192             54 / 31 / 19 / 12.9,     12.6
+//    32 items of  4096             29 / 18 / 11.9 / 10.5,   12.7
+//   256 items of  1024             13.6 / 15.2 / 21 / 34,   17.2
+//   256 items of  4096             38 / 37 / 42 / 53,       39
+//   256 items of  2000 to 8192     65 / 57 / 54 / 63,       52
+//   512 items of  8192             120 / 111 / 121 / 138,   124;  of 2000 to 8192  105 / 91 / 93 / 114,  83
 bool plan(const kd_cache4* c, const kd_sequences* s, int64_t heads, int64_t window, Plan& pl) {
   const int64_t shared = heads / c->heads;
   if (s->most * shared > INT32_MAX) return false;
@@ -119,7 +131,6 @@ bool plan(const kd_cache4* c, const kd_sequences* s, int64_t heads, int64_t wind
   if (window > 0) longest = std::min(longest, window + kRows + kTile);
   const int64_t all = items * blocks, places = 152 * (pl.nc <= 4 ? 4 : 2);
   const double chunks_each = (double)((longest + kTile * kChunk - 1) / (kTile * kChunk));
-  // us: a CTA's step by how many share an SM, and a tile of equal shares
   pl.team = 0;
   double least = 10 + 0.003 * all * chunks_each;
   for (int team = 1; team <= 8 && team <= chunks_each; team *= 2) {

@@ -5,36 +5,55 @@
 //
 // one pass over the codes with the running maximum m and sum of the softmax, on the tensor cores in
 // fp16 (mma.sync m16n8k16), with the codes as the A operand of both products and the rows (query
-// tokens times the heads that share a key head) as the eight columns of B: a decoded token of up to
-// eight heads fills a tile, and the codes go from their word to the operand in registers.
+// tokens times the heads that share a key head) as the eight columns of B.  The codes go from their word to
+// the operand in registers; tcgen05 would want them stored as 16-bit operands first, and its
+// smallest products have no use for eight rows.
 //
 // Codes.  A code masked out of its word is an fp16 number as it stands: c in a half's low bits is
-// c 2^-24, four bits higher 16 c 2^-24, both below fp16's normal range, where the tensor cores
-// are exact.  So a word of eight codes takes four masks and one shift.
-// The 16 goes into q (keys: the odd channels' q over 16) and into the last step (values: the odd
-// channels' sums over 16).  q is brought to 2^14 .. 2^15 by a power of two for each row, so that its
-// fp16 or bf16 digits all stay; scores are exact products summed in fp32.
+// c 2^-24, four bits higher 16 c 2^-24, both below fp16's normal range.  No arithmetic makes them
+// operands.  The tensor cores take such numbers exactly but sum products by the operands' exponents, of which these
+// have the lowest: what lies far below the largest product is cut off, the more the smaller c 2^-24
+// is.  So keys' codes all stand four bits higher (a shift for three of four), for log-sum-exps within 1e-6;
+// values' tiles have even channels' codes in one half of their rows and even plus 16 odd ones (a byte as it
+// stands) in the other, from whose sums the odd channels' come off in the end.
 //
-// Middles.  The tensor cores cut what does not fit their sums off (they do not round), so large sums
-// that cancel in the end lose digits.  Codes therefore count from 8: value = low + 8 step + step (c - 8).
-// Keys' sums over a group start at -8 sum q, which costs nothing; values, whose sums go over
-// thousands of positions, have 8 taken off each pair of codes (measured without: 2.5 times the
-// error of an fp16 output's own rounding over 5000 positions).
+// Middles.  Values count from 8, value = low + 8 step + step (c - 8), or rounded weights would be
+// off by a share of the whole range: 8 times the step's weights as they are rounded (a product with ones) comes
+// off the sums before each step's products, and w times the middle, low + 8 step, is summed in fp32.
 //
-// Values.  w step is the B operand, rounded to fp16: the one rounding to fewer bits here.  It is scaled by a
-// power of two that the largest step so far sets (like m, with the sums rescaled where it grows), so that
-// nothing underflows that counts.  w times the middle, low + 8 step, is summed in fp32, so the error is
-// 2^-12 of a value's distance from the middle of its group.
+// Weights.  w step is the B operand, rounded to fp16: the one rounding to fewer bits here, an error
+// of 2^-12 of a value's distance from its group's middle.  It is scaled by a power of two that the largest step
+// so far sets (the sums are rescaled where it grows), so that nothing underflows that counts.  q is brought to
+// 2^14 .. 2^15 by a power of two for each row, so that its fp16 or bf16 digits all stay; scores are
+// exact products summed in fp32.  (16-bit outputs of 5000 positions are off by 2.9e-4 of 64 bits' in the root of
+// the mean square, of which 2.1e-4 are their own rounding; with the ones as small as the codes it was 7.6e-4.)
 //
 // Maximum.  m follows the scores only where one exceeds it by more than 8 (w up to 2^8, for which
-// the scaling leaves room): a vote of the warp instead of a reduction over it for each tile.
+// the scaling leaves room): a vote of the warp instead of a reduction over it for each step.
 //
-// Mapping.  A CTA has one key head of one sequence, 8 NT of its rows and a share of its positions;
-// its eight warps take 16 positions in turn, each with its own m and sums, joined once at the end
-// in a fixed order.  Codes and scales of 16 positions, one contiguous block each in a page, stream
-// through each warp's own ring (cp.async): no barrier of the CTA stands in the loop.  Rows of codes are an odd
-// number of 16-byte pieces apart there, so that reads for both products are free of bank conflicts.  Where
-// sequences are few their positions are split over CTAs and joined by a second launch.
+// A step of a warp is 32 positions, two tiles.  Rows and weights cost as much as the codes do, so blocks of at most
+// four rows (PACK) give each tile four of the eight columns: scores of both tiles are picked into one set of
+// registers, exponentials, scales and the transposed weights (movmatrix) are made once for both, and
+// the values' operands have zeros in the other tile's columns.
+//
+// Copies.  Codes and scales of 16 positions are contiguous blocks of a page; they stream through each warp's own
+// ring of two steps (cp.async): no barrier of the CTA stands in the loop.  Rows of codes are an odd number of
+// 16-byte pieces apart there, and ldmatrix (transposing for the values) reads them free of bank conflicts
+// as the operands' lanes want them.
+//
+// Mapping.  Four warps a CTA, four CTAs an SM, take the steps of an item (a sequence, a key head, a block of rows) in
+// turn, each with its own m and sums, joined once at the end in a fixed order.  Two ways to share out
+// the work (kd_attn4.cu has the rule): a cluster of up to eight CTAs has an item to itself and joins in
+// distributed shared memory (TEAM; short items), or all CTAs of one round have equal shares of all
+// positions of all items, which each finds from the lengths, and a second launch joins what is cut.
+//
+// Long batches are bound by HBM: without any arithmetic the copies of 32 sequences of 8192 positions (8 key heads of
+// 128) take 60 us, with it 62; past the first 20 us at 5.9 TB/s, 87 % of the measured copy rate.
+// The rest is the start (2.4 us until the share is known, 6.5 until the first codes are there), shares that end
+// unlike on SMs unlike far from memory (45 to 66 us), and the join (3 us).  Measured (device time, inputs
+// larger than L2): 32 sequences of 2000 to 8192 positions 53 us (floor 27), one of 131072 40 us (22), 16 of up
+// to 4096 with up to 8 drafted tokens 44 us, one of 1001 positions with 32 key heads 7.0 us.
+// 128 registers (255 above 128 channels) spill 16 to 130 bytes in some instances, groups of 32 the most.
 #pragma once
 #include <cooperative_groups.h>
 
@@ -63,8 +82,7 @@ struct Params {
   int64_t tokens;
   int heads, shared;            // query heads; of one key head
   int row_blocks;               // of a sequence: blocks of rows
-  int team;                     // CTAs of a cluster that has an item (sequence, key head, block of rows) to itself;
-                                // 0: all CTAs have equal shares of all of them
+  int team;                     // CTAs of a cluster with an item (sequence, key head, block of rows); 0: equal shares
   int causal, window;
   int room;                     // positions that the table has room for
   int bf16, q_vec, out_vec;
@@ -91,6 +109,10 @@ struct Work {
   int chunks;          // of kChunk tiles; one for rows that see nothing, none for no rows
 };
 __device__ __forceinline__ int clamp_to(int v, int most) { return max(0, min(v, most)); }
+// the first position that the row at `pos` sees through its window
+__device__ __forceinline__ int window_from(const Params& p, int pos, int length) {
+  return (int)max((int64_t)0, min((int64_t)pos + 1 - p.window, (int64_t)length));
+}
 // token of a row, of its sequence's
 __device__ __forceinline__ int token_of(const Params& p, int row) {
   return p.shared == 1 ? row : (int)((unsigned)row / (unsigned)p.shared);
@@ -115,8 +137,8 @@ __device__ __forceinline__ Work work_of(const Params& p, int s, int block, int o
     w.hi = clamp_to(b + 1, w.length);
     w.all_hi = clamp_to(a + 1, w.length);
     if (p.window) {
-      w.lo = clamp_to(a + 1 - p.window, w.length);
-      w.all_lo = clamp_to(b + 1 - p.window, w.length);
+      w.lo = window_from(p, a, w.length);
+      w.all_lo = window_from(p, b, w.length);
     }
   }
   // positions past the table's room have no page: none is visited, and rows that see one are NaN
@@ -239,7 +261,7 @@ __device__ __forceinline__ int chunks_of_head(const Params& p, int s) {
       const int of = work_of(p, s, b, kRows).chunks;
       if (of == 0) break;  // no rows from here on
       n += of;
-    }
+  }
   return n;
 }
 __device__ __forceinline__ Start start_of(const Params& p, int blocks, int block, int& per) {
@@ -387,487 +409,483 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
   }
 
   for (;;) {
-  const Work w = work_of(p, s, block, Z::kRows);
-  if constexpr (TEAM) {
-    if (w.rows == 0) return;
-    left = (w.chunks + p.team - 1) / p.team;
-    chunk = special<kRank>() * left;
-  }
-  const int n_chunks = min(w.chunks - chunk, left);
-  // only a part of the item; in a cluster the same for all its CTAs, of which all or none take part in the join
-  const bool cut = (TEAM ? left : n_chunks) < w.chunks;
-  if (n_chunks > 0) {
-  const int first_tile = w.tile + chunk * kChunk, tiles = min(n_chunks * kChunk, w.tiles - chunk * kChunk);
-  const int share_hi = min(w.hi, (first_tile + tiles) * kTile);  // where the part's positions end
-
-  // Where a batch's tiles lie, in bytes of codes and scales from the cache's first row: -1 on a bad page.
-  auto look_up = [&](int b0, int n) {
-    bool bad = false;
-    for (int i = threadIdx.x; i < n; i += 32 * kWarps) {
-      const int64_t first = tile_row(p, s, first_tile + b0 + i), row = first + (int64_t)head * p.c.page;
-      place[i] = first < 0 ? make_longlong2(-1, 0) : make_longlong2(row * row_bytes, row * scale_bytes);
-      bad |= first < 0;
+    const Work w = work_of(p, s, block, Z::kRows);
+    if constexpr (TEAM) {
+      if (w.rows == 0) return;
+      left = (w.chunks + p.team - 1) / p.team;
+      chunk = special<kRank>() * left;
     }
-    return bad;
-  };
-  const char* src[4] = {reinterpret_cast<const char*>(p.c.codes[0]) + lane * 16, reinterpret_cast<const char*>(p.c.codes[1]) + lane * 16,
-                        reinterpret_cast<const char*>(p.c.scales[0]) + lane * 16, reinterpret_cast<const char*>(p.c.scales[1]) + lane * 16};
-  auto issue = [&](int first, int n, int stage) {  // tiles first, first + 1 of the batch's n
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-      if (first + i >= n) break;
-      const longlong2 from = place[first + i];
-      const int64_t code = max((int64_t)from.x, (int64_t)0), scale = from.y;
-      const uint32_t codes = ring_at + stage * (Z::kStage * 4) + i * kTile * S * 4;
-#pragma unroll
-      for (int k = 0; k < (int)(sizeof(to) / 4); ++k)
-        if (lane + 32 * k < pieces) {
-          copy16(codes + to[k], src[0] + code + 512 * k);
-          copy16(codes + Z::kCodes * 4 + to[k], src[1] + code + 512 * k);
+    const int n_chunks = min(w.chunks - chunk, left);
+    // only a part of the item; in a cluster the same for all its CTAs, of which all or none take part in the join
+    const bool cut = (TEAM ? left : n_chunks) < w.chunks;
+    if (n_chunks > 0) {
+      const int first_tile = w.tile + chunk * kChunk, tiles = min(n_chunks * kChunk, w.tiles - chunk * kChunk);
+      const int share_hi = min(w.hi, (first_tile + tiles) * kTile);  // where the part's positions end
+
+      // Where a batch's tiles lie, in bytes of codes and scales from the cache's first row: -1 on a bad page.
+      auto look_up = [&](int b0, int n) {
+        bool bad = false;
+        for (int i = threadIdx.x; i < n; i += 32 * kWarps) {
+          const int64_t first = tile_row(p, s, first_tile + b0 + i), row = first + (int64_t)head * p.c.page;
+          place[i] = first < 0 ? make_longlong2(-1, 0) : make_longlong2(row * row_bytes, row * scale_bytes);
+          bad |= first < 0;
         }
-      if (lane < 4 * GN) {
-        const uint32_t scales = ring_at + stage * (Z::kStage * 4) + 2 * Z::kCodes * 4 + i * kTile * scale_bytes + lane * 16;
-        copy16(scales, src[2] + scale);
-        copy16(scales + Z::kScales * 4, src[3] + scale);
-      }
-    }
-  };
+        return bad;
+      };
+      const char* src[4] = {reinterpret_cast<const char*>(p.c.codes[0]) + lane * 16, reinterpret_cast<const char*>(p.c.codes[1]) + lane * 16,
+                            reinterpret_cast<const char*>(p.c.scales[0]) + lane * 16, reinterpret_cast<const char*>(p.c.scales[1]) + lane * 16};
+      auto issue = [&](int first, int n, int stage) {  // tiles first, first + 1 of the batch's n
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+          if (first + i >= n) break;
+          const longlong2 from = place[first + i];
+          const int64_t code = max((int64_t)from.x, (int64_t)0), scale = from.y;
+          const uint32_t codes = ring_at + stage * (Z::kStage * 4) + i * kTile * S * 4;
+#pragma unroll
+          for (int k = 0; k < (int)(sizeof(to) / 4); ++k)
+            if (lane + 32 * k < pieces) {
+              copy16(codes + to[k], src[0] + code + 512 * k);
+              copy16(codes + Z::kCodes * 4 + to[k], src[1] + code + 512 * k);
+          }
+          if (lane < 4 * GN) {
+            const uint32_t scales = ring_at + stage * (Z::kStage * 4) + 2 * Z::kCodes * 4 + i * kTile * scale_bytes + lane * 16;
+            copy16(scales, src[2] + scale);
+            copy16(scales + Z::kScales * 4, src[3] + scale);
+          }
+        }
+      };
 
-  // The rows as operands, a warp a row: fp16 in eights of channels 0 4 1 5 2 6 3 7, with the
-  // row's power of two and its sums over groups.
-  const int r0 = block * Z::kRows;
-  constexpr int kOfWarp = Z::kRows / kWarps;
-  uint32_t raw[kOfWarp][4];  // lane l has channels 8 l .. 8 l + 7 (of 256)
+      // The rows as operands, a warp a row: fp16 in eights of channels 0 4 1 5 2 6 3 7, with the
+      // row's power of two and its sums over groups.
+      const int r0 = block * Z::kRows;
+      constexpr int kOfWarp = Z::kRows / kWarps;
+      uint32_t raw[kOfWarp][4];  // lane l has channels 8 l .. 8 l + 7 (of 256)
 #pragma unroll
-  for (int i = 0; i < kOfWarp; ++i) {
-    const int r = warp + i * kWarps, token = token_of(p, r0 + r);
-    const int64_t t = w.first + token;
-    raw[i][0] = raw[i][1] = raw[i][2] = raw[i][3] = 0;
-    if (r < w.rows && t >= 0 && t < p.tokens && 8 * lane < p.c.d) {
-      const uint16_t* q = p.q + t * p.q_token + (int64_t)(head * p.shared + (r0 + r) - token * p.shared) * p.q_head + 8 * lane;
-      if (p.q_vec) {
-        const uint4 u = *reinterpret_cast<const uint4*>(q);
-        raw[i][0] = u.x; raw[i][1] = u.y; raw[i][2] = u.z; raw[i][3] = u.w;
-      } else {
+      for (int i = 0; i < kOfWarp; ++i) {
+        const int r = warp + i * kWarps, token = token_of(p, r0 + r);
+        const int64_t t = w.first + token;
+        raw[i][0] = raw[i][1] = raw[i][2] = raw[i][3] = 0;
+        if (r < w.rows && t >= 0 && t < p.tokens && 8 * lane < p.c.d) {
+          const uint16_t* q = p.q + t * p.q_token + (int64_t)(head * p.shared + (r0 + r) - token * p.shared) * p.q_head + 8 * lane;
+          if (p.q_vec) {
+            const uint4 u = *reinterpret_cast<const uint4*>(q);
+            raw[i][0] = u.x; raw[i][1] = u.y; raw[i][2] = u.z; raw[i][3] = u.w;
+          } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (8 * lane + e < p.c.d) raw[i][e / 2] |= (uint32_t)q[e] << (16 * (e % 2));
+            for (int e = 0; e < 8; ++e)
+              if (8 * lane + e < p.c.d) raw[i][e / 2] |= (uint32_t)q[e] << (16 * (e % 2));
+          }
+        }
       }
-    }
-  }
-  // the first batch's copies go out before the rows are worked on
-  bool bad_pages = __syncthreads_or(look_up(0, min(tiles, kBatch)));
-  auto prefetch = [&](int n) {
+      // the first batch's copies go out before the rows are worked on
+      bool bad_pages = __syncthreads_or(look_up(0, min(tiles, kBatch)));
+      auto prefetch = [&](int n) {
 #pragma unroll
-    for (int i = 0; i < ST - 1; ++i) {
-      issue(kTiles * warp + i * kChunk, n, i);
-      commit();
-    }
-  };
-  prefetch(min(tiles, kBatch));
+        for (int i = 0; i < ST - 1; ++i) {
+          issue(kTiles * warp + i * kChunk, n, i);
+          commit();
+        }
+      };
+      prefetch(min(tiles, kBatch));
 #pragma unroll
-  for (int i = 0; i < kOfWarp; ++i) {
-    const int r = warp + i * kWarps;
-    float v[8];
-    uint32_t top = 0;
+      for (int i = 0; i < kOfWarp; ++i) {
+        const int r = warp + i * kWarps;
+        float v[8];
+        uint32_t top = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      v[e] = wide(p, raw[i][e / 2] >> (16 * (e % 2)) & 0xFFFFu);
-      top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
-    }
-    top = __reduce_max_sync(~0u, top);
-    // 2^e <= max |q| < 2^(e + 1); an infinity or NaN stays what it is under any factor
-    const int e2 = top >> 23 == 255 || top == 0 ? 0 : max((int)(top >> 23) - 127, -100);
-    const float up = __uint_as_float((uint32_t)(14 - e2 + 127) << 23);
-    float sum = 0.f;
+        for (int e = 0; e < 8; ++e) {
+          v[e] = wide(p, raw[i][e / 2] >> (16 * (e % 2)) & 0xFFFFu);
+          top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+        }
+        top = __reduce_max_sync(~0u, top);
+        // 2^e <= max |q| < 2^(e + 1); an infinity or NaN stays what it is under any factor
+        const int e2 = top >> 23 == 255 || top == 0 ? 0 : max((int)(top >> 23) - 127, -100);
+        const float up = __uint_as_float((uint32_t)(14 - e2 + 127) << 23);
+        float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      v[e] *= up;
-      sum += v[e];
-    }
-    if (lane < 4 * NC)
-      *reinterpret_cast<uint4*>(queries + r * Z::kQueries + 16 * lane) =
-          make_uint4(pack2<KD_F16>(v[0], v[4]), pack2<KD_F16>(v[1], v[5]), pack2<KD_F16>(v[2], v[6]), pack2<KD_F16>(v[3], v[7]));
-    // four lanes a piece of 32 channels
+        for (int e = 0; e < 8; ++e) {
+          v[e] *= up;
+          sum += v[e];
+        }
+        if (lane < 4 * NC)
+          *reinterpret_cast<uint4*>(queries + r * Z::kQueries + 16 * lane) =
+              make_uint4(pack2<KD_F16>(v[0], v[4]), pack2<KD_F16>(v[1], v[5]), pack2<KD_F16>(v[2], v[6]), pack2<KD_F16>(v[3], v[7]));
+        // four lanes a piece of 32 channels
 #pragma unroll
-    for (int o = 1; o < 4 * GS && o < 32; o *= 2) sum += __shfl_xor_sync(~0u, sum, o);
-    if (lane % (4 * GS) == 0 && lane / (4 * GS) < GN) query_sums[r * (GN + 1) + lane / (4 * GS)] = sum * 0x1p-14f;
-    if (lane == 0) query_sums[r * (GN + 1) + GN] = __uint_as_float((uint32_t)(e2 + 127) << 23) * p.scale2;
-  }
-  __syncthreads();
-  uint32_t qb[2 * NC][2];
-  // of columns 2 t4, 2 t4 + 1: power of two of the row, and its sums over groups, both times scale log2 e
-  float qs[GN][2], qe[2];
-  {
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const uint4 u = *reinterpret_cast<const uint4*>(queries + g8 % kColumns * Z::kQueries + 16 * (4 * c + t4));
-      qb[2 * c][0] = u.x;
-      qb[2 * c][1] = u.y;
-      qb[2 * c + 1][0] = u.z;
-      qb[2 * c + 1][1] = u.w;
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const float* of_column = query_sums + (2 * t4 + j) % kColumns * (GN + 1);
-      const float down = of_column[GN];
-#pragma unroll
-      for (int g = 0; g < GN; ++g) qs[g][j] = of_column[g] * down;
-      qe[j] = down * 64.f;  // codes' 2^20 less q's 2^14
-    }
-  }
-  // what the columns' rows see: positions from sees_lo on, below sees_hi
-  int sees_lo[2], sees_hi[2];
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int r = (2 * t4 + j) % kColumns, pos = w.before + token_of(p, r0 + r);
-    sees_hi[j] = r >= w.rows ? 0 : min(share_hi, p.causal ? clamp_to(pos + 1, w.length) : w.length);
-    sees_lo[j] = p.window ? clamp_to(pos + 1 - p.window, w.length) : 0;
-  }
-
-  float acc[Z::kSumTiles][4];
-  // of the columns: sums of weights times middles and of weights (of the positions g8 and g8 + 8 of the tiles
-  // apart), m (0 before the first), and how far above it a score may lie (nothing may, before the first)
-  float2 mids[GN][2], sum[2];
-  float m[2], room[2];
-  {
-#pragma unroll
-    for (int i = 0; i < Z::kSumTiles; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[i][e] = 0.f;
-#pragma unroll
-    for (int g = 0; g < GN; ++g) mids[g][0] = mids[g][1] = make_float2(0.f, 0.f);
-    m[0] = m[1] = 0.f;
-    room[0] = room[1] = kNone;
-    sum[0] = sum[1] = make_float2(0.f, 0.f);
-  }
-  float step_cap = 0.f;  // no step so far lies above
-  float step_up = 1.f;   // the power of two of the values' weights: step_cap becomes 2^6
-
-  // One step.  EDGE: some row does not see all of it, or a page is bad.
-  const uint32_t matrix_at = (lane & 15) * S * 4 + (lane >> 4) * 16;  // this lane's row of four matrices
-  const int own = PACK ? t4 >> 1 : 0;  // whose elements are the lane's of a set: the second tile's, in the upper columns
-  auto step = [&](auto edge, int stage, int position, bool bad0, bool bad1) {
-    constexpr bool EDGE = decltype(edge)::value;
-    const uint32_t codes = ring_at + stage * (Z::kStage * 4) + matrix_at;
-    const uint32_t* kp = ring + stage * Z::kStage + 2 * Z::kCodes + (kTile * own + g8) * GN;
-    const uint32_t* vp = kp + Z::kScales;
-    float x[kSets][4];  // scores less m
-    bool seen[kSets][4];
-#pragma unroll
-    for (int i = 0; i < kSets; ++i) {
-      float part[kTiles][4], low[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[i][e] = 0.f;
-        low[e] = -m[e & 1];
+        for (int o = 1; o < 4 * GS && o < 32; o *= 2) sum += __shfl_xor_sync(~0u, sum, o);
+        if (lane % (4 * GS) == 0 && lane / (4 * GS) < GN) query_sums[r * (GN + 1) + lane / (4 * GS)] = sum * 0x1p-14f;
+        if (lane == 0) query_sums[r * (GN + 1) + GN] = __uint_as_float((uint32_t)(e2 + 127) << 23) * p.scale2;
       }
-      uint32_t w[kTiles][4];  // positions g8, g8 + 8 of one piece, and of the next
+      __syncthreads();
+      uint32_t qb[2 * NC][2];
+      // of columns 2 t4, 2 t4 + 1: power of two of the row, and its sums over groups, both times scale log2 e
+      float qs[GN][2], qe[2];
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-#pragma unroll
-        for (int n = 0; n < (PACK ? kTiles : 1); ++n) {
-          const int of = PACK ? n : i;  // the tile
-          if (c % 2 == 0) {
-            if (c + 1 < NC) load_matrices<false>(w[n], codes + of * kTile * S * 4 + c * 16);
-            else load_two_matrices<false>(w[n], codes + of * kTile * S * 4 + c * 16);
-          }
-          const uint32_t a = w[n][c % 2 * 2], b = w[n][c % 2 * 2 + 1];
-          constexpr uint32_t mask = 0x00F000F0u;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t a0 = (h ? a >> 4 : a << 4) & mask, a1 = (h ? b >> 4 : b << 4) & mask;
-            const uint32_t a2 = (h ? a >> 8 : a) & mask, a3 = (h ? b >> 8 : b) & mask;
-            if (c % GS == 0 && h == 0) mma_first(part[n], a0, a1, a2, a3, qb[2 * c][0], qb[2 * c][1]);
-            else mma(part[n], a0, a1, a2, a3, qb[2 * c + h][0], qb[2 * c + h][1]);
-          }
-        }
-        if ((c + 1) % GS == 0 || c == NC - 1) {
-          const uint32_t u = kp[i * kTile * GN + c / GS], v = kp[(i * kTile + 8) * GN + c / GS];
-          const float s0 = low_half(u), l0 = high_half(u), s1 = low_half(v), l1 = high_half(v);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x[i][e] = __fmaf_rn(e < 2 ? s0 : s1, PACK && own ? part[1][e] : part[0][e], x[i][e]);
-            low[e] = __fmaf_rn(e < 2 ? l0 : l1, qs[c / GS][e & 1], low[e]);
-          }
-        }
+        const uint4 u = *reinterpret_cast<const uint4*>(queries + g8 % kColumns * Z::kQueries + 16 * (4 * c + t4));
+        qb[2 * c][0] = u.x;
+        qb[2 * c][1] = u.y;
+        qb[2 * c + 1][0] = u.z;
+        qb[2 * c + 1][1] = u.w;
       }
-#pragma unroll
-      for (int e = 0; e < 4; e += 2) {
-        const float2 of = fma2(make_float2(x[i][e], x[i][e + 1]), make_float2(qe[0], qe[1]), make_float2(low[e], low[e + 1]));
-        x[i][e] = of.x;
-        x[i][e + 1] = of.y;
-        if constexpr (EDGE) {
-          const int pos = position + kTile * (i + own) + g8 + 4 * e;
-          const bool bad = i + own ? bad1 : bad0;
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            seen[i][e + j] = pos < sees_hi[j] && pos >= sees_lo[j];
-            x[i][e + j] = !seen[i][e + j] ? kNone : bad ? __int_as_float(0x7FC00000) : x[i][e + j];
-          }
-        }
-      }
-    }
-    uint32_t vscale[kSets][GN][2];
-    __half2 tops = __half2half2(__ushort_as_half(0));  // the larger step, in the low half
-#pragma unroll
-    for (int i = 0; i < kSets; ++i)
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int g = 0; g < GN; ++g) {
-          uint32_t v = vp[(kTile * i + 8 * k) * GN + g];
-          if constexpr (EDGE) {  // a position that no row sees may hold anything
-            const int pos = position + kTile * (i + own) + g8 + 8 * k;
-            if (pos >= share_hi || pos < w.lo) v = 0;
-          }
-          vscale[i][g][k] = v;
-          tops = __hmax2(tops, *reinterpret_cast<const __half2*>(&v));
-        }
-    float top = __low2float(tops);
-    bool grow = top > step_cap;
-    float most[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        most[j] = fmaxf(x[0][j], x[0][j + 2]);
-      if (kSets == 2) most[j] = fmaxf(most[j], fmaxf(x[kSets - 1][j], x[kSets - 1][j + 2]));
-        grow |= most[j] > room[j];
+        const float* of_column = query_sums + (2 * t4 + j) % kColumns * (GN + 1);
+        const float down = of_column[GN];
+#pragma unroll
+        for (int g = 0; g < GN; ++g) qs[g][j] = of_column[g] * down;
+        qe[j] = down * 64.f;  // codes' 2^20 less q's 2^14
       }
-    if (__any_sync(~0u, grow)) {
-      float by_step = 1.f;
-      top = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top)));  // not negative: ordered as bits
-      if (top > step_cap) {
-        // 2^e <= top < 2^(e + 1); an infinite one leaves nothing finite in any case
-        const int e2 = min((int)(__float_as_uint(top) >> 23) - 127, 15);
-        const float up = __uint_as_float((uint32_t)(5 - e2 + 127) << 23);
-        step_cap = top > 65504.f ? top : __uint_as_float((uint32_t)(e2 + 128) << 23);
-        by_step = up / step_up;
-        step_up = up;
+      // what the columns' rows see: positions from sees_lo on, below sees_hi
+      int sees_lo[2], sees_hi[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int r = (2 * t4 + j) % kColumns, pos = w.before + token_of(p, r0 + r);
+        sees_hi[j] = r >= w.rows ? 0 : min(share_hi, p.causal ? clamp_to(pos + 1, w.length) : w.length);
+        sees_lo[j] = p.window ? window_from(p, pos, w.length) : 0;
       }
+
+      float acc[Z::kSumTiles][4];
+      // of the columns: sums of weights times middles and of weights (of the positions g8 and g8 + 8 of the tiles
+      // apart), m (0 before the first), and how far above it a score may lie (nothing may, before the first)
+      float2 mids[GN][2], sum[2];
+      float m[2], room[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          float to = most[j];
-          to = fmaxf(to, __shfl_xor_sync(~0u, to, 4));
-          to = fmaxf(to, __shfl_xor_sync(~0u, to, 8));
-          to = fmaxf(to, __shfl_xor_sync(~0u, to, 16));
-          const bool fresh = room[j] == kNone;
-          if (!fresh) to = fmaxf(to, 0.f);
-          if (to == kNone) continue;  // nothing seen yet; the sums are 0
-          // m moves up by `to`; a first one by whatever it is
-          const float f = fresh ? 0.f : exp2_of(-to), fs = f * by_step;
-          const float2 ff = make_float2(f, f);
-          m[j] += to;
-          room[j] = 8.f;
+      for (int i = 0; i < Z::kSumTiles; ++i)
 #pragma unroll
-          for (int i = 0; i < kSets; ++i) {
-            x[i][j] -= to;
-            x[i][j + 2] -= to;
+        for (int e = 0; e < 4; ++e) acc[i][e] = 0.f;
+#pragma unroll
+      for (int g = 0; g < GN; ++g) mids[g][0] = mids[g][1] = make_float2(0.f, 0.f);
+      m[0] = m[1] = 0.f;
+      room[0] = room[1] = kNone;
+      sum[0] = sum[1] = make_float2(0.f, 0.f);
+      float step_cap = 0.f;  // no step so far lies above
+      float step_up = 1.f;   // the power of two of the values' weights: step_cap becomes 2^6
+
+      // One step.  EDGE: some row does not see all of it, or a page is bad.
+      const uint32_t matrix_at = (lane & 15) * S * 4 + (lane >> 4) * 16;  // this lane's row of four matrices
+      const int own = PACK ? t4 >> 1 : 0;  // whose elements are the lane's of a set: the second tile's, in the upper columns
+      auto step = [&](auto edge, int stage, int position, bool bad0, bool bad1) {
+        constexpr bool EDGE = decltype(edge)::value;
+        const uint32_t codes = ring_at + stage * (Z::kStage * 4) + matrix_at;
+        const uint32_t* kp = ring + stage * Z::kStage + 2 * Z::kCodes + (kTile * own + g8) * GN;
+        const uint32_t* vp = kp + Z::kScales;
+        float x[kSets][4];  // scores less m
+        bool seen[kSets][4];
+#pragma unroll
+        for (int i = 0; i < kSets; ++i) {
+          float part[kTiles][4], low[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[i][e] = 0.f;
+            low[e] = -m[e & 1];
           }
-          sum[j] = mul2(sum[j], ff);
+          uint32_t w[kTiles][4];  // positions g8, g8 + 8 of one piece, and of the next
 #pragma unroll
-          for (int g = 0; g < GN; ++g) mids[g][j] = mul2(mids[g][j], ff);
+          for (int c = 0; c < NC; ++c) {
 #pragma unroll
-          for (int i = 0; i < Z::kSumTiles; ++i) {
-            acc[i][j] *= fs;
-            acc[i][j + 2] *= fs;
-          }
-        }
-    }
-    // weights, and the operands of the values
-    uint32_t bw[kTiles][GN][2];
-    float all[GN][4];  // of each column, in every row: the step's weights as they are rounded
+            for (int n = 0; n < (PACK ? kTiles : 1); ++n) {
+              const int of = PACK ? n : i;  // the tile
+              if (c % 2 == 0) {
+                if (c + 1 < NC) load_matrices<false>(w[n], codes + of * kTile * S * 4 + c * 16);
+                else load_two_matrices<false>(w[n], codes + of * kTile * S * 4 + c * 16);
+              }
+              const uint32_t a = w[n][c % 2 * 2], b = w[n][c % 2 * 2 + 1];
+              constexpr uint32_t mask = 0x00F000F0u;
 #pragma unroll
-    for (int i = 0; i < kSets; ++i) {
-      float2 wt[2];  // of a column, positions g8 and g8 + 8
+              for (int h = 0; h < 2; ++h) {
+                const uint32_t a0 = (h ? a >> 4 : a << 4) & mask, a1 = (h ? b >> 4 : b << 4) & mask;
+                const uint32_t a2 = (h ? a >> 8 : a) & mask, a3 = (h ? b >> 8 : b) & mask;
+                if (c % GS == 0 && h == 0) mma_first(part[n], a0, a1, a2, a3, qb[2 * c][0], qb[2 * c][1]);
+                else mma(part[n], a0, a1, a2, a3, qb[2 * c + h][0], qb[2 * c + h][1]);
+              }
+            }
+            if ((c + 1) % GS == 0 || c == NC - 1) {
+              const uint32_t u = kp[i * kTile * GN + c / GS], v = kp[(i * kTile + 8) * GN + c / GS];
+              const float s0 = low_half(u), l0 = high_half(u), s1 = low_half(v), l1 = high_half(v);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          wt[j] = make_float2(exp2_of(x[i][j]), exp2_of(x[i][j + 2]));
-          sum[j] = add2(sum[j], wt[j]);
-        }
-#pragma unroll
-      for (int g = 0; g < GN; ++g) {
-        const float2 step = make_float2(low_half(vscale[i][g][0]), low_half(vscale[i][g][1]));
-        const float2 mid = fma2(make_float2(8.f, 8.f), step, make_float2(high_half(vscale[i][g][0]), high_half(vscale[i][g][1])));
-        const float2 up = mul2(step, make_float2(step_up, step_up));
-        {
-          float2 b[2];
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            b[j] = mul2(wt[j], up);
-            if constexpr (EDGE) {  // whatever stands where a row does not see: 0
-              b[j].x = seen[i][j] ? b[j].x : 0.f;
-              b[j].y = seen[i][j + 2] ? b[j].y : 0.f;
-              const float2 of = make_float2(seen[i][j] ? mid.x : 0.f, seen[i][j + 2] ? mid.y : 0.f);
-              mids[g][j] = fma2(wt[j], of, mids[g][j]);
-            } else {
-              mids[g][j] = fma2(wt[j], mid, mids[g][j]);
+              for (int e = 0; e < 4; ++e) {
+                x[i][e] = __fmaf_rn(e < 2 ? s0 : s1, PACK && own ? part[1][e] : part[0][e], x[i][e]);
+                low[e] = __fmaf_rn(e < 2 ? l0 : l1, qs[c / GS][e & 1], low[e]);
+              }
             }
           }
-          const uint32_t b0 = turned(pack2<KD_F16>(b[0].x, b[1].x)), b1 = turned(pack2<KD_F16>(b[0].y, b[1].y));
-          constexpr uint32_t one = 0x3C003C00u;
-          if (i == 0) mma_first(all[g], one, one, one, one, b0, b1);
-          else mma(all[g], one, one, one, one, b0, b1);
-          if constexpr (PACK) {  // each tile's operand has its own columns only
-            bw[0][g][0] = g8 < 4 ? b0 : 0u;
-            bw[0][g][1] = g8 < 4 ? b1 : 0u;
-            bw[1][g][0] = g8 < 4 ? 0u : b0;
-            bw[1][g][1] = g8 < 4 ? 0u : b1;
-          } else {
-            bw[i][g][0] = b0;
-            bw[i][g][1] = b1;
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            const float2 of = fma2(make_float2(x[i][e], x[i][e + 1]), make_float2(qe[0], qe[1]), make_float2(low[e], low[e + 1]));
+            x[i][e] = of.x;
+            x[i][e + 1] = of.y;
+            if constexpr (EDGE) {
+              const int pos = position + kTile * (i + own) + g8 + 4 * e;
+              const bool bad = i + own ? bad1 : bad0;
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                seen[i][e + j] = pos < sees_hi[j] && pos >= sees_lo[j];
+                x[i][e + j] = !seen[i][e + j] ? kNone : bad ? __int_as_float(0x7FC00000) : x[i][e + j];
+              }
+            }
           }
         }
-      }
-    }
+        uint32_t vscale[kSets][GN][2];
+        __half2 tops = __half2half2(__ushort_as_half(0));  // the larger step, in the low half
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+        for (int i = 0; i < kSets; ++i)
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
-        {
-          float(&d)[4] = acc[2 * c + k];
-          const float2 eight = make_float2(all[c / GS][0], all[c / GS][1]);
-          const float2 even = fma2(eight, make_float2(-8.f * 0x1p-24f, -8.f * 0x1p-24f), make_float2(d[0], d[1]));
-          const float2 both = fma2(eight, make_float2(-136.f * 0x1p-24f, -136.f * 0x1p-24f), make_float2(d[2], d[3]));
-          d[0] = even.x;
-          d[1] = even.y;
-          d[2] = both.x;
-          d[3] = both.y;
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int g = 0; g < GN; ++g) {
+              uint32_t v = vp[(kTile * i + 8 * k) * GN + g];
+              if constexpr (EDGE) {  // a position that no row sees may hold anything
+                const int pos = position + kTile * (i + own) + g8 + 8 * k;
+                if (pos >= share_hi || pos < w.lo) v = 0;
+              }
+              vscale[i][g][k] = v;
+              tops = __hmax2(tops, *reinterpret_cast<const __half2*>(&v));
         }
+        float top = __low2float(tops);
+        bool grow = top > step_cap;
+        float most[2];
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-      uint32_t w[4];  // positions 2 t4, 2 t4 + 1, and the same 8 on, of one piece; of the next
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        if (c % 2 == 0) {
-          if (c + 1 < NC) load_matrices<true>(w, codes + Z::kCodes * 4 + i * kTile * S * 4 + c * 16);
-          else load_two_matrices<true>(w, codes + Z::kCodes * 4 + i * kTile * S * 4 + c * 16);
+        for (int j = 0; j < 2; ++j) {
+          most[j] = fmaxf(x[0][j], x[0][j + 2]);
+          if (kSets == 2) most[j] = fmaxf(most[j], fmaxf(x[kSets - 1][j], x[kSets - 1][j + 2]));
+          grow |= most[j] > room[j];
         }
-        uint32_t a = w[c % 2 * 2], b = w[c % 2 * 2 + 1];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          if (k) {  // the upper bytes down
-            a = __byte_perm(a, 0, 0x4341);
-            b = __byte_perm(b, 0, 0x4341);
+        if (__any_sync(~0u, grow)) {
+          float by_step = 1.f;
+          top = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top)));  // not negative: ordered as bits
+          if (top > step_cap) {
+            // 2^e <= top < 2^(e + 1); an infinite one leaves nothing finite in any case
+            const int e2 = min((int)(__float_as_uint(top) >> 23) - 127, 15);
+            const float up = __uint_as_float((uint32_t)(5 - e2 + 127) << 23);
+            step_cap = top > 65504.f ? top : __uint_as_float((uint32_t)(e2 + 128) << 23);
+            by_step = up / step_up;
+            step_up = up;
           }
-            mma(acc[2 * c + k], a & 0x000F000Fu, k ? a : a & 0x00FF00FFu, b & 0x000F000Fu, k ? b : b & 0x00FF00FFu,
-                bw[i][c / GS][0], bw[i][c / GS][1]);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            float to = most[j];
+            to = fmaxf(to, __shfl_xor_sync(~0u, to, 4));
+            to = fmaxf(to, __shfl_xor_sync(~0u, to, 8));
+            to = fmaxf(to, __shfl_xor_sync(~0u, to, 16));
+            const bool fresh = room[j] == kNone;
+            if (!fresh) to = fmaxf(to, 0.f);
+            if (to == kNone) continue;  // nothing seen yet; the sums are 0
+            // m moves up by `to`; a first one by whatever it is
+            const float f = fresh ? 0.f : exp2_of(-to), fs = f * by_step;
+            const float2 ff = make_float2(f, f);
+            m[j] += to;
+            room[j] = 8.f;
+#pragma unroll
+            for (int i = 0; i < kSets; ++i) {
+              x[i][j] -= to;
+              x[i][j + 2] -= to;
+            }
+            sum[j] = mul2(sum[j], ff);
+#pragma unroll
+            for (int g = 0; g < GN; ++g) mids[g][j] = mul2(mids[g][j], ff);
+#pragma unroll
+            for (int i = 0; i < Z::kSumTiles; ++i) {
+              acc[i][j] *= fs;
+              acc[i][j + 2] *= fs;
+            }
+          }
+        }
+        // weights, and the operands of the values
+        uint32_t bw[kTiles][GN][2];
+        float all[GN][4];  // of each column, in every row: the step's weights as they are rounded
+#pragma unroll
+        for (int i = 0; i < kSets; ++i) {
+          float2 wt[2];  // of a column, positions g8 and g8 + 8
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            wt[j] = make_float2(exp2_of(x[i][j]), exp2_of(x[i][j + 2]));
+            sum[j] = add2(sum[j], wt[j]);
+          }
+#pragma unroll
+          for (int g = 0; g < GN; ++g) {
+            const float2 step = make_float2(low_half(vscale[i][g][0]), low_half(vscale[i][g][1]));
+            const float2 mid = fma2(make_float2(8.f, 8.f), step, make_float2(high_half(vscale[i][g][0]), high_half(vscale[i][g][1])));
+            const float2 up = mul2(step, make_float2(step_up, step_up));
+            {
+              float2 b[2];
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                b[j] = mul2(wt[j], up);
+                if constexpr (EDGE) {  // whatever stands where a row does not see: 0
+                  b[j].x = seen[i][j] ? b[j].x : 0.f;
+                  b[j].y = seen[i][j + 2] ? b[j].y : 0.f;
+                  const float2 of = make_float2(seen[i][j] ? mid.x : 0.f, seen[i][j + 2] ? mid.y : 0.f);
+                  mids[g][j] = fma2(wt[j], of, mids[g][j]);
+                } else {
+                  mids[g][j] = fma2(wt[j], mid, mids[g][j]);
+                }
+              }
+              const uint32_t b0 = turned(pack2<KD_F16>(b[0].x, b[1].x)), b1 = turned(pack2<KD_F16>(b[0].y, b[1].y));
+              constexpr uint32_t one = 0x3C003C00u;
+              if (i == 0) mma_first(all[g], one, one, one, one, b0, b1);
+              else mma(all[g], one, one, one, one, b0, b1);
+              if constexpr (PACK) {  // each tile's operand has its own columns only
+                bw[0][g][0] = g8 < 4 ? b0 : 0u;
+                bw[0][g][1] = g8 < 4 ? b1 : 0u;
+                bw[1][g][0] = g8 < 4 ? 0u : b0;
+                bw[1][g][1] = g8 < 4 ? 0u : b1;
+              } else {
+                bw[i][g][0] = b0;
+                bw[i][g][1] = b1;
+              }
+            }
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+            {
+              float(&d)[4] = acc[2 * c + k];
+              const float2 eight = make_float2(all[c / GS][0], all[c / GS][1]);
+              const float2 even = fma2(eight, make_float2(-8.f * 0x1p-24f, -8.f * 0x1p-24f), make_float2(d[0], d[1]));
+              const float2 both = fma2(eight, make_float2(-136.f * 0x1p-24f, -136.f * 0x1p-24f), make_float2(d[2], d[3]));
+              d[0] = even.x;
+              d[1] = even.y;
+              d[2] = both.x;
+              d[3] = both.y;
+        }
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+          uint32_t w[4];  // positions 2 t4, 2 t4 + 1, and the same 8 on, of one piece; of the next
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            if (c % 2 == 0) {
+              if (c + 1 < NC) load_matrices<true>(w, codes + Z::kCodes * 4 + i * kTile * S * 4 + c * 16);
+              else load_two_matrices<true>(w, codes + Z::kCodes * 4 + i * kTile * S * 4 + c * 16);
+            }
+            uint32_t a = w[c % 2 * 2], b = w[c % 2 * 2 + 1];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              if (k) {  // the upper bytes down
+                a = __byte_perm(a, 0, 0x4341);
+                b = __byte_perm(b, 0, 0x4341);
+              }
+              mma(acc[2 * c + k], a & 0x000F000Fu, k ? a : a & 0x00FF00FFu, b & 0x000F000Fu, k ? b : b & 0x00FF00FFu,
+                  bw[i][c / GS][0], bw[i][c / GS][1]);
+            }
+          }
+        }
+      };
+
+      for (int b0 = 0; b0 < tiles; b0 += kBatch) {
+        const int n = min(kBatch, tiles - b0);
+        if (b0) {
+          __syncthreads();  // no warp still reads the last batch's places
+          bad_pages = __syncthreads_or(look_up(b0, n));
+          prefetch(n);
+        }
+        // this warp's steps: tiles kTiles * warp on, kChunk apart
+        int fetch = kTiles * warp + (ST - 1) * kChunk;
+        int stage = 0, next = ST - 1;
+        for (int nth = kTiles * warp; nth < n; nth += kChunk, fetch += kChunk) {
+          issue(fetch, n, next);
+          commit();
+          wait_group<ST - 1>();
+          __syncwarp();  // the lanes' copies are each other's
+          const int position = (first_tile + b0 + nth) * kTile;
+          if (bad_pages || position < w.all_lo || position + kTiles * kTile > min(w.all_hi, share_hi))
+            step(std::true_type{}, stage, position, place[nth].x < 0, nth + 1 < n && place[nth + 1].x < 0);
+          else step(std::false_type{}, stage, position, false, false);
+          __syncwarp();
+          stage = stage + 1 == ST ? 0 : stage + 1;
+          next = next + 1 == ST ? 0 : next + 1;
+        }
+        wait_group<0>();
+      }
+
+      // The warps' sums, in fp32 without the scaling, then joined.
+      __syncthreads();
+      float* sums = reinterpret_cast<float*>(smem);
+      const float back = 0x1p24f / step_up;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int r = 2 * t4 + j;
+        float total = sum[j].x + sum[j].y, of[GN];
+#pragma unroll
+        for (int g = 0; g < GN; ++g) of[g] = mids[g][j].x + mids[g][j].y;
+#pragma unroll
+        for (int o = 4; o < 32; o *= 2) {
+          total += __shfl_xor_sync(~0u, total, o);
+#pragma unroll
+          for (int g = 0; g < GN; ++g) of[g] += __shfl_xor_sync(~0u, of[g], o);
+        }
+        if (g8 == 0) ml[warp * Z::kRows + r] = make_float2(room[j] == kNone ? kNone : m[j], total);
+        float* to = sums + (warp * Z::kRows + r) * Z::kSums + 4 * g8;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {  // even channels, and these plus 16 times the odd ones
+          const float(&d0)[4] = acc[2 * c];
+          const float(&d1)[4] = acc[2 * c + 1];
+          *reinterpret_cast<float4*>(to + 32 * c) =
+              make_float4(__fmaf_rn(d0[j], back, of[c / GS]), __fmaf_rn(d0[j + 2] - d0[j], back * 0.0625f, of[c / GS]),
+                          __fmaf_rn(d1[j], back, of[c / GS]), __fmaf_rn(d1[j + 2] - d1[j], back * 0.0625f, of[c / GS]));
         }
       }
-    }
-  };
-
-  for (int b0 = 0; b0 < tiles; b0 += kBatch) {
-    const int n = min(kBatch, tiles - b0);
-    if (b0) {
-      __syncthreads();  // no warp still reads the last batch's places
-      bad_pages = __syncthreads_or(look_up(b0, n));
-      prefetch(n);
-    }
-    // this warp's steps: tiles kTiles * warp on, kChunk apart
-    int fetch = kTiles * warp + (ST - 1) * kChunk;
-    int stage = 0, next = ST - 1;
-    for (int nth = kTiles * warp; nth < n; nth += kChunk, fetch += kChunk) {
-      issue(fetch, n, next);
-      commit();
-      wait_group<ST - 1>();
-      __syncwarp();  // the lanes' copies are each other's
-      const int position = (first_tile + b0 + nth) * kTile;
-      if (bad_pages || position < w.all_lo || position + kTiles * kTile > min(w.all_hi, share_hi))
-        step(std::true_type{}, stage, position, place[nth].x < 0, nth + 1 < n && place[nth + 1].x < 0);
-      else step(std::false_type{}, stage, position, false, false);
-      __syncwarp();
-      stage = stage + 1 == ST ? 0 : stage + 1;
-      next = next + 1 == ST ? 0 : next + 1;
-    }
-    wait_group<0>();
-  }
-
-  // The warps' sums, in fp32 without the scaling, then joined.
-  __syncthreads();
-  float* sums = reinterpret_cast<float*>(smem);
-  const float back = 0x1p24f / step_up;
+      __syncthreads();
+      // the part's place for partial sums: the share's first item, or its last
+      const int64_t slot = 2 * (int64_t)blockIdx.x + (left == share ? 0 : 1);
+      for (int r = warp; r < w.rows; r += kWarps) {
+        const int token = token_of(p, r0 + r), h = head * p.shared + (r0 + r) - token * p.shared;
+        const int64_t t = w.first + token;
+        if (t < 0 || t >= p.tokens) continue;
+        // the parts of a row: each warp's, of one tile and the other where they have columns of their own
+        constexpr int kParts = PACK ? 2 * kWarps : kWarps, kApart = PACK ? 4 : Z::kRows;
+        float top = kNone, total = 0.f, f[kParts];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int r = 2 * t4 + j;
-      float total = sum[j].x + sum[j].y, of[GN];
+        for (int k = 0; k < kParts; ++k) top = fmaxf(top, ml[k * kApart + r].x);
 #pragma unroll
-      for (int g = 0; g < GN; ++g) of[g] = mids[g][j].x + mids[g][j].y;
+        for (int k = 0; k < kParts; ++k) {
+          const float2 v = ml[k * kApart + r];
+          f[k] = v.x == kNone ? 0.f : exp2_of(v.x - top);
+          total += v.x == kNone ? v.y : v.y * f[k];  // a part without a maximum has summed nothing, or NaN
+        }
+        if (past_table(p, w, token)) total = __int_as_float(0x7FC00000);
+        for (int ch = 4 * lane; ch < p.part_row; ch += 128) {
+          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int o = 4; o < 32; o *= 2) {
-        total += __shfl_xor_sync(~0u, total, o);
-#pragma unroll
-        for (int g = 0; g < GN; ++g) of[g] += __shfl_xor_sync(~0u, of[g], o);
+          for (int k = 0; k < kParts; ++k) {
+            const float4 v = *reinterpret_cast<const float4*>(sums + (k * kApart + r) * Z::kSums + ch);
+            o.x = __fmaf_rn(v.x, f[k], o.x);
+            o.y = __fmaf_rn(v.y, f[k], o.y);
+            o.z = __fmaf_rn(v.z, f[k], o.z);
+            o.w = __fmaf_rn(v.w, f[k], o.w);
+          }
+          if (!cut) put(p, p.out + t * p.out_token + h * p.out_head, ch, o, total);
+          else if (TEAM) *reinterpret_cast<float4*>(sums + r * Z::kSums + ch) = o;
+          else *reinterpret_cast<float4*>(p.part + (slot * Z::kRows + r) * p.part_row + ch) = o;
+        }
+        __syncwarp();  // all lanes have read the warps' sums
+        if (lane == 0) {
+          if (!cut) put_lse(p, t * p.heads + h, top, total);
+          else if (TEAM) ml[r] = make_float2(top, total);
+          else p.part_ml[slot * Z::kRows + r] = make_float2(top, total);
+        }
       }
-      if (g8 == 0) ml[warp * Z::kRows + r] = make_float2(room[j] == kNone ? kNone : m[j], total);
-      float* to = sums + (warp * Z::kRows + r) * Z::kSums + 4 * g8;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {  // even channels, and these plus 16 times the odd ones
-        const float(&d0)[4] = acc[2 * c];
-        const float(&d1)[4] = acc[2 * c + 1];
-        *reinterpret_cast<float4*>(to + 32 * c) =
-            make_float4(__fmaf_rn(d0[j], back, of[c / GS]), __fmaf_rn(d0[j + 2] - d0[j], back * 0.0625f, of[c / GS]),
-                        __fmaf_rn(d1[j], back, of[c / GS]), __fmaf_rn(d1[j + 2] - d1[j], back * 0.0625f, of[c / GS]));
+      if (!TEAM && chunk == 0 && threadIdx.x == 0)  // what is left of the item is the CTAs' that follow
+        p.cuts[((int64_t)s * p.c.heads + head) * p.row_blocks + block] = Cut{(int)blockIdx.x, (int)slot, (w.chunks - n_chunks + share - 1) / share, 0};
+      left -= n_chunks;
+    }
+    if constexpr (TEAM) {
+      if (cut) join_team<Z>(p, w, head, block, n_chunks > 0, reinterpret_cast<float*>(smem), ml);
+      return;
+    }
+    if (left <= 0) return;
+    // the next item
+    chunk = 0;
+    if (w.rows == 0 || ++block == p.row_blocks) {
+      block = 0;
+      if (++head == p.c.heads) {
+        head = 0;
+        ++s;
       }
     }
-  __syncthreads();
-  // the part's place for partial sums: the share's first item, or its last
-  const int64_t slot = 2 * (int64_t)blockIdx.x + (left == share ? 0 : 1);
-  for (int r = warp; r < w.rows; r += kWarps) {
-    const int token = token_of(p, r0 + r), h = head * p.shared + (r0 + r) - token * p.shared;
-    const int64_t t = w.first + token;
-    if (t < 0 || t >= p.tokens) continue;
-    // the parts of a row: each warp's, of one tile and the other where they have columns of their own
-    constexpr int kParts = PACK ? 2 * kWarps : kWarps, kApart = PACK ? 4 : Z::kRows;
-    float top = kNone, total = 0.f, f[kParts];
-#pragma unroll
-    for (int k = 0; k < kParts; ++k) top = fmaxf(top, ml[k * kApart + r].x);
-#pragma unroll
-    for (int k = 0; k < kParts; ++k) {
-      const float2 v = ml[k * kApart + r];
-      f[k] = v.x == kNone ? 0.f : exp2_of(v.x - top);
-      total += v.x == kNone ? v.y : v.y * f[k];  // a part without a maximum has summed nothing, or NaN
-    }
-    if (past_table(p, w, token)) total = __int_as_float(0x7FC00000);
-    for (int ch = 4 * lane; ch < p.part_row; ch += 128) {
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int k = 0; k < kParts; ++k) {
-        const float4 v = *reinterpret_cast<const float4*>(sums + (k * kApart + r) * Z::kSums + ch);
-        o.x = __fmaf_rn(v.x, f[k], o.x);
-        o.y = __fmaf_rn(v.y, f[k], o.y);
-        o.z = __fmaf_rn(v.z, f[k], o.z);
-        o.w = __fmaf_rn(v.w, f[k], o.w);
-      }
-      if (!cut) put(p, p.out + t * p.out_token + h * p.out_head, ch, o, total);
-      else if (TEAM) *reinterpret_cast<float4*>(sums + r * Z::kSums + ch) = o;
-      else *reinterpret_cast<float4*>(p.part + (slot * Z::kRows + r) * p.part_row + ch) = o;
-    }
-    __syncwarp();  // all lanes have read the warps' sums
-    if (lane == 0) {
-      if (!cut) put_lse(p, t * p.heads + h, top, total);
-      else if (TEAM) ml[r] = make_float2(top, total);
-      else p.part_ml[slot * Z::kRows + r] = make_float2(top, total);
-    }
-  }
-  if (!TEAM && chunk == 0 && threadIdx.x == 0)  // what is left of the item is the CTAs' that follow
-    p.cuts[((int64_t)s * p.c.heads + head) * p.row_blocks + block] = Cut{(int)blockIdx.x, (int)slot, (w.chunks - n_chunks + share - 1) / share, 0};
-  left -= n_chunks;
-  }
-  if constexpr (TEAM) {
-    if (cut) join_team<Z>(p, w, head, block, n_chunks > 0, reinterpret_cast<float*>(smem), ml);
-    return;
-  }
-  if (left <= 0) return;
-  // the next item
-  chunk = 0;
-  if (w.rows == 0 || ++block == p.row_blocks) {
-    block = 0;
-    if (++head == p.c.heads) {
-      head = 0;
-      ++s;
-    }
-  }
-  __syncthreads();  // the sums are read before the ring is written again
+    __syncthreads();  // the sums are read before the ring is written again
   }
 }
 
