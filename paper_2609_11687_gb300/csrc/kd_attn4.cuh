@@ -432,25 +432,23 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
         }
         return bad;
       };
-      const char* src[4] = {reinterpret_cast<const char*>(p.c.codes[0]) + lane * 16, reinterpret_cast<const char*>(p.c.codes[1]) + lane * 16,
-                            reinterpret_cast<const char*>(p.c.scales[0]) + lane * 16, reinterpret_cast<const char*>(p.c.scales[1]) + lane * 16};
       auto issue = [&](int first, int n, int stage) {  // tiles first, first + 1 of the batch's n
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) {
           if (first + i >= n) break;
           const longlong2 from = place[first + i];
-          const int64_t code = max((int64_t)from.x, (int64_t)0), scale = from.y;
+          const int64_t code = max((int64_t)from.x, (int64_t)0) + lane * 16, scale = from.y + lane * 16;
           const uint32_t codes = ring_at + stage * (Z::kStage * 4) + i * kTile * S * 4;
 #pragma unroll
           for (int k = 0; k < (int)(sizeof(to) / 4); ++k)
             if (lane + 32 * k < pieces) {
-              copy16(codes + to[k], src[0] + code + 512 * k);
-              copy16(codes + Z::kCodes * 4 + to[k], src[1] + code + 512 * k);
+              copy16(codes + to[k], reinterpret_cast<const char*>(p.c.codes[0]) + code + 512 * k);
+              copy16(codes + Z::kCodes * 4 + to[k], reinterpret_cast<const char*>(p.c.codes[1]) + code + 512 * k);
           }
           if (lane < 4 * GN) {
             const uint32_t scales = ring_at + stage * (Z::kStage * 4) + 2 * Z::kCodes * 4 + i * kTile * scale_bytes + lane * 16;
-            copy16(scales, src[2] + scale);
-            copy16(scales + Z::kScales * 4, src[3] + scale);
+            copy16(scales, reinterpret_cast<const char*>(p.c.scales[0]) + scale);
+            copy16(scales + Z::kScales * 4, reinterpret_cast<const char*>(p.c.scales[1]) + scale);
           }
         }
       };
@@ -536,15 +534,6 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
         for (int g = 0; g < GN; ++g) qs[g][j] = of_column[g] * down;
         qe[j] = down * 64.f;  // codes' 2^20 less q's 2^14
       }
-      // what the columns' rows see: positions from sees_lo on, below sees_hi
-      int sees_lo[2], sees_hi[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int r = (2 * t4 + j) % kColumns, pos = w.before + token_of(p, r0 + r);
-        sees_hi[j] = r >= w.rows ? 0 : min(share_hi, p.causal ? clamp_to(pos + 1, w.length) : w.length);
-        sees_lo[j] = p.window ? window_from(p, pos, w.length) : 0;
-      }
-
       float acc[Z::kSumTiles][4];
       // of the columns: sums of weights times middles and of weights (of the positions g8 and g8 + 8 of the tiles
       // apart), m (0 before the first), and how far above it a score may lie (nothing may, before the first)
@@ -572,6 +561,15 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
         const uint32_t* vp = kp + Z::kScales;
         float x[kSets][4];  // scores less m
         bool seen[kSets][4];
+        int sees_lo[2], sees_hi[2];  // what the columns' rows see: positions from sees_lo on, below sees_hi
+        if constexpr (EDGE) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int r = (2 * t4 + j) % kColumns, pos = w.before + token_of(p, r0 + r);
+            sees_hi[j] = r >= w.rows ? 0 : min(share_hi, p.causal ? clamp_to(pos + 1, w.length) : w.length);
+            sees_lo[j] = p.window ? window_from(p, pos, w.length) : 0;
+          }
+        }
 #pragma unroll
         for (int i = 0; i < kSets; ++i) {
           float part[kTiles][4], low[4];
