@@ -654,7 +654,7 @@ kd_status kd_rope_turns(const double* frequencies, int64_t count, uint64_t* turn
  *   q, k       operands (host structs; k may be NULL), of one dtype: KD_F32, KD_F16, KD_BF16.
  *   positions  device int64, `tokens` of them; negative ones turn the other way.
  *   turns      device, rot/2 values as kd_rope_turns makes them.
- * 1 <= d <= 1024, rot even, 2 <= rot <= d, tokens x heads below 2^31.  fp32 arithmetic, rounded once; a head whose sum of
+ * 1 <= d <= 1024, rot even, 2 <= rot <= d, up to 65535 heads an operand, tokens x heads below 2^31.  fp32 arithmetic, rounded once; a head whose sum of
  * squares is no finite number is NaN throughout (with a norm).
  * Rows on 16-byte boundaries with rot a multiple of 32 bytes take wide loads.
  * Errors: KD_ERR_INVALID_ARG (sizes, rot, layout, types, eps < 0 or NaN, amplitude not finite,
@@ -692,6 +692,7 @@ typedef struct kd_cache4 {
  *   lengths  device int32: tokens of each sequence, the rows of this call among them.
  *   starts   device int32, seqs + 1 values that do not decrease; NULL: every sequence has `most`
  *            rows.
+ *   seqs     at most 2^30.
  *   most     rows of one sequence at most.
  *   longest  the largest length, as far as the host knows it: a hint for how attention is split, not
  *            a limit.
@@ -742,9 +743,11 @@ size_t kd_attention_4bit_workspace(const kd_cache4* cache, const kd_sequences* s
  * with the keys and values of head h / (heads / cache heads), p over the row's sequence: with
  * `causal` the positions up to the row's own, of which with window > 0 the last `window`; else all
  * lengths[s] of them.
- *   q, out   dtype KD_F16 or KD_BF16, head h of row t at q + t*q_token + h*q_head; `tokens` rows.
+ *   q, out   dtype KD_F16 or KD_BF16, head h of row t at q + t*q_token + h*q_head; `tokens` rows.  out may be q
+ *            itself with the same strides.
  *   heads    a multiple of the cache's.
  *   lse      optional, fp32 tokens x heads: ln sum_p exp(scale <q, key[p]>).
+ * Sequences of up to 2^31 - 17 positions; rows that see more are NaN.
  * A row that sees nothing: out 0, lse -infinity.  What a row does not see does not touch it,
  * whatever is there.  A bad page that a row sees makes it NaN, and so do NaN there and in q.
  * Meant for few rows of a sequence (decoding, drafted tokens): eight rows times heads for each cache
@@ -755,7 +758,7 @@ size_t kd_attention_4bit_workspace(const kd_cache4* cache, const kd_sequences* s
  *   workspace  device, 16-byte aligned, ws_bytes >= kd_attention_4bit_workspace(...); it must not
  *              be shared by calls in flight on different streams.
  * Errors: KD_ERR_INVALID_ARG (cache, sequences, heads, type, window < 0 or without causal, scale
- * not finite, strides below 0, overlapping rows of out, missing or unaligned pointers, more than
+ * (or its product with log2 e) not finite, strides below 0, overlapping rows of out, missing or unaligned pointers, more than
  * 2^31 - 1 blocks of work), KD_ERR_UNSUPPORTED_N (d), KD_ERR_WORKSPACE, KD_ERR_CUDA.  Nothing to
  * do enqueues nothing. */
 kd_status kd_attention_4bit(const kd_cache4* cache, const kd_sequences* seqs, int64_t tokens, int64_t heads,

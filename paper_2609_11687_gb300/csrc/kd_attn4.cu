@@ -12,6 +12,7 @@ namespace {
 // A block for an item and 32 of its channels: eight lanes have a part, so that a warp has four and the block up to 32 of
 // them in flight; four rows at a time, each with a running maximum, joined over lanes and warps in a fixed order.
 constexpr int kJoinWarps = 8, kJoinRows = 4;  // warps at most
+constexpr float kLog2e = 1.4426950408889634f;
 
 struct Sum {  // of one row: maximum, weights, four channels
   float m, l;
@@ -155,14 +156,6 @@ kd_status check(const kd_cache4* cache, const kd_sequences* seqs, int64_t heads,
   return cache->d < 1 || cache->d > kMaxD ? KD_ERR_UNSUPPORTED_N : KD_OK;
 }
 
-// rows of `heads` x `tokens` vectors of d elements do not overlap
-bool rows_apart(int64_t tokens, int64_t heads, int64_t d, int64_t token, int64_t head) {
-  if (tokens > 1 && heads > 1)
-    return (head >= d && token >= d && (token - d) / head >= heads - 1) ||
-           (token >= d && head >= d && (head - d) / token >= tokens - 1);
-  return (tokens <= 1 || token >= d) && (heads <= 1 || head >= d);
-}
-
 }  // namespace
 }  // namespace attn4
 }  // namespace kd
@@ -182,7 +175,7 @@ extern "C" kd_status kd_attention_4bit(const kd_cache4* cache, const kd_sequence
   using namespace kd::attn4;
   const kd_status st = check(cache, seqs, heads, causal, window);
   if (st != KD_OK) return st;
-  if (tokens < 0 || tokens > INT32_MAX || (dtype != KD_F16 && dtype != KD_BF16) || !std::isfinite(scale) || q_token < 0 ||
+  if (tokens < 0 || tokens > INT32_MAX || (dtype != KD_F16 && dtype != KD_BF16) || !std::isfinite(scale * kLog2e) || q_token < 0 ||
       q_head < 0 || out_token < 0 || out_head < 0)
     return KD_ERR_INVALID_ARG;
   Plan pl;
@@ -213,7 +206,7 @@ extern "C" kd_status kd_attention_4bit(const kd_cache4* cache, const kd_sequence
   p.bf16 = dtype == KD_BF16;
   p.q_vec = cache->d % 8 == 0 && aligned(q, 16) && (tokens == 1 || q_token % 8 == 0) && (heads == 1 || q_head % 8 == 0);
   p.out_vec = cache->d % 4 == 0 && aligned(out, 8) && (tokens == 1 || out_token % 4 == 0) && (heads == 1 || out_head % 4 == 0);
-  p.scale2 = scale * 1.4426950408889634f;
+  p.scale2 = scale * kLog2e;
   if (!pl.team) {
     p.cuts = static_cast<Cut*>(workspace);
     p.part_ml = reinterpret_cast<float2*>(p.cuts + pl.items);

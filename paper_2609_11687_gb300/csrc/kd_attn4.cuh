@@ -51,9 +51,9 @@
 // 128) take 60 us, with it 62; past the first 20 us at 5.9 TB/s, 87 % of the measured copy rate.
 // The rest is the start (2.4 us until the share is known, 6.5 until the first codes are there), shares that end
 // unlike on SMs unlike far from memory (45 to 66 us), and the join (3 us).  Measured (device time, inputs
-// larger than L2): 32 sequences of 2000 to 8192 positions 53 us (floor 27), one of 131072 40 us (22), 16 of up
-// to 4096 with up to 8 drafted tokens 44 us, one of 1001 positions with 32 key heads 7.0 us.
-// 128 registers (255 above 128 channels) spill 16 to 130 bytes in some instances, groups of 32 the most.
+// larger than L2): 32 sequences of 2000 to 8192 positions 51 us (floor 27), one of 131072 39 us (22), 16 of up
+// to 4096 with up to 8 drafted tokens 43 us (6.6), one of 1001 positions with 32 key heads 7.1 us (0.7).
+// 128 registers (255 above 128 channels) spill up to 88 bytes in some instances, groups of 32 the most.
 #pragma once
 #include <cooperative_groups.h>
 
@@ -202,7 +202,7 @@ __device__ __forceinline__ void load_two_matrices(uint32_t (&d)[4], uint32_t at)
     asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0, %1}, [%2];" : "=r"(d[0]), "=r"(d[1]) : "r"(at) : "memory");
   else asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0, %1}, [%2];" : "=r"(d[0]), "=r"(d[1]) : "r"(at) : "memory");
 }
-// an 8 x 8 matrix of halves, a row to four lanes, turned// an 8 x 8 matrix of halves, a row to four lanes, turned
+// an 8 x 8 matrix of halves, a row to four lanes, turned
 __device__ __forceinline__ uint32_t turned(uint32_t v) {
   uint32_t r;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
@@ -228,7 +228,7 @@ template <int NC, int GS>
 struct Shape {
   static constexpr int kGroups = (NC + GS - 1) / GS;
   static constexpr int kRows = attn4::kRows;
-  static constexpr int kStages = NC <= 4 ? 2 : 2;
+  static constexpr int kStages = 2;
   static constexpr int kStride = 4 * (NC | 1);                       // words of a row of codes in the ring
   // words of a stage, keys or values
   static constexpr int kCodes = kTiles * kTile * kStride, kScales = kTiles * kTile * kGroups;
@@ -788,7 +788,8 @@ __global__ void __launch_bounds__(32 * kWarps, NC <= 4 ? 4 : 2) attn4_kernel(con
           wait_group<ST - 1>();
           __syncwarp();  // the lanes' copies are each other's
           const int position = (first_tile + b0 + nth) * kTile;
-          if (bad_pages || position < w.all_lo || position + kTiles * kTile > min(w.all_hi, share_hi))
+          // `position` may be the last of 31 bits: nothing is added to it
+          if (bad_pages || position < w.all_lo || position > min(w.all_hi, share_hi) - kTiles * kTile)
             step(std::true_type{}, stage, position, place[nth].x < 0, nth + 1 < n && place[nth + 1].x < 0);
           else step(std::false_type{}, stage, position, false, false);
           __syncwarp();

@@ -8,7 +8,7 @@ namespace cache4 {
 
 using namespace serve;
 
-constexpr int64_t kMaxD = 256;
+constexpr int64_t kMaxD = 256, kMaxSeqs = (int64_t)1 << 30;
 
 // host checks, in parts: those of sizes, and of pointers that a call with work to do needs
 inline bool cache_sizes_ok(const kd_cache4* c) {
@@ -20,11 +20,19 @@ inline bool cache_pointers_ok(const kd_cache4* c) {
          aligned(c->v_codes, 16) && aligned(c->v_scales, 16) && c->pages > 0;
 }
 inline bool sequences_sizes_ok(const kd_sequences* s) {
-  return s && s->seqs >= 0 && s->seqs < INT32_MAX && s->wide >= 0 && s->wide <= INT32_MAX && s->ld_table >= s->wide &&
+  return s && s->seqs >= 0 && s->seqs <= kMaxSeqs && s->wide >= 0 && s->wide <= INT32_MAX && s->ld_table >= s->wide &&
          s->most >= 0 && s->most <= INT32_MAX && s->longest >= 0;
 }
 inline bool sequences_pointers_ok(const kd_sequences* s) {
   return s->table && s->lengths && aligned(s->table, 4) && aligned(s->lengths, 4) && aligned(s->starts, 4) && s->wide > 0;
+}
+
+// rows of `heads` x `tokens` vectors of d elements do not overlap
+inline bool rows_apart(int64_t tokens, int64_t heads, int64_t d, int64_t token, int64_t head) {
+  if (tokens > 1 && heads > 1)
+    return (head >= d && token >= d && (token - d) / head >= heads - 1) ||
+           (token >= d && head >= d && (head - d) / token >= tokens - 1);
+  return (tokens <= 1 || token >= d) && (heads <= 1 || head >= d);
 }
 
 // what the device needs of both

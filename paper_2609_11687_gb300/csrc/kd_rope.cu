@@ -16,6 +16,10 @@
 // and one round of heads where there are few, so that one token's heads are spread over the GPU.
 // Heads that do not start on 16-byte boundaries, or whose parts are no whole vectors, go pair by
 // pair, a warp a head, and are read twice (the second time from L1).
+//
+// Bound by instructions and HBM about alike: 2048 tokens of 32 + 8 heads of 128 bf16 channels, normed, take 10.6 us
+// (42 MB, 4.0 TB/s; a plain copy of as much runs at 5.9), issue slots 63 % busy.  One token's heads take 1.8 us,
+// 333 tokens of 10 + 2 heads of 80 channels 1.9: latency.
 #include <cmath>
 
 #include "kd_serve.cuh"
@@ -25,7 +29,7 @@ namespace {
 
 using namespace serve;
 
-constexpr int64_t kRopeMaxD = 1024;
+constexpr int64_t kRopeMaxD = 1024, kRopeMaxHeads = 65535;
 constexpr int kRopeWarps = 4;  // of a CTA
 
 struct RopeSide {
@@ -317,12 +321,12 @@ extern "C" kd_status kd_rope(const kd_heads* q, const kd_heads* k, kd_dtype dtyp
   const kd_heads* sides[2] = {q, k ? k : &none};
   int64_t heads = 0;
   for (const kd_heads* h : sides) {
-    if (h->heads < 0 || h->heads > INT32_MAX || h->x_token < 0 || h->x_head < 0 || h->y_token < 0 || h->y_head < 0 ||
+    if (h->heads < 0 || h->heads > kRopeMaxHeads || h->x_token < 0 || h->x_head < 0 || h->y_token < 0 || h->y_head < 0 ||
         (h->weight && h->weight_dtype != dtype && h->weight_dtype != KD_F32))
       return KD_ERR_INVALID_ARG;
     heads += h->heads;
   }
-  if (heads > INT32_MAX || tokens * heads > INT32_MAX) return KD_ERR_INVALID_ARG;
+  if (tokens * heads > INT32_MAX) return KD_ERR_INVALID_ARG;
   if (tokens == 0 || heads == 0) return KD_OK;
   const int64_t eb = type_bytes(dtype), V = 16 / eb;
   bool vec = rot % (2 * V) == 0 && d % V == 0 && (rot + (d - rot + 2 * V - 1) / (2 * V) * (2 * V)) / (2 * V) <= 32;

@@ -40,7 +40,7 @@ def _rope(kd, q={}, k=None, **more):
     dict(q=dict(x=NULL)), dict(q=dict(y=NULL)), dict(q=dict(x=A + 1)), dict(q=dict(y=A + 1)), dict(q=dict(heads=-1)),
     dict(q=dict(x_token=-1)), dict(q=dict(x_head=-64)), dict(q=dict(y_token=-1)), dict(q=dict(y_head=-1)),
     dict(q=dict(y_head=63)), dict(q=dict(y_token=127)), dict(q=dict(weight=A, weight_dtype=2)), dict(q=dict(weight=A + 1)),
-    dict(q=dict(weight=A + 2, weight_dtype=0)), dict(q=dict(heads=2 ** 31)), dict(q=dict(heads=2 ** 30, y_token=2 ** 36)),
+    dict(q=dict(weight=A + 2, weight_dtype=0)), dict(q=dict(heads=2 ** 31)), dict(q=dict(heads=65536)), dict(k=dict(heads=65536), tokens=1), dict(q=dict(heads=2 ** 30, y_token=2 ** 36)),
     dict(k=dict(y_head=63)), dict(k=dict(x=NULL)), dict(k=dict(weight=A, weight_dtype=7))])
 def test_rope_refusals(kd, bad):
     assert _rope(kd, **bad) == kd.KD_ERR_INVALID_ARG
@@ -137,7 +137,7 @@ BAD_CACHE = [dict(k_codes=NULL), dict(k_scales=NULL), dict(v_codes=NULL), dict(v
              dict(v_codes=A + 4), dict(v_scales=A + 2), dict(pages=-1), dict(pages=0), dict(pages=2 ** 31), dict(heads=0), dict(heads=65536),
              dict(page=8), dict(page=24), dict(page=0), dict(page=65552), dict(group=16), dict(group=256)]
 BAD_SEQUENCES = [dict(table=NULL), dict(lengths=NULL), dict(table=A + 2), dict(lengths=A + 1), dict(starts=A + 2), dict(ld_table=2),
-                 dict(seqs=-1), dict(seqs=2 ** 31), dict(wide=-1), dict(wide=0), dict(wide=2 ** 31, ld_table=2 ** 32), dict(most=-1),
+                 dict(seqs=-1), dict(seqs=2 ** 31), dict(seqs=2 ** 30 + 1), dict(wide=-1), dict(wide=0), dict(wide=2 ** 31, ld_table=2 ** 32), dict(most=-1),
                  dict(most=2 ** 31), dict(longest=-1)]
 
 
@@ -247,7 +247,7 @@ def _attend(kd, cache={}, seqs={}, **more):
 @pytest.mark.parametrize("bad", [dict(cache=b) for b in BAD_CACHE] + [dict(seqs=b) for b in BAD_SEQUENCES] + [
     dict(tokens=-1), dict(tokens=2 ** 31), dict(heads=0), dict(heads=3), dict(heads=-2), dict(heads=2 ** 31), dict(dtype=0), dict(dtype=3),
     dict(q=NULL), dict(out=NULL), dict(q=A + 1), dict(out=A + 1), dict(lse=A + 2), dict(q_token=-1), dict(q_head=-1), dict(out_token=-1),
-    dict(out_head=63), dict(out_token=255), dict(out_head=0), dict(scale=math.inf), dict(scale=math.nan), dict(window=-1),
+    dict(out_head=63), dict(out_token=255), dict(out_head=0), dict(scale=math.inf), dict(scale=2.5e38), dict(scale=-2.5e38), dict(scale=math.nan), dict(window=-1),
     dict(window=5, causal=0), dict(window=2 ** 31), dict(seqs=dict(most=2 ** 31 - 1)), dict(seqs=dict(seqs=2 ** 30, most=64))])
 def test_attention_refusals(kd, bad):
     assert _attend(kd, **bad) == kd.KD_ERR_INVALID_ARG

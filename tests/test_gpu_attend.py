@@ -81,8 +81,8 @@ def test_prompt_then_tokens(kd, hidden, heads, kv_heads, d, rot, dt):
 
 
 def test_drafted_tokens_are_decoded_tokens(kd):
-    """Several tokens of a sequence in one call leave the cache's bits and, to their rounding, the outputs of
-    as many calls of one."""
+    """Several tokens of a sequence in one call leave, to the products' rounding and a code of the cache, the outputs and
+    the cached rows of as many calls of one."""
     step, randn = _step(kd, 256, 4, 2, 64, torch.float16)
     other, _ = _step(kd, 256, 4, 2, 64, torch.float16)
     table = torch.randperm(40, device="cuda")[:24].view(2, 12).int()

@@ -430,6 +430,36 @@ def test_a_cache_past_32_bits(kd):
     assert torch.equal(a, b) and torch.isfinite(a).all() and a.abs().max() > 0
 
 
+def test_positions_of_31_bits(kd):
+    """The last positions that a sequence may have: what a window sees there is what it sees of the same pages in a
+    short sequence (to the bit: the windows start alike in their tiles)."""
+    cache = kd.new_cache_4bit(1, 2, 64, 65536, 64)
+    x = torch.randn((65536, 2, 64), device="cuda")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    whole = kd.Sequences(torch.zeros((1, 1), **i32), torch.full((1,), 65536, **i32), most=65536)
+    kd.cache_write_4bit(cache, x, x.roll(1, 0), whole)
+    q = torch.randn((2, 4, 64), device="cuda").half()
+    tables = torch.zeros((1, 2), **i32), torch.zeros((1, 32768), **i32)
+    for length, window in ((2 ** 31 - 17, 100), (2 ** 31 - 17, 1), (2 ** 31 - 20, 333), (2 ** 31 - 17, 20000)):
+        short = length - (2 ** 31 - 2 * 65536)
+        got = []
+        for table, n in zip(tables, (short, length)):
+            lse = torch.empty((2, 4), dtype=F32, device="cuda")
+            s = kd.Sequences(table, torch.full((1,), n, **i32), most=2, longest=window + 1)
+            got.append((kd.attention_4bit(cache, q, s, window=window, lse=lse), lse))
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+        assert torch.isfinite(got[0][0]).all()
+    s = kd.Sequences(tables[1], torch.full((1,), 2 ** 31 - 1, **i32), most=2, longest=100)
+    assert kd.attention_4bit(cache, q, s, window=100).isnan().all()
+
+
+def test_in_place(kd):
+    for c in (Case(kd, [300, 2000], [1, 3], 8, 2, 64), Case(kd, [30000, 50], [2, 1], 8, 1, 128, room=200000)):
+        want = c.run(kd)[0][:int(c.starts[-1])].clone()
+        assert kd.attention_4bit(c.cache, c.q, c.seqs, out=c.q) is c.q
+        assert torch.equal(c.q[:int(c.starts[-1])], want)
+
+
 def test_nothing_to_do(kd):
     cache = kd.new_cache_4bit(2, 2, 64, 16, 64)
     i32 = dict(dtype=torch.int32, device="cuda")
