@@ -134,7 +134,7 @@ bool plan(const kd_cache4* c, const kd_sequences* s, int64_t heads, int64_t wind
   const double chunks_each = (double)((longest + kTile * kChunk - 1) / (kTile * kChunk));
   pl.team = 0;
   double least = 10 + 0.003 * all * chunks_each;
-  for (int team = 1; team <= 8 && team <= chunks_each; team *= 2) {
+  for (int team = 1; team <= kTeam && team <= chunks_each; team *= 2) {
     const double rounds = std::ceil((double)all * team / places), on_sm = std::min((double)all * team, (double)places) / 152;
     const double cost = 4.5 + (team > 1 ? 1.2 : 0) + rounds * std::ceil(chunks_each / team) * std::max(0.86, 0.5 + 0.38 * on_sm);
     if (cost < least) {

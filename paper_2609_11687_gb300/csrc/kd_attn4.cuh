@@ -71,6 +71,7 @@ constexpr int kRows = 8;      // of a block: columns of a tensor-core tile
 constexpr int kTile = 16;     // positions of a tensor-core tile, all on one page
 constexpr int kTiles = 2;     // of one step of a warp
 constexpr int kChunk = kTiles * kWarps;  // tiles of one step of a CTA: what work is shared out in
+constexpr int kTeam = 8;      // CTAs of a cluster at most
 constexpr int kBatch = 256;   // tiles whose places are looked up at a time
 
 struct Params {
@@ -335,20 +336,26 @@ __device__ __forceinline__ void join_team(const Params& p, const Work& w, int he
     if (t < 0 || t >= p.tokens) continue;
     float top = kNone, total = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k = 0; k < p.team; ++k) top = fmaxf(top, cl.map_shared_rank(ml, k)[r].x);
-    for (int k = 0; k < p.team; ++k) {
-      const float2 n = cl.map_shared_rank(ml, k)[r];
-      if (n.x == kNone) {  // no sums there, or NaN
-        total += n.y;
-        continue;
-      }
-      const float f = exp2_of(n.x - top);
-      total += n.y * f;
-      const float4 v = *reinterpret_cast<const float4*>(cl.map_shared_rank(sums, k) + r * Z::kSums + ch);
-      o.x = __fmaf_rn(v.x, f, o.x);
-      o.y = __fmaf_rn(v.y, f, o.y);
-      o.z = __fmaf_rn(v.z, f, o.z);
-      o.w = __fmaf_rn(v.w, f, o.w);
+    float2 n[kTeam];
+#pragma unroll
+    for (int k = 0; k < kTeam; ++k) {
+      n[k] = k < p.team ? cl.map_shared_rank(ml, k)[r] : make_float2(kNone, 0.f);
+      top = fmaxf(top, n[k].x);
+    }
+    float4 v[kTeam];  // all on their way together
+#pragma unroll
+    for (int k = 0; k < kTeam; ++k) {
+      v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (n[k].x != kNone) v[k] = *reinterpret_cast<const float4*>(cl.map_shared_rank(sums, k) + r * Z::kSums + ch);
+    }
+#pragma unroll
+    for (int k = 0; k < kTeam; ++k) {
+      const float f = n[k].x == kNone ? 0.f : exp2_of(n[k].x - top);
+      total += n[k].x == kNone ? n[k].y : n[k].y * f;  // no sums there, or NaN
+      o.x = __fmaf_rn(v[k].x, f, o.x);
+      o.y = __fmaf_rn(v[k].y, f, o.y);
+      o.z = __fmaf_rn(v[k].z, f, o.z);
+      o.w = __fmaf_rn(v[k].w, f, o.w);
     }
     put(p, p.out + t * p.out_token + h * p.out_head, ch, o, total);
     if (ch == 0) put_lse(p, t * p.heads + h, top, total);

@@ -967,7 +967,8 @@ def _serve():
     if raw is None:
         def raw(index):
             return torch.cuda.current_stream(index).cuda_stream
-    return floats, rows4, torch.float32, torch.float8_e4m3fn, raw, torch.cuda.current_device
+    device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return floats, rows4, torch.float32, torch.float8_e4m3fn, raw, device
 
 
 def _refuse(t, name, types, index, shape):
@@ -1313,12 +1314,12 @@ def _ld3(t, name, types, index, shape=None, out=False):
     """Strides over tokens and heads of a (tokens, heads, d) operand after its checks: a CUDA tensor of
     one of ``types`` on device ``index``, of ``shape``, with unit inner stride and, of an output, rows that do
     not overlap.  What a size of 1 leaves open is as if the rows were dense."""
-    size, stride = t.shape, t.stride()
+    size = t.shape
     if len(size) != 3 or t.dtype not in types or t.get_device() != index or index < 0 \
             or (shape is not None and size != shape):
         _refuse3(t, name, types, index, shape)
     tokens, heads, d = size
-    a, b, c = stride
+    a, b, c = t.stride()
     if d > 1 and c != 1:
         _refuse3(t, name, types, index, shape)
     if tokens <= 1:
@@ -1353,8 +1354,9 @@ def rope(q, k, positions, rotation: Rotation, q_norm=None, k_norm=None, eps: flo
     if rotation.rot > d:
         raise ValueError(f"the rotation turns {rotation.rot} channels of {d}")
     if yq is None:
-        yq = _new(stream, shape, dt, q.device)
-    ot, oh = _ld3(yq, "out's q", (dt,), index, shape, True)
+        yq, ot, oh = _new(stream, shape, dt, q.device), heads * d, d
+    else:
+        ot, oh = _ld3(yq, "out's q", (dt,), index, shape, True)
     weight = wt = 0
     if q_norm is not None:
         _vec(q_norm, "q_norm", (dt, f32), index, d)
@@ -1365,8 +1367,9 @@ def rope(q, k, positions, rotation: Rotation, q_norm=None, k_norm=None, eps: flo
         if k.shape[0] != tokens or k.shape[2] != d:
             raise ValueError("q and k must have the same tokens and channels")
         if yk is None:
-            yk = _new(stream, k.shape, dt, k.device)
-        ot, oh = _ld3(yk, "out's k", (dt,), index, k.shape, True)
+            yk, ot, oh = _new(stream, k.shape, dt, k.device), k.shape[1] * d, d
+        else:
+            ot, oh = _ld3(yk, "out's k", (dt,), index, k.shape, True)
         weight = wt = 0
         if k_norm is not None:
             _vec(k_norm, "k_norm", (dt, f32), index, d)
@@ -1532,8 +1535,9 @@ def attention_4bit(cache: Cache4, q, seqs: Sequences, scale: Optional[float] = N
     if seqs.index != index:
         raise ValueError("the sequences must be on the cache's device")
     if out is None:
-        out = _new(stream, q.shape, dt, q.device)
-    ot, oh = _ld3(out, "out", (dt,), index, q.shape, True)
+        out, ot, oh = _new(stream, q.shape, dt, q.device), heads * d, d
+    else:
+        ot, oh = _ld3(out, "out", (dt,), index, q.shape, True)
     if lse is not None and (lse.dtype != f32 or lse.shape != q.shape[:2] or lse.get_device() != index or not lse.is_contiguous()):
         raise ValueError(f"lse must be a contiguous torch.float32 {(tokens, heads)} tensor on the cache's device")
     if window < 0 or (window and not causal):
