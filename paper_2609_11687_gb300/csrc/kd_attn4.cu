@@ -101,17 +101,26 @@ struct Plan {
 // How the work is cut: a cluster for each item (sequence, key head, block of rows), or equal shares of all of it.
 // Clusters need no search and no second launch, but are done when the longest is; equal shares take all SMs
 // whatever the lengths.  The rule estimates both in microseconds from the longest length that the host knows:
-//   a cluster of t CTAs: 4.5, 1.2 for its join, and for each round of CTAs that fit the GPU its steps of 128 positions
-//   at 0.86 where a CTA has an SM to itself, up to 2 where four share it;
-//   equal shares: 10, and 3 ns for each such step of all items (HBM's rate).
+//   clusters: 3.8, 0.9 for their join, 6 ns a CTA, and their steps of 128 positions at 0.69, or 0.24 + 0.45 for each
+//   CTA that an SM has (above 128 channels 0.98, or 0.95 for each, and clusters of eight put two on some SMs
+//   early); times the rounds of CTAs where they do not all fit;
+//   equal shares: 11, and 3.2 ns for each such step of all items (HBM's rate; 0.64 more for each 32 channels above 128).
 // Measured for heads of 128 channels, groups of 64, four rows, clusters of 1 / 2 / 4 / 8 and equal shares:
-//     8 items of  1024 positions   10.4 / 9.4 / 7.8 / 7.4,   8.7
-//     8 items of  8192             54 / 31 / 19 / 12.9,     12.6
-//    32 items of  4096             29 / 18 / 11.9 / 10.5,   12.7
-//   256 items of  1024             13.6 / 15.2 / 21 / 34,   17.2
-//   256 items of  4096             38 / 37 / 42 / 53,       39
-//   256 items of  2000 to 8192     65 / 57 / 54 / 63,       52
-//   512 items of  8192             120 / 111 / 121 / 138,   124;  of 2000 to 8192  105 / 91 / 93 / 114,  83
+//     8 items of  1024 positions   9.3 / 8.4 / 7.1 / 6.4,   8.4
+//     8 items of  8192             48 / 28 / 16.7 / 11.3,   12.2
+//    32 items of  4096             26 / 16 / 10.9 / 9.9,    12.5
+//    32 items of 16384             95 / 51 / 28 / 22,       24
+//   256 items of  1024             13.3 / 14.8 / 20 / 30,   16.9
+//   256 items of  4096             37 / 36 / 40 / 49,       39
+//   256 items of  2000 to 8192     62 / 56 / 52 / 59,       51
+//   512 items of  8192             118 / 110 / 118 / 132,   117;  of 2000 to 8192  104 / 90 / 90 / 107,  81
+// Several blocks of rows of a key head read the same codes, as CTAs side by side from L2 (steps at 1.7 at most) but in equal
+// shares one after the other: 14, and 3.7 ns a step.  Where sequences have rows of their own number, a part of the blocks
+// is empty and lengths differ too: 0.7 of the items and 0.65 of their steps are counted.  Four blocks of eight rows:
+//   512 items of  1000 to 4096, 1 to 8 tokens    54 / 37 / 43 / 57,        44
+//   256 items of  the same                       37 / 32 / 22 / 28,        28
+//  2048 items of  the same                       100 / 109 / 138 / 198,    118
+//  1024 items of  4096, 8 tokens                 100 / 111 / 131 / 174,    146;  of 16384  368 / 370 / 381 / 417,  503
 bool plan(const kd_cache4* c, const kd_sequences* s, int64_t heads, int64_t window, Plan& pl) {
   const int64_t shared = heads / c->heads;
   if (s->most * shared > INT32_MAX) return false;
@@ -133,10 +142,15 @@ bool plan(const kd_cache4* c, const kd_sequences* s, int64_t heads, int64_t wind
   const int64_t all = items * blocks, places = 152 * (pl.nc <= 4 ? 4 : 2);
   const double chunks_each = (double)((longest + kTile * kChunk - 1) / (kTile * kChunk));
   pl.team = 0;
-  double least = 10 + 0.003 * all * chunks_each;
+  const bool several = blocks > 1, uneven = several && s->seqs > 1 && s->starts;
+  const double live = (uneven ? 0.7 : 1) * (double)all, mean = uneven ? 0.65 : 1, wide = 1 + 0.2 * std::max(pl.nc - 4, 0);
+  double least = several ? 14 + 0.0037 * wide * live * mean * chunks_each : 11 + 0.0032 * wide * live * chunks_each;
   for (int team = 1; team <= kTeam && team <= chunks_each; team *= 2) {
-    const double rounds = std::ceil((double)all * team / places), on_sm = std::min((double)all * team, (double)places) / 152;
-    const double cost = 4.5 + (team > 1 ? 1.2 : 0) + rounds * std::ceil(chunks_each / team) * std::max(0.86, 0.5 + 0.38 * on_sm);
+    const double ctas = live * team, fit = std::min(ctas, (double)places), on_sm = fit / 152;
+    double step = pl.nc <= 4 ? std::max(0.69, 0.24 + 0.45 * on_sm) : std::max(0.98, 0.95 * std::min(2.0, team == kTeam ? 2 * on_sm : on_sm));
+    if (several) step = std::min(step, 1.7);
+    const double start = 3.8 + (team > 1 ? 0.9 : 0) + 0.006 * fit, steps = std::ceil(chunks_each / team) * step;
+    const double cost = std::max(start + steps, ctas / fit * (start + mean * steps));
     if (cost < least) {
       least = cost;
       pl.team = team;

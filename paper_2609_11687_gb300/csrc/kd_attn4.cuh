@@ -52,7 +52,7 @@
 // The rest is the start (2.4 us until the share is known, 6.5 until the first codes are there), shares that end
 // unlike on SMs unlike far from memory (45 to 66 us), and the join (3 us).  Measured (device time, inputs
 // larger than L2): 32 sequences of 2000 to 8192 positions 51 us (floor 27), one of 131072 39 us (22), 16 of up
-// to 4096 with up to 8 drafted tokens 43 us (6.6), one of 1001 positions with 32 key heads 7.1 us (0.7).
+// to 4096 with up to 8 drafted tokens 37 us (6.6), one of 1001 positions with 32 key heads 6.7 us (0.7).
 // 128 registers (255 above 128 channels) spill up to 88 bytes in some instances, groups of 32 the most.
 #pragma once
 #include <cooperative_groups.h>
