@@ -101,10 +101,11 @@ struct Plan {
 // How the work is cut: a cluster for each item (sequence, key head, block of rows), or equal shares of all of it.
 // Clusters need no search and no second launch, but are done when the longest is; equal shares take all SMs
 // whatever the lengths.  The rule estimates both in microseconds from the longest length that the host knows:
-//   clusters: 3.8, 0.9 for their join, 6 ns a CTA, and their steps of 128 positions at 0.69, or 0.24 + 0.45 for each
-//   CTA that an SM has (above 128 channels 0.98, or 0.95 for each, and clusters of eight put two on some SMs
-//   early); times the rounds of CTAs where they do not all fit;
-//   equal shares: 11, and 3.2 ns for each such step of all items (HBM's rate; 0.64 more for each 32 channels above 128).
+//   clusters: 4, 1.2 for their join, 2.5 ns a CTA, and their steps of 128 positions at 0.69, or 0.24 + 0.45 for each
+//   CTA that an SM has (0.63 of that for 64 channels; above 128 channels 0.98, or 0.95 for each, and clusters of eight
+//   put two on some SMs early); times the rounds of CTAs where they do not all fit;
+//   equal shares: 11, and 3.2 ns for each such step of all items (HBM's rate; 2 for 64 channels, 5.8 for 256), 3.0 of
+//   several sequences, which are seldom all as long as the longest.
 // Measured for heads of 128 channels, groups of 64, four rows, clusters of 1 / 2 / 4 / 8 and equal shares:
 //     8 items of  1024 positions   9.3 / 8.4 / 7.1 / 6.4,   8.4
 //     8 items of  8192             48 / 28 / 16.7 / 11.3,   12.2
@@ -143,13 +144,13 @@ bool plan(const kd_cache4* c, const kd_sequences* s, int64_t heads, int64_t wind
   const double chunks_each = (double)((longest + kTile * kChunk - 1) / (kTile * kChunk));
   pl.team = 0;
   const bool several = blocks > 1, uneven = several && s->seqs > 1 && s->starts;
-  const double live = (uneven ? 0.7 : 1) * (double)all, mean = uneven ? 0.65 : 1, wide = 1 + 0.2 * std::max(pl.nc - 4, 0);
-  double least = several ? 14 + 0.0037 * wide * live * mean * chunks_each : 11 + 0.0032 * wide * live * chunks_each;
+  const double live = (uneven ? 0.7 : 1) * (double)all, mean = uneven ? 0.65 : 1, wide = pl.nc <= 4 ? 0.25 + 0.1875 * pl.nc : 0.2 + 0.2 * pl.nc;
+  double least = several ? 14 + 0.0037 * wide * live * mean * chunks_each : 11 + (s->seqs > 1 ? 0.003 : 0.0032) * wide * live * chunks_each;
   for (int team = 1; team <= kTeam && team <= chunks_each; team *= 2) {
     const double ctas = live * team, fit = std::min(ctas, (double)places), on_sm = fit / 152;
-    double step = pl.nc <= 4 ? std::max(0.69, 0.24 + 0.45 * on_sm) : std::max(0.98, 0.95 * std::min(2.0, team == kTeam ? 2 * on_sm : on_sm));
-    if (several) step = std::min(step, 1.7);
-    const double start = 3.8 + (team > 1 ? 0.9 : 0) + 0.006 * fit, steps = std::ceil(chunks_each / team) * step;
+    double step = pl.nc <= 4 ? wide * std::max(0.69, 0.24 + 0.45 * on_sm) : std::max(0.98, 0.95 * std::min(2.0, team == kTeam ? 2 * on_sm : on_sm));
+    if (several) step = std::min(step, 1.7 * wide);
+    const double start = 4 + (team > 1 ? 1.2 : 0) + 0.0025 * fit, steps = std::ceil(chunks_each / team) * step;
     const double cost = std::max(start + steps, ctas / fit * (start + mean * steps));
     if (cost < least) {
       least = cost;
