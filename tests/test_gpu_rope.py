@@ -3,8 +3,8 @@ and negative positions, special values, in place, streams and graphs.
 
 Tolerance of an output y = A (a cos - b sin): half a step of its type, and of A (|a| + |b|) what
 fp32 leaves: the angle 2 pi (2^-26 + 2^-33) = 9.5e-8, sine, cosine and amplitude 3 2^-24, product
-and sum 2 2^-24: 4e-7.  With a norm (sums of up to 1024 squares in chains of at most 36, root, quotient,
-two products) 44 2^-24 = 2.6e-6 more."""
+and sum 2 2^-24: 4e-7.  With a norm (sums of up to 1024 squares in chains of at most 36, of which the root
+halves the error; the reciprocal root itself 4, two products) less than 44 2^-24 = 2.6e-6 more."""
 
 import math
 
