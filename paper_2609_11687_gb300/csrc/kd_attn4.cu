@@ -108,19 +108,19 @@ struct Plan {
 //   several sequences, which are seldom all as long as the longest.
 // Measured for heads of 128 channels, groups of 64, four rows, clusters of 1 / 2 / 4 / 8 and equal shares:
 //     8 items of  1024 positions   9.3 / 8.4 / 7.1 / 6.4,   8.4
-//     8 items of  8192             48 / 28 / 16.7 / 11.3,   12.2
+//     8 items of  8192             48 / 28 / 16.7 / 11.2,   11.9
 //    32 items of  4096             26 / 16 / 10.9 / 9.9,    12.5
-//    32 items of 16384             95 / 51 / 28 / 22,       24
-//   256 items of  1024             13.3 / 14.8 / 20 / 30,   16.9
-//   256 items of  4096             37 / 36 / 40 / 49,       39
+//    32 items of 16384             95 / 51 / 28 / 22.5,     24.6
+//   256 items of  1024             13.1 / 14.8 / 20 / 30,   19
+//   256 items of  4096             37 / 36 / 40 / 49,       37
 //   256 items of  2000 to 8192     62 / 56 / 52 / 59,       51
-//   512 items of  8192             118 / 110 / 118 / 132,   117;  of 2000 to 8192  104 / 90 / 90 / 107,  81
+//   512 items of  8192             118 / 110 / 117 / 132,   112;  of 2000 to 8192  105 / 89 / 90 / 107,  82
 // Several blocks of rows of a key head read the same codes, as CTAs side by side from L2 (steps at 1.7 at most) but in equal
 // shares one after the other: 14, and 3.7 ns a step.  Where sequences have rows of their own number, a part of the blocks
 // is empty and lengths differ too: 0.7 of the items and 0.65 of their steps are counted.  Four blocks of eight rows:
 //   512 items of  1000 to 4096, 1 to 8 tokens    54 / 37 / 43 / 57,        44
 //   256 items of  the same                       37 / 32 / 22 / 28,        28
-//  2048 items of  the same                       100 / 109 / 138 / 198,    118
+//  2048 items of  the same                       100 / 109 / 138 / 198,    119
 //  1024 items of  4096, 8 tokens                 100 / 111 / 131 / 174,    146;  of 16384  368 / 370 / 381 / 417,  503
 bool plan(const kd_cache4* c, const kd_sequences* s, int64_t heads, int64_t window, Plan& pl) {
   const int64_t shared = heads / c->heads;
@@ -140,15 +140,15 @@ bool plan(const kd_cache4* c, const kd_sequences* s, int64_t heads, int64_t wind
   pl.items = items * blocks;
   int64_t longest = std::min(s->longest, room);
   if (window > 0) longest = std::min(longest, window + kRows + kTile);
-  const int64_t all = items * blocks, places = 152 * (pl.nc <= 4 ? 4 : 2);
+  const int64_t all = items * blocks, places = 152 * on_sm(pl.nc, true);
   const double chunks_each = (double)((longest + kTile * kChunk - 1) / (kTile * kChunk));
   pl.team = 0;
   const bool several = blocks > 1, uneven = several && s->seqs > 1 && s->starts;
   const double live = (uneven ? 0.7 : 1) * (double)all, mean = uneven ? 0.65 : 1, wide = pl.nc <= 4 ? 0.25 + 0.1875 * pl.nc : 0.2 + 0.2 * pl.nc;
   double least = several ? 14 + 0.0037 * wide * live * mean * chunks_each : 11 + (s->seqs > 1 ? 0.003 : 0.0032) * wide * live * chunks_each;
   for (int team = 1; team <= kTeam && team <= chunks_each; team *= 2) {
-    const double ctas = live * team, fit = std::min(ctas, (double)places), on_sm = fit / 152;
-    double step = pl.nc <= 4 ? wide * std::max(0.69, 0.24 + 0.45 * on_sm) : std::max(0.98, 0.95 * std::min(2.0, team == kTeam ? 2 * on_sm : on_sm));
+    const double ctas = live * team, fit = std::min(ctas, (double)places), of_sm = fit / 152;
+    double step = pl.nc <= 4 ? wide * std::max(0.69, 0.24 + 0.45 * of_sm) : std::max(0.98, 0.95 * std::min(2.0, team == kTeam ? 2 * of_sm : of_sm));
     if (several) step = std::min(step, 1.7 * wide);
     const double start = 4 + (team > 1 ? 1.2 : 0) + 0.0025 * fit, steps = std::ceil(chunks_each / team) * step;
     const double cost = std::max(start + steps, ctas / fit * (start + mean * steps));
@@ -157,7 +157,7 @@ bool plan(const kd_cache4* c, const kd_sequences* s, int64_t heads, int64_t wind
       pl.team = team;
     }
   }
-  pl.grid = (int)(pl.team ? all * pl.team : std::min(places, all * chunks_of(longest)));
+  pl.grid = (int)(pl.team ? all * pl.team : std::min<int64_t>(152 * on_sm(pl.nc, false), all * chunks_of(longest)));
   pl.workspace = 0;
   if (!pl.team) pl.workspace = (size_t)all * sizeof(Cut) + (size_t)pl.grid * 2 * kRows * (8 + 4 * (size_t)((c->d + 3) / 4 * 4));
   pl.workspace = (pl.workspace + 15) / 16 * 16;
