@@ -22,11 +22,14 @@
 // off the sums before each step's products, and w times the middle, low + 8 step, is summed in fp32.
 //
 // Weights.  w step is the B operand, rounded to fp16: the one rounding to fewer bits here, an error
-// of 2^-12 of a value's distance from its group's middle.  It is scaled by a power of two that the largest step
-// so far sets (the sums are rescaled where it grows), so that nothing underflows that counts.  q is brought to
-// 2^14 .. 2^15 by a power of two for each row, so that its fp16 or bf16 digits all stay; scores are
-// exact products summed in fp32.  (16-bit outputs of 5000 positions are off by 2.9e-4 of 64 bits' in the root of
-// the mean square, of which 2.1e-4 are their own rounding; with the ones as small as the codes it was 7.6e-4.)
+// of 2^-12 of a value's distance from its group's middle.  Each row has a power of two for each group that brings the
+// largest w step that the row has seen so far to 2^5 .. 2^14 (the sums are rescaled where it changes), so that what
+// falls below fp16's normal range is off by 2^-30 of the largest at most: other rows' steps, large steps without weight and other
+// groups' take no digits.  (One power of two for all, from the largest step, was 1 to 3 % faster, with groups of 32 11 to 16 %, and
+// lost them.)  q is brought to 2^14 .. 2^15 by a power of two for each row: its digits stay but those below 2^-38 of the row's
+// largest channel, where fp16 ends; scores are exact products summed in fp32.  (16-bit outputs of 5000 positions
+// are off by 2.9e-4 of 64 bits' in the root of the mean square, of which 2.1e-4 are their own rounding; with the ones as
+// small as the codes it was 7.6e-4.)
 //
 // Maximum.  m follows the scores only where one exceeds it by more than 8 (w up to 2^8, for which
 // the scaling leaves room): a vote of the warp instead of a reduction over it for each step.
@@ -219,10 +222,19 @@ __device__ __forceinline__ float exp2_of(float x) {  // 2^-22 of its value off a
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+__device__ __forceinline__ float log2_of(float x) {  // off by 2^-22 of it at most, or of 1 where it is less
+  float r;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
 __device__ __forceinline__ float low_half(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)w)); }
 __device__ __forceinline__ float high_half(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w >> 16))); }
 
 constexpr float kNone = -__builtin_inff();
+// Weights times steps as fp16 operands: the largest so far between 2^5 and kMost (small ones as many times larger as that takes,
+// kUpMost at most, which brings the smallest step there)
+constexpr float kMost = 0x1p14f, kUpMost = 0x1p29f;
+constexpr float kMostLog = 13.99f;  // the logarithm of kMost, less what log2_of is off by
 
 // NC: 32-channel pieces of a row; GS: of a group
 template <int NC, int GS>
@@ -559,8 +571,9 @@ __global__ void __launch_bounds__(32 * kWarps, on_sm(NC, TEAM)) attn4_kernel(con
       m[0] = m[1] = 0.f;
       room[0] = room[1] = kNone;
       sum[0] = sum[1] = make_float2(0.f, 0.f);
-      float step_cap = 0.f;  // no step so far lies above
-      float step_up = 1.f;   // the power of two of the values' weights: step_cap becomes 2^6
+      float up[GN][2];  // the columns' weights times steps, by powers of two
+#pragma unroll
+      for (int g = 0; g < GN; ++g) up[g][0] = up[g][1] = kUpMost;
 
       // One step.  EDGE: some row does not see all of it, or a page is bad.
       const uint32_t matrix_at = (lane & 15) * S * 4 + (lane >> 4) * 16;  // this lane's row of four matrices
@@ -636,7 +649,9 @@ __global__ void __launch_bounds__(32 * kWarps, on_sm(NC, TEAM)) attn4_kernel(con
           }
         }
         uint32_t vscale[kSets][GN][2];
-        __half2 tops = __half2half2(__ushort_as_half(0));  // the larger step, in the low half
+        __half2 tops[GN];  // the largest step, in the low half
+#pragma unroll
+        for (int g = 0; g < GN; ++g) tops[g] = __half2half2(__ushort_as_half(0));
 #pragma unroll
         for (int i = 0; i < kSets; ++i)
 #pragma unroll
@@ -649,54 +664,78 @@ __global__ void __launch_bounds__(32 * kWarps, on_sm(NC, TEAM)) attn4_kernel(con
                 if (pos >= share_hi || pos < w.lo) v = 0;
               }
               vscale[i][g][k] = v;
-              tops = __hmax2(tops, *reinterpret_cast<const __half2*>(&v));
-        }
-        float top = __low2float(tops);
-        bool grow = top > step_cap;
+              tops[g] = __hmax2(tops[g], *reinterpret_cast<const __half2*>(&v));
+            }
+        bool grow = false;
         float most[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           most[j] = fmaxf(x[0][j], x[0][j + 2]);
           if (kSets == 2) most[j] = fmaxf(most[j], fmaxf(x[kSets - 1][j], x[kSets - 1][j + 2]));
-          grow |= most[j] > room[j];
+          // the heaviest weight times the largest step, which need not be one position's, come to kMost at most
+          float most_step = 0.f;
+#pragma unroll
+          for (int g = 0; g < GN; ++g) most_step = fmaxf(most_step, __low2float(tops[g]) * up[g][j]);
+          grow |= most[j] > fminf(room[j], kMostLog - log2_of(most_step));
         }
+        // A column moves for what it sees alone, so that what its row does not see changes none of its bits.
         if (__any_sync(~0u, grow)) {
-          float by_step = 1.f;
-          top = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top)));  // not negative: ordered as bits
-          if (top > step_cap) {
-            // 2^e <= top < 2^(e + 1); an infinite one leaves nothing finite in any case
-            const int e2 = min((int)(__float_as_uint(top) >> 23) - 127, 15);
-            const float up = __uint_as_float((uint32_t)(5 - e2 + 127) << 23);
-            step_cap = top > 65504.f ? top : __uint_as_float((uint32_t)(e2 + 128) << 23);
-            by_step = up / step_up;
-            step_up = up;
-          }
+          float f[2], less[2];  // what weighs less now, by `less` about, leaves room to what comes
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            float to = most[j];
-            to = fmaxf(to, __shfl_xor_sync(~0u, to, 4));
-            to = fmaxf(to, __shfl_xor_sync(~0u, to, 8));
-            to = fmaxf(to, __shfl_xor_sync(~0u, to, 16));
-            const bool fresh = room[j] == kNone;
-            if (!fresh) to = fmaxf(to, 0.f);
-            if (to == kNone) continue;  // nothing seen yet; the sums are 0
-            // m moves up by `to`; a first one by whatever it is
-            const float f = fresh ? 0.f : exp2_of(-to), fs = f * by_step;
-            const float2 ff = make_float2(f, f);
+            float top = most[j];
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
+            const bool moves = top > room[j], fresh = room[j] == kNone;
+            // m moves up by `to`; a first one by whatever it is, with sums that are 0
+            const float to = moves ? top : 0.f;
+            f[j] = !moves ? 1.f : fresh ? 0.f : exp2_of(-to);
+            less[j] = fresh ? 1.f : __uint_as_float((uint32_t)((int)ceilf(fminf(to, 64.f)) + 127) << 23);
             m[j] += to;
-            room[j] = 8.f;
+            if (moves) room[j] = 8.f;
 #pragma unroll
             for (int i = 0; i < kSets; ++i) {
               x[i][j] -= to;
               x[i][j + 2] -= to;
             }
-            sum[j] = mul2(sum[j], ff);
+            sum[j] = mul2(sum[j], make_float2(f[j], f[j]));
 #pragma unroll
-            for (int g = 0; g < GN; ++g) mids[g][j] = mul2(mids[g][j], ff);
+            for (int g = 0; g < GN; ++g) mids[g][j] = mul2(mids[g][j], make_float2(f[j], f[j]));
+          }
+          // the largest weights times steps, down to a power of two
+          __nv_bfloat162 bars[GN];
 #pragma unroll
-            for (int i = 0; i < Z::kSumTiles; ++i) {
-              acc[i][j] *= fs;
-              acc[i][j + 2] *= fs;
+          for (int g = 0; g < GN; ++g) bars[g] = __floats2bfloat162_rn(0.f, 0.f);
+#pragma unroll
+          for (int i = 0; i < kSets; ++i)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const float a = exp2_of(x[i][2 * k]), b = exp2_of(x[i][2 * k + 1]);
+#pragma unroll
+              for (int g = 0; g < GN; ++g) {  // (what is not seen weighs 0, and 0 times an infinity is not the larger)
+                const float step = low_half(vscale[i][g][k]);
+                const uint32_t of = __byte_perm(__float_as_uint(a * step), __float_as_uint(b * step), 0x7632);
+                bars[g] = __hmax2(bars[g], *reinterpret_cast<const __nv_bfloat162*>(&of));
+              }
+            }
+#pragma unroll
+          for (int g = 0; g < GN; ++g) {
+#pragma unroll
+            for (int o = 4; o < 32; o *= 2) bars[g] = __hmax2(bars[g], __shfl_xor_sync(~0u, bars[g], o));
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const float bar = j ? __high2float(bars[g]) : __low2float(bars[g]);
+              // `want` brings 2^e <= bar < 2^(e + 1) to 2^5; an infinity leaves nothing finite in any case
+              const int e2 = max((int)(__float_as_uint(bar) >> 23) - 127, -24);
+              const float was = up[g][j], want = e2 == 128 ? was : __uint_as_float((uint32_t)(5 - e2 + 127) << 23);
+              up[g][j] = bar * was >= kMost ? want : fmaxf(was, fminf(was * less[j], want));
+              const float by = f[j] * up[g][j] * __uint_as_float(0x7F000000u - __float_as_uint(was));  // powers of two
+#pragma unroll
+              for (int i = 2 * g * GS; i < Z::kSumTiles && i < 2 * (g + 1) * GS; ++i) {
+                acc[i][j] *= by;
+                acc[i][j + 2] *= by;
+              }
             }
           }
         }
@@ -715,12 +754,11 @@ __global__ void __launch_bounds__(32 * kWarps, on_sm(NC, TEAM)) attn4_kernel(con
           for (int g = 0; g < GN; ++g) {
             const float2 step = make_float2(low_half(vscale[i][g][0]), low_half(vscale[i][g][1]));
             const float2 mid = fma2(make_float2(8.f, 8.f), step, make_float2(high_half(vscale[i][g][0]), high_half(vscale[i][g][1])));
-            const float2 up = mul2(step, make_float2(step_up, step_up));
             {
               float2 b[2];
 #pragma unroll
               for (int j = 0; j < 2; ++j) {
-                b[j] = mul2(wt[j], up);
+                b[j] = mul2(wt[j], mul2(step, make_float2(up[g][j], up[g][j])));
                 if constexpr (EDGE) {  // whatever stands where a row does not see: 0
                   b[j].x = seen[i][j] ? b[j].x : 0.f;
                   b[j].y = seen[i][j + 2] ? b[j].y : 0.f;
@@ -813,7 +851,6 @@ __global__ void __launch_bounds__(32 * kWarps, on_sm(NC, TEAM)) attn4_kernel(con
       // The warps' sums, in fp32 without the scaling, then joined.
       __syncthreads();
       float* sums = reinterpret_cast<float*>(smem);
-      const float back = 0x1p24f / step_up;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int r = 2 * t4 + j;
@@ -830,6 +867,7 @@ __global__ void __launch_bounds__(32 * kWarps, on_sm(NC, TEAM)) attn4_kernel(con
         float* to = sums + (warp * Z::kRows + r) * Z::kSums + 4 * g8;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {  // even channels, and these plus 16 times the odd ones
+          const float back = 0x1p24f / up[c / GS][j];
           const float(&d0)[4] = acc[2 * c];
           const float(&d1)[4] = acc[2 * c + 1];
           *reinterpret_cast<float4*>(to + 32 * c) =
