@@ -24,7 +24,7 @@ class AttentionStep:
     """``norm``: the input norm's weight (hidden,); ``qkv``: a Weight4, or the dense matrix to quantise, of the
     query, key and value projections ((heads + 2 kv_heads) d, hidden); ``out``: likewise (hidden, heads d);
     ``cache``: the Cache4 of its keys and values (whose heads and d it goes by); ``rotation``; ``q_norm``,
-    ``k_norm``: the head norms' weights (d,), if the model has them."""
+    ``k_norm``: the head norms' weights (d,), if the model has them; ``eps``: of all its norms."""
 
     def __init__(self, norm, qkv, out, cache: kd.Cache4, rotation: kd.Rotation, q_norm=None, k_norm=None,
                  eps: float = 1e-5, group: int = 128):
@@ -45,7 +45,7 @@ class AttentionStep:
         d, h, k = self.cache.d, self.heads, self.cache.heads
         x = kd.matmul_4bit(self.qkv, r.q, scale=r.scale, out_dtype=rows.dtype, stream=stream).view(rows.shape[0], h + 2 * k, d)
         q, key, value = x[:, :h], x[:, h:h + k], x[:, h + k:]
-        kd.rope(q, key, positions, self.rotation, self.q_norm, self.k_norm, out=(q, key), stream=stream)
+        kd.rope(q, key, positions, self.rotation, self.q_norm, self.k_norm, self.eps, out=(q, key), stream=stream)
         return q, key, value, r.residual
 
     def step(self, rows, positions, seqs: kd.Sequences, residual=None, window: int = 0, stream=None):
