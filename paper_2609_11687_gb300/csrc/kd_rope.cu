@@ -17,8 +17,8 @@
 // Heads that do not start on 16-byte boundaries, or whose parts are no whole vectors, go pair by
 // pair, a warp a head, and are read twice (the second time from L1).
 //
-// Bound by instructions and HBM about alike: 2048 tokens of 32 + 8 heads of 128 bf16 channels, normed, take 10.3 us
-// (42 MB, 4.1 TB/s; a plain copy of as much runs at 5.9), issue slots 63 % busy.  One token's heads take 1.7 us,
+// Bound by instructions and HBM about alike: 2048 tokens of 32 + 8 heads of 128 bf16 channels, normed, take 10.5 us
+// (42 MB, 4.0 TB/s; a plain copy of as much runs at 5.9), issue slots 63 % busy.  One token's heads take 1.8 us,
 // 333 tokens of 10 + 2 heads of 80 channels 1.9: latency.
 #include <cmath>
 
@@ -94,9 +94,9 @@ __device__ __forceinline__ void load_weights(const RopeSide& s, int c, float2 (&
   }
 }
 
-// off by two units in the last place at most (a root and a quotient: 0.3 us more of a prompt's 10.3)
+// a root and a quotient, as kd_rmsnorm's (rsqrtf is off by two units in the last place, and saves 0.4 of a prompt's 10.5 us)
 __device__ __forceinline__ float inverse_root(float sum, const RopeParams& p) {
-  return isfinite(sum) ? rsqrtf(sum * p.inv_d + p.eps) : __int_as_float(0x7FC00000);
+  return isfinite(sum) ? 1.f / sqrtf(sum * p.inv_d + p.eps) : __int_as_float(0x7FC00000);
 }
 
 template <int DT>
@@ -264,7 +264,7 @@ cudaError_t launch(RopeParams p, int64_t tokens, bool vec, cudaStream_t s) {
   while (vec && (1 << p.lanes_log) < slots) ++p.lanes_log;
   const int rounds = vec ? (heads + (32 >> p.lanes_log) - 1) >> (5 - p.lanes_log) : heads;
   // as many parts of a token's rounds as all fit the GPU at a time (28 warps an SM), at least one: 2048 tokens of
-  // ten rounds take 10.3 us in two parts, 13 in one, three or more
+  // ten rounds take 10.5 us in two parts, 13 in one, three or more
   const int64_t share = 152 * 28 / tokens;
   p.parts = (int)(share < 1 ? 1 : share > rounds ? rounds : share);
   p.per = (rounds + p.parts - 1) / p.parts;
