@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(32 * kCacheWarps) cache_write_kernel(const __g
         // rounded by adding 1.5 2^23, whose last digit is 1; the code is then in the low bits
         constexpr float kRound = 12582912.f;
         uint32_t c[8];
-        float off = inverse < 0x1p100f ? 0.f : 1.f;  // a reciprocal out of range decides nothing
+        float off = 0.f;  // the reciprocal is 2^24 at most: a step is no smaller than 2^-24
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
           const float2 q = mul2(add2(make_float2(v[e], v[e + 1]), make_float2(-flow, -flow)), make_float2(inverse, inverse));
