@@ -50,7 +50,8 @@ class AttentionStep:
 
     def step(self, rows, positions, seqs: kd.Sequences, residual=None, window: int = 0, stream=None):
         """The block's output rows (fp32) for the hidden ``rows`` (fp16 or bf16) of the sequences' last
-        tokens at ``positions`` (int64), and the new residual.  Writes their keys and values first."""
+        tokens at ``positions`` (int64), and the new residual.  Writes their keys and values first.  Rows of no sequence, as
+        a padded batch has behind the last one, touch nothing of the others', and mean nothing in the output."""
         q, key, value, residual = self.heads_of(rows, positions, residual, stream)
         kd.cache_write_4bit(self.cache, key, value, seqs, stream=stream)
         y = kd.attention_4bit(self.cache, q, seqs, window=window, stream=stream)

@@ -1439,7 +1439,8 @@ class Sequences:
     or None: ``most`` rows each; ``most``: rows of a sequence at most; ``longest``: the largest
     length as far as it is known here, by which attention is split (all that the table has room
     for without it).  The tensors are kept and read on the device at each call: a step rewrites
-    them in place, a captured graph too.  Rows of no sequence are left as they are."""
+    them in place, a captured graph too.  Rows of no sequence (padding behind the last one) are not written: an `out` keeps
+    what it has there, and a tensor that a call makes has whatever its memory held."""
 
     __slots__ = ("table", "lengths", "starts", "most", "longest", "index", "desc", "ref")
 
@@ -1485,7 +1486,7 @@ def cache_write_4bit(cache: Cache4, k, v, seqs: Sequences, stream=None) -> None:
 def cache_read_4bit(cache: Cache4, seqs: Sequences, tokens: Optional[int] = None, dtype=None, out=None, stream=None):
     """The rows of the sequences' last tokens out of the cache: the pair of ``out``, either of which
     may be None, or new ones of ``tokens`` rows (every sequence's ``most`` without it and without
-    ``starts``) in ``dtype`` (fp16) (kd_cache_read_4bit)."""
+    ``starts``) in ``dtype`` (fp16) (kd_cache_read_4bit).  Rows of no sequence are not written."""
     floats, index = _serve()[0], cache.index
     if out is None:
         if tokens is None:
@@ -1517,7 +1518,7 @@ def cache_read_4bit(cache: Cache4, seqs: Sequences, tokens: Optional[int] = None
 def attention_4bit(cache: Cache4, q, seqs: Sequences, scale: Optional[float] = None, causal: bool = True, window: int = 0,
                    out=None, lse=None, workspace=None, stream=None):
     """Attention of the rows ``q`` (tokens, heads, d; fp16 or bf16), the sequences' last tokens,
-    over the cache (kd_attention_4bit); returns ``out``, of q's shape and type.
+    over the cache (kd_attention_4bit); returns ``out``, of q's shape and type.  Rows of no sequence are not written.
 
     ``scale``: of the scores, d^-0.5 without it; ``causal``: a row sees the positions up to its
     own, with ``window`` > 0 the last ``window`` of them, else its whole sequence; ``lse``: fp32
