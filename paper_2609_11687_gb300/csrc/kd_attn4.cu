@@ -122,6 +122,13 @@ struct Plan {
 //   256 items of  the same                       37 / 32 / 22 / 28,        28
 //  2048 items of  the same                       100 / 109 / 138 / 198,    119
 //  1024 items of  4096, 8 tokens                 100 / 111 / 131 / 174,    146;  of 16384  368 / 370 / 381 / 417,  503
+// From eight blocks on (parts of prompts) there are clusters only: each CTA of equal shares would walk the blocks to find its
+// own, and join what each of its many short items is cut into.  Clusters of 1 / 2 / 4 and equal shares:
+//  1024 items of  1000, 16 sequences of 32 tokens     72 / 100 / 148,     88;   of up to 1000 and 32    32 / 44 / 69,      51
+//  2048 items of  4096, 32 sequences of 16            221 / 240 / 287,    233;  of up to 4096 and 16    114 / 124 / 156,   123
+// 16000 items of  1000, 4 prompts of as many tokens   349 / 582 / 932,    849;  of up to as many        151 / 256 / 428,   519
+//  4000 items, one prompt of 1000 tokens              97 / 151 / 236,     386
+constexpr int64_t kBlocksInShares = 7;
 bool plan(const kd_cache4* c, const kd_sequences* s, int64_t heads, int64_t window, Plan& pl) {
   const int64_t shared = heads / c->heads;
   if (s->most * shared > INT32_MAX) return false;
@@ -145,8 +152,8 @@ bool plan(const kd_cache4* c, const kd_sequences* s, int64_t heads, int64_t wind
   pl.team = 0;
   const bool several = blocks > 1, uneven = several && s->seqs > 1 && s->starts;
   const double live = (uneven ? 0.7 : 1) * (double)all, mean = uneven ? 0.65 : 1, wide = pl.nc <= 4 ? 0.25 + 0.1875 * pl.nc : 0.2 + 0.2 * pl.nc;
-  double least = several ? 14 + 0.0037 * wide * live * mean * chunks_each : 11 + (s->seqs > 1 ? 0.003 : 0.0032) * wide * live * chunks_each;
-  for (int team = 1; team <= kTeam && team <= chunks_each; team *= 2) {
+  double least = blocks > kBlocksInShares ? HUGE_VAL : several ? 14 + 0.0037 * wide * live * mean * chunks_each : 11 + (s->seqs > 1 ? 0.003 : 0.0032) * wide * live * chunks_each;
+  for (int team = 1; team <= kTeam && (team <= chunks_each || (team == 1 && blocks > kBlocksInShares)); team *= 2) {
     const double ctas = live * team, fit = std::min(ctas, (double)places), of_sm = fit / 152;
     double step = pl.nc <= 4 ? wide * std::max(0.69, 0.24 + 0.45 * of_sm) : std::max(0.98, 0.95 * std::min(2.0, team == kTeam ? 2 * of_sm : of_sm));
     if (several) step = std::min(step, 1.7 * wide);
