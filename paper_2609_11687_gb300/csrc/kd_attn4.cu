@@ -107,21 +107,22 @@ struct Plan {
 //   equal shares: 11, and 3.2 ns for each such step of all items (HBM's rate; 2 for 64 channels, 5.8 for 256), 3.0 of
 //   several sequences, which are seldom all as long as the longest.
 // Measured for heads of 128 channels, groups of 64, four rows, clusters of 1 / 2 / 4 / 8 and equal shares:
-//     8 items of  1024 positions   9.3 / 8.4 / 7.1 / 6.4,   8.4
-//     8 items of  8192             48 / 28 / 16.7 / 11.2,   11.9
-//    32 items of  4096             26 / 16 / 10.9 / 9.9,    12.5
-//    32 items of 16384             95 / 51 / 28 / 22.5,     24.6
-//   256 items of  1024             13.1 / 14.8 / 20 / 30,   19
-//   256 items of  4096             37 / 36 / 40 / 49,       37
-//   256 items of  2000 to 8192     62 / 56 / 52 / 59,       51
-//   512 items of  8192             118 / 110 / 117 / 132,   112;  of 2000 to 8192  105 / 89 / 90 / 107,  82
+//     8 items of  1024 positions   9.8 / 8.9 / 7.3 / 6.6,     8.6
+//     8 items of  8192             50 / 29 / 17.4 / 11.7,     12.2
+//    32 items of  4096             27 / 17.5 / 12.0 / 10.6,   15.8
+//    32 items of 16384             101 / 54 / 30 / 23.6,      25.1
+//   256 items of  1024             14.0 / 16.0 / 21 / 32,     20
+//   256 items of  4096             39 / 37 / 41 / 50,         38
+//   256 items of  2000 to 8192     66 / 59 / 55 / 60,         53
+//   512 items of  8192             120 / 112 / 117 / 135,     112;  of 2000 to 8192  107 / 91 / 93 / 110,  84
 // Several blocks of rows of a key head read the same codes, as CTAs side by side from L2 (steps at 1.7 at most) but in equal
 // shares one after the other: 14, and 3.7 ns a step.  Where sequences have rows of their own number, a part of the blocks
-// is empty and lengths differ too: 0.7 of the items and 0.65 of their steps are counted.  Four blocks of eight rows:
-//   512 items of  1000 to 4096, 1 to 8 tokens    54 / 37 / 43 / 57,        44
-//   256 items of  the same                       37 / 32 / 22 / 28,        28
-//  2048 items of  the same                       100 / 109 / 138 / 198,    119
-//  1024 items of  4096, 8 tokens                 100 / 111 / 131 / 174,    146;  of 16384  368 / 370 / 381 / 417,  503
+// is empty and lengths differ too: 0.7 of the items and 0.65 of their steps are counted.  Four blocks of eight rows, groups
+// of 128:
+//   512 items of  1000 to 4096, 1 to 8 tokens    56 / 38 / 44 / 59,        45
+//   256 items of  the same                       43 / 33 / 23 / 30,        31
+//  2048 items of  the same                       99 / 108 / 139 / 201,     115
+//  1024 items of  4096, 8 tokens                 103 / 114 / 134 / 179,    113;  of 16384  380 / 380 / 391 / 428,  388
 // From eight blocks on (parts of prompts) there are clusters only: each CTA of equal shares would walk the blocks to find its
 // own, and join what each of its many short items is cut into.  Clusters of 1 / 2 / 4 and equal shares:
 //  1024 items of  1000, 16 sequences of 32 tokens     72 / 100 / 148,     88;   of up to 1000 and 32    32 / 44 / 69,      51

@@ -44,19 +44,19 @@
 // 16-byte pieces apart there, and ldmatrix (transposing for the values) reads them free of bank conflicts
 // as the operands' lanes want them.
 //
-// Mapping.  Four warps a CTA, three or four CTAs an SM, take the steps of an item (a sequence, a key head, a block of rows) in
+// Mapping.  Four warps a CTA, two to four CTAs an SM, take the steps of an item (a sequence, a key head, a block of rows) in
 // turn, each with its own m and sums, joined once at the end in a fixed order.  Two ways to share out
 // the work (kd_attn4.cu has the rule): a cluster of up to eight CTAs has an item to itself and joins in
 // distributed shared memory (TEAM; short items), or all CTAs of one round have equal shares of all
 // positions of all items, which each finds from the lengths, and a second launch joins what is cut.
 //
-// Long batches are bound by HBM: without any arithmetic the copies of 32 sequences of 8192 positions (8 key heads of
-// 128) take 60 us, with it 62; past the first 12 us at 6.0 TB/s, 88 % of the measured copy rate.
-// The rest is the start (2.4 us until the share is known, 6.5 until the first codes are there), shares that end
-// unlike on SMs unlike far from memory (45 to 66 us), and the join (3 us).  Measured (device time, inputs
-// larger than L2): 32 sequences of 2000 to 8192 positions 51 us (floor 27), one of 131072 37 us (22), 16 of up
-// to 4096 with up to 8 drafted tokens 37 us (6.6), one of 1001 positions with 32 key heads 6.7 us (0.7).
-// 128 or 168 registers (255 above 128 channels) spill up to 88 bytes in some instances, groups of 32 the most.
+// Long batches are bound by these copies: without any arithmetic those of 32 sequences of 8192 positions (8 key heads of
+// 128, 0.30 GB) take 64 us, with it 62, where HBM would take 44.  The start (2.4 us until the share is known, 6.5 until the
+// first codes are there), shares that end unlike on SMs unlike far from memory (45 to 66 us) and the join (3 us) are in
+// both.  The next wait of these kernels is for instructions: the step stands twice, unrolled, in each.  Measured (device
+// time, inputs larger than L2): 32 sequences of 2000 to 8192 positions 53 us (floor 27), one of 131072 38 us (22), 16 of
+// up to 4096 with up to 8 drafted tokens 38 us (6.6), one of 1001 positions with 32 key heads 6.9 us (0.7).
+// 128 or 168 registers (255 above 128 channels) spill up to 116 bytes in some instances, groups of 32 the most.
 #pragma once
 #include <cooperative_groups.h>
 
@@ -376,7 +376,7 @@ __device__ __forceinline__ void join_team(const Params& p, const Work& w, int he
 }
 
 // CTAs that an SM has: of heads of up to 128 channels four where they are many and short, three where each has a share of
-// everything (168 registers instead of 128: 32 sequences of 8192 positions 61.3 us, with four 64.0)
+// everything (168 registers instead of 128: 32 sequences of 8192 positions 2.7 us less)
 constexpr int on_sm(int nc, bool team) { return nc > 4 ? 2 : team ? 4 : 3; }
 
 // TEAM: a cluster of p.team CTAs has an item to itself; else all CTAs have equal shares of all of them

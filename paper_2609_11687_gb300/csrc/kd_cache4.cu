@@ -16,8 +16,9 @@
 //
 // Writing 1361 tokens of four sequences (8 heads of 128, bf16) takes 9.6 us, 8 tokens and their way back 4.6 in two
 // launches: a chain of loads (starts, lengths, table) stands before a row's place, and the row's own are issued before it.
-// Reading 19,500 tokens into fp16 takes 27 us for 22 MB of codes and 80 MB of rows; writes alone reach 4.0 TB/s here,
-// 20 us (a quarter fewer instructions left the 27 as they were).  (CTAs that look up a batch of tokens' places once and then share its
+// Reading 19,500 tokens into bf16 takes 27 us for 22 MB of codes and 80 MB of rows, of which 27 MB reach HBM meanwhile.  Writes
+// alone run at 3.7 to 4.0 TB/s, also to memory that stays in L2 (a fill of 84 MB 21.8 us): the way to L2 is what bounds
+// them, with issue slots 72 % busy the other half of it (a quarter fewer instructions left the 27 as they were).  (CTAs that look up a batch of tokens' places once and then share its
 // rows took 14.8 and 27.8 us.)
 #include "kd_cache4.cuh"
 

@@ -17,9 +17,10 @@
 // Heads that do not start on 16-byte boundaries, or whose parts are no whole vectors, go pair by
 // pair, a warp a head, and are read twice (the second time from L1).
 //
-// Bound by instructions and HBM about alike: 2048 tokens of 32 + 8 heads of 128 bf16 channels, normed, take 10.5 us
-// (42 MB, 4.0 TB/s; a plain copy of as much runs at 5.9), issue slots 63 % busy.  One token's heads take 1.8 us,
-// 333 tokens of 10 + 2 heads of 80 channels 1.9: latency.
+// Bound by instructions: 2048 tokens of 32 + 8 heads of 128 bf16 channels, normed, take 10.5 us (42 MB, 4.0 TB/s; a
+// plain copy of as much runs at 5.9), issue slots 63 % busy, 345 instructions for a warp's four heads.  One token's heads take 1.8 us,
+// 333 tokens of 10 + 2 heads of 80 channels 1.9: latency.  Pair by pair the 2048 tokens take 41 us (one element further in
+// memory; 32 without norms) or 48 (100 of 128 channels turned), 333 of them 9.4 and 11: an element a lane, each read twice.
 #include <cmath>
 
 #include "kd_serve.cuh"
