@@ -753,9 +753,10 @@ size_t kd_attention_4bit_workspace(const kd_cache4* cache, const kd_sequences* s
  * Meant for few rows of a sequence (decoding, drafted tokens): eight rows times heads for each cache
  * head share a pass over its codes, more take more passes (for a long prompt kd_cache_read_4bit and a
  * dense product are the shorter way).  Scores are exact products summed in fp32, of q without what lies below 2^-38 of the
- * largest channel of its row and head; the weights are rounded to fp16 as factors of a value's distance from the middle of
- * its group (times the group's step, to 2^-12 of it and 2^-30 of the largest that the row sees in those channels), their sums are
- * fp32; the whole is rounded once.  The order of all sums is fixed by the sizes and lengths (deterministic results).
+ * largest channel of its row and head.  The weights, times a group's step, are rounded to fp16 (off by up to 2^-11 of each and
+ * 2^-30 of the largest that the row sees in those channels) as factors of a value's code, counted from 8, the group's middle; sums
+ * of sixteen such products drop what lies below 2^-12 of the largest of these rounded weights.  All other sums are fp32 and the whole
+ * is rounded once.  The order of all sums is fixed by the sizes and lengths (deterministic results).
  *   workspace  device, 16-byte aligned, ws_bytes >= kd_attention_4bit_workspace(...); it must not
  *              be shared by calls in flight on different streams.
  * Errors: KD_ERR_INVALID_ARG (cache, sequences, heads, type, window < 0 or without causal, scale
